@@ -357,6 +357,167 @@ bsm_status bsm_gemm(const void* a, const void* b, void* c, int64_t batch, int32_
                     int32_t k, bsm_gemm_layout layout, bsm_dtype out_dtype, float alpha,
                     bsm_schedule schedule, void* stream);
 
+/* --------------------------------------------------------------------------- attention
+ * Attention of ragged sequences in one call, its gradient, and attention over a paged cache of
+ * keys and values.  Sequence b has q_len[b] query rows and kv_len[b] keys; query head h reads
+ * key/value head h / (heads_q / heads_kv).  Query row i stands at position
+ * p = i + kv_len - q_len (the queries are the last ones of the keys), and
+ *     s_ij  = scale * q_i . k_j     over the keys j that the row sees
+ *     o_i   = sum_j exp(s_ij - lse_i) v_j,   lse_i = ln sum_j exp(s_ij)
+ * It sees every key, or, where `causal`, the keys j <= p, and with a window w > 0 of these only
+ * j > p - w.  A row that sees no key, or only scores of -inf, has o = 0 and lse = -inf.
+ *
+ * All operands are bf16, products are summed in fp32 on the matrix cores and the softmax is fp32;
+ * the probabilities (and the scores' gradients) are rounded to bf16 once, as operands of the next
+ * product, and the results once more.  The scores are never stored.
+ *
+ * NaN and infinities: what lies outside a sequence's rows (other rows of a padded batch, the rest
+ * of a page, pages of other requests) is never read or counts as nothing.  Inside a sequence, a
+ * NaN or infinity in v (in the backward pass: in q, k, v, dout too) can reach every row whose mask
+ * hides it but not all of its 64-row block, since 0 * NaN = NaN.  A NaN score, or one of +inf,
+ * makes its row NaN.
+ *
+ * Results depend on the operands and sizes only: no sum's order depends on timing, so repeated
+ * calls give the same bits under every schedule. */
+
+/* Element (b, row, head, d) of an operand lies at data + b*seq + row*row + head*head + d, in
+ * elements, so packed tokens (seq 0), padded batches, heads-first layouts and views of a fused
+ * projection all fit; the head dimension itself is contiguous.  Strides are >= 0, 0 included for
+ * operands that are only read; rows may start at any element. */
+typedef struct bsm_heads {
+    void* data;
+    int64_t seq;  /* elements between sequences, on top of their first rows */
+    int64_t row;  /* ... between rows (tokens) */
+    int64_t head; /* ... between heads */
+} bsm_heads;
+
+typedef struct bsm_attention_stats {
+    int64_t batch;
+    int64_t total_q, total_kv;     /* query rows and keys over all sequences */
+    int64_t q_units, kv_units;     /* workgroups of the forward pass and dq, and of dk and dv */
+    int64_t lse_elems;             /* fp32 values of lse: heads_q * total_q */
+    int64_t workspace_bytes;       /* what bsm_attention_backward needs */
+    int64_t pairs;                 /* query/key pairs that the mask leaves, of one query head */
+    int32_t heads_q, heads_kv, head_dim;
+    int32_t causal, window;
+    int32_t schedule, n_xcd;
+    int32_t reserved;
+} bsm_attention_stats;
+
+typedef struct bsm_attention_plan_s* bsm_attention_plan;
+
+/* Plan of the forward and backward passes over one batch's geometry.
+ *   q_len, kv_len      [batch] rows per sequence, 0 .. 2^30 (0: no rows, or no keys)
+ *   q_start, kv_start  [batch] first row of each sequence in the operands, or NULL: sequences
+ *                      packed one after the other (row b starts where b - 1 ended)
+ *   heads_q, heads_kv  heads_q is a multiple of heads_kv
+ *   head_dim           a multiple of 8 up to 128 (else BSM_ERR_UNSUPPORTED)
+ *   causal, window     the mask; window > 0 needs causal
+ *   schedule           order of the work, 128 rows of one head at a time: RR as the sequences
+ *                      come; BALANCED the longest first; XCD every key/value head's work on one
+ *                      XCD, the heads dealt to the XCDs by their cost, the longest first
+ *   topology           NULL = the device's defaults; only n_xcd is used
+ *   device             HIP device ordinal; -1 builds a host-only plan (topology required)
+ * The plan's table is uploaded before this returns.  It serves any number of calls, streams and
+ * layers, and must outlive every graph that captured one of them. */
+bsm_status bsm_attention_plan_create(bsm_attention_plan* out_plan, const int32_t* q_len,
+                                     const int32_t* kv_len, const int64_t* q_start,
+                                     const int64_t* kv_start, int64_t batch, int32_t heads_q,
+                                     int32_t heads_kv, int32_t head_dim, int32_t causal,
+                                     int32_t window, bsm_schedule schedule,
+                                     const bsm_topology* topology, int device);
+
+bsm_status bsm_attention_plan_describe(bsm_attention_plan plan, bsm_attention_stats* stats);
+
+/* Free a plan; one that has been executed waits for its device first, as bsm_plan_destroy. */
+bsm_status bsm_attention_plan_destroy(bsm_attention_plan plan);
+
+/* Forward pass.  lse: NULL, or heads_q * total_q fp32 values, row (head, n) for the n-th query row
+ * of the batch counted over the sequences in order.  scale is finite and > 0.  o overlaps no
+ * operand and its rows do not overlap each other (rows of two sequences that share query rows
+ * would: BSM_ERR_INVALID_ARG); rows that belong to no sequence are left as they are. */
+bsm_status bsm_attention_execute(bsm_attention_plan plan, const bsm_heads* q, const bsm_heads* k,
+                                 const bsm_heads* v, const bsm_heads* o, float* lse, float scale,
+                                 void* stream);
+
+/* Backward pass: with P_ij = exp(s_ij - lse_i), dP_ij = dout_i . v_j, D_i = dout_i . o_i and
+ * dS_ij = P_ij (dP_ij - D_i),
+ *     dq_i = scale sum_j dS_ij k_j,  dk_j = scale sum_i dS_ij q_i,  dv_j = sum_i P_ij dout_i
+ * (dk and dv summed over the query heads of the group).  q, k, v, o and lse are the forward pass's;
+ * the gradients are written, not added to, for every row of every sequence.  A key/value row that
+ * two sequences share, or an operand with a stride of 0, has no one place for its gradient: give
+ * each (sequence, row, head) a place of its own and add them up.  workspace: workspace_bytes of
+ * the plan's stats, not shared with a call that may run at the same time.  dq, dk and dv overlap
+ * no operand (they may interleave with each other, as views of one tensor). */
+bsm_status bsm_attention_backward(bsm_attention_plan plan, const bsm_heads* q, const bsm_heads* k,
+                                  const bsm_heads* v, const bsm_heads* o, const float* lse,
+                                  const bsm_heads* dout, const bsm_heads* dq, const bsm_heads* dk,
+                                  const bsm_heads* dv, float scale, void* workspace,
+                                  int64_t workspace_bytes, void* stream);
+
+/* A cache of keys and values in pages: element (page, row, head, d) at page*page_stride +
+ * row*row_stride + head*head_stride + d, the same for k and v (bf16). */
+typedef struct bsm_cache {
+    void* k;
+    void* v;
+    int64_t n_pages;
+    int64_t page_stride, row_stride, head_stride;
+    int32_t page_size; /* tokens per page, any number >= 1 */
+    int32_t heads;     /* key/value heads */
+    int32_t head_dim;  /* a multiple of 8 up to 128 */
+    int32_t reserved;
+} bsm_cache;
+
+/* Block table and slot map of a step, from the requests' lengths.  All arrays are on the device.
+ *   cached, fresh  [batch] tokens that a request has in the cache, and new ones (< 0 counts as 0)
+ *   table          [batch][width] pages of every request, in order; entries of the pages that hold
+ *                  its cached tokens are read, those of its new pages written
+ *   free_pages     [free_cap] the free list, of which the first *n_free are taken in order
+ *   q_start        [batch + 1] out: first new token of every request (their running sum)
+ *   kv_len         [batch] out: cached + fresh
+ *   slots          [n_slots] out: page * page_size + row of every new token, -1 past the last one
+ *   taken          [2] out: pages taken from the free list, requests refused
+ * Requests are served in order.  One is refused, whole, if its pages do not fit the table's width,
+ * the free list has too few left (it and all later ones that need pages), or its tokens go past
+ * n_slots: its slots are -1, its kv_len is 0, so that attention over it gives zeros, and its table
+ * row is left as it is.  A table or free-list entry that names no page gives slots of -1.  The
+ * outputs, the table and the inputs must not overlap. */
+bsm_status bsm_cache_slots(const int32_t* cached, const int32_t* fresh, int64_t batch,
+                           int32_t page_size, int64_t n_pages, int32_t* table, int32_t width,
+                           const int32_t* free_pages, int64_t free_cap, const int32_t* n_free,
+                           int32_t* q_start, int32_t* kv_len, int64_t* slots, int64_t n_slots,
+                           int32_t* taken, void* stream);
+
+/* Writes row t of k and v ((row, head) strides; seq is not used) to slots[t] of the cache, t <
+ * tokens; slots outside the cache are skipped.  The slots of one call differ from each other: of
+ * two tokens with the same slot, which one's bytes remain is not said. */
+bsm_status bsm_cache_append(const bsm_cache* cache, const bsm_heads* k, const bsm_heads* v,
+                            const int64_t* slots, int64_t tokens, void* stream);
+
+/* Attention of each request's new tokens over its pages (its new keys and values already
+ * written): causal, with an optional window.  Rows q_start[b] .. q_start[b + 1] - 1 of q and o are
+ * request b's chunk, the last of its kv_len[b] keys; key j lies in page table[b][j / page_size].
+ * q_start, kv_len and table are on the device and may change between replays of a captured call;
+ * the host gives bounds:
+ *   tokens   rows of q and o; q_start is clamped to it
+ *   max_q    longest chunk: a request's rows past it are not computed, nor written
+ *   max_kv   longest kv_len, which only decides how the work is cut (a longer one is right, but
+ *            slow); 0: width * page_size
+ * A kv_len past the table's width counts up to it.  A table entry that names no page reads as a
+ * page of zeros.  workspace: bsm_attention_paged_workspace bytes for the same sizes, not shared
+ * with a call that may run at the same time.  o overlaps no operand. */
+bsm_status bsm_attention_paged(const bsm_cache* cache, const bsm_heads* q, const bsm_heads* o,
+                               const int32_t* table, int32_t width, const int32_t* q_start,
+                               const int32_t* kv_len, int64_t batch, int64_t tokens,
+                               int32_t heads_q, int32_t max_q, int32_t max_kv, int32_t window,
+                               float scale, void* workspace, int64_t workspace_bytes,
+                               void* stream);
+
+/* Bytes of workspace (0 or more) that bsm_attention_paged needs on `device` for these sizes. */
+bsm_status bsm_attention_paged_workspace(int64_t batch, int64_t tokens, int32_t heads_q,
+                                         int32_t heads_kv, int32_t head_dim, int32_t max_q,
+                                         int32_t max_kv, int device, int64_t* bytes);
+
 bsm_status bsm_plan_describe(bsm_plan plan, bsm_plan_stats* stats);
 
 /* Copy the host work table out: worker_ptr [n_workers + 1] (CSR row pointer: worker v owns

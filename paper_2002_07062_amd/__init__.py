@@ -14,3 +14,7 @@ from .bsm import (  # noqa: F401
     GEMM_LAYOUTS, bsm_gemm,
     bsm_gemm_execute, bsm_gemm_plan_create,
     bsm_topology, load)
+from .attention import (  # noqa: F401
+    AttentionPlan, bsm_attention_backward, bsm_attention_execute, bsm_attention_paged,
+    bsm_attention_paged_workspace, bsm_attention_plan_create, bsm_attention_plan_describe,
+    bsm_attention_plan_destroy, bsm_cache_append, bsm_cache_slots)

@@ -1,0 +1,357 @@
+"""ctypes binding of the attention entry points of include/bsm.h: ragged sequences with their
+gradient, and the paged key/value cache.
+
+Operands are bfloat16 GPU tensors of any strides whose last dimension is contiguous:
+(tokens, heads, dim), or (batch, rows, heads, dim) for padded batches (a heads-first tensor is
+passed transposed). Nothing is copied or computed here.
+"""
+
+from __future__ import annotations
+
+import ctypes
+import math
+
+import numpy as np
+import torch
+
+from . import bsm as _b
+from .bsm import _arr, _check, _schedule_code, _stream_of, bsm_topology
+
+_vp, _i64, _i32, _f32 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_float
+
+
+class bsm_heads(ctypes.Structure):
+    _fields_ = [("data", _vp), ("seq", _i64), ("row", _i64), ("head", _i64)]
+
+
+class bsm_cache(ctypes.Structure):
+    _fields_ = [("k", _vp), ("v", _vp), ("n_pages", _i64), ("page_stride", _i64),
+                ("row_stride", _i64), ("head_stride", _i64), ("page_size", _i32),
+                ("heads", _i32), ("head_dim", _i32), ("reserved", _i32)]
+
+
+class bsm_attention_stats(ctypes.Structure):
+    _fields_ = [("batch", _i64), ("total_q", _i64), ("total_kv", _i64), ("q_units", _i64),
+                ("kv_units", _i64), ("lse_elems", _i64), ("workspace_bytes", _i64),
+                ("pairs", _i64), ("heads_q", _i32), ("heads_kv", _i32), ("head_dim", _i32),
+                ("causal", _i32), ("window", _i32), ("schedule", _i32), ("n_xcd", _i32),
+                ("reserved", _i32)]
+
+
+_lib = None
+
+
+def _load() -> ctypes.CDLL:
+    global _lib
+    if _lib is not None:
+        return _lib
+    lib = _b.load()
+    P = ctypes.POINTER
+    H = P(bsm_heads)
+    c_int = ctypes.c_int
+    sig = {
+        "bsm_attention_plan_create": [P(_vp), P(_i32), P(_i32), P(_i64), P(_i64), _i64, _i32, _i32,
+                                      _i32, _i32, _i32, c_int, P(bsm_topology), c_int],
+        "bsm_attention_plan_describe": [_vp, P(bsm_attention_stats)],
+        "bsm_attention_plan_destroy": [_vp],
+        "bsm_attention_execute": [_vp, H, H, H, H, _vp, _f32, _vp],
+        "bsm_attention_backward": [_vp, H, H, H, H, _vp, H, H, H, H, _f32, _vp, _i64, _vp],
+        "bsm_cache_slots": [_vp, _vp, _i64, _i32, _i64, _vp, _i32, _vp, _i64, _vp, _vp, _vp, _vp,
+                            _i64, _vp, _vp],
+        "bsm_cache_append": [P(bsm_cache), H, H, _vp, _i64, _vp],
+        "bsm_attention_paged": [P(bsm_cache), H, H, _vp, _i32, _vp, _vp, _i64, _i64, _i32, _i32,
+                                _i32, _i32, _f32, _vp, _i64, _vp],
+        "bsm_attention_paged_workspace": [_i64, _i64, _i32, _i32, _i32, _i32, _i32, c_int,
+                                          P(_i64)],
+    }
+    for name, args in sig.items():
+        fn = getattr(lib, name)
+        fn.argtypes = args
+        fn.restype = c_int
+    _lib = lib
+    return lib
+
+
+def _same_device(device, *tensors) -> None:
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise ValueError(f"expected tensors on {device}, got one on {t.device}")
+
+
+def _contiguous(t, dtype, n, name) -> int:
+    """Pointer of a contiguous GPU tensor of `dtype` with at least n elements."""
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous GPU tensor")
+    if t.numel() < n:
+        raise ValueError(f"{name} has {t.numel()} elements, needs {n}")
+    return t.data_ptr()
+
+
+def _operand(t, rows, batch, heads, dim, name) -> bsm_heads:
+    """`t` as (tokens, heads, dim) with at least `rows` tokens, or (batch, rows, heads, dim)."""
+    if t.dtype != torch.bfloat16:
+        raise TypeError(f"{name} must be bfloat16, got {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor")
+    if t.dim() not in (3, 4) or t.shape[-2] != heads or t.shape[-1] != dim:
+        raise ValueError(f"{name} of shape {tuple(t.shape)} is no (tokens, {heads}, {dim}) or "
+                         f"(batch, rows, {heads}, {dim})")
+    if t.stride(-1) != 1 and dim > 1:
+        raise ValueError(f"{name}: the last dimension must be contiguous")
+    if t.shape[-3] < rows or (t.dim() == 4 and t.shape[0] < batch):
+        raise ValueError(f"{name} of shape {tuple(t.shape)} is shorter than the sequences "
+                         f"({batch} sequences, rows up to {rows})")
+    return bsm_heads(t.data_ptr(), t.stride(0) if t.dim() == 4 else 0, t.stride(-3), t.stride(-2))
+
+
+def _ref(x):
+    return ctypes.byref(x)
+
+
+# ------------------------------------------------------------------------- ragged sequences
+class AttentionPlan:
+    """A plan of one batch's geometry (bsm_attention_plan). Use bsm_attention_plan_create."""
+
+    def __init__(self, handle: int, device: int, stats: bsm_attention_stats, q_end: int,
+                 kv_end: int):
+        self.handle = handle
+        self.device = device
+        self.batch = int(stats.batch)
+        self.heads_q, self.heads_kv, self.head_dim = stats.heads_q, stats.heads_kv, stats.head_dim
+        self.total_q, self.total_kv = int(stats.total_q), int(stats.total_kv)
+        self.lse_elems, self.workspace_bytes = int(stats.lse_elems), int(stats.workspace_bytes)
+        self.q_end, self.kv_end = q_end, kv_end
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.destroy()
+
+    def destroy(self):
+        if self.handle:
+            h, self.handle = self.handle, None
+            _check(_load().bsm_attention_plan_destroy(h))
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+    def _q(self, t, name):
+        return _operand(t, self.q_end, self.batch, self.heads_q, self.head_dim, name)
+
+    def _kv(self, t, name):
+        return _operand(t, self.kv_end, self.batch, self.heads_kv, self.head_dim, name)
+
+
+def _lengths(a, n=None):
+    a = np.asarray(a.cpu() if isinstance(a, torch.Tensor) else a).reshape(-1)
+    if a.size and (a.max() > 2**31 - 1 or a.min() < -2**31):
+        raise ValueError("sequence lengths must fit in 32 bits")
+    return np.ascontiguousarray(a, dtype=np.int32)
+
+
+def _first_rows(start, lengths):
+    if start is None:
+        return None, int(lengths.astype(np.int64).sum())
+    s = np.asarray(start.cpu() if isinstance(start, torch.Tensor) else start, dtype=np.int64)
+    s = np.ascontiguousarray(np.broadcast_to(s.reshape(-1), lengths.shape))
+    live = lengths > 0
+    return s, int((s[live] + lengths[live]).max()) if live.any() else 0
+
+
+def bsm_attention_plan_create(q_len, kv_len=None, *, heads_q, heads_kv=None, head_dim,
+                              causal=False, window=0, q_start=None, kv_start=None,
+                              schedule="balanced", topology=None, device=0) -> AttentionPlan:
+    """Plan of attention over sequences of q_len query rows and kv_len keys (default: as many).
+    q_start / kv_start: first row of each sequence in the operands; None for sequences packed one
+    after the other, 0 for (batch, rows, heads, dim) operands. device=-1 makes a host-only plan
+    (needs a topology)."""
+    lib = _load()
+    q_len = _lengths(q_len)
+    kv_len = q_len if kv_len is None else _lengths(kv_len)
+    if q_len.shape != kv_len.shape:
+        raise ValueError(f"{q_len.size} query lengths, {kv_len.size} key lengths")
+    q_start, q_end = _first_rows(q_start, q_len)
+    kv_start, kv_end = _first_rows(kv_start, kv_len)
+    topo = None
+    if topology is not None:
+        topo = topology if isinstance(topology, bsm_topology) else bsm_topology(**topology)
+    keep = [_arr(q_len, np.int32), _arr(kv_len, np.int32), _arr(q_start, np.int64),
+            _arr(kv_start, np.int64)]
+    handle = _vp()
+    _check(lib.bsm_attention_plan_create(
+        _ref(handle), keep[0][1], keep[1][1], keep[2][1], keep[3][1], q_len.size, int(heads_q),
+        int(heads_q if heads_kv is None else heads_kv), int(head_dim), int(bool(causal)),
+        int(window), _schedule_code(schedule), _ref(topo) if topo is not None else None,
+        int(device)))
+    st = bsm_attention_stats()
+    _check(lib.bsm_attention_plan_describe(handle.value, _ref(st)))
+    return AttentionPlan(handle.value, int(device), st, q_end, kv_end)
+
+
+def bsm_attention_plan_describe(plan: AttentionPlan) -> dict:
+    st = bsm_attention_stats()
+    _check(_load().bsm_attention_plan_describe(plan.handle, _ref(st)))
+    return {name: getattr(st, name) for name, _ in st._fields_ if name != "reserved"}
+
+
+def bsm_attention_plan_destroy(plan: AttentionPlan) -> None:
+    plan.destroy()
+
+
+def _scale_of(scale, dim) -> float:
+    return 1.0 / math.sqrt(dim) if scale is None else float(scale)
+
+
+def bsm_attention_execute(plan: AttentionPlan, q, k, v, o, lse=None, scale=None, stream=None):
+    """o = attention of q over k and v under the plan (see bsm.h); lse: None or a float32 tensor
+    of heads_q * total_q elements for the rows' log-sum-exp, which the backward pass needs.
+    scale: default 1 / sqrt(head_dim). Returns o."""
+    lib = _load()
+    a = [plan._q(q, "q"), plan._kv(k, "k"), plan._kv(v, "v"), plan._q(o, "o")]
+    lp = None if lse is None else _contiguous(lse, torch.float32, plan.lse_elems, "lse")
+    dev = torch.device("cuda", plan.device)
+    _same_device(dev, q, k, v, o, lse)
+    with torch.cuda.device(dev):
+        _check(lib.bsm_attention_execute(plan.handle, *map(_ref, a), lp,
+                                         _scale_of(scale, plan.head_dim), _stream_of(q, stream)))
+    return o
+
+
+def bsm_attention_backward(plan: AttentionPlan, q, k, v, o, lse, dout, dq, dk, dv, scale=None,
+                           workspace=None, stream=None):
+    """Gradients of bsm_attention_execute: dq, dk and dv from q, k, v, its o and lse, and dout
+    (see bsm.h). workspace: None (allocated for the call on the current stream) or a tensor of
+    plan.workspace_bytes bytes. Returns (dq, dk, dv)."""
+    lib = _load()
+    a = [plan._q(q, "q"), plan._kv(k, "k"), plan._kv(v, "v"), plan._q(o, "o")]
+    g = [plan._q(dout, "dout"), plan._q(dq, "dq"), plan._kv(dk, "dk"), plan._kv(dv, "dv")]
+    lp = _contiguous(lse, torch.float32, plan.lse_elems, "lse")
+    dev = torch.device("cuda", plan.device)
+    _same_device(dev, q, k, v, o, lse, dout, dq, dk, dv, workspace)
+    if workspace is None:
+        if stream is not None:
+            raise ValueError("a call on a stream of its own needs its own workspace")
+        with torch.cuda.device(dev):
+            workspace = torch.empty(plan.workspace_bytes, dtype=torch.uint8, device=dev)
+    elif not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    with torch.cuda.device(dev):
+        _check(lib.bsm_attention_backward(
+            plan.handle, *map(_ref, a), lp, *map(_ref, g), _scale_of(scale, plan.head_dim),
+            workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+            _stream_of(q, stream)))
+    return dq, dk, dv
+
+
+# ------------------------------------------------------------------------------ paged cache
+def _cache_of(k_cache, v_cache) -> bsm_cache:
+    """k_cache, v_cache: bfloat16 GPU tensors (pages, page size, heads, dim) of the same strides."""
+    for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
+        if t.dtype != torch.bfloat16:
+            raise TypeError(f"{name} must be bfloat16, got {t.dtype}")
+        if not t.is_cuda or t.dim() != 4:
+            raise ValueError(f"{name} must be a GPU tensor (pages, page size, heads, dim)")
+        if t.stride(3) != 1 and t.shape[3] > 1:
+            raise ValueError(f"{name}: the last dimension must be contiguous")
+    if k_cache.shape != v_cache.shape or k_cache.stride() != v_cache.stride():
+        raise ValueError("k_cache and v_cache must have the same shape and strides")
+    n, page, heads, dim = k_cache.shape
+    return bsm_cache(k_cache.data_ptr(), v_cache.data_ptr(), n, *k_cache.stride()[:3], page,
+                     heads, dim, 0)
+
+
+def bsm_cache_slots(cached, fresh, page_size, n_pages, table, free_pages, n_free, q_start, kv_len,
+                    slots, taken, stream=None):
+    """Block table and slot map of a step from the requests' lengths (see bsm.h). int32 tensors on
+    one GPU: cached, fresh, kv_len (batch), table (batch, width), free_pages, n_free (1),
+    q_start (batch + 1), taken (2); slots: int64, as many as the step has room for tokens."""
+    lib = _load()
+    batch = cached.numel()
+    if table.dim() != 2 or table.shape[0] < batch:
+        raise ValueError(f"table of shape {tuple(table.shape)} has no row for each of {batch}")
+    i32 = torch.int32
+    p = [_contiguous(cached, i32, batch, "cached"), _contiguous(fresh, i32, batch, "fresh")]
+    dev = cached.device
+    _same_device(dev, fresh, table, free_pages, n_free, q_start, kv_len, slots, taken)
+    with torch.cuda.device(dev):
+        _check(lib.bsm_cache_slots(
+            *p, batch, int(page_size), int(n_pages), _contiguous(table, i32, 0, "table"),
+            table.shape[1], _contiguous(free_pages, i32, 0, "free_pages"), free_pages.numel(),
+            _contiguous(n_free, i32, 1, "n_free"), _contiguous(q_start, i32, batch + 1, "q_start"),
+            _contiguous(kv_len, i32, batch, "kv_len"),
+            _contiguous(slots, torch.int64, 0, "slots"), slots.numel(),
+            _contiguous(taken, i32, 2, "taken"), _stream_of(cached, stream)))
+
+
+def bsm_cache_append(k, v, slots, k_cache, v_cache, stream=None):
+    """Writes the tokens of k and v (tokens, heads, dim) to their slots of the cache."""
+    lib = _load()
+    cache = _cache_of(k_cache, v_cache)
+    tokens = slots.numel()
+    if k.dim() != 3 or v.dim() != 3:
+        raise ValueError("k and v must be (tokens, heads, dim)")
+    kh = _operand(k, tokens, 1, cache.heads, cache.head_dim, "k")
+    vh = _operand(v, tokens, 1, cache.heads, cache.head_dim, "v")
+    sp = _contiguous(slots, torch.int64, 0, "slots")
+    _same_device(k_cache.device, v_cache, k, v, slots)
+    with torch.cuda.device(k_cache.device):
+        _check(lib.bsm_cache_append(_ref(cache), _ref(kh), _ref(vh), sp, tokens,
+                                    _stream_of(k_cache, stream)))
+
+
+def bsm_attention_paged_workspace(batch, tokens, heads_q, heads_kv, head_dim, max_q, max_kv,
+                                  device=0) -> int:
+    """Bytes of workspace that bsm_attention_paged needs for these sizes."""
+    n = _i64()
+    _check(_load().bsm_attention_paged_workspace(int(batch), int(tokens), int(heads_q),
+                                                 int(heads_kv), int(head_dim), int(max_q),
+                                                 int(max_kv), int(device), _ref(n)))
+    return int(n.value)
+
+
+def bsm_attention_paged(q, k_cache, v_cache, table, q_start, kv_len, o, max_q, max_kv=None,
+                        window=0, scale=None, workspace=None, stream=None):
+    """o = causal attention of every request's new tokens over its pages (see bsm.h). q, o:
+    (tokens, heads, dim); table: int32 (batch, width); q_start: int32 (batch + 1); kv_len: int32
+    (batch). max_q, max_kv: host bounds on a chunk and on kv_len (default: the table's width).
+    workspace: None (allocated for the call on the current stream) or a tensor of
+    bsm_attention_paged_workspace bytes. Returns o."""
+    lib = _load()
+    cache = _cache_of(k_cache, v_cache)
+    if q.dim() != 3 or o.dim() != 3:
+        raise ValueError("q and o must be (tokens, heads, dim)")
+    tokens, heads_q = q.shape[0], q.shape[1]
+    batch = kv_len.numel()
+    if table.dim() != 2 or table.shape[0] < batch:
+        raise ValueError(f"table of shape {tuple(table.shape)} has no row for each of {batch}")
+    qh = _operand(q, tokens, 1, heads_q, cache.head_dim, "q")
+    oh = _operand(o, tokens, 1, heads_q, cache.head_dim, "o")
+    i32 = torch.int32
+    tp = _contiguous(table, i32, 0, "table")
+    sp = _contiguous(q_start, i32, batch + 1, "q_start")
+    lp = _contiguous(kv_len, i32, 0, "kv_len")
+    dev = q.device
+    _same_device(dev, k_cache, v_cache, table, q_start, kv_len, o, workspace)
+    width = table.shape[1]
+    max_kv = width * cache.page_size if max_kv is None else int(max_kv)
+    with torch.cuda.device(dev):
+        if workspace is None:
+            if stream is not None:
+                raise ValueError("a call on a stream of its own needs its own workspace")
+            workspace = torch.empty(
+                bsm_attention_paged_workspace(batch, tokens, heads_q, cache.heads, cache.head_dim,
+                                              max_q, max_kv, dev.index),
+                dtype=torch.uint8, device=dev)
+        elif not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous")
+        _check(lib.bsm_attention_paged(
+            _ref(cache), _ref(qh), _ref(oh), tp, width, sp, lp, batch, tokens, heads_q, int(max_q),
+            max_kv, int(window), _scale_of(scale, cache.head_dim), workspace.data_ptr(),
+            workspace.numel() * workspace.element_size(), _stream_of(q, stream)))
+    return o

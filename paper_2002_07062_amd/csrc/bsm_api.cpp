@@ -20,6 +20,7 @@
 #include <vector>
 
 #include "bsm.h"
+#include "bsm_error.hpp"
 #include "bsm_launch.hpp"
 #include "bsm_plan.hpp"
 #include "bsm_tile.hpp"
@@ -1132,6 +1133,8 @@ bsm_status softmax_noalloc(const void* in, void* out, const int64_t* slice_offse
 }
 
 }  // namespace
+
+bsm_status bsm::report(bsm_status st, const char* message) { return fail(st, "%s", message); }
 
 extern "C" {
 

@@ -1,0 +1,337 @@
+// Attention of ragged sequences in one pass over the keys, and its gradient, which forms the
+// probabilities again from the saved log-sum-exp of every row.
+#include "bsm_attention.hpp"
+
+namespace bsm_att {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kKeys = 64;  // keys (or query rows, for dk and dv) per step
+
+__device__ __forceinline__ const uint16_t* at(const Heads& t, const Unit& u, int64_t start, int head) {
+    return t.p + u.seq * t.seq + start * t.row + head * t.head;
+}
+
+// The keys that query row i of a sequence sees are lo .. hi.
+struct Seen {
+    int lo, hi;
+};
+__device__ __forceinline__ Seen seen_keys(int i, int q_len, int kv_len, Mask m) {
+    Seen s = {0, kv_len - 1};
+    if (m.causal) {
+        const int p = i + kv_len - q_len;
+        s.hi = p < s.hi ? p : s.hi;
+        if (m.window > 0 && p - m.window + 1 > 0) s.lo = p - m.window + 1;
+    }
+    return s;
+}
+
+// ------------------------------------------------------------------------------------ forward
+template <int D>
+__global__ __launch_bounds__(kThreads, 2) void attention_kernel(const SequenceArgs a, const Unit* __restrict__ units) {
+    __shared__ __align__(16) uint16_t lds[2][2][kKeys * D];  // buffer, K or V
+    const Unit u = units[blockIdx.x];
+    if (u.rows <= 0) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, li = lane & 31, h = lane >> 5;
+    const int chunks = a.dim / 8;
+    const int i0 = u.first + kRows * wave, i = i0 + li;
+    const bool live = i < u.first + u.rows;
+    RowOperand<D> q;
+    q.load(at(a.q, u, u.q_start + i, u.head), live, h, chunks);
+
+    const Seen mine = seen_keys(i, u.q_len, u.kv_len, a.mask);
+    // keys that some row of the wave sees, that all its rows see, and that some row of the unit sees
+    const int last = u.first + u.rows - 1;
+    const Seen w0 = seen_keys(i0, u.q_len, u.kv_len, a.mask), w1 = seen_keys(i0 + kRows - 1, u.q_len, u.kv_len, a.mask);
+    const Seen u0 = seen_keys(u.first, u.q_len, u.kv_len, a.mask), u1 = seen_keys(last, u.q_len, u.kv_len, a.mask);
+    const int begin = u0.lo / kKeys * kKeys, end = u1.hi + 1;
+    const bool any_row = i0 <= last;
+
+    const uint16_t* kp = at(a.k, u, u.kv_start, u.head / a.group);
+    const uint16_t* vp = at(a.v, u, u.kv_start, u.head / a.group);
+    Stage<D, kKeys, kThreads> sk, sv;
+    Online<D> st;
+    st.init();
+    const float c = a.scale * kLog2e;
+    if (begin < end) {
+        sk.load(tid, kp + begin * a.k.row, a.k.row, u.kv_len - begin, chunks);
+        sv.load(tid, vp + begin * a.v.row, a.v.row, u.kv_len - begin, chunks);
+        sk.store(tid, lds[0][0]);
+        sv.store(tid, lds[0][1]);
+    }
+    int buf = 0;
+    for (int j0 = begin; j0 < end; j0 += kKeys, buf ^= 1) {
+        lds_barrier();
+        const int next = j0 + kKeys;
+        if (next < end) {
+            sk.load(tid, kp + next * a.k.row, a.k.row, u.kv_len - next, chunks);
+            sv.load(tid, vp + next * a.v.row, a.v.row, u.kv_len - next, chunks);
+        }
+        if (any_row && j0 <= w1.hi && next > w0.lo) {
+            f32x16 s[kKeys / 32];
+#pragma unroll
+            for (int k = 0; k < kKeys / 32; ++k) s[k] = row_product<D>(lds[buf][0], 32 * k, q, lane);
+            if (j0 < w1.lo || next - 1 > w0.hi) {
+#pragma unroll
+                for (int k = 0; k < kKeys / 32; ++k) mask_block(s[k], j0 + 32 * k, h, mine.lo, mine.hi);
+            }
+            st.weigh(s, c);
+#pragma unroll
+            for (int k = 0; k < kKeys / 32; ++k) col_product<D>(st.o, lds[buf][1], 32 * k, s[k], lane);
+        }
+        if (next < end) {
+            sk.store(tid, lds[buf ^ 1][0]);
+            sv.store(tid, lds[buf ^ 1][1]);
+        }
+    }
+    const float total = st.row_sum();
+    // a row that sees nothing, or only scores of -inf, is zero
+    const float f = total == 0.0f ? 0.0f : 1.0f / total;
+    uint16_t* out = a.o.p + u.seq * a.o.seq + (u.q_start + i) * a.o.row + u.head * a.o.head;
+    store_row<D>(out, live, st.o, f, h, chunks);
+    if (a.lse && live && h == 0) a.lse[u.head * a.total_q + u.lse_row + i] = st.statistic(total);
+}
+
+// ----------------------------------------------------------------------------------- backward
+// A row's statistic as the reference of its exponents: rows that saw nothing get +inf, which makes
+// every probability 0.
+__device__ __forceinline__ float reference(float lse) { return lse == -kInf ? kInf : lse * kLog2e; }
+
+// dq = scale * sum_j dS_ij k_j, with dS = P (dP - delta), P = exp(s - lse), dP = do . v: query rows
+// stay in registers as in the forward pass, the keys stream through LDS.  Also leaves delta.
+template <int D>
+__global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(const SequenceArgs a, const Unit* __restrict__ units) {
+    __shared__ __align__(16) uint16_t lds[2][2][kKeys * D];
+    const Unit u = units[blockIdx.x];
+    if (u.rows <= 0) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, li = lane & 31, h = lane >> 5;
+    const int chunks = a.dim / 8;
+    const int i0 = u.first + kRows * wave, i = i0 + li;
+    const bool live = i < u.first + u.rows;
+    RowOperand<D> q, dout;
+    q.load(at(a.q, u, u.q_start + i, u.head), live, h, chunks);
+    dout.load(at(a.dout, u, u.q_start + i, u.head), live, h, chunks);
+    float delta = 0.0f, lse = -kInf;
+    {
+        RowOperand<D> o;
+        o.load(at(a.o, u, u.q_start + i, u.head), live, h, chunks);
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                delta = __builtin_fmaf(static_cast<float>(o.f[s][e]), static_cast<float>(dout.f[s][e]), delta);
+        delta += other_half(delta);
+        const int64_t r = u.head * a.total_q + u.lse_row + i;
+        if (live) {
+            lse = a.lse[r];
+            if (h == 0) a.delta[r] = delta;
+        }
+    }
+    const float ref = reference(lse);
+    const Seen mine = seen_keys(i, u.q_len, u.kv_len, a.mask);
+    const int last = u.first + u.rows - 1;
+    const Seen w0 = seen_keys(i0, u.q_len, u.kv_len, a.mask), w1 = seen_keys(i0 + kRows - 1, u.q_len, u.kv_len, a.mask);
+    const Seen u0 = seen_keys(u.first, u.q_len, u.kv_len, a.mask), u1 = seen_keys(last, u.q_len, u.kv_len, a.mask);
+    const int begin = u0.lo / kKeys * kKeys, end = u1.hi + 1;
+    const bool any_row = i0 <= last;
+    const uint16_t* kp = at(a.k, u, u.kv_start, u.head / a.group);
+    const uint16_t* vp = at(a.v, u, u.kv_start, u.head / a.group);
+    Stage<D, kKeys, kThreads> sk, sv;
+    f32x16 dq[D / 32];
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t) dq[t] = zero16();
+    const float c = a.scale * kLog2e;
+    if (begin < end) {
+        sk.load(tid, kp + begin * a.k.row, a.k.row, u.kv_len - begin, chunks);
+        sv.load(tid, vp + begin * a.v.row, a.v.row, u.kv_len - begin, chunks);
+        sk.store(tid, lds[0][0]);
+        sv.store(tid, lds[0][1]);
+    }
+    int buf = 0;
+    for (int j0 = begin; j0 < end; j0 += kKeys, buf ^= 1) {
+        lds_barrier();
+        const int next = j0 + kKeys;
+        if (next < end) {
+            sk.load(tid, kp + next * a.k.row, a.k.row, u.kv_len - next, chunks);
+            sv.load(tid, vp + next * a.v.row, a.v.row, u.kv_len - next, chunks);
+        }
+        if (any_row && j0 <= w1.hi && next > w0.lo) {
+            const bool masked = j0 < w1.lo || next - 1 > w0.hi;
+#pragma unroll
+            for (int k = 0; k < kKeys / 32; ++k) {
+                f32x16 s = row_product<D>(lds[buf][0], 32 * k, q, lane);
+                const f32x16 dp = row_product<D>(lds[buf][1], 32 * k, dout, lane);
+                if (masked) mask_block(s, j0 + 32 * k, h, mine.lo, mine.hi);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -ref));
+                    const float ds = p * (dp[e] - delta);
+                    // a masked score contributes nothing, whatever v holds there
+                    s[e] = masked && s[e] == -kInf ? 0.0f : ds;
+                }
+                col_product<D>(dq, lds[buf][0], 32 * k, s, lane);
+            }
+        }
+        if (next < end) {
+            sk.store(tid, lds[buf ^ 1][0]);
+            sv.store(tid, lds[buf ^ 1][1]);
+        }
+    }
+    if (lse == -kInf) {  // the row saw nothing: no gradient, whatever dout holds
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t) dq[t] = zero16();
+    }
+    uint16_t* out = a.dq.p + u.seq * a.dq.seq + (u.q_start + i) * a.dq.row + u.head * a.dq.head;
+    store_row<D>(out, live, dq, a.scale, h, chunks);
+}
+
+// dv_j = sum_i P_ij do_i and dk_j = scale * sum_i dS_ij q_i over the rows of all query heads that
+// share the key/value head: a wave keeps 32 keys (k, v and both sums in registers), the query
+// rows stream through LDS.  No sum crosses a workgroup, so the result does not depend on timing.
+template <int D>
+__global__ __launch_bounds__(kThreads, 1) void attention_dkv_kernel(const SequenceArgs a, const Unit* __restrict__ units) {
+    __shared__ __align__(16) uint16_t lds[2][2][kKeys * D];  // buffer, q or dout
+    __shared__ __align__(16) float stat[2][2][kKeys];        // buffer, reference or delta
+    const Unit u = units[blockIdx.x];
+    if (u.rows <= 0) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, li = lane & 31, h = lane >> 5;
+    const int chunks = a.dim / 8;
+    const int j0 = u.first + kRows * wave, j = j0 + li;
+    const bool live = j < u.first + u.rows;
+    RowOperand<D> k, v;
+    k.load(at(a.k, u, u.kv_start + j, u.head), live, h, chunks);
+    v.load(at(a.v, u, u.kv_start + j, u.head), live, h, chunks);
+    f32x16 dk[D / 32], dv[D / 32];
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t) dk[t] = dv[t] = zero16();
+    const float c = a.scale * kLog2e;
+    // Query rows that see a key of the unit: i + off >= j, and i + off < j + window.
+    const int off = u.kv_len - u.q_len;
+    const int last = u.first + u.rows - 1;
+    int begin = 0, end = u.q_len;
+    if (a.mask.causal) {
+        begin = max(0, u.first - off) / kKeys * kKeys;
+        if (a.mask.window > 0 && static_cast<int64_t>(last) + a.mask.window - off < end) end = last + a.mask.window - off;
+    }
+    const int steps = end > begin ? (end - begin + kKeys - 1) / kKeys : 0;
+    const int64_t total = static_cast<int64_t>(steps) * a.group;
+    const bool any_row = j0 <= last;
+
+    Stage<D, kKeys, kThreads> sq, sd;
+    float ref = kInf, delta = 0.0f;  // of row `tid` of the step, threads 0 .. kKeys - 1
+    // Rows that saw nothing (their statistic says so) count as zeros, whatever they hold.
+    auto fetch = [&](int g, int r0) {
+        const int head = u.head * a.group + g;
+        const uint16_t* qp = at(a.q, u, u.q_start + r0, head);
+        const uint16_t* dp = at(a.dout, u, u.q_start + r0, head);
+        const int64_t r = head * a.total_q + u.lse_row + r0;
+        sq.load(tid, qp, a.q.row, end - r0, chunks);
+        sd.load(tid, dp, a.dout.row, end - r0, chunks);
+#pragma unroll
+        for (int n = 0; n < sq.kN; ++n) {
+            const int row = sq.row(tid, n);
+            if (row < end - r0 && a.lse[r + row] == -kInf) sq.r[n] = sd.r[n] = u32x4{0, 0, 0, 0};
+        }
+        ref = kInf;
+        delta = 0.0f;
+        if (tid < kKeys && tid < end - r0) {
+            ref = reference(a.lse[r + tid]);
+            delta = a.delta[r + tid];
+            if (ref == kInf) delta = 0.0f;
+        }
+    };
+    auto put = [&](int buf) {
+        sq.store(tid, lds[buf][0]);
+        sd.store(tid, lds[buf][1]);
+        if (tid < kKeys) {
+            stat[buf][0][tid] = ref;
+            stat[buf][1][tid] = delta;
+        }
+    };
+    if (total > 0) {
+        fetch(0, begin);
+        put(0);
+    }
+    int buf = 0, r0 = begin, g = 0;
+    for (int64_t n = 0; n < total; ++n, buf ^= 1) {
+        lds_barrier();
+        int next_r0 = r0 + kKeys, next_g = g;
+        if (next_r0 >= end) {
+            next_r0 = begin;
+            ++next_g;
+        }
+        if (n + 1 < total) fetch(next_g, next_r0);
+        // whether the mask hides some pair, or every pair, of these query rows and the wave's keys
+        bool masked = false, none = !any_row;
+        if (a.mask.causal) {
+            const int p0 = r0 + off, p1 = min(r0 + kKeys, end) - 1 + off;
+            masked = p0 < j0 + kRows - 1;
+            none = none || p1 < j0;
+            if (a.mask.window > 0) {
+                masked = masked || static_cast<int64_t>(p1) - a.mask.window >= j0;
+                none = none || static_cast<int64_t>(p0) - a.mask.window >= j0 + kRows - 1;
+            }
+        }
+        if (!none) {
+#pragma unroll
+            for (int b = 0; b < kKeys / 32; ++b) {
+                f32x16 p = row_product<D>(lds[buf][0], 32 * b, k, lane);
+                f32x16 ds = row_product<D>(lds[buf][1], 32 * b, v, lane);
+#pragma unroll
+                for (int e4 = 0; e4 < 4; ++e4) {
+                    const f32x4 rr = *reinterpret_cast<const f32x4*>(&stat[buf][0][32 * b + 8 * e4 + 4 * h]);
+                    const f32x4 dd = *reinterpret_cast<const f32x4*>(&stat[buf][1][32 * b + 8 * e4 + 4 * h]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int x = 4 * e4 + e;
+                        float pv = __builtin_amdgcn_exp2f(__builtin_fmaf(p[x], c, -rr[e]));
+                        float dv_ = pv * (ds[x] - dd[e]);
+                        if (masked) {
+                            const Seen s = seen_keys(r0 + 32 * b + 8 * e4 + 4 * h + e, u.q_len, u.kv_len, a.mask);
+                            const bool sees = j >= s.lo && j <= s.hi;
+                            pv = sees ? pv : 0.0f;
+                            dv_ = sees ? dv_ : 0.0f;
+                        }
+                        p[x] = pv;
+                        ds[x] = dv_;
+                    }
+                }
+                col_product<D>(dv, lds[buf][1], 32 * b, p, lane);
+                col_product<D>(dk, lds[buf][0], 32 * b, ds, lane);
+            }
+        }
+        if (n + 1 < total) put(buf ^ 1);
+        r0 = next_r0;
+        g = next_g;
+    }
+    const int64_t row = u.kv_start + j;
+    store_row<D>(a.dk.p + u.seq * a.dk.seq + row * a.dk.row + u.head * a.dk.head, live, dk, a.scale, h, chunks);
+    store_row<D>(a.dv.p + u.seq * a.dv.seq + row * a.dv.row + u.head * a.dv.head, live, dv, 1.0f, h, chunks);
+}
+
+}  // namespace
+
+hipError_t launch_attention(const SequenceArgs& a, const Unit* units, int64_t n, hipStream_t stream) {
+    if (n == 0) return hipSuccess;
+    if (a.dim <= 64) attention_kernel<64><<<static_cast<unsigned>(n), kThreads, 0, stream>>>(a, units);
+    else attention_kernel<128><<<static_cast<unsigned>(n), kThreads, 0, stream>>>(a, units);
+    return hipGetLastError();
+}
+
+hipError_t launch_attention_backward(const SequenceArgs& a, const Unit* q_units, int64_t n_q, const Unit* kv_units,
+                                     int64_t n_kv, hipStream_t stream) {
+    if (n_q > 0) {
+        if (a.dim <= 64) attention_dq_kernel<64><<<static_cast<unsigned>(n_q), kThreads, 0, stream>>>(a, q_units);
+        else attention_dq_kernel<128><<<static_cast<unsigned>(n_q), kThreads, 0, stream>>>(a, q_units);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (n_kv > 0) {
+        if (a.dim <= 64) attention_dkv_kernel<64><<<static_cast<unsigned>(n_kv), kThreads, 0, stream>>>(a, kv_units);
+        else attention_dkv_kernel<128><<<static_cast<unsigned>(n_kv), kThreads, 0, stream>>>(a, kv_units);
+        return hipGetLastError();
+    }
+    return hipSuccess;
+}
+
+}  // namespace bsm_att

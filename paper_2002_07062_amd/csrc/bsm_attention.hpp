@@ -1,0 +1,270 @@
+// Device code shared by the attention kernels: operand tiles in LDS, matrix-core fragments of
+// them, and the online softmax of a wave's 32 query rows.
+//
+// Every kernel keeps one row of the result per lane.  v_mfma_f32_32x32x16_bf16 returns, in lane
+// (li, h) = (lane & 31, lane >> 5), column li and rows 8 (i / 4) + 4 h + i % 4, i = 0..15.  So the
+// transposed scores S^T = K Q^T give each lane one query (column li) and 16 of 32 keys: the row
+// maximum and sum are taken in the lane, with one exchange between lanes l and l + 32, and the
+// factors that rescale a row are one register.  Its registers are also the second operand of the
+// next product, O^T = V^T P^T, without any exchange: an operand lane holds 8 values of the
+// reduction axis, and which 8 keys those are is free as long as both operands agree.  They are
+// the keys 4 h + {0..3} and 8 + 4 h + {0..3} of a block of 16, which registers 8 s .. 8 s + 7 of
+// the scores hold.  V^T's lanes read the same keys of one column with ds_read_b64_tr_b16.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "bsm_attention_launch.hpp"
+
+namespace bsm_att {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+// 16-byte accesses at any element boundary
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
+typedef f32x4 f32x4_any __attribute__((aligned(4)));
+
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.69314718055994530942f;
+constexpr int kWave = 64;
+constexpr int kRows = 32;  // rows of the result per wave
+constexpr float kInf = __builtin_huge_valf();
+
+// ------------------------------------------------------------------------------- LDS tiles
+// A tile is ROWS x D bf16, row after row, in 16-byte chunks whose place in the row is permuted
+// (an exclusive or with bits of the row).  Fragments are read two ways: 16 consecutive rows at one
+// chunk (row_frag), and 4 consecutive rows at 4 neighbouring chunks (col_frag); with these bits
+// both touch every one of the 64 banks once per 256 bytes.
+template <int D>
+struct Tile {
+    static_assert(D == 64 || D == 128, "head dimensions are padded to 64 or 128");
+    static constexpr int kChunks = D / 8;
+    __device__ static __forceinline__ int place(int row, int chunk) {
+        const int f = D == 128 ? ((row & 3) << 2) | ((row >> 2) & 3) : (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
+        return row * kChunks + (chunk ^ f);
+    }
+    // lane (li, h): element 16 step + 8 h .. + 7 of `row`
+    __device__ static __forceinline__ bf16x8 row_frag(const uint16_t* lds, int row, int step, int h) {
+        return *reinterpret_cast<const bf16x8*>(lds + 8 * place(row, 2 * step + h));
+    }
+    // lane (li, h): column 32 t + li of rows r0 + 4 h + {0..3} and r0 + 8 + 4 h + {0..3}; r0 a
+    // multiple of 16.  ds_read_b64_tr_b16 works in groups of 16 lanes: lane s points at row s / 4,
+    // columns 4 (s % 4) .. + 3 of a 4 x 16 block and receives the block's column s.
+    __device__ static __forceinline__ bf16x8 col_frag(const uint16_t* lds, int r0, int t, int lane) {
+        const int g = lane >> 4, s = lane & 15;
+        const int row = r0 + 4 * (g >> 1) + (s >> 2), col = 32 * t + 16 * (g & 1) + 4 * (s & 3);
+        const uint16_t* p0 = lds + 8 * place(row, col >> 3) + (col & 7);
+        const uint16_t* p1 = lds + 8 * place(row + 8, col >> 3) + (col & 7);
+        union {
+            i16x4 half[2];
+            bf16x8 all;
+        } u;
+        u.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)p0);
+        u.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)p1);
+        return u.all;
+    }
+};
+
+// The pieces of a ROWS x D tile that one of THREADS threads carries from memory to LDS.  Rows and
+// chunks that do not exist are zero (a masked probability times what lies there must be zero).
+template <int D, int ROWS, int THREADS>
+struct Stage {
+    static constexpr int kN = ROWS * Tile<D>::kChunks / THREADS;
+    static_assert(kN >= 1 && ROWS * Tile<D>::kChunks % THREADS == 0, "");
+    u32x4 r[kN];
+    __device__ static __forceinline__ int row(int tid, int j) { return (tid + THREADS * j) / Tile<D>::kChunks; }
+    __device__ static __forceinline__ int chunk(int tid) { return tid % Tile<D>::kChunks; }
+    // `rows` of the tile exist; `p` is its first row
+    __device__ __forceinline__ void load(int tid, const uint16_t* p, int64_t stride, int rows, int chunks) {
+        const int c = chunk(tid);
+#pragma unroll
+        for (int j = 0; j < kN; ++j) {
+            const int i = row(tid, j);
+            r[j] = u32x4{0, 0, 0, 0};
+            if (i < rows && c < chunks) r[j] = *reinterpret_cast<const u32x4_any*>(p + i * stride + 8 * c);
+        }
+    }
+    __device__ __forceinline__ void store(int tid, uint16_t* lds) const {
+        const int c = chunk(tid);
+#pragma unroll
+        for (int j = 0; j < kN; ++j) *reinterpret_cast<u32x4*>(lds + 8 * Tile<D>::place(row(tid, j), c)) = r[j];
+    }
+};
+
+// The second operand of a product whose columns are 32 rows of a matrix in memory: lane (li, h)
+// holds elements 16 step + 8 h .. + 7 of its row; zero where the row does not exist.
+template <int D>
+struct RowOperand {
+    bf16x8 f[D / 16];
+    __device__ __forceinline__ void load(const uint16_t* row, bool live, int h, int chunks) {
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) {
+            u32x4 v = {0, 0, 0, 0};
+            if (live && 2 * s + h < chunks) v = *reinterpret_cast<const u32x4_any*>(row + 8 * (2 * s + h));
+            f[s] = __builtin_bit_cast(bf16x8, v);
+        }
+    }
+};
+
+__device__ __forceinline__ f32x16 zero16() {
+    f32x16 z;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) z[i] = 0.0f;
+    return z;
+}
+
+__device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+
+// 32 rows of the tile (from row r0) times the operand's 32 rows: lane (li, h) gets column li
+// (operand row) and tile rows r0 + 8 (i / 4) + 4 h + i % 4.
+template <int D>
+__device__ __forceinline__ f32x16 row_product(const uint16_t* lds, int r0, const RowOperand<D>& q, int lane) {
+    f32x16 acc = zero16();
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) acc = mfma(Tile<D>::row_frag(lds, r0 + (lane & 31), s, lane >> 5), q.f[s], acc);
+    return acc;
+}
+
+// Registers 8 s .. 8 s + 7 rounded to bf16 (nearest even): probabilities and score gradients are
+// rounded once, as operands of the next product, whose sums stay in fp32.
+__device__ __forceinline__ bf16x8 half_operand(const f32x16& x, int s) {
+    bf16x8 v;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = static_cast<__bf16>(x[8 * s + e]);
+    return v;
+}
+
+// acc[t] += (columns 32 t .. of tile rows r0 .. r0 + 31)^T times x: lane li keeps its column of x,
+// rows 32 t + 8 (i / 4) + 4 h + i % 4 of the tile's columns.
+template <int D>
+__device__ __forceinline__ void col_product(f32x16 (&acc)[D / 32], const uint16_t* lds, int r0, const f32x16& x, int lane) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        const bf16x8 b = half_operand(x, s);
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t) acc[t] = mfma(Tile<D>::col_frag(lds, r0 + 16 * s, t, lane), b, acc[t]);
+    }
+}
+
+// Value of the other half of the wave (lanes l and l + 32 exchanged).
+__device__ __forceinline__ float other_half(float v) {
+    return __shfl_xor(v, 32, 64);
+}
+
+// Index along the tile's rows of register i in half h.
+__device__ __forceinline__ constexpr int reg_row(int i) { return 8 * (i >> 2) + (i & 3); }
+
+// Columns 32 t .. 32 t + 31 of lane li's row of the result, f * acc, as bf16 (nearest even): the two
+// halves of a wave exchange 4-element groups so that each stores 16 bytes.
+__device__ __forceinline__ void store_block(uint16_t* row, bool live, const f32x16& acc, float f, int t, int h, int chunks) {
+#pragma unroll
+    for (int g = 0; g < 4; g += 2) {
+        unsigned int a[2], b[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const bf16x2 va = {static_cast<__bf16>(f * acc[4 * g + 2 * e]), static_cast<__bf16>(f * acc[4 * g + 2 * e + 1])};
+            const bf16x2 vb = {static_cast<__bf16>(f * acc[4 * g + 4 + 2 * e]), static_cast<__bf16>(f * acc[4 * g + 5 + 2 * e])};
+            a[e] = __builtin_bit_cast(unsigned int, va);
+            b[e] = __builtin_bit_cast(unsigned int, vb);
+        }
+        const auto p0 = __builtin_amdgcn_permlane32_swap(a[0], b[0], false, false);
+        const auto p1 = __builtin_amdgcn_permlane32_swap(a[1], b[1], false, false);
+        const int c = 4 * t + g + h;
+        const u32x4 v = {p0[0], p1[0], p0[1], p1[1]};
+        if (live && c < chunks) *reinterpret_cast<u32x4_any*>(row + 8 * c) = v;
+    }
+}
+template <int D>
+__device__ __forceinline__ void store_row(uint16_t* row, bool live, const f32x16 (&acc)[D / 32], float f, int h, int chunks) {
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t) store_block(row, live, acc[t], f, t, h, chunks);
+}
+
+// Barrier that orders the workgroup's LDS accesses and leaves loads from memory in flight.
+__device__ __forceinline__ void lds_barrier() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// ------------------------------------------------------------------------- online softmax
+// One pass over the keys for 32 query rows, row li in lanes li and li + 32: m is the reference
+// that the exponents of a row are taken from, in log2 units of the scaled scores, l the lane's
+// part of the row's sum, o the unnormalised output.  m is the row's maximum when it was last
+// moved; it moves when a tile exceeds it by more than kSlack (then l and o are rescaled), so
+// that probabilities stay below 2^kSlack, which neither l nor o in fp32 nor the rounding of P to
+// bf16, which is relative, minds.
+constexpr float kSlack = 8.0f;
+
+template <int D>
+struct Online {
+    f32x16 o[D / 32];
+    float m, l;
+
+    __device__ __forceinline__ void init() {
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t) o[t] = zero16();
+        m = -kInf;
+        l = 0.0f;
+    }
+    // Takes KT blocks of 32 keys whose raw scores are s (column li, this half's 16 keys of each
+    // block, -inf where masked); c = scale * log2(e) > 0.  s becomes the probabilities.
+    template <int KT>
+    __device__ __forceinline__ void weigh(f32x16 (&s)[KT], float c) {
+        float top = s[0][0];
+#pragma unroll
+        for (int k = 0; k < KT; ++k)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[k][i]);
+        top = fmaxf(top, other_half(top)) * c;
+        // (also where m is still -inf; a NaN leaves m as it is and reaches l below)
+        if (__any(top > m + kSlack)) {
+            const float next = fmaxf(m, top);
+            const float f = next == -kInf ? 1.0f : __builtin_amdgcn_exp2f(m - next);
+            m = next;
+            l *= f;
+#pragma unroll
+            for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[t][i] *= f;
+        }
+        const float ref = m == -kInf ? 0.0f : m;
+        float sum = 0.0f;
+#pragma unroll
+        for (int k = 0; k < KT; ++k)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[k][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k][i], c, -ref));
+                sum += s[k][i];
+            }
+        l += sum;
+    }
+    __device__ __forceinline__ float row_sum() const { return l + other_half(l); }
+    // natural-log statistic of a row with sum `total`
+    __device__ __forceinline__ float statistic(float total) const {
+        return total == 0.0f ? -kInf : (m + __builtin_amdgcn_logf(total)) * kLn2;
+    }
+};
+
+// Scores of keys that the row does not see become -inf: `first` is the key of register 0 in half 0
+// of the block, keys lo .. hi are seen.
+__device__ __forceinline__ void mask_block(f32x16& s, int first, int h, int lo, int hi) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const int j = first + 4 * h + reg_row(i);
+        s[i] = j >= lo && j <= hi ? s[i] : -kInf;
+    }
+}
+
+}  // namespace bsm_att

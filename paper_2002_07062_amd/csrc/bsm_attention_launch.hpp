@@ -1,0 +1,100 @@
+// Attention launches: what the C-ABI layer hands to the kernels (internal).
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+namespace bsm_att {
+
+// One piece of work of a plan: 128 rows (kTileRows) of one head of one sequence, query rows for the
+// forward pass and dq, key rows for dk and dv.  A unit without rows (rows == 0) does nothing.
+struct Unit {
+    int64_t q_start, kv_start;  // the sequence's first row in the caller's tensors
+    int64_t lse_row;            // its first row in the compact numbering of the plan
+    int32_t seq, head;          // head: query head, or key/value head
+    int32_t first, rows;        // the unit's rows within the sequence
+    int32_t q_len, kv_len;
+};
+static_assert(sizeof(Unit) == 48, "");
+
+constexpr int kTileRows = 128;
+
+// A caller's tensor: element (b, row, head, d) at p + b seq + row row + head head + d.
+struct Heads {
+    uint16_t* p;
+    int64_t seq, row, head;
+};
+
+struct Mask {
+    int32_t causal, window;  // window 0: none
+};
+
+struct SequenceArgs {
+    Heads q, k, v, o, dout, dq, dk, dv;
+    float* lse;       // [heads_q][total_q]
+    float* delta;     // [heads_q][total_q]: sum of dout * o over a row (backward)
+    int64_t total_q;
+    int32_t group;    // query heads per key/value head
+    int32_t dim;
+    Mask mask;
+    float scale;
+};
+
+hipError_t launch_attention(const SequenceArgs& a, const Unit* units, int64_t n, hipStream_t stream);
+// dq (and delta), then dk and dv, which read delta
+hipError_t launch_attention_backward(const SequenceArgs& a, const Unit* q_units, int64_t n_q, const Unit* kv_units,
+                                     int64_t n_kv, hipStream_t stream);
+
+// ------------------------------------------------------------------------------ paged cache
+struct Cache {
+    uint16_t *k, *v;
+    int64_t page, row, head;  // strides in elements
+    int64_t n_pages;
+    int32_t page_size, heads, dim;
+};
+
+struct PagedArgs {
+    Cache cache;
+    Heads q, o;               // seq strides are not used: rows are token indices
+    const int32_t* table;     // [batch][width]
+    const int32_t* q_start;   // [batch + 1]
+    const int32_t* kv_len;    // [batch]
+    int64_t batch, tokens;
+    int32_t width, max_q;
+    int32_t group;
+    int32_t window;
+    float scale;
+    // how the work is cut, from bounds on the lengths alone
+    int32_t tile_rows;        // 32 (the four waves take turns at the keys) or 128
+    int32_t tiles;            // per request and key/value head
+    int32_t splits;           // pieces of the key axis
+    int32_t split_keys;       // keys of a piece, a multiple of kKeyTile
+    float* part;              // splits > 1: pieces' outputs and statistics
+};
+
+constexpr int kKeyTile = 128;
+
+hipError_t launch_attention_paged(const PagedArgs& a, hipStream_t stream);
+
+struct SlotArgs {
+    const int32_t *cached, *fresh;
+    int64_t batch;
+    int32_t page_size, width;
+    int64_t n_pages;
+    int32_t* table;           // [batch][width]
+    const int32_t* free_pages;
+    int64_t free_cap;         // entries of free_pages
+    const int32_t* n_free;
+    int32_t *q_start, *kv_len;
+    int64_t* slots;
+    int64_t n_slots;
+    int32_t* taken;           // [2]
+};
+
+hipError_t launch_cache_slots(const SlotArgs& a, int n_cu, hipStream_t stream);
+
+hipError_t launch_cache_append(const Cache& c, const Heads& k, const Heads& v, const int64_t* slots, int64_t tokens,
+                               int n_cu, hipStream_t stream);
+
+}  // namespace bsm_att

@@ -1,0 +1,170 @@
+#include "bsm_attention_plan.hpp"
+
+#include <algorithm>
+#include <numeric>
+
+namespace bsm_att {
+namespace {
+
+constexpr int kStep = 64;  // keys or query rows that a workgroup takes at a time
+
+bool any_shared(const std::vector<int64_t>& start, const std::vector<int32_t>& len) {
+    std::vector<std::pair<int64_t, int64_t>> spans;
+    for (size_t b = 0; b < start.size(); ++b)
+        if (len[b] > 0) spans.emplace_back(start[b], start[b] + len[b]);
+    std::sort(spans.begin(), spans.end());
+    for (size_t i = 1; i < spans.size(); ++i)
+        if (spans[i].first < spans[i - 1].second) return true;
+    return false;
+}
+
+int64_t fill(const int64_t* given, const std::vector<int32_t>& len, std::vector<int64_t>* start, int64_t* end, bool* shared) {
+    int64_t total = 0;
+    *end = 0;
+    start->resize(len.size());
+    for (size_t b = 0; b < len.size(); ++b) {
+        (*start)[b] = given ? given[b] : total;
+        total += len[b];
+        if (len[b] > 0) *end = std::max(*end, (*start)[b] + len[b]);
+    }
+    *shared = given && any_shared(*start, len);
+    return total;
+}
+
+int64_t up_to(int64_t n) { return n * (n + 1) / 2; }  // 1 + .. + n
+
+// Pairs that the mask leaves: row i of n sees min(p + 1, window) keys, p = i + m - n, none if p < 0.
+int64_t visible(int64_t n, int64_t m, Mask mask) {
+    if (!mask.causal) return n * m;
+    const int64_t lo = std::max<int64_t>(0, m - n), hi = m;  // rows see lo + 1 .. hi keys (those that see some)
+    const int64_t w = mask.window > 0 ? mask.window : hi;
+    if (w >= hi) return up_to(hi) - up_to(lo);
+    if (w <= lo) return (hi - lo) * w;
+    return up_to(w) - up_to(lo) + (hi - w) * w;
+}
+
+// Steps of the other axis that a unit of rows first .. first + rows - 1 takes.
+int64_t query_steps(const Sequences& s, int64_t b, int64_t first, int64_t rows) {
+    int64_t lo = 0, hi = s.kv_len[b];
+    if (s.mask.causal) {
+        const int64_t off = static_cast<int64_t>(s.kv_len[b]) - s.q_len[b];
+        hi = std::min<int64_t>(hi, first + rows + off);
+        if (s.mask.window > 0) lo = std::max<int64_t>(0, first + off - s.mask.window + 1);
+    }
+    return hi > lo ? (hi - lo / kStep * kStep + kStep - 1) / kStep : 0;
+}
+int64_t key_steps(const Sequences& s, int64_t b, int64_t first, int64_t rows) {
+    int64_t lo = 0, hi = s.q_len[b];
+    if (s.mask.causal) {
+        const int64_t off = static_cast<int64_t>(s.kv_len[b]) - s.q_len[b];
+        lo = std::max<int64_t>(0, first - off);
+        if (s.mask.window > 0) hi = std::min<int64_t>(hi, first + rows - 1 + s.mask.window - off);
+    }
+    return hi > lo ? (hi - lo / kStep * kStep + kStep - 1) / kStep * (s.heads_q / s.heads_kv) : 0;
+}
+
+struct Costed {
+    Unit unit;
+    int64_t cost, kv_head;  // kv_head: index of the (sequence, key/value head) whose rows it reads
+};
+
+std::vector<Unit> order(std::vector<Costed>& units, bsm_schedule schedule, int n_xcd, int64_t kv_heads) {
+    auto longest_first = [&](std::vector<int64_t>& index) {
+        std::stable_sort(index.begin(), index.end(), [&](int64_t x, int64_t y) { return units[x].cost > units[y].cost; });
+    };
+    std::vector<Unit> out;
+    if (schedule != BSM_SCHED_XCD) {
+        std::vector<int64_t> index(units.size());
+        std::iota(index.begin(), index.end(), 0);
+        if (schedule == BSM_SCHED_BALANCED) longest_first(index);
+        out.reserve(units.size());
+        for (int64_t i : index) out.push_back(units[i].unit);
+        return out;
+    }
+    // the costliest key/value head goes to the least loaded XCD, and so on
+    std::vector<int64_t> cost(kv_heads, 0), by_cost(kv_heads), home(kv_heads), load(n_xcd, 0);
+    for (const Costed& c : units) cost[c.kv_head] += c.cost;
+    std::iota(by_cost.begin(), by_cost.end(), 0);
+    std::stable_sort(by_cost.begin(), by_cost.end(), [&](int64_t x, int64_t y) { return cost[x] > cost[y]; });
+    for (int64_t k : by_cost) {
+        home[k] = std::min_element(load.begin(), load.end()) - load.begin();
+        load[home[k]] += cost[k];
+    }
+    std::vector<std::vector<int64_t>> lists(n_xcd);
+    for (size_t i = 0; i < units.size(); ++i) lists[home[units[i].kv_head]].push_back(static_cast<int64_t>(i));
+    size_t longest = 0;
+    for (auto& list : lists) {
+        longest_first(list);
+        longest = std::max(longest, list.size());
+    }
+    Unit none{};
+    out.reserve(longest * n_xcd);
+    for (size_t i = 0; i < longest; ++i)
+        for (int x = 0; x < n_xcd; ++x) out.push_back(i < lists[x].size() ? units[lists[x][i]].unit : none);
+    while (!out.empty() && out.back().rows == 0) out.pop_back();
+    return out;
+}
+
+}  // namespace
+
+void finish_sequences(Sequences* s, const int64_t* q_start, const int64_t* kv_start) {
+    s->total_q = fill(q_start, s->q_len, &s->q_start, &s->q_end, &s->q_shared);
+    s->total_kv = fill(kv_start, s->kv_len, &s->kv_start, &s->kv_end, &s->kv_shared);
+    s->pairs = 0;
+    for (int64_t b = 0; b < s->batch; ++b) s->pairs += visible(s->q_len[b], s->kv_len[b], s->mask);
+}
+
+std::vector<Unit> query_units(const Sequences& s, bsm_schedule schedule, int n_xcd) {
+    std::vector<Costed> units;
+    const int group = s.heads_q / s.heads_kv;
+    int64_t lse_row = 0;
+    for (int64_t b = 0; b < s.batch; ++b) {
+        for (int head = 0; head < s.heads_q; ++head)
+            for (int64_t first = 0; first < s.q_len[b]; first += kTileRows) {
+                const int64_t rows = std::min<int64_t>(kTileRows, s.q_len[b] - first);
+                units.push_back({{s.q_start[b], s.kv_start[b], lse_row, static_cast<int32_t>(b), head,
+                                  static_cast<int32_t>(first), static_cast<int32_t>(rows), s.q_len[b], s.kv_len[b]},
+                                 2 + query_steps(s, b, first, rows), b * s.heads_kv + head / group});
+            }
+        lse_row += s.q_len[b];
+    }
+    return order(units, schedule, n_xcd, s.batch * s.heads_kv);
+}
+
+std::vector<Unit> key_units(const Sequences& s, bsm_schedule schedule, int n_xcd) {
+    std::vector<Costed> units;
+    int64_t lse_row = 0;
+    for (int64_t b = 0; b < s.batch; ++b) {
+        for (int head = 0; head < s.heads_kv; ++head)
+            for (int64_t first = 0; first < s.kv_len[b]; first += kTileRows) {
+                const int64_t rows = std::min<int64_t>(kTileRows, s.kv_len[b] - first);
+                units.push_back({{s.q_start[b], s.kv_start[b], lse_row, static_cast<int32_t>(b), head,
+                                  static_cast<int32_t>(first), static_cast<int32_t>(rows), s.q_len[b], s.kv_len[b]},
+                                 2 + key_steps(s, b, first, rows), b * s.heads_kv + head});
+            }
+        lse_row += s.q_len[b];
+    }
+    return order(units, schedule, n_xcd, s.batch * s.heads_kv);
+}
+
+PagedCut cut_paged(int64_t batch, int64_t tokens, int32_t heads_kv, int32_t group, int32_t dim, int32_t max_q,
+                   int32_t max_kv, int n_cu) {
+    PagedCut c{};
+    const int64_t rows = std::min<int64_t>(max_q, tokens) * group;
+    c.tile_rows = rows <= 32 ? 32 : kTileRows;
+    c.tiles = static_cast<int32_t>(std::max<int64_t>(1, (rows + c.tile_rows - 1) / c.tile_rows));
+    // Two workgroups fit a CU.  Requests differ in length, so there are pieces for eight rounds of
+    // them where the axis is long enough: short pieces even out what long requests take.
+    const int64_t units = std::max<int64_t>(1, batch * heads_kv * c.tiles);
+    const int64_t want = (8 * 2 * static_cast<int64_t>(n_cu) + units - 1) / units;
+    const int64_t keys = std::max<int64_t>(1, max_kv), most = (keys + 255) / 256;
+    const int64_t splits = std::max<int64_t>(1, std::min(want, most));
+    const int64_t each = ((keys + splits - 1) / splits + kKeyTile - 1) / kKeyTile * kKeyTile;
+    c.split_keys = static_cast<int32_t>(each);
+    c.splits = static_cast<int32_t>((keys + each - 1) / each);
+    const int padded = dim <= 64 ? 64 : 128;
+    c.part_floats = c.splits > 1 ? units * c.splits * c.tile_rows * (padded + 2) : 0;
+    return c;
+}
+
+}  // namespace bsm_att

@@ -1,0 +1,41 @@
+// Host planner of attention over ragged sequences: sequence lengths -> work units in the order of
+// the schedule.  Pure C++17, no HIP runtime calls.
+#pragma once
+
+#include <cstdint>
+#include <vector>
+
+#include "bsm.h"
+#include "bsm_attention_launch.hpp"
+
+namespace bsm_att {
+
+struct Sequences {
+    int64_t batch = 0;
+    std::vector<int32_t> q_len, kv_len;
+    std::vector<int64_t> q_start, kv_start;  // first rows in the operands
+    int32_t heads_q = 1, heads_kv = 1, dim = 8;
+    Mask mask{0, 0};
+    int64_t total_q = 0, total_kv = 0;
+    int64_t q_end = 0, kv_end = 0;           // largest row + 1
+    bool q_shared = false, kv_shared = false;  // some row belongs to two sequences
+    int64_t pairs = 0;
+};
+
+// Fills the starts (packed where null) and the totals from the lengths.
+void finish_sequences(Sequences* s, const int64_t* q_start, const int64_t* kv_start);
+
+// Units of 128 query rows (forward pass, dq) or of 128 keys (dk, dv), in launch order; the unit of
+// workgroup w is expected to run on XCD w mod n_xcd.
+std::vector<Unit> query_units(const Sequences& s, bsm_schedule schedule, int n_xcd);
+std::vector<Unit> key_units(const Sequences& s, bsm_schedule schedule, int n_xcd);
+
+// How attention over a paged cache is cut.
+struct PagedCut {
+    int32_t tile_rows, tiles, splits, split_keys;
+    int64_t part_floats;
+};
+PagedCut cut_paged(int64_t batch, int64_t tokens, int32_t heads_kv, int32_t group, int32_t dim, int32_t max_q,
+                   int32_t max_kv, int n_cu);
+
+}  // namespace bsm_att

@@ -1,0 +1,272 @@
+"""Attention of ragged sequences and its gradient against the fp64 oracle, through the C ABI."""
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2002_07062_amd as bsm
+from attention_util import Batch, check_backward, check_forward
+
+pytestmark = pytest.mark.gpu
+
+# q_len, kv_len (None: the same), query heads, kv heads, head dim, causal, window, layout
+CASES = [
+    ([1], None, 1, 1, 64, False, 0, "packed"),
+    ([64, 64], None, 2, 2, 64, False, 0, "packed"),
+    ([31, 32, 33, 1], None, 2, 1, 64, True, 0, "packed"),
+    ([63, 64, 65, 127, 128, 129], None, 2, 2, 128, True, 0, "packed"),
+    ([200, 77], None, 4, 2, 128, False, 0, "fused"),
+    ([300, 1, 150], None, 4, 1, 64, True, 0, "fused"),
+    ([5, 130], [90, 333], 2, 2, 80, True, 0, "packed"),      # a prefix before the queries
+    ([130, 40], [70, 40], 2, 1, 64, True, 0, "packed"),      # more queries than keys: rows that see nothing
+    ([17, 0, 20], [40, 30, 0], 2, 2, 64, False, 0, "packed"),  # no queries; no keys
+    ([17, 0, 20], [40, 30, 0], 3, 3, 128, True, 0, "shifted"),
+    ([200, 90], None, 2, 2, 64, True, 1, "packed"),          # every row sees itself alone
+    ([300, 129], [310, 200], 2, 1, 128, True, 70, "packed"),
+    ([100, 260], None, 3, 3, 8, True, 33, "packed"),
+    ([100, 37], None, 2, 2, 24, False, 0, "padded"),
+    ([66, 150], [150, 151], 8, 2, 96, True, 0, "padded"),
+    ([140, 33], None, 4, 4, 72, True, 0, "heads_first"),
+    ([64, 129], [200, 64], 6, 2, 120, False, 0, "heads_first"),
+    ([95, 96, 97], None, 5, 1, 40, True, 64, "shifted"),
+    ([513], None, 1, 1, 128, True, 0, "packed"),
+]
+
+
+def _name(c):
+    return "-".join(str(x) for x in (c[0], c[1] or "", *c[2:])).replace(" ", "")
+
+
+def _batch(case, seed=3):
+    q_len, kv_len, hq, hk, d, _, _, layout = case
+    return Batch(q_len, kv_len or q_len, hq, hk, d, layout, seed)
+
+
+def _run(batch, causal, window, schedule="balanced", scale=None, lse=True):
+    plan = bsm.bsm_attention_plan_create(**batch.plan_args(causal, window, schedule))
+    o = batch.empty("q")
+    rows = torch.full((batch.hq, sum(batch.q_len)), 7.0, device="cuda") if lse else None
+    bsm.bsm_attention_execute(plan, batch.q, batch.k, batch.v, o, lse=rows, scale=scale)
+    torch.cuda.synchronize()
+    return plan, o, rows
+
+
+@pytest.mark.parametrize("case", CASES, ids=_name)
+def test_forward_matches_the_oracle(case):
+    batch, scale = _batch(case), 1 / np.sqrt(case[4])
+    plan, o, lse = _run(batch, case[5], case[6])
+    check_forward(batch, o, lse, float(np.float32(scale)), case[5], case[6])
+    plan.destroy()
+
+
+@pytest.mark.parametrize("case", CASES, ids=_name)
+def test_backward_matches_the_oracle(case):
+    batch, scale = _batch(case, 5), float(np.float32(1 / np.sqrt(case[4])))
+    plan, o, lse = _run(batch, case[5], case[6])
+    dout = batch.operand("q")
+    dq, dk, dv = batch.empty("q"), batch.empty("kv"), batch.empty("kv")
+    bsm.bsm_attention_backward(plan, batch.q, batch.k, batch.v, o, lse, dout, dq, dk, dv)
+    torch.cuda.synchronize()
+    check_backward(batch, o, lse, dout, dq, dk, dv, scale, case[5], case[6])
+    plan.destroy()
+
+
+@pytest.mark.parametrize("case", [CASES[3], CASES[5], CASES[11]], ids=_name)
+def test_schedules_and_repeats_give_the_same_bits(case):
+    batch = _batch(case, 7)
+    dout = batch.operand("q")
+    seen = []
+    for schedule in ("balanced", "xcd", "rr", "balanced"):
+        plan, o, lse = _run(batch, case[5], case[6], schedule)
+        grads = [batch.empty("q"), batch.empty("kv"), batch.empty("kv")]
+        bsm.bsm_attention_backward(plan, batch.q, batch.k, batch.v, o, lse, dout, *grads)
+        torch.cuda.synchronize()
+        seen.append([x.contiguous().view(torch.int16) for x in (o, *grads)] + [lse.view(torch.int32)])
+        plan.destroy()
+    for other in seen[1:]:
+        for x, y in zip(seen[0], other):
+            assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("scale", [1e-3, 1.0, 8.0])
+def test_scales(scale):
+    """Flat rows, and rows that one key takes almost whole (scores of several hundred)."""
+    batch = Batch([150, 70], [150, 90], 2, 1, 64, "packed", 11, sigma=1.0)
+    plan, o, lse = _run(batch, True, 0, scale=scale)
+    check_forward(batch, o, lse, float(np.float32(scale)), True)
+    dout = batch.operand("q")
+    grads = [batch.empty("q"), batch.empty("kv"), batch.empty("kv")]
+    bsm.bsm_attention_backward(plan, batch.q, batch.k, batch.v, o, lse, dout, *grads, scale=scale)
+    check_backward(batch, o, lse, dout, *grads, float(np.float32(scale)), True)
+    plan.destroy()
+
+
+def test_rising_scores_move_the_reference():
+    """Keys whose scores grow by steps of 1 to 40 along the sequence, so that a row's reference
+    moves at some tiles and not at others."""
+    batch = Batch([80], [700], 1, 1, 64, "packed", 13, sigma=0.0)
+    j = torch.arange(700, dtype=torch.float32)
+    batch.q[:, 0, 0] = torch.linspace(0.25, 4.0, 80).to(torch.bfloat16).cuda()
+    batch.k[:, 0] = 0
+    batch.k[:, 0, 0] = (j // 64 * torch.linspace(0.1, 10, 700)).to(torch.bfloat16).cuda()
+    plan, o, lse = _run(batch, False, 0, scale=1.0)
+    check_forward(batch, o, lse, 1.0, False)
+    plan.destroy()
+
+
+def test_scores_of_infinity():
+    """Scores of -inf take no weight, a row of nothing else is zero, +inf or NaN makes its row NaN;
+    other rows keep their values."""
+    batch = Batch([40], [70], 1, 1, 64, "packed", 17)
+    inf = float("inf")
+    batch.q[:, 0, 0] = 1.0
+    batch.k[:, 0, 0] = 0.0
+    batch.k[5, 0] = 0.0
+    batch.k[5, 0, 0] = -inf            # -inf for every query
+    plan, o, lse = _run(batch, False, 0)
+    check = Batch([40], [69], 1, 1, 64, "packed", 17)
+    keep = [j for j in range(70) if j != 5]
+    check.q, check.k, check.v = batch.q, batch.k[keep], batch.v[keep]
+    check_forward(check, o, lse, 0.125, False)
+    batch.k[:, 0] = 0.0
+    batch.k[:, 0, 0] = -inf
+    plan, o, lse = _run(batch, False, 0)
+    assert (o == 0).all() and (lse == -inf).all()
+    batch.k[:, 0, 0] = 0.0
+    batch.k[9, 0, 0] = inf             # +inf where q > 0, -inf where q < 0
+    batch.q[::2, 0, 0] = -1.0
+    plan, o, lse = _run(batch, False, 0)
+    assert torch.isnan(o[1::2]).all() and torch.isnan(lse[0, 1::2]).all()
+    assert torch.isfinite(o[::2].float()).all()
+
+
+def test_rows_that_see_nothing_take_no_gradient_whatever_they_hold():
+    batch = Batch([100], [60], 2, 1, 64, "packed", 19)
+    plan, o, lse = _run(batch, True, 0)
+    dout = batch.operand("q")
+    dout[:40] = float("nan")
+    batch.q[:40] = float("inf")
+    o[:40] = float("nan")
+    grads = [batch.empty("q"), batch.empty("kv"), batch.empty("kv")]
+    bsm.bsm_attention_backward(plan, batch.q, batch.k, batch.v, o, lse, dout, *grads)
+    torch.cuda.synchronize()
+    assert (grads[0][:40] == 0).all()
+    check_backward(batch, o, lse, dout, *grads, 0.125, True)
+    plan.destroy()
+
+
+def test_gradients_match_differences():
+    """Central differences of the fp64 forward pass along random directions."""
+    import oracle.attention as oa
+    batch = Batch([37], [50], 2, 1, 64, "packed", 23, sigma=1.0)
+    plan, o, lse = _run(batch, True, 0)
+    dout = batch.operand("q")
+    grads = [batch.empty("q"), batch.empty("kv"), batch.empty("kv")]
+    bsm.bsm_attention_backward(plan, batch.q, batch.k, batch.v, o, lse, dout, *grads)
+    q, k, v, do = (x.double().cpu().numpy() for x in (batch.q, batch.k, batch.v, dout))
+    got = [x.double().cpu().numpy() for x in grads]
+
+    def loss(q, k, v):
+        return sum((oa.forward(q[:, h], k[:, 0], v[:, 0], 0.125, True)[0] * do[:, h]).sum() for h in range(2))
+
+    rng = np.random.default_rng(1)
+    for i, x in enumerate((q, k, v)):
+        d = rng.standard_normal(x.shape)
+        step = 1e-5
+        args = [[q, k, v], [q, k, v]]
+        args[0][i], args[1][i] = x + step * d, x - step * d
+        want = (loss(*args[0]) - loss(*args[1])) / (2 * step)
+        # errors of the gradients' elements are independent roundings of about 2^-8, four deviations
+        tol = 4 * 2 ** -8 * np.sqrt(((got[i] * d) ** 2).sum()) + 1e-3 * abs(want)
+        assert abs((got[i] * d).sum() - want) <= tol
+    plan.destroy()
+
+
+def test_a_fused_gradient_tensor():
+    """dq, dk and dv as views of one tensor, like q, k and v."""
+    batch = Batch([90, 61], [90, 61], 4, 2, 64, "fused", 29)
+    plan, o, lse = _run(batch, True, 0)
+    dout = batch.operand("q")
+    x = torch.full((151, 8, 64), float("nan"), dtype=torch.bfloat16, device="cuda")
+    dq, dk, dv = x[:, :4], x[:, 4:6], x[:, 6:]
+    bsm.bsm_attention_backward(plan, batch.q, batch.k, batch.v, o, lse, dout, dq, dk, dv)
+    check_backward(batch, o, lse, dout, dq, dk, dv, 0.125, True)
+    plan.destroy()
+
+
+def test_shared_keys_and_values():
+    """Two sequences that read the same keys, and heads that read one by a stride of 0; their
+    gradients are refused in the shared rows and right in rows of their own."""
+    g = torch.Generator().manual_seed(31)
+    q = torch.randn((60, 4, 64), generator=g).to(torch.bfloat16).cuda()
+    kv = torch.randn((50, 1, 64), generator=g).to(torch.bfloat16).cuda()
+    wide = kv.expand(-1, 2, -1)
+    plan = bsm.bsm_attention_plan_create([30, 30], [50, 50], heads_q=4, heads_kv=2, head_dim=64, kv_start=[0, 0])
+    o, lse = torch.empty_like(q), torch.empty((4, 60), device="cuda")
+    bsm.bsm_attention_execute(plan, q, wide, wide, o, lse=lse)
+    batch = Batch([30, 30], [50, 50], 4, 2, 64, "packed", 1)
+    batch.q = q
+    batch.k = batch.v = torch.cat([wide, wide]).contiguous()
+    check_forward(batch, o, lse, 0.125, False)
+    dk = torch.empty((50, 2, 64), dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(bsm.BsmError) as e:
+        bsm.bsm_attention_backward(plan, q, wide, wide, o, lse, q, torch.empty_like(q), dk, torch.empty_like(dk))
+    assert e.value.status == bsm.BSM_ERR_INVALID_ARG
+    own = bsm.bsm_attention_plan_create([30, 30], [50, 50], heads_q=4, heads_kv=2, head_dim=64)
+    dout = batch.operand("q")
+    grads = [batch.empty("q"), batch.empty("kv"), batch.empty("kv")]
+    bsm.bsm_attention_backward(own, q, batch.k, batch.v, o, lse, dout, *grads)
+    check_backward(batch, o, lse, dout, *grads, 0.125, False)
+
+
+def test_two_streams_with_their_own_workspaces():
+    batches = [Batch([300, 120], [300, 120], 4, 2, 128, "packed", s) for s in (41, 42)]
+    plan, _, _ = _run(batches[0], True, 0)
+    streams = [torch.cuda.Stream() for _ in batches]
+    outs = []
+    for batch in batches:
+        outs.append([batch.empty("q"), torch.empty((4, 420), device="cuda"), batch.operand("q"),
+                     batch.empty("q"), batch.empty("kv"), batch.empty("kv"),
+                     torch.empty(plan.workspace_bytes, dtype=torch.uint8, device="cuda")])
+    torch.cuda.synchronize()
+    for batch, st, (o, lse, dout, dq, dk, dv, ws) in zip(batches, streams, outs):
+        bsm.bsm_attention_execute(plan, batch.q, batch.k, batch.v, o, lse=lse, stream=st)
+        bsm.bsm_attention_backward(plan, batch.q, batch.k, batch.v, o, lse, dout, dq, dk, dv, workspace=ws, stream=st)
+    torch.cuda.synchronize()
+    scale = float(np.float32(128 ** -0.5))
+    for batch, (o, lse, dout, dq, dk, dv, _) in zip(batches, outs):
+        check_forward(batch, o, lse, scale, True)
+        check_backward(batch, o, lse, dout, dq, dk, dv, scale, True)
+    plan.destroy()
+
+
+def test_a_captured_step_replays():
+    """Forward and backward in one captured graph, replayed after new inputs, with eager work in
+    between: every replay equals the eager result bit for bit."""
+    batch = Batch([130, 77], [130, 77], 4, 2, 64, "packed", 43)
+    plan = bsm.bsm_attention_plan_create(**batch.plan_args(True))
+    o, lse, dout = batch.empty("q"), torch.empty((4, 207), device="cuda"), batch.operand("q")
+    grads = [batch.empty("q"), batch.empty("kv"), batch.empty("kv")]
+
+    def step(ws=None):
+        bsm.bsm_attention_execute(plan, batch.q, batch.k, batch.v, o, lse=lse)
+        bsm.bsm_attention_backward(plan, batch.q, batch.k, batch.v, o, lse, dout, *grads, workspace=ws)
+
+    step()
+    torch.cuda.synchronize()
+    ws = torch.empty(plan.workspace_bytes, dtype=torch.uint8, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(ws)
+    for _ in range(3):
+        for x in (batch.q, batch.k, batch.v, dout):
+            x.copy_(torch.randn(x.shape, generator=batch.gen).to(torch.bfloat16))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [x.clone() for x in (o, lse, *grads)]
+        step()
+        torch.cuda.synchronize()
+        for x, y in zip(got, (o, lse, *grads)):
+            assert torch.equal(x, y)
+    del graph
+    plan.destroy()

@@ -1,0 +1,313 @@
+"""The paged key/value cache through the C ABI: slot maps bit for bit, appended tokens, attention of
+chunks and single tokens over the pages against the fp64 oracle, and a serving loop of all three."""
+
+import numpy as np
+import pytest
+import torch
+
+import oracle.attention as oa
+import paper_2002_07062_amd as bsm
+from attention_util import U, forward_bound, to64
+
+pytestmark = pytest.mark.gpu
+
+NAN = float("nan")
+
+
+def i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+class Cache:
+    """Pages in no order, NaN wherever no token of a request lies."""
+
+    def __init__(self, kv_len, page, hk, d, seed=0, extra=3, layout="page_first"):
+        g = torch.Generator().manual_seed(seed)
+        counts = [-(-n // page) for n in kv_len]
+        n_pages = sum(counts) + extra
+        shape = (n_pages, page, hk, d)
+        if layout == "heads_first":   # (pages, heads, page, dim)
+            self.k, self.v = (torch.full((n_pages, hk, page, d), NAN, dtype=torch.bfloat16).transpose(1, 2) for _ in "kv")
+        elif layout == "shifted":     # off every 16-byte boundary
+            n = int(np.prod(shape))
+            self.k, self.v = (torch.full((n + 5,), NAN, dtype=torch.bfloat16)[3:3 + n].view(shape) for _ in "kv")
+        else:
+            self.k, self.v = (torch.full(shape, NAN, dtype=torch.bfloat16) for _ in "kv")
+        order = torch.randperm(n_pages, generator=g).tolist()
+        self.table = torch.full((len(kv_len), max(counts, default=0) + 2), -1, dtype=torch.int32)
+        self.tokens = []              # (k, v) of every request, (kv_len, hk, d) fp64
+        for b, n in enumerate(kv_len):
+            pages = [order.pop() for _ in range(counts[b])]
+            self.table[b, :counts[b]] = torch.tensor(pages, dtype=torch.int32)
+            mine = []
+            for x in (self.k, self.v):
+                t = torch.randn((n, hk, d), generator=g).to(torch.bfloat16)
+                for j in range(n):
+                    x[pages[j // page], j % page] = t[j]
+                mine.append(to64(t))
+            self.tokens.append(mine)
+        if layout == "shifted":
+            n = int(np.prod(shape))
+            out = []
+            for x in (self.k, self.v):
+                y = torch.full((n + 5,), NAN, dtype=torch.bfloat16, device="cuda")
+                y[3:3 + n] = x.reshape(-1).cuda()
+                out.append(y[3:3 + n].view(shape))
+            self.k, self.v = out
+        else:
+            self.k, self.v = self.k.cuda(), self.v.cuda()
+        self.table = self.table.cuda()
+
+
+def _check(o, q, cache, new, kv_len, group, scale, window=0):
+    at = 0
+    for b, n in enumerate(new):
+        k, v = cache.tokens[b]
+        for h in range(q.shape[1]):
+            qq = to64(q[at:at + n, h])
+            ref, lse, p = oa.forward(qq, k[:, h // group], v[:, h // group], scale, True, window)
+            tol, _ = forward_bound(qq, k[:, h // group], v[:, h // group], scale, True, window, p, lse, ref)
+            err = np.abs(to64(o[at:at + n, h]) - ref)
+            assert (err <= tol).all(), f"request {b} head {h}: worst excess {(err - tol).max():.3e} at {np.argwhere(~(err <= tol))[:4].tolist()}"
+        at += n
+
+
+# new tokens, kv_len, page, query heads, kv heads, head dim, window, layout
+CASES = [
+    ([1], [1], 16, 1, 1, 64, 0, "page_first"),
+    ([1, 1, 1], [5, 64, 200], 16, 8, 2, 128, 0, "page_first"),
+    ([1, 1], [3000, 31], 16, 4, 4, 64, 0, "page_first"),       # pieces of the key axis
+    ([1, 1], [3000, 700], 24, 8, 1, 128, 0, "page_first"),
+    ([1, 2, 1], [1500, 90, 0], 1, 4, 2, 80, 0, "page_first"),  # a page per token; a request without keys
+    ([3, 1, 4], [700, 65, 4], 7, 6, 2, 96, 0, "heads_first"),
+    ([33, 1, 100], [33, 513, 400], 16, 4, 2, 64, 0, "page_first"),
+    ([130, 1, 0, 64], [900, 2000, 77, 64], 64, 8, 2, 128, 0, "page_first"),
+    ([60, 20], [30, 20], 32, 2, 2, 128, 0, "shifted"),         # rows before the first key
+    ([1, 1, 50], [1000, 20, 300], 16, 4, 1, 64, 100, "page_first"),
+    ([1, 2], [2500, 2049], 128, 2, 1, 128, 1, "heads_first"),
+    ([9, 5], [300, 400], 16, 5, 5, 8, 64, "shifted"),
+    ([1, 1], [600, 601], 16, 64, 1, 64, 0, "page_first"),      # a group of 64
+    ([300], [1800], 16, 3, 1, 128, 500, "page_first"),
+]
+
+
+def _name(c):
+    return "-".join(str(x) for x in c).replace(" ", "")
+
+
+@pytest.mark.parametrize("case", CASES, ids=_name)
+def test_paged_attention_matches_the_oracle(case):
+    new, kv_len, page, hq, hk, d, window, layout = case
+    cache = Cache(kv_len, page, hk, d, 3, layout=layout)
+    g = torch.Generator().manual_seed(4)
+    tokens = sum(new)
+    q = (2 * torch.randn((tokens + 2, hq, d), generator=g)).to(torch.bfloat16).cuda()
+    o = torch.full_like(q, NAN)
+    start = i32([0] + list(np.cumsum(new)))
+    scale = float(np.float32(d ** -0.5))
+    seen = []
+    for max_q, max_kv in ((max(new), max(kv_len)), (max(new), None), (max(new) + 40, 64)):
+        o.fill_(NAN)
+        bsm.bsm_attention_paged(q, cache.k, cache.v, cache.table, start, i32(kv_len), o, max_q=max_q, max_kv=max_kv, window=window)
+        torch.cuda.synchronize()
+        _check(o, q, cache, new, kv_len, hq // hk, scale, window)
+        assert torch.isnan(o[tokens:]).all(), "rows behind the last request were written"
+
+
+def test_bounds_keep_bad_lengths_and_pages_inside():
+    """Entries that name no page read as zeros, lengths past the table count up to it, starts past
+    the tokens are clamped, rows past max_q are left alone."""
+    cache = Cache([64, 64], 16, 1, 64, 9)
+    table = cache.table[:, :4].contiguous()
+    table[0, 1] = -7
+    table[0, 2] = 1 << 30
+    g = torch.Generator().manual_seed(5)
+    q = torch.randn((4, 1, 64), generator=g).to(torch.bfloat16).cuda()
+    o = torch.full_like(q, NAN)
+    bsm.bsm_attention_paged(q, cache.k, cache.v, table, i32([0, 3, 9]), i32([64, 1 << 30]), o, max_q=2)
+    torch.cuda.synchronize()
+    for x in cache.tokens[0]:
+        x[16:48] = 0
+    qq = to64(q[:3, 0])
+    for at, n, b in ((0, 3, 0), (3, 1, 1)):
+        k, v = (x[:, 0] for x in cache.tokens[b])
+        qq = to64(q[at:at + n, 0])
+        ref, lse, p = oa.forward(qq, k, v, 0.125, True)
+        tol, _ = forward_bound(qq, k, v, 0.125, True, 0, p, lse, ref)
+        err = np.abs(to64(o[at:at + n, 0]) - ref)[:2]
+        assert (err <= tol[:2]).all()
+    assert torch.isnan(o[2]).all(), "a row past max_q was written"
+
+
+def test_paged_attention_replays_with_new_lengths():
+    """A captured call whose lengths, table and chunk starts change between replays."""
+    cache = Cache([900, 40, 300], 16, 2, 64, 21)
+    g = torch.Generator().manual_seed(6)
+    q = torch.randn((8, 4, 64), generator=g).to(torch.bfloat16).cuda()
+    o = torch.full_like(q, NAN)
+    start, kv, table = i32([0, 1, 2, 3]), i32([900, 40, 300]), cache.table.clone()
+    ws = torch.empty(bsm.bsm_attention_paged_workspace(3, 8, 4, 2, 64, 4, 900), dtype=torch.uint8, device="cuda")
+
+    def call(w, out):
+        bsm.bsm_attention_paged(q, cache.k, cache.v, table, start, kv, out, max_q=4, max_kv=900, workspace=w)
+
+    call(ws, o)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(ws, o)
+    order = [0, 1, 2]
+    for new, lens, perm in (([1, 1, 1], [900, 40, 300], [0, 1, 2]), ([4, 1, 3], [40, 300, 900], [1, 2, 0]),
+                            ([1, 4, 0], [299, 77, 0], [2, 0, 1])):
+        start.copy_(i32([0] + list(np.cumsum(new))))
+        kv.copy_(i32(lens))
+        table.copy_(cache.table[perm])
+        o.fill_(NAN)
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = torch.full_like(q, NAN)
+        call(None, eager)
+        torch.cuda.synchronize()
+        assert torch.equal(o.view(torch.int16), eager.view(torch.int16))
+        at = 0
+        for b, n in enumerate(new):
+            for h in range(4):
+                k, v = (x[:lens[b], h // 2] for x in cache.tokens[perm[b]])
+                qq = to64(q[at:at + n, h])
+                ref, lse, p = oa.forward(qq, k, v, 0.125, True)
+                tol, _ = forward_bound(qq, k, v, 0.125, True, 0, p, lse, ref)
+                assert (np.abs(to64(o[at:at + n, h]) - ref) <= tol).all()
+            at += n
+    del graph, order
+
+
+# ---------------------------------------------------------------------------------------- slots
+def _slots(cached, fresh, page, n_pages, table, free, n_free, n_slots):
+    b = len(cached)
+    t = i32(table).view(b, -1) if b else torch.empty((0, 4), dtype=torch.int32, device="cuda")
+    q_start, kv_len = torch.full((b + 3,), -5, dtype=torch.int32, device="cuda"), torch.full((b + 2,), -5, dtype=torch.int32, device="cuda")
+    slots, taken = torch.full((n_slots,), -9, dtype=torch.int64, device="cuda"), i32([-5, -5, -5])
+    bsm.bsm_cache_slots(i32(cached), i32(fresh), page, n_pages, t, i32(free), i32([n_free]), q_start, kv_len, slots, taken)
+    torch.cuda.synchronize()
+    ref = oa.slots(cached, fresh, page, n_pages, np.asarray(table).reshape(b, t.shape[1]), free, n_free, n_slots)
+    assert q_start[:b + 1].tolist() == ref[0]
+    assert kv_len[:b].tolist() == ref[1]
+    assert np.array_equal(t.cpu().numpy(), ref[2])
+    assert np.array_equal(slots.cpu().numpy(), ref[3])
+    assert taken.tolist() == ref[4] + [-5]
+    assert (q_start[b + 1:] == -5).all() and (kv_len[b:] == -5).all()
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_slots_of_random_steps(seed):
+    rng = np.random.default_rng(seed)
+    b = int(rng.choice([0, 1, 3, 255, 256, 257, 700]))
+    page = int(rng.choice([1, 3, 16, 64]))
+    hi = int(rng.choice([1, 2, 40, 300]))
+    cached, fresh = rng.integers(0, 5 * page + 2, b), rng.integers(0, hi + 1, b)
+    if seed % 3 == 0 and b:
+        cached[rng.integers(0, b)] = -4
+        fresh[rng.integers(0, b)] = -1
+    cached, fresh = cached.tolist(), fresh.tolist()
+    need = sum(-(-(max(c, 0) + max(f, 0)) // page) + -(-max(c, 0) // page) for c, f in zip(cached, fresh))
+    n_pages = need + 10
+    width = max([-(-(max(c, 0) + max(f, 0)) // page) for c, f in zip(cached, fresh)], default=0) + 1
+    if seed % 4 == 1:
+        width = max(1, width // 2)
+    table = rng.integers(0, n_pages, (b, width))
+    free = rng.permutation(n_pages).tolist()
+    if seed % 4 == 2:
+        table[rng.integers(0, max(b, 1), 5) % max(b, 1), 0] = n_pages if b else 0
+        free[:3] = [-1, n_pages, 2**31 - 1]
+    n_free = n_pages if seed % 2 == 0 else need // 4
+    total = sum(max(f, 0) for f in fresh)
+    _slots(cached, fresh, page, n_pages, table.tolist(), free, n_free, total + 70 if seed % 5 else max(0, total - 3))
+
+
+def test_slots_bounds():
+    _slots([0, 0], [4, 4], 4, 8, [[-1], [-1]], [], 0, 8)                       # an empty free list
+    _slots([0, 0], [4, 4], 4, 8, [[-1], [-1]], [3], 1000, 8)                   # n_free past the list
+    _slots([2**31 - 1, 5], [2**31 - 1, 1], 4, 8, [[1, 2], [3, 4]], [0], 1, 4)  # lengths near 2^31
+    _slots([0], [0], 4, 8, [[-1]], [0], 1, 0)
+
+
+# --------------------------------------------------------------------------------------- append
+@pytest.mark.parametrize("tokens,page,hk,d,layout", [
+    (1, 16, 1, 8, "page_first"), (77, 16, 2, 64, "page_first"), (300, 24, 8, 128, "page_first"),
+    (50, 7, 3, 96, "heads_first"), (33, 1, 1, 40, "shifted")])
+def test_append_writes_the_slots_and_nothing_else(tokens, page, hk, d, layout):
+    g = torch.Generator().manual_seed(tokens)
+    n_pages = -(-tokens // page) + 4
+    cache = Cache([], page, hk, d, extra=n_pages, layout=layout)
+    slots = torch.randperm(n_pages * page, generator=g)[:tokens].cuda()
+    slots[tokens // 2] = -1
+    slots[tokens // 3] = n_pages * page
+    fused = torch.randn((tokens, 2 * hk, d), generator=g).to(torch.bfloat16).cuda()
+    k, v = fused[:, :hk], fused[:, hk:]
+    bsm.bsm_cache_append(k, v, slots, cache.k, cache.v)
+    torch.cuda.synchronize()
+    for x, y in ((k, cache.k), (v, cache.v)):
+        want = torch.full((n_pages * page, hk, d), NAN, dtype=torch.bfloat16, device="cuda")
+        ok = (slots >= 0) & (slots < n_pages * page)
+        want[slots[ok]] = x[ok]
+        assert torch.equal(want.view(torch.int16), y.contiguous().view(-1, hk, d).view(torch.int16))
+
+
+# ---------------------------------------------------------------------------------- all together
+def test_a_serving_loop():
+    """Prompts in chunks, then single tokens: every step takes its slots, writes its keys and values
+    and attends over the pages; the outputs are those of the whole sequences so far."""
+    g = torch.Generator().manual_seed(77)
+    hq, hk, d, page, n_pages, width = 4, 2, 64, 16, 64, 12
+    k_cache, v_cache = (torch.full((n_pages, page, hk, d), NAN, dtype=torch.bfloat16, device="cuda") for _ in "kv")
+    table = torch.full((3, width), -1, dtype=torch.int32, device="cuda")
+    free = torch.randperm(n_pages, generator=g).to(torch.int32).cuda()
+    cached = i32([0, 0, 0])
+    history = [[], [], []]
+    steps = [[40, 7, 0], [40, 1, 100], [13, 1, 1], [1, 1, 1], [1, 1, 1], [0, 1, 16]]
+    for fresh in steps:
+        t = sum(fresh)
+        qkv = torch.randn((t, hq + 2 * hk, d), generator=g).to(torch.bfloat16).cuda()
+        q, k, v = qkv[:, :hq], qkv[:, hq:hq + hk], qkv[:, hq + hk:]
+        q_start, kv_len = torch.empty(4, dtype=torch.int32, device="cuda"), torch.empty(3, dtype=torch.int32, device="cuda")
+        slots, taken = torch.empty(t, dtype=torch.int64, device="cuda"), i32([0, 0])
+        bsm.bsm_cache_slots(cached, i32(fresh), page, n_pages, table, free, i32([free.numel()]), q_start, kv_len, slots, taken)
+        bsm.bsm_cache_append(k, v, slots, k_cache, v_cache)
+        o = torch.full((t, hq, d), NAN, dtype=torch.bfloat16, device="cuda")
+        bsm.bsm_attention_paged(q, k_cache, v_cache, table, q_start, kv_len, o, max_q=max(fresh))
+        torch.cuda.synchronize()
+        pages, refused = taken.tolist()
+        assert refused == 0
+        free = free[pages:].contiguous()
+        cached = kv_len
+        at = 0
+        for b, n in enumerate(fresh):
+            history[b].append((to64(k[at:at + n]), to64(v[at:at + n])))
+            kk, vv = (np.concatenate([x[i] for x in history[b]]) for i in (0, 1))
+            for h in range(hq):
+                qq = to64(q[at:at + n, h])
+                ref, lse, p = oa.forward(qq, kk[:, h // 2], vv[:, h // 2], 0.125, True)
+                tol, _ = forward_bound(qq, kk[:, h // 2], vv[:, h // 2], 0.125, True, 0, p, lse, ref)
+                assert (np.abs(to64(o[at:at + n, h]) - ref) <= tol).all()
+            at += n
+    assert U == 2.0 ** -8
+
+
+def test_a_refused_request_comes_out_empty():
+    """The free list holds pages for the first request only: the second has no slots, its rows of the
+    output are zeros, and the cache holds nothing of it."""
+    hk, d, page = 1, 64, 16
+    k_cache, v_cache = (torch.full((4, page, hk, d), NAN, dtype=torch.bfloat16, device="cuda") for _ in "kv")
+    table = torch.full((2, 4), -1, dtype=torch.int32, device="cuda")
+    q_start, kv_len = torch.empty(3, dtype=torch.int32, device="cuda"), torch.empty(2, dtype=torch.int32, device="cuda")
+    slots, taken = torch.empty(40, dtype=torch.int64, device="cuda"), i32([0, 0])
+    bsm.bsm_cache_slots(i32([0, 0]), i32([20, 20]), page, 4, table, i32([2, 0, 1]), i32([3]), q_start, kv_len, slots, taken)
+    g = torch.Generator().manual_seed(1)
+    q, k, v = (torch.randn((40, 1, d), generator=g).to(torch.bfloat16).cuda() for _ in "qkv")
+    bsm.bsm_cache_append(k, v, slots, k_cache, v_cache)
+    o = torch.full_like(q, NAN)
+    bsm.bsm_attention_paged(q, k_cache, v_cache, table, q_start, kv_len, o, max_q=20)
+    torch.cuda.synchronize()
+    assert taken.tolist() == [2, 1] and kv_len.tolist() == [20, 0] and (slots[20:] == -1).all()
+    assert (o[20:] == 0).all() and torch.isfinite(o[:20].float()).all()
+    assert torch.isnan(k_cache[[1, 3]]).all()

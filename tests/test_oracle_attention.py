@@ -1,0 +1,245 @@
+"""Pins of the fp64 attention oracle, and the library's refusals of bad attention calls, which come
+before any HIP call (no GPU here)."""
+
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import oracle.attention as oa
+import paper_2002_07062_amd as bsm
+from paper_2002_07062_amd import attention as att
+
+TOPO = dict(n_xcd=8)
+
+
+# ------------------------------------------------------------------------------------ oracle
+@pytest.mark.parametrize("n,m,causal,window", [(7, 7, False, 0), (7, 7, True, 0), (5, 12, True, 0),
+                                               (12, 5, True, 0), (9, 9, True, 3), (4, 11, True, 6), (1, 1, True, 1)])
+def test_oracle_matches_float64_autograd(n, m, causal, window):
+    g = torch.Generator().manual_seed(n * m)
+    q, k, v, do = (torch.randn((r, 6), generator=g, dtype=torch.float64) for r in (n, m, m, n))
+    mask = torch.tensor([[not causal or (j <= i + m - n and (window == 0 or j > i + m - n - window))
+                          for j in range(m)] for i in range(n)])
+    live = mask.any(1)
+    args = [x.clone().requires_grad_() for x in (q, k, v)]
+    s = (args[0] @ args[1].T) * 0.4
+    p = torch.softmax(s[live].masked_fill(~mask[live], -torch.inf), 1)
+    o = torch.zeros((n, 6), dtype=torch.float64)
+    o = o.index_put((live.nonzero()[:, 0],), p @ args[2])
+    o.backward(do)
+    mine, lse, _ = oa.forward(q, k, v, 0.4, causal, window)
+    np.testing.assert_allclose(mine, o.detach(), atol=1e-13)
+    assert np.array_equal(lse == -np.inf, ~live.numpy())
+    for got, x in zip(oa.backward(q, k, v, mine, lse, do, 0.4, causal, window), args):
+        np.testing.assert_allclose(got, x.grad if x.grad is not None else 0, atol=1e-12)
+
+
+def test_oracle_by_hand():
+    """Two keys with scores 0 and ln 3: weights 1/4 and 3/4."""
+    q, k, v = np.array([[1.0]]), np.array([[0.0], [np.log(3)]]), np.array([[4.0], [8.0]])
+    o, lse, p = oa.forward(q, k, v, 1.0)
+    np.testing.assert_allclose(p, [[0.25, 0.75]])
+    np.testing.assert_allclose(o, [[7.0]])
+    np.testing.assert_allclose(lse, [np.log(4)])
+
+
+def test_oracle_slots_by_hand():
+    """Pages of 4: request 0 fills its page and takes one, 1 is new and takes two, 2 finds none left,
+    3 needs none."""
+    table = [[9, -1, -1], [-1, -1, -1], [-1, -1, -1], [5, -1, -1]]
+    q_start, kv_len, out, slots, taken = oa.slots([3, 0, 0, 1], [2, 5, 1, 2], 4, 12, table, [7, 2, 11, 3], 3, 12)
+    assert q_start == [0, 2, 7, 8, 10] and kv_len == [5, 5, 0, 3] and taken == [3, 1]
+    assert out.tolist() == [[9, 7, -1], [2, 11, -1], [-1, -1, -1], [5, -1, -1]]
+    assert slots.tolist() == [39, 28, 8, 9, 10, 11, 44, -1, 21, 22, -1, -1]
+
+
+# -------------------------------------------------------------------------------------- plans
+def _status(fn, *a, **k):
+    try:
+        fn(*a, **k)
+    except bsm.BsmError as e:
+        return e.status, e.message
+    return bsm.BSM_OK, ""
+
+
+def _plan(q_len=(4, 5), kv_len=None, **k):
+    args = dict(heads_q=4, heads_kv=2, head_dim=64, topology=TOPO, device=-1)
+    args.update(k)
+    return bsm.bsm_attention_plan_create(list(q_len), kv_len if kv_len is None else list(kv_len), **args)
+
+
+@pytest.mark.parametrize("kwargs,status,msg", [
+    (dict(heads_q=5), "INVALID_ARG", "multiple"),
+    (dict(heads_kv=0), "INVALID_ARG", "multiple"),
+    (dict(heads_q=0, heads_kv=1), "INVALID_ARG", "multiple"),
+    (dict(head_dim=0), "INVALID_ARG", "head_dim"),
+    (dict(head_dim=60), "UNSUPPORTED", "head_dim"),
+    (dict(head_dim=136), "UNSUPPORTED", "head_dim"),
+    (dict(window=4), "INVALID_ARG", "causal"),
+    (dict(window=-1, causal=True), "INVALID_ARG", "window"),
+    (dict(q_len=(4, -1)), "INVALID_ARG", "lengths"),
+    (dict(kv_len=(4, 2**30 + 1)), "INVALID_ARG", "lengths"),
+    (dict(q_start=[0, -2]), "INVALID_ARG", "first rows"),
+    (dict(schedule=9), "INVALID_ARG", "schedule"),
+    (dict(topology=None), "INVALID_ARG", "topology"),
+    (dict(topology=dict(n_xcd=17)), "INVALID_ARG", "n_xcd"),
+    (dict(device=-2), "INVALID_ARG", "device"),
+    (dict(q_len=[2**30] * 8, heads_q=256, heads_kv=256), "INVALID_ARG", "too many"),
+])
+def test_plan_refusals(kwargs, status, msg):
+    st, m = _status(_plan, **kwargs)
+    assert st == getattr(bsm, "BSM_ERR_" + status), m
+    assert msg in m
+
+
+def test_plan_python_checks():
+    with pytest.raises(ValueError):
+        _plan(q_len=(4, 5), kv_len=(4,))
+    with pytest.raises(ValueError):
+        _plan(q_len=(2**31,))
+
+
+@pytest.mark.parametrize("q_len,kv_len,causal,window", [
+    ([7, 300, 0], [7, 300, 12], False, 0), ([7, 300, 1], [9, 512, 40], True, 0), ([30, 5], [10, 0], True, 0),
+    ([300, 40], [300, 90], True, 17), ([300], [20], True, 5), ([5], [300], True, 100)])
+def test_plan_stats(q_len, kv_len, causal, window):
+    p = _plan(q_len, kv_len, causal=causal, window=window)
+    d = bsm.bsm_attention_plan_describe(p)
+    assert d["pairs"] == sum(int(oa.seen(n, m, causal, window).sum()) for n, m in zip(q_len, kv_len))
+    assert d["q_units"] == 4 * sum(-(-n // 128) for n in q_len)
+    assert d["kv_units"] == 2 * sum(-(-m // 128) for m in kv_len)
+    assert d["lse_elems"] == 4 * sum(q_len) and d["workspace_bytes"] == 16 * sum(q_len)
+    assert (d["total_q"], d["total_kv"], d["causal"], d["window"]) == (sum(q_len), sum(kv_len), causal, window)
+
+
+def test_plan_allocation_failure(monkeypatch):
+    monkeypatch.setenv("BSM_TEST_ALLOC_FAIL", "host")
+    assert _status(_plan)[0] == bsm.BSM_ERR_OOM
+    monkeypatch.delenv("BSM_TEST_ALLOC_FAIL")
+    _plan().destroy()
+
+
+def test_empty_batch_plans():
+    for q_len in ([], [0, 0]):
+        d = bsm.bsm_attention_plan_describe(_plan(q_len))
+        assert d["q_units"] == 0 and d["workspace_bytes"] == 0
+    assert att._load().bsm_attention_plan_destroy(None) == bsm.BSM_ERR_INVALID_ARG
+
+
+# ----------------------------------------------------------------- refusals of paged cache calls
+def _heads(at, row=256, head=64, seq=0):
+    return ctypes.byref(att.bsm_heads(at, seq, row, head))
+
+
+def _cache(**k):
+    a = dict(k=1 << 30, v=1 << 31, n_pages=8, page_stride=16 * 128, row_stride=128, head_stride=64, page_size=16, heads=2,
+             head_dim=64, reserved=0)
+    a.update(k)
+    return ctypes.byref(att.bsm_cache(**a))
+
+
+def _paged(cache=None, q=None, o=None, table=1 << 40, width=4, q_start=1 << 41, kv_len=1 << 42, batch=2, tokens=6, heads_q=4,
+           max_q=3, max_kv=60, window=0, scale=0.125, ws=1 << 43, ws_bytes=1 << 30):
+    return att._load().bsm_attention_paged(cache or _cache(), q or _heads(1 << 44), o or _heads(1 << 45), table, width, q_start,
+                                           kv_len, batch, tokens, heads_q, max_q, max_kv, window, scale, ws, ws_bytes, None)
+
+
+@pytest.mark.parametrize("kwargs,status,msg", [
+    (dict(cache=_cache(head_dim=20)), "UNSUPPORTED", "head_dim"),
+    (dict(cache=_cache(page_size=0)), "INVALID_ARG", "pages"),
+    (dict(cache=_cache(n_pages=-1)), "INVALID_ARG", "pages"),
+    (dict(cache=_cache(k=0)), "INVALID_ARG", "NULL"),
+    (dict(cache=_cache(k=(1 << 30) + 1)), "INVALID_ARG", "aligned"),
+    (dict(cache=_cache(row_stride=-8)), "INVALID_ARG", "strides"),
+    (dict(heads_q=3), "INVALID_ARG", "multiple"),
+    (dict(width=-1), "INVALID_ARG", "width"),
+    (dict(width=2**27), "INVALID_ARG", "2^30"),
+    (dict(window=-1), "INVALID_ARG", "window"),
+    (dict(scale=0.0), "INVALID_ARG", "scale"),
+    (dict(scale=float("nan")), "INVALID_ARG", "scale"),
+    (dict(batch=-1), "INVALID_ARG", "batch"),
+    (dict(tokens=-1), "INVALID_ARG", "tokens"),
+    (dict(max_q=-1), "INVALID_ARG", "max_q"),
+    (dict(max_kv=2**30 + 1), "INVALID_ARG", "max_kv"),
+    (dict(q=_heads(None)), "INVALID_ARG", "NULL"),
+    (dict(o=_heads(1 << 45, row=128)), "INVALID_ARG", "overlap"),
+    (dict(o=_heads(1 << 45, head=0)), "INVALID_ARG", "overlap"),
+    (dict(o=_heads(1 << 44)), "ALIAS", "overlaps"),
+    (dict(o=_heads((1 << 30) + 64)), "ALIAS", "overlaps"),
+    (dict(o=_heads((1 << 40) + 8)), "ALIAS", "overlaps"),
+    (dict(table=None), "INVALID_ARG", "NULL"),
+    (dict(q_start=None), "INVALID_ARG", "NULL"),
+])
+def test_paged_refusals(kwargs, status, msg):
+    st = _paged(**kwargs)
+    assert st == getattr(bsm, "BSM_ERR_" + status), bsm.bsm_last_error()
+    assert msg in bsm.bsm_last_error()
+
+
+def test_paged_calls_without_work_touch_no_gpu():
+    for k in (dict(batch=0), dict(tokens=0, q=_heads(None), o=_heads(None)), dict(max_q=0)):
+        assert _paged(**k) == bsm.BSM_OK
+
+
+def _slots(cached=1 << 30, fresh=1 << 31, batch=4, page_size=16, n_pages=64, table=1 << 32, width=8, free=1 << 33, cap=32,
+           n_free=1 << 34, q_start=1 << 35, kv_len=1 << 36, slots=1 << 37, n_slots=10, taken=1 << 38):
+    return att._load().bsm_cache_slots(cached, fresh, batch, page_size, n_pages, table, width, free, cap, n_free, q_start, kv_len,
+                                       slots, n_slots, taken, None)
+
+
+@pytest.mark.parametrize("kwargs,status,msg", [
+    (dict(batch=-1), "INVALID_ARG", "batch"),
+    (dict(page_size=0), "INVALID_ARG", "page_size"),
+    (dict(width=-1), "INVALID_ARG", "width"),
+    (dict(width=2**27), "INVALID_ARG", "2^30"),
+    (dict(cap=-1), "INVALID_ARG", "free_cap"),
+    (dict(n_slots=-1), "INVALID_ARG", "n_slots"),
+    (dict(cached=None), "INVALID_ARG", "NULL"),
+    (dict(table=None), "INVALID_ARG", "NULL"),
+    (dict(n_free=None), "INVALID_ARG", "NULL"),
+    (dict(slots=None), "INVALID_ARG", "NULL"),
+    (dict(slots=(1 << 37) + 4), "INVALID_ARG", "aligned"),
+    (dict(fresh=(1 << 31) + 2), "INVALID_ARG", "aligned"),
+    (dict(kv_len=1 << 30), "ALIAS", "input"),
+    (dict(q_start=(1 << 33) + 64), "ALIAS", "input"),
+    (dict(taken=(1 << 32) + 32), "ALIAS", "outputs"),
+])
+def test_slots_refusals(kwargs, status, msg):
+    st = _slots(**kwargs)
+    assert st == getattr(bsm, "BSM_ERR_" + status), bsm.bsm_last_error()
+    assert msg in bsm.bsm_last_error()
+
+
+def _append(cache=None, k=None, v=None, slots=1 << 40, tokens=6):
+    return att._load().bsm_cache_append(cache or _cache(), k or _heads(1 << 44, 128), v or _heads(1 << 45, 128), slots, tokens, None)
+
+
+@pytest.mark.parametrize("kwargs,status,msg", [
+    (dict(cache=_cache(page_stride=0)), "INVALID_ARG", "overlap"),
+    (dict(cache=_cache(row_stride=64)), "INVALID_ARG", "overlap"),
+    (dict(cache=_cache(v=1 << 30)), "ALIAS", "same place"),
+    (dict(tokens=-1), "INVALID_ARG", "tokens"),
+    (dict(k=_heads((1 << 44) + 1, 128)), "INVALID_ARG", "aligned"),
+    (dict(v=_heads(None, 128)), "INVALID_ARG", "NULL"),
+    (dict(k=_heads((1 << 30) + 32, 128)), "ALIAS", "overlaps"),
+    (dict(slots=(1 << 31) + 16), "ALIAS", "overlaps"),
+    (dict(slots=None), "INVALID_ARG", "NULL"),
+    (dict(slots=(1 << 40) + 4), "INVALID_ARG", "aligned"),
+])
+def test_append_refusals(kwargs, status, msg):
+    st = _append(**kwargs)
+    assert st == getattr(bsm, "BSM_ERR_" + status), bsm.bsm_last_error()
+    assert msg in bsm.bsm_last_error()
+
+
+def test_append_without_tokens_touches_no_gpu():
+    assert _append(tokens=0, k=_heads(None), v=_heads(None), slots=None) == bsm.BSM_OK
+    assert _append(cache=_cache(n_pages=0, k=0, v=0)) == bsm.BSM_OK
+
+
+def test_host_only_plans_do_not_run():
+    p = _plan()
+    st = att._load().bsm_attention_execute(p.handle, *[_heads(1 << (40 + i)) for i in range(4)], None, 0.125, None)
+    assert st == bsm.BSM_ERR_UNSUPPORTED
