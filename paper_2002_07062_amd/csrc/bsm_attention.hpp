@@ -31,7 +31,7 @@ typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
 // 16-byte accesses at any element boundary
 typedef u32x4 u32x4_any __attribute__((aligned(2)));
-typedef f32x4 f32x4_any __attribute__((aligned(4)));
+typedef u32x2 u32x2_any __attribute__((aligned(2)));
 
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
@@ -74,6 +74,13 @@ struct Tile {
     }
 };
 
+// Where rows and chunks that do not exist are read: a load that is always done, from one place or the
+// other, stays in flight; one inside a branch is waited for at the branch's end.
+static __device__ __attribute__((aligned(16))) const uint16_t kZeros[8] = {};
+__device__ __forceinline__ u32x4 load_or_zero(const uint16_t* p, bool live) {
+    return *reinterpret_cast<const u32x4_any*>(live ? p : kZeros);
+}
+
 // The pieces of a ROWS x D tile that one of THREADS threads carries from memory to LDS.  Rows and
 // chunks that do not exist are zero (a masked probability times what lies there must be zero).
 template <int D, int ROWS, int THREADS>
@@ -89,8 +96,7 @@ struct Stage {
 #pragma unroll
         for (int j = 0; j < kN; ++j) {
             const int i = row(tid, j);
-            r[j] = u32x4{0, 0, 0, 0};
-            if (i < rows && c < chunks) r[j] = *reinterpret_cast<const u32x4_any*>(p + i * stride + 8 * c);
+            r[j] = load_or_zero(p + i * stride + 8 * c, i < rows && c < chunks);
         }
     }
     __device__ __forceinline__ void store(int tid, uint16_t* lds) const {
@@ -108,9 +114,7 @@ struct RowOperand {
     __device__ __forceinline__ void load(const uint16_t* row, bool live, int h, int chunks) {
 #pragma unroll
         for (int s = 0; s < D / 16; ++s) {
-            u32x4 v = {0, 0, 0, 0};
-            if (live && 2 * s + h < chunks) v = *reinterpret_cast<const u32x4_any*>(row + 8 * (2 * s + h));
-            f[s] = __builtin_bit_cast(bf16x8, v);
+            f[s] = __builtin_bit_cast(bf16x8, load_or_zero(row + 8 * (2 * s + h), live && 2 * s + h < chunks));
         }
     }
 };

@@ -66,7 +66,7 @@ struct PagedArgs {
     int32_t window;
     float scale;
     // how the work is cut, from bounds on the lengths alone
-    int32_t tile_rows;        // 32 (the four waves take turns at the keys) or 128
+    int32_t tile_rows;        // 16 or 32 (the four waves take turns at the keys) or 128
     int32_t tiles;            // per request and key/value head
     int32_t splits;           // pieces of the key axis
     int32_t split_keys;       // keys of a piece, a multiple of kKeyTile

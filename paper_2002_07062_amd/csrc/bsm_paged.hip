@@ -18,10 +18,10 @@ struct Request {
     int rows;          // q_len (at most max_q) * group
 };
 
-__device__ __forceinline__ Request request(const PagedArgs& a, int64_t unit) {
+__device__ __forceinline__ Request request(const PagedArgs& a, int64_t b, int head) {
     Request r;
-    r.b = static_cast<int>(unit / a.cache.heads);
-    r.head = static_cast<int>(unit % a.cache.heads);
+    r.b = static_cast<int>(b);
+    r.head = head;
     const int64_t q0 = a.q_start[r.b], q1 = a.q_start[r.b + 1];
     r.q0 = q0 < 0 ? 0 : q0 < a.tokens ? q0 : a.tokens;
     const int64_t e = q1 < r.q0 ? r.q0 : q1 < a.tokens ? q1 : a.tokens;
@@ -64,8 +64,27 @@ __device__ __forceinline__ Pieces pieces(const PagedArgs& a, const Request& r, i
 }
 
 // Floats of one piece's part: its rows' outputs, then their references and sums.
-__device__ __forceinline__ int64_t part_at(const PagedArgs& a, int D, int64_t unit, int tile, int piece) {
-    return ((unit * a.tiles + tile) * a.splits + piece) * a.tile_rows * (D + 2);
+__device__ __forceinline__ int64_t part_at(const PagedArgs& a, int D, const Request& r, int tile, int piece) {
+    return (((static_cast<int64_t>(r.b) * a.cache.heads + r.head) * a.tiles + tile) * a.splits + piece) * a.tile_rows * (D + 2);
+}
+
+// What workgroup w does.  The workgroups of all requests and heads follow each other, tile after tile,
+// piece after piece, so the tiles that read the same keys run on one XCD (w mod 8 where requests times
+// heads is a multiple of 8).  The heads are rotated from request to request and piece to piece: a page
+// has its heads side by side, and an XCD that only ever read one of 8 heads of 128 would use 2 of its 16
+// L2 channels, which lie 256 bytes apart.
+struct Place {
+    int64_t b;
+    int head, tile, piece;
+};
+__device__ __forceinline__ Place place_of(const PagedArgs& a, int64_t w) {
+    const int64_t units = a.batch * a.cache.heads, unit = w % units, rest = w / units;
+    Place p;
+    p.tile = static_cast<int>(rest % a.tiles);
+    p.piece = static_cast<int>(rest / a.tiles);
+    p.b = unit / a.cache.heads;
+    p.head = static_cast<int>((unit + p.b + p.piece) % a.cache.heads);
+    return p;
 }
 
 // The rows of K and V that a thread stages: tile row i is key j0 + i of the request.  Keys past its
@@ -76,12 +95,12 @@ struct PagedStage {
     S k, v;
     int page[S::kN];
     __device__ __forceinline__ static int divide(const PagedArgs& a, int j) { return j / a.cache.page_size; }
-    // table entries of the tile at j0 (-1: none)
+    // table entries of the tile at j0 (-1: none); the request has keys 0 .. end - 1
     __device__ __forceinline__ void find(const PagedArgs& a, const int32_t* table, int tid, int j0, int end) {
 #pragma unroll
         for (int n = 0; n < S::kN; ++n) {
-            const int j = j0 + S::row(tid, n);
-            page[n] = j < end ? table[divide(a, j)] : -1;
+            const int j = j0 + S::row(tid, n), entry = table[divide(a, min(j, end - 1))];
+            page[n] = j < end && entry < a.cache.n_pages ? entry : -1;
         }
     }
     __device__ __forceinline__ void load(const PagedArgs& a, int head, int tid, int j0, int chunks) {
@@ -89,43 +108,23 @@ struct PagedStage {
 #pragma unroll
         for (int n = 0; n < S::kN; ++n) {
             const int j = j0 + S::row(tid, n);
-            k.r[n] = v.r[n] = u32x4{0, 0, 0, 0};
-            if (page[n] >= 0 && page[n] < a.cache.n_pages && c < chunks) {
-                const int64_t at = page[n] * a.cache.page + (j - divide(a, j) * a.cache.page_size) * a.cache.row +
-                                   head * a.cache.head + 8 * c;
-                k.r[n] = *reinterpret_cast<const u32x4_any*>(a.cache.k + at);
-                v.r[n] = *reinterpret_cast<const u32x4_any*>(a.cache.v + at);
-            }
+            const bool live = page[n] >= 0 && c < chunks;
+            const int64_t at = page[n] * a.cache.page + (j - divide(a, j) * a.cache.page_size) * a.cache.row +
+                               head * a.cache.head + 8 * c;
+            k.r[n] = load_or_zero(a.cache.k + at, live);
+            v.r[n] = load_or_zero(a.cache.v + at, live);
         }
     }
 };
 
+// Many rows (chunks of prompts): a tile has 128 rows, 32 per wave, and the waves share the staged keys.
 template <int D>
-__device__ __forceinline__ void put_part(float* part, int tile_rows, int row, const f32x16& acc, int t, int h) {
-#pragma unroll
-    for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<f32x4*>(part + static_cast<int64_t>(row) * D + 32 * t + 8 * g + 4 * h) =
-            f32x4{acc[4 * g], acc[4 * g + 1], acc[4 * g + 2], acc[4 * g + 3]};
-    (void)tile_rows;
-}
-
-// TEAM 4: a tile has 128 rows, 32 per wave, and the waves share the staged keys.
-// TEAM 1: a tile has 32 rows, the waves take turns at blocks of 32 keys, each staging its own, and
-// join their rows at the end: few rows over many keys (decode) are bound by reading the cache, and
-// four waves that never wait for each other keep more of it in flight.
-template <int D, int TEAM>
 __global__ __launch_bounds__(kThreads, 2) void paged_kernel(const PagedArgs a) {
-    constexpr int kKeys = TEAM == 4 ? 64 : 32;
-    constexpr int kTeamThreads = TEAM * kWave;
-    constexpr int kBuffers = TEAM == 4 ? 2 : 1;
-    constexpr int kTileElems = kKeys * D;
-    __shared__ __align__(16) uint16_t lds[kBuffers * (4 / TEAM) * 2 * kTileElems];
-    __shared__ float stat[2][4][kRows];
-    const int64_t units = a.batch * a.cache.heads;
-    const int64_t unit = blockIdx.x % units;
-    const int rest = static_cast<int>(blockIdx.x / units);
-    const int tile = rest % a.tiles, piece = rest / a.tiles;
-    const Request r = request(a, unit);
+    constexpr int kKeys = 64, kTileElems = kKeys * D;
+    __shared__ __align__(16) uint16_t lds[2][2][kTileElems];  // buffer, K or V
+    const Place at = place_of(a, blockIdx.x);
+    const int tile = at.tile, piece = at.piece;
+    const Request r = request(a, at.b, at.head);
     const int tile0 = tile * a.tile_rows;
     if (tile0 >= r.rows) return;
     const Pieces ps = pieces(a, r, tile0);
@@ -133,8 +132,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_kernel(const PagedArgs a) {
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, li = lane & 31, h = lane >> 5;
     const int chunks = a.cache.dim / 8;
-    const int row0 = TEAM == 4 ? tile0 + kRows * wave : tile0;  // of the wave
-    const int row = row0 + li;
+    const int row0 = tile0 + kRows * wave, row = row0 + li;
     const bool live = row < r.rows;
     const bool any_row = row0 < r.rows;
     const int token = row / a.group, q_head = r.head * a.group + row % a.group;
@@ -144,155 +142,336 @@ __global__ __launch_bounds__(kThreads, 2) void paged_kernel(const PagedArgs a) {
     const Keys mine = seen_keys(a, r, token);
     const Keys w0 = seen_keys(a, r, row0 / a.group), w1 = seen_keys(a, r, (row0 + kRows - 1) / a.group);
 
-    const int team_tid = TEAM == 4 ? tid : lane;
-    const int step = TEAM == 4 ? kKeys : kKeys * kWaves;
     const int from = max(ps.keys.lo, piece * a.split_keys);
     const int end = piece == a.splits - 1 ? ps.keys.hi + 1 : min(ps.keys.hi + 1, (piece + 1) * a.split_keys);
-    const int begin = from / kKeys * kKeys + (TEAM == 4 ? 0 : wave * kKeys);
+    const int begin = from / kKeys * kKeys;
     const int32_t* table = a.table + static_cast<int64_t>(r.b) * a.width;
-    uint16_t* mem = lds + (TEAM == 4 ? 0 : wave * 2 * kTileElems);
 
     Online<D> st;
     st.init();
     const float c = a.scale * kLog2e;
-    PagedStage<D, kKeys, kTeamThreads> stage;
+    PagedStage<D, kKeys, kThreads> stage;
     if (begin < end) {
-        stage.find(a, table, team_tid, begin, r.kv_len);
-        stage.load(a, r.head, team_tid, begin, chunks);
-        stage.find(a, table, team_tid, begin + step, r.kv_len);
-        if (TEAM == 4) {
-            stage.k.store(team_tid, mem);
-            stage.v.store(team_tid, mem + kTileElems);
-        }
+        stage.find(a, table, tid, begin, r.kv_len);
+        stage.load(a, r.head, tid, begin, chunks);
+        stage.find(a, table, tid, begin + kKeys, r.kv_len);
+        stage.k.store(tid, lds[0][0]);
+        stage.v.store(tid, lds[0][1]);
     }
     int buf = 0;
-    for (int j0 = begin; j0 < end; j0 += step) {
-        const int next = j0 + step;
-        if (TEAM == 4) {
-            lds_barrier();
-        } else {
-            stage.k.store(team_tid, mem);
-            stage.v.store(team_tid, mem + kTileElems);
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup", "local");
-            __builtin_amdgcn_wave_barrier();
-        }
+    for (int j0 = begin; j0 < end; j0 += kKeys, buf ^= 1) {
+        const int next = j0 + kKeys;
+        lds_barrier();
         if (next < end) {
-            stage.load(a, r.head, team_tid, next, chunks);
-            stage.find(a, table, team_tid, next + step, r.kv_len);
+            stage.load(a, r.head, tid, next, chunks);
+            stage.find(a, table, tid, next + kKeys, r.kv_len);
         }
-        const uint16_t* now = mem + buf * 2 * kTileElems;
-        if (any_row && j0 <= w1.hi && j0 + kKeys > w0.lo) {
+        if (any_row && j0 <= w1.hi && next > w0.lo) {
             f32x16 s[kKeys / 32];
 #pragma unroll
-            for (int k = 0; k < kKeys / 32; ++k) s[k] = row_product<D>(now, 32 * k, q, lane);
-            if (j0 < w1.lo || j0 + kKeys - 1 > w0.hi || end < j0 + kKeys) {
+            for (int k = 0; k < kKeys / 32; ++k) s[k] = row_product<D>(lds[buf][0], 32 * k, q, lane);
+            if (j0 < w1.lo || next - 1 > w0.hi || end < next) {
 #pragma unroll
                 for (int k = 0; k < kKeys / 32; ++k) mask_block(s[k], j0 + 32 * k, h, mine.lo, min(mine.hi, end - 1));
             }
             st.weigh(s, c);
 #pragma unroll
-            for (int k = 0; k < kKeys / 32; ++k) col_product<D>(st.o, now + kTileElems, 32 * k, s[k], lane);
+            for (int k = 0; k < kKeys / 32; ++k) col_product<D>(st.o, lds[buf][1], 32 * k, s[k], lane);
         }
-        if (TEAM == 4) {
-            if (next < end) {
-                buf ^= 1;
-                stage.k.store(team_tid, mem + buf * 2 * kTileElems);
-                stage.v.store(team_tid, mem + buf * 2 * kTileElems + kTileElems);
-            }
-        } else {
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup", "local");
-            __builtin_amdgcn_wave_barrier();
+        if (next < end) {
+            stage.k.store(tid, lds[buf ^ 1][0]);
+            stage.v.store(tid, lds[buf ^ 1][1]);
         }
     }
-
-    const bool whole = ps.first == ps.last;
-    float* part = whole ? nullptr : a.part + part_at(a, D, unit, tile, piece);
-    uint16_t* out = a.o.p + q_row * a.o.row + q_head * a.o.head;
-    float total = st.row_sum();
-    if (TEAM == 4) {
-        if (whole) {
-            store_row<D>(out, live, st.o, total == 0.0f ? 0.0f : 1.0f / total, h, chunks);
-        } else if (live) {
-#pragma unroll
-            for (int t = 0; t < D / 32; ++t) put_part<D>(part, a.tile_rows, row - tile0, st.o[t], t, h);
-            if (h == 0) {
-                part[a.tile_rows * D + row - tile0] = st.m;
-                part[a.tile_rows * (D + 1) + row - tile0] = total;
-            }
-        }
-        return;
-    }
-    // join the four waves' rows
-    float* sums = reinterpret_cast<float*>(lds);  // [wave][register][lane]
-    constexpr int kRegs = D / 2;
-    static_assert(sizeof(lds) >= 4 * kRegs * kWave * sizeof(float) || TEAM == 4, "");
-    if (h == 0) {
-        stat[0][wave][li] = st.m;
-        stat[1][wave][li] = total;
-    }
-    __syncthreads();
-    float m = -kInf;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) m = fmaxf(m, stat[0][w][li]);
-    total = 0.0f;
-#pragma unroll
-    for (int w = 0; w < 4; ++w)
-        total += stat[0][w][li] == -kInf ? stat[1][w][li] : stat[1][w][li] * __builtin_amdgcn_exp2f(stat[0][w][li] - m);
-    const float f = st.m == -kInf ? 1.0f : __builtin_amdgcn_exp2f(st.m - m);
-#pragma unroll
-    for (int t = 0; t < D / 32; ++t)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sums[(wave * kRegs + 16 * t + i) * kWave + lane] = st.o[t][i] * f;
-    __syncthreads();
-    if (wave >= D / 32) return;
-    f32x16 acc;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        float x = 0.0f;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) x += sums[(w * kRegs + 16 * wave + i) * kWave + lane];
-        acc[i] = x;
-    }
-    if (whole) {
-        store_block(out, live, acc, total == 0.0f ? 0.0f : 1.0f / total, wave, h, chunks);
+    const float total = st.row_sum();
+    if (ps.first == ps.last) {
+        uint16_t* out = a.o.p + q_row * a.o.row + q_head * a.o.head;
+        store_row<D>(out, live, st.o, total == 0.0f ? 0.0f : 1.0f / total, h, chunks);
     } else if (live) {
-        put_part<D>(part, a.tile_rows, row - tile0, acc, wave, h);
-        if (h == 0 && wave == 0) {
-            part[a.tile_rows * D + row - tile0] = m;
+        float* part = a.part + part_at(a, D, r, tile, piece);
+        float* to = part + (row - tile0) * D + 4 * h;
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<f32x4*>(to + 32 * t + 8 * g) =
+                    f32x4{st.o[t][4 * g], st.o[t][4 * g + 1], st.o[t][4 * g + 2], st.o[t][4 * g + 3]};
+        if (h == 0) {
+            part[a.tile_rows * D + row - tile0] = st.m;
             part[a.tile_rows * (D + 1) + row - tile0] = total;
         }
     }
 }
 
-// Joins the pieces of the rows that more than one piece holds: one wave per row.
+// Few rows over many keys (decode) are bound by reading the cache, so what counts is how much of it is
+// in flight: the waves never wait for each other, each takes every fourth block of 32 keys and joins
+// its rows with the others' at the end.  v_mfma_f32_16x16x32_bf16 keeps 16 rows (NQ times) in a quarter
+// of the registers that 32 x 32 tiles take.  Its lane (n, quad) = (lane & 15, lane >> 4) returns column
+// n and rows 4 quad + i, and reads 8 values of the reduction axis; as in the other kernels the scores'
+// registers are the next operand: keys 4 quad + i and 16 + 4 quad + i of a block.
+// A lane reads two keys' rows, n and n + 16, of K and of V.  K goes to the matrix cores as it comes; V is
+// turned in LDS.  The next block's loads are issued when the scores have left K's registers.
+template <int D, int NQ>
+__global__ __launch_bounds__(kThreads, 2) void paged_few_kernel(const PagedArgs a) {
+    constexpr int kKeys = 32, kSteps = D / 32, kTiles = D / 16;
+    constexpr int kRegs = NQ * kTiles * 4;  // outputs of a lane
+    constexpr int kBytes = kWaves * (kRegs * kWave * 4 > kKeys * D * 2 ? kRegs * kWave * 4 : kKeys * D * 2);
+    __shared__ __align__(16) unsigned char lds[kBytes];
+    __shared__ float stat[2][kWaves][16 * NQ];
+    const Place at = place_of(a, blockIdx.x);
+    const int tile = at.tile, piece = at.piece;
+    const Request r = request(a, at.b, at.head);
+    const int tile0 = tile * a.tile_rows;
+    if (tile0 >= r.rows) return;
+    const Pieces ps = pieces(a, r, tile0);
+    if (piece < ps.first || piece > ps.last) return;
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, quad = lane >> 4;
+    const int chunks = a.cache.dim / 8;
+    bf16x8 q[NQ][kSteps];
+    Keys mine[NQ];
+    uint16_t* out[NQ];
+#pragma unroll
+    for (int x = 0; x < NQ; ++x) {
+        const int row = tile0 + 16 * x + n, token = row / a.group, head = r.head * a.group + row % a.group;
+        mine[x] = seen_keys(a, r, token);
+        out[x] = row < r.rows ? a.o.p + (r.q0 + token) * a.o.row + head * a.o.head : nullptr;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            const uint16_t* from = a.q.p + (r.q0 + token) * a.q.row + head * a.q.head + 8 * (4 * s + quad);
+            q[x][s] = __builtin_bit_cast(bf16x8, load_or_zero(from, row < r.rows && 4 * s + quad < chunks));
+        }
+    }
+    // keys that every row of the tile sees
+    const int all_lo = seen_keys(a, r, min(tile0 + a.tile_rows, r.rows) / a.group).lo, all_hi = seen_keys(a, r, tile0 / a.group).hi;
+    const int from = max(ps.keys.lo, piece * a.split_keys);
+    const int end = piece == a.splits - 1 ? ps.keys.hi + 1 : min(ps.keys.hi + 1, (piece + 1) * a.split_keys);
+    const int begin = from / kKeys * kKeys + wave * kKeys;
+    const int32_t* table = a.table + static_cast<int64_t>(r.b) * a.width;
+    uint16_t* mem = reinterpret_cast<uint16_t*>(lds) + wave * kKeys * D;
+
+    f32x4 o[NQ][kTiles];
+    float m[NQ], l[NQ];
+#pragma unroll
+    for (int x = 0; x < NQ; ++x) {
+        m[x] = -kInf;
+        l[x] = 0.0f;
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) o[x][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    const float c = a.scale * kLog2e;
+    u32x4 k[2][kSteps], v[2][kSteps];
+    int page[2];
+    auto find = [&](int j0) {
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+            const int j = j0 + 16 * y + n, entry = table[min(j, r.kv_len - 1) / a.cache.page_size];
+            page[y] = j < r.kv_len && entry < a.cache.n_pages ? entry : -1;
+        }
+    };
+    auto load = [&](int j0) {
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+            const int j = j0 + 16 * y + n;
+            const bool live = page[y] >= 0;
+            const int64_t from = page[y] * a.cache.page + (j % a.cache.page_size) * a.cache.row + r.head * a.cache.head + 8 * quad;
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) {
+                k[y][s] = load_or_zero(a.cache.k + from + 32 * s, live && 4 * s + quad < chunks);
+                v[y][s] = load_or_zero(a.cache.v + from + 32 * s, live && 4 * s + quad < chunks);
+            }
+        }
+    };
+    constexpr int step = kKeys * kWaves;
+    if (begin < end) {
+        find(begin);
+        load(begin);
+        find(begin + step);
+    }
+    for (int j0 = begin; j0 < end; j0 += step) {
+        f32x4 s[NQ][2];
+#pragma unroll
+        for (int x = 0; x < NQ; ++x)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                s[x][y] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int e = 0; e < kSteps; ++e)
+                    s[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[y][e]), q[x][e], s[x][y], 0, 0, 0);
+            }
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+#pragma unroll
+            for (int e = 0; e < kSteps; ++e)
+                *reinterpret_cast<u32x4*>(mem + 8 * Tile<D>::place(16 * y + n, 4 * e + quad)) = v[y][e];
+        const int next = j0 + step;
+        if (next < end) {
+            load(next);
+            find(next + step);
+        }
+        // the wave's own writes, before its lanes read each other's
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup", "local");
+        __builtin_amdgcn_wave_barrier();
+        const bool masked = j0 < all_lo || j0 + kKeys - 1 > all_hi || j0 + kKeys > end;
+#pragma unroll
+        for (int x = 0; x < NQ; ++x) {
+            if (masked) {
+#pragma unroll
+                for (int y = 0; y < 2; ++y)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int j = j0 + 16 * y + 4 * quad + i;
+                        s[x][y][i] = j >= mine[x].lo && j <= mine[x].hi && j < end ? s[x][y][i] : -kInf;
+                    }
+            }
+            float top = s[x][0][0];
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) top = fmaxf(top, s[x][y][i]);
+            top = fmaxf(top, __shfl_xor(top, 16, 64));
+            top = fmaxf(top, __shfl_xor(top, 32, 64)) * c;
+            if (__any(top > m[x] + kSlack)) {
+                const float to = fmaxf(m[x], top);
+                const float f = to == -kInf ? 1.0f : __builtin_amdgcn_exp2f(m[x] - to);
+                m[x] = to;
+                l[x] *= f;
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[x][t][i] *= f;
+            }
+            const float ref = m[x] == -kInf ? 0.0f : m[x];
+            bf16x8 p;
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][y][i], c, -ref));
+                    l[x] += e;
+                    p[4 * y + i] = static_cast<__bf16>(e);
+                }
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) {
+                // lane (n, quad): column 16 t + n of rows 4 quad + {0..3} and 16 + 4 quad + {0..3}
+                const int row = 4 * quad + (n >> 2), col = 16 * t + 4 * (n & 3);
+                union {
+                    i16x4 half[2];
+                    bf16x8 all;
+                } u;
+                u.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(mem + 8 * Tile<D>::place(row, col >> 3) + (col & 7)));
+                u.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(mem + 8 * Tile<D>::place(row + 16, col >> 3) + (col & 7)));
+                o[x][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(u.all, p, o[x][t], 0, 0, 0);
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup", "local");
+        __builtin_amdgcn_wave_barrier();
+    }
+
+    // join the four waves' rows
+    float* sums = reinterpret_cast<float*>(lds);  // [wave][register][lane]
+#pragma unroll
+    for (int x = 0; x < NQ; ++x) {
+        l[x] += __shfl_xor(l[x], 16, 64);
+        l[x] += __shfl_xor(l[x], 32, 64);
+        if (quad == 0) {
+            stat[0][wave][16 * x + n] = m[x];
+            stat[1][wave][16 * x + n] = l[x];
+        }
+    }
+    __syncthreads();
+    float top[NQ], total[NQ];
+#pragma unroll
+    for (int x = 0; x < NQ; ++x) {
+        top[x] = -kInf;
+        total[x] = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) top[x] = fmaxf(top[x], stat[0][w][16 * x + n]);
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const float mw = stat[0][w][16 * x + n], lw = stat[1][w][16 * x + n];
+            total[x] += mw == -kInf ? lw : lw * __builtin_amdgcn_exp2f(mw - top[x]);
+        }
+        const float f = m[x] == -kInf ? 1.0f : __builtin_amdgcn_exp2f(m[x] - top[x]);
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sums[(wave * kRegs + (x * kTiles + t) * 4 + i) * kWave + lane] = o[x][t][i] * f;
+    }
+    __syncthreads();
+    const bool whole = ps.first == ps.last;
+    float* part = whole ? nullptr : a.part + part_at(a, D, r, tile, piece);
+#pragma unroll
+    for (int x = 0; x < NQ; ++x) {
+        if (!out[x]) continue;
+        const float inv = total[x] == 0.0f ? 0.0f : 1.0f / total[x];
+        for (int t = wave; t < kTiles; t += kWaves) {
+            f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) y[i] += sums[(w * kRegs + (x * kTiles + t) * 4 + i) * kWave + lane];
+            const int d = 16 * t + 4 * quad;
+            if (!whole) {
+                *reinterpret_cast<f32x4*>(part + (16 * x + n) * D + d) = y;
+            } else if (d < a.cache.dim) {
+                const bf16x2 lo = {static_cast<__bf16>(y[0] * inv), static_cast<__bf16>(y[1] * inv)};
+                const bf16x2 hi = {static_cast<__bf16>(y[2] * inv), static_cast<__bf16>(y[3] * inv)};
+                *reinterpret_cast<u32x2_any*>(out[x] + d) =
+                    u32x2{__builtin_bit_cast(unsigned int, lo), __builtin_bit_cast(unsigned int, hi)};
+            }
+        }
+        if (!whole && wave == 0 && quad == 0) {
+            part[a.tile_rows * D + 16 * x + n] = top[x];
+            part[a.tile_rows * (D + 1) + 16 * x + n] = total[x];
+        }
+    }
+}
+
+// Joins the pieces of the rows that more than one piece holds: one wave per row, a lane per piece for
+// the statistics, then a lane per D / 64 columns.
 template <int D>
 __global__ __launch_bounds__(kThreads) void paged_join_kernel(const PagedArgs a) {
-    const int64_t units = a.batch * a.cache.heads;
-    const int64_t unit = blockIdx.x % units;
-    const int tile = static_cast<int>(blockIdx.x / units);
-    const Request r = request(a, unit);
+    const Place at = place_of(a, blockIdx.x);
+    const int tile = at.tile;
+    const Request r = request(a, at.b, at.head);
     const int tile0 = tile * a.tile_rows;
     if (tile0 >= r.rows) return;
     const Pieces ps = pieces(a, r, tile0);
     if (ps.first == ps.last) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = ps.last - ps.first + 1;
     constexpr int kPer = D / 64;
     const int64_t piece_floats = static_cast<int64_t>(a.tile_rows) * (D + 2);
     for (int i = wave; i < a.tile_rows && tile0 + i < r.rows; i += kWaves) {
-        const float* part = a.part + part_at(a, D, unit, tile, ps.first);
+        const float* part = a.part + part_at(a, D, r, tile, ps.first);
         const float* m_at = part + a.tile_rows * D + i;
         const float* l_at = m_at + a.tile_rows;
-        float m = -kInf;
-        for (int p = 0; p <= ps.last - ps.first; ++p) m = fmaxf(m, m_at[p * piece_floats]);
-        float total = 0.0f, acc[kPer];
+        float m = -kInf, total = 0.0f, acc[kPer];
 #pragma unroll
         for (int e = 0; e < kPer; ++e) acc[e] = 0.0f;
-        for (int p = 0; p <= ps.last - ps.first; ++p) {
-            const float mp = m_at[p * piece_floats];
-            const float f = mp == -kInf ? 1.0f : __builtin_amdgcn_exp2f(mp - m);
-            total += f * l_at[p * piece_floats];
+        for (int p0 = 0; p0 < n; p0 += kWave) {
+            const bool mine = p0 + lane < n;
+            const float mp = mine ? m_at[(p0 + lane) * piece_floats] : -kInf;
+            const float lp = mine ? l_at[(p0 + lane) * piece_floats] : 0.0f;
+            float top = fmaxf(m, mp);
 #pragma unroll
-            for (int e = 0; e < kPer; ++e) acc[e] += f * part[p * piece_floats + static_cast<int64_t>(i) * D + kPer * lane + e];
+            for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d, 64));
+            const float f = mp == -kInf ? 1.0f : __builtin_amdgcn_exp2f(mp - top);
+            const float old = m == -kInf ? 1.0f : __builtin_amdgcn_exp2f(m - top);
+            float sum = f * lp;
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d, 64);
+            total = total * old + sum;
+            m = top;
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) acc[e] *= old;
+            const int count = min(n - p0, kWave);
+            const float* from = part + p0 * piece_floats + i * D + kPer * lane;
+            for (int p = 0; p < count; ++p) {
+                const float fp = __shfl(f, p, 64);
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) acc[e] += fp * from[p * piece_floats + e];
+            }
         }
         const float inv = total == 0.0f ? 0.0f : 1.0f / total;
         const int row = tile0 + i, d = kPer * lane;
@@ -469,8 +648,9 @@ template <int D>
 hipError_t launch_paged(const PagedArgs& a, hipStream_t stream) {
     const int64_t tiles = a.batch * a.cache.heads * a.tiles;
     const unsigned grid = static_cast<unsigned>(tiles * a.splits);
-    if (a.tile_rows == kRows) paged_kernel<D, 1><<<grid, kThreads, 0, stream>>>(a);
-    else paged_kernel<D, 4><<<grid, kThreads, 0, stream>>>(a);
+    if (a.tile_rows == 16) paged_few_kernel<D, 1><<<grid, kThreads, 0, stream>>>(a);
+    else if (a.tile_rows == 32) paged_few_kernel<D, 2><<<grid, kThreads, 0, stream>>>(a);
+    else paged_kernel<D><<<grid, kThreads, 0, stream>>>(a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;
     paged_join_kernel<D><<<static_cast<unsigned>(tiles), kThreads, 0, stream>>>(a);
