@@ -27,7 +27,7 @@ __device__ __forceinline__ Seen seen_keys(int i, int q_len, int kv_len, Mask m) 
 }
 
 // ------------------------------------------------------------------------------------ forward
-template <int D>
+template <int D, bool DIRECT>
 __global__ __launch_bounds__(kThreads, 2) void attention_kernel(const SequenceArgs a, const Unit* __restrict__ units) {
     __shared__ __align__(16) uint16_t lds[2][2][kKeys * D];  // buffer, K or V
     const Unit u = units[blockIdx.x];
@@ -49,39 +49,37 @@ __global__ __launch_bounds__(kThreads, 2) void attention_kernel(const SequenceAr
 
     const uint16_t* kp = at(a.k, u, u.kv_start, u.head / a.group);
     const uint16_t* vp = at(a.v, u, u.kv_start, u.head / a.group);
-    Stage<D, kKeys, kThreads> sk, sv;
+    Stage<D, kKeys, kThreads, DIRECT> sk, sv;
     Online<D> st;
     st.init();
     const float c = a.scale * kLog2e;
     if (begin < end) {
-        sk.load(tid, kp + begin * a.k.row, a.k.row, u.kv_len - begin, chunks);
-        sv.load(tid, vp + begin * a.v.row, a.v.row, u.kv_len - begin, chunks);
-        sk.store(tid, lds[0][0]);
-        sv.store(tid, lds[0][1]);
+        sk.begin(tid, lds[0][0], kp + begin * a.k.row, a.k.row, 0, u.kv_len - begin, chunks);
+        sv.begin(tid, lds[0][1], vp + begin * a.v.row, a.v.row, 0, u.kv_len - begin, chunks);
+        sk.end(tid, lds[0][0]);
+        sv.end(tid, lds[0][1]);
     }
     int buf = 0;
     for (int j0 = begin; j0 < end; j0 += kKeys, buf ^= 1) {
-        lds_barrier();
+        tile_barrier<DIRECT>();
         const int next = j0 + kKeys;
         if (next < end) {
-            sk.load(tid, kp + next * a.k.row, a.k.row, u.kv_len - next, chunks);
-            sv.load(tid, vp + next * a.v.row, a.v.row, u.kv_len - next, chunks);
+            sk.begin(tid, lds[buf ^ 1][0], kp + next * a.k.row, a.k.row, 0, u.kv_len - next, chunks);
+            sv.begin(tid, lds[buf ^ 1][1], vp + next * a.v.row, a.v.row, 0, u.kv_len - next, chunks);
         }
         if (any_row && j0 <= w1.hi && next > w0.lo) {
             f32x16 s[kKeys / 32];
-#pragma unroll
-            for (int k = 0; k < kKeys / 32; ++k) s[k] = row_product<D>(lds[buf][0], 32 * k, q, lane);
+            row_product<D>(s, lds[buf][0], 0, q, lane);
             if (j0 < w1.lo || next - 1 > w0.hi) {
 #pragma unroll
                 for (int k = 0; k < kKeys / 32; ++k) mask_block(s[k], j0 + 32 * k, h, mine.lo, mine.hi);
             }
             st.weigh(s, c);
-#pragma unroll
-            for (int k = 0; k < kKeys / 32; ++k) col_product<D>(st.o, lds[buf][1], 32 * k, s[k], lane);
+            col_product<D>(st.o, lds[buf][1], 0, s, lane);
         }
         if (next < end) {
-            sk.store(tid, lds[buf ^ 1][0]);
-            sv.store(tid, lds[buf ^ 1][1]);
+            sk.end(tid, lds[buf ^ 1][0]);
+            sv.end(tid, lds[buf ^ 1][1]);
         }
     }
     const float total = st.row_sum();
@@ -99,7 +97,7 @@ __device__ __forceinline__ float reference(float lse) { return lse == -kInf ? kI
 
 // dq = scale * sum_j dS_ij k_j, with dS = P (dP - delta), P = exp(s - lse), dP = do . v: query rows
 // stay in registers as in the forward pass, the keys stream through LDS.  Also leaves delta.
-template <int D>
+template <int D, bool DIRECT>
 __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(const SequenceArgs a, const Unit* __restrict__ units) {
     __shared__ __align__(16) uint16_t lds[2][2][kKeys * D];
     const Unit u = units[blockIdx.x];
@@ -136,45 +134,46 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(const Sequenc
     const bool any_row = i0 <= last;
     const uint16_t* kp = at(a.k, u, u.kv_start, u.head / a.group);
     const uint16_t* vp = at(a.v, u, u.kv_start, u.head / a.group);
-    Stage<D, kKeys, kThreads> sk, sv;
+    Stage<D, kKeys, kThreads, DIRECT> sk, sv;
     f32x16 dq[D / 32];
 #pragma unroll
     for (int t = 0; t < D / 32; ++t) dq[t] = zero16();
     const float c = a.scale * kLog2e;
     if (begin < end) {
-        sk.load(tid, kp + begin * a.k.row, a.k.row, u.kv_len - begin, chunks);
-        sv.load(tid, vp + begin * a.v.row, a.v.row, u.kv_len - begin, chunks);
-        sk.store(tid, lds[0][0]);
-        sv.store(tid, lds[0][1]);
+        sk.begin(tid, lds[0][0], kp + begin * a.k.row, a.k.row, 0, u.kv_len - begin, chunks);
+        sv.begin(tid, lds[0][1], vp + begin * a.v.row, a.v.row, 0, u.kv_len - begin, chunks);
+        sk.end(tid, lds[0][0]);
+        sv.end(tid, lds[0][1]);
     }
     int buf = 0;
     for (int j0 = begin; j0 < end; j0 += kKeys, buf ^= 1) {
-        lds_barrier();
+        tile_barrier<DIRECT>();
         const int next = j0 + kKeys;
         if (next < end) {
-            sk.load(tid, kp + next * a.k.row, a.k.row, u.kv_len - next, chunks);
-            sv.load(tid, vp + next * a.v.row, a.v.row, u.kv_len - next, chunks);
+            sk.begin(tid, lds[buf ^ 1][0], kp + next * a.k.row, a.k.row, 0, u.kv_len - next, chunks);
+            sv.begin(tid, lds[buf ^ 1][1], vp + next * a.v.row, a.v.row, 0, u.kv_len - next, chunks);
         }
         if (any_row && j0 <= w1.hi && next > w0.lo) {
             const bool masked = j0 < w1.lo || next - 1 > w0.hi;
 #pragma unroll
             for (int k = 0; k < kKeys / 32; ++k) {
-                f32x16 s = row_product<D>(lds[buf][0], 32 * k, q, lane);
-                const f32x16 dp = row_product<D>(lds[buf][1], 32 * k, dout, lane);
-                if (masked) mask_block(s, j0 + 32 * k, h, mine.lo, mine.hi);
+                f32x16 s[1], dp[1];
+                row_product<D>(s, lds[buf][0], 32 * k, q, lane);
+                row_product<D>(dp, lds[buf][1], 32 * k, dout, lane);
+                if (masked) mask_block(s[0], j0 + 32 * k, h, mine.lo, mine.hi);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -ref));
-                    const float ds = p * (dp[e] - delta);
+                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[0][e], c, -ref));
+                    const float ds = p * (dp[0][e] - delta);
                     // a masked score contributes nothing, whatever v holds there
-                    s[e] = masked && s[e] == -kInf ? 0.0f : ds;
+                    s[0][e] = masked && s[0][e] == -kInf ? 0.0f : ds;
                 }
                 col_product<D>(dq, lds[buf][0], 32 * k, s, lane);
             }
         }
         if (next < end) {
-            sk.store(tid, lds[buf ^ 1][0]);
-            sv.store(tid, lds[buf ^ 1][1]);
+            sk.end(tid, lds[buf ^ 1][0]);
+            sv.end(tid, lds[buf ^ 1][1]);
         }
     }
     if (lse == -kInf) {  // the row saw nothing: no gradient, whatever dout holds
@@ -188,7 +187,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(const Sequenc
 // dv_j = sum_i P_ij do_i and dk_j = scale * sum_i dS_ij q_i over the rows of all query heads that
 // share the key/value head: a wave keeps 32 keys (k, v and both sums in registers), the query
 // rows stream through LDS.  No sum crosses a workgroup, so the result does not depend on timing.
-template <int D>
+template <int D, bool DIRECT>
 __global__ __launch_bounds__(kThreads, 1) void attention_dkv_kernel(const SequenceArgs a, const Unit* __restrict__ units) {
     __shared__ __align__(16) uint16_t lds[2][2][kKeys * D];  // buffer, q or dout
     __shared__ __align__(16) float stat[2][2][kKeys];        // buffer, reference or delta
@@ -205,11 +204,13 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dkv_kernel(const Sequen
 #pragma unroll
     for (int t = 0; t < D / 32; ++t) dk[t] = dv[t] = zero16();
     const float c = a.scale * kLog2e;
-    // Query rows that see a key of the unit: i + off >= j, and i + off < j + window.
+    // Query rows that see a key of the unit: i + off >= j, and i + off < j + window.  Rows before the
+    // first key (`dead` of them, where there are more queries than keys) count as zeros, whatever they hold.
     const int off = u.kv_len - u.q_len;
     const int last = u.first + u.rows - 1;
-    int begin = 0, end = u.q_len;
+    int begin = 0, end = u.q_len, dead = 0;
     if (a.mask.causal) {
+        dead = max(0, -off);
         begin = max(0, u.first - off) / kKeys * kKeys;
         if (a.mask.window > 0 && static_cast<int64_t>(last) + a.mask.window - off < end) end = last + a.mask.window - off;
     }
@@ -217,50 +218,43 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dkv_kernel(const Sequen
     const int64_t total = static_cast<int64_t>(steps) * a.group;
     const bool any_row = j0 <= last;
 
-    Stage<D, kKeys, kThreads> sq, sd;
+    Stage<D, kKeys, kThreads, DIRECT> sq, sd;
     float ref = kInf, delta = 0.0f;  // of row `tid` of the step, threads 0 .. kKeys - 1
-    // Rows that saw nothing (their statistic says so) count as zeros, whatever they hold.
-    auto fetch = [&](int g, int r0) {
+    auto fetch = [&](int g, int r0, int buf) {
         const int head = u.head * a.group + g;
-        const uint16_t* qp = at(a.q, u, u.q_start + r0, head);
-        const uint16_t* dp = at(a.dout, u, u.q_start + r0, head);
-        const int64_t r = head * a.total_q + u.lse_row + r0;
-        sq.load(tid, qp, a.q.row, end - r0, chunks);
-        sd.load(tid, dp, a.dout.row, end - r0, chunks);
-#pragma unroll
-        for (int n = 0; n < sq.kN; ++n) {
-            const int row = sq.row(tid, n);
-            if (row < end - r0 && a.lse[r + row] == -kInf) sq.r[n] = sd.r[n] = u32x4{0, 0, 0, 0};
-        }
-        ref = kInf;
-        delta = 0.0f;
-        if (tid < kKeys && tid < end - r0) {
-            ref = reference(a.lse[r + tid]);
-            delta = a.delta[r + tid];
-            if (ref == kInf) delta = 0.0f;
+        sq.begin(tid, lds[buf][0], at(a.q, u, u.q_start + r0, head), a.q.row, dead - r0, end - r0, chunks);
+        sd.begin(tid, lds[buf][1], at(a.dout, u, u.q_start + r0, head), a.dout.row, dead - r0, end - r0, chunks);
+        if (tid < kKeys) {
+            const int64_t r = head * a.total_q + u.lse_row + min(r0 + tid, end - 1);
+            ref = reference(a.lse[r]);
+            delta = a.delta[r];
+            if (r0 + tid >= end || ref == kInf) {
+                ref = kInf;
+                delta = 0.0f;
+            }
         }
     };
     auto put = [&](int buf) {
-        sq.store(tid, lds[buf][0]);
-        sd.store(tid, lds[buf][1]);
+        sq.end(tid, lds[buf][0]);
+        sd.end(tid, lds[buf][1]);
         if (tid < kKeys) {
             stat[buf][0][tid] = ref;
             stat[buf][1][tid] = delta;
         }
     };
     if (total > 0) {
-        fetch(0, begin);
+        fetch(0, begin, 0);
         put(0);
     }
     int buf = 0, r0 = begin, g = 0;
     for (int64_t n = 0; n < total; ++n, buf ^= 1) {
-        lds_barrier();
+        tile_barrier<DIRECT>();
         int next_r0 = r0 + kKeys, next_g = g;
         if (next_r0 >= end) {
             next_r0 = begin;
             ++next_g;
         }
-        if (n + 1 < total) fetch(next_g, next_r0);
+        if (n + 1 < total) fetch(next_g, next_r0, buf ^ 1);
         // whether the mask hides some pair, or every pair, of these query rows and the wave's keys
         bool masked = false, none = !any_row;
         if (a.mask.causal) {
@@ -275,8 +269,9 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dkv_kernel(const Sequen
         if (!none) {
 #pragma unroll
             for (int b = 0; b < kKeys / 32; ++b) {
-                f32x16 p = row_product<D>(lds[buf][0], 32 * b, k, lane);
-                f32x16 ds = row_product<D>(lds[buf][1], 32 * b, v, lane);
+                f32x16 p[1], ds[1];
+                row_product<D>(p, lds[buf][0], 32 * b, k, lane);
+                row_product<D>(ds, lds[buf][1], 32 * b, v, lane);
 #pragma unroll
                 for (int e4 = 0; e4 < 4; ++e4) {
                     const f32x4 rr = *reinterpret_cast<const f32x4*>(&stat[buf][0][32 * b + 8 * e4 + 4 * h]);
@@ -284,16 +279,16 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dkv_kernel(const Sequen
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int x = 4 * e4 + e;
-                        float pv = __builtin_amdgcn_exp2f(__builtin_fmaf(p[x], c, -rr[e]));
-                        float dv_ = pv * (ds[x] - dd[e]);
+                        float pv = __builtin_amdgcn_exp2f(__builtin_fmaf(p[0][x], c, -rr[e]));
+                        float dv_ = pv * (ds[0][x] - dd[e]);
                         if (masked) {
                             const Seen s = seen_keys(r0 + 32 * b + 8 * e4 + 4 * h + e, u.q_len, u.kv_len, a.mask);
                             const bool sees = j >= s.lo && j <= s.hi;
                             pv = sees ? pv : 0.0f;
                             dv_ = sees ? dv_ : 0.0f;
                         }
-                        p[x] = pv;
-                        ds[x] = dv_;
+                        p[0][x] = pv;
+                        ds[0][x] = dv_;
                     }
                 }
                 col_product<D>(dv, lds[buf][1], 32 * b, p, lane);
@@ -311,24 +306,41 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dkv_kernel(const Sequen
 
 }  // namespace
 
+// Whether 16-byte pieces of an operand lie on 16-byte boundaries.
+bool aligned_pieces(const Heads& t) {
+    return reinterpret_cast<uintptr_t>(t.p) % 16 == 0 && (t.seq | t.row | t.head) % 8 == 0;
+}
+
 hipError_t launch_attention(const SequenceArgs& a, const Unit* units, int64_t n, hipStream_t stream) {
     if (n == 0) return hipSuccess;
-    if (a.dim <= 64) attention_kernel<64><<<static_cast<unsigned>(n), kThreads, 0, stream>>>(a, units);
-    else attention_kernel<128><<<static_cast<unsigned>(n), kThreads, 0, stream>>>(a, units);
+    const bool direct = aligned_pieces(a.k) && aligned_pieces(a.v);
+    const unsigned grid = static_cast<unsigned>(n);
+    if (a.dim <= 64 && direct) attention_kernel<64, true><<<grid, kThreads, 0, stream>>>(a, units);
+    else if (a.dim <= 64) attention_kernel<64, false><<<grid, kThreads, 0, stream>>>(a, units);
+    else if (direct) attention_kernel<128, true><<<grid, kThreads, 0, stream>>>(a, units);
+    else attention_kernel<128, false><<<grid, kThreads, 0, stream>>>(a, units);
     return hipGetLastError();
 }
 
 hipError_t launch_attention_backward(const SequenceArgs& a, const Unit* q_units, int64_t n_q, const Unit* kv_units,
                                      int64_t n_kv, hipStream_t stream) {
     if (n_q > 0) {
-        if (a.dim <= 64) attention_dq_kernel<64><<<static_cast<unsigned>(n_q), kThreads, 0, stream>>>(a, q_units);
-        else attention_dq_kernel<128><<<static_cast<unsigned>(n_q), kThreads, 0, stream>>>(a, q_units);
+        const bool direct = aligned_pieces(a.k) && aligned_pieces(a.v);
+        const unsigned grid = static_cast<unsigned>(n_q);
+        if (a.dim <= 64 && direct) attention_dq_kernel<64, true><<<grid, kThreads, 0, stream>>>(a, q_units);
+        else if (a.dim <= 64) attention_dq_kernel<64, false><<<grid, kThreads, 0, stream>>>(a, q_units);
+        else if (direct) attention_dq_kernel<128, true><<<grid, kThreads, 0, stream>>>(a, q_units);
+        else attention_dq_kernel<128, false><<<grid, kThreads, 0, stream>>>(a, q_units);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     if (n_kv > 0) {
-        if (a.dim <= 64) attention_dkv_kernel<64><<<static_cast<unsigned>(n_kv), kThreads, 0, stream>>>(a, kv_units);
-        else attention_dkv_kernel<128><<<static_cast<unsigned>(n_kv), kThreads, 0, stream>>>(a, kv_units);
+        const bool direct = aligned_pieces(a.q) && aligned_pieces(a.dout);
+        const unsigned grid = static_cast<unsigned>(n_kv);
+        if (a.dim <= 64 && direct) attention_dkv_kernel<64, true><<<grid, kThreads, 0, stream>>>(a, kv_units);
+        else if (a.dim <= 64) attention_dkv_kernel<64, false><<<grid, kThreads, 0, stream>>>(a, kv_units);
+        else if (direct) attention_dkv_kernel<128, true><<<grid, kThreads, 0, stream>>>(a, kv_units);
+        else attention_dkv_kernel<128, false><<<grid, kThreads, 0, stream>>>(a, kv_units);
         return hipGetLastError();
     }
     return hipSuccess;

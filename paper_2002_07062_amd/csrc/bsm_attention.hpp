@@ -38,6 +38,8 @@ constexpr float kLn2 = 0.69314718055994530942f;
 constexpr int kWave = 64;
 constexpr int kRows = 32;  // rows of the result per wave
 constexpr float kInf = __builtin_huge_valf();
+constexpr int kAhead = 4;      // fragments read ahead of their use
+constexpr int kMayCross = 0x6; // of the fixed order: vector and scalar arithmetic may move
 
 // ------------------------------------------------------------------------------- LDS tiles
 // A tile is ROWS x D bf16, row after row, in 16-byte chunks whose place in the row is permuted
@@ -81,28 +83,44 @@ __device__ __forceinline__ u32x4 load_or_zero(const uint16_t* p, bool live) {
     return *reinterpret_cast<const u32x4_any*>(live ? p : kZeros);
 }
 
-// The pieces of a ROWS x D tile that one of THREADS threads carries from memory to LDS.  Rows and
-// chunks that do not exist are zero (a masked probability times what lies there must be zero).
-template <int D, int ROWS, int THREADS>
+// Carries a ROWS x D tile from memory to LDS, 16 bytes at a time: `begin` starts the loads of the tile
+// whose first row is at p and of which rows lo .. hi - 1 exist, `end` leaves them in LDS; then a
+// tile_barrier makes them visible.  Rows and chunks that do not exist are zeros (a masked
+// probability times what lies there must be zero).
+// DIRECT: memory to LDS without registers on the way, which takes 16-byte aligned pieces.  The place of a
+// lane's 16 bytes in LDS is fixed (64 lanes side by side), so the lane reads the chunk that belongs there.
+template <int D, int ROWS, int THREADS, bool DIRECT>
 struct Stage {
     static constexpr int kN = ROWS * Tile<D>::kChunks / THREADS;
     static_assert(kN >= 1 && ROWS * Tile<D>::kChunks % THREADS == 0, "");
-    u32x4 r[kN];
+    u32x4 r[DIRECT ? 1 : kN];
     __device__ static __forceinline__ int row(int tid, int j) { return (tid + THREADS * j) / Tile<D>::kChunks; }
-    __device__ static __forceinline__ int chunk(int tid) { return tid % Tile<D>::kChunks; }
-    // `rows` of the tile exist; `p` is its first row
-    __device__ __forceinline__ void load(int tid, const uint16_t* p, int64_t stride, int rows, int chunks) {
-        const int c = chunk(tid);
-#pragma unroll
-        for (int j = 0; j < kN; ++j) {
-            const int i = row(tid, j);
-            r[j] = load_or_zero(p + i * stride + 8 * c, i < rows && c < chunks);
+    __device__ static __forceinline__ int chunk(int tid, int j) {
+        const int c = tid % Tile<D>::kChunks;
+        return DIRECT ? Tile<D>::place(row(tid, j), c) % Tile<D>::kChunks : c;
+    }
+    __device__ __forceinline__ void piece(int tid, int j, uint16_t* lds, const uint16_t* p, bool live) {
+        const uint16_t* from = live ? p : kZeros;
+        if constexpr (DIRECT) {
+            uint16_t* to = lds + 8 * ((tid & ~63) + THREADS * j);
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+                                             (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+        } else {
+            r[j] = *reinterpret_cast<const u32x4_any*>(from);
         }
     }
-    __device__ __forceinline__ void store(int tid, uint16_t* lds) const {
-        const int c = chunk(tid);
+    __device__ __forceinline__ void begin(int tid, uint16_t* lds, const uint16_t* p, int64_t stride, int lo, int hi, int chunks) {
 #pragma unroll
-        for (int j = 0; j < kN; ++j) *reinterpret_cast<u32x4*>(lds + 8 * Tile<D>::place(row(tid, j), c)) = r[j];
+        for (int j = 0; j < kN; ++j) {
+            const int i = row(tid, j), c = chunk(tid, j);
+            piece(tid, j, lds, p + i * stride + 8 * c, i >= lo && i < hi && c < chunks);
+        }
+    }
+    __device__ __forceinline__ void end(int tid, uint16_t* lds) const {
+        if constexpr (!DIRECT) {
+#pragma unroll
+            for (int j = 0; j < kN; ++j) *reinterpret_cast<u32x4*>(lds + 8 * Tile<D>::place(row(tid, j), chunk(tid, j))) = r[j];
+        }
     }
 };
 
@@ -130,14 +148,34 @@ __device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
 
-// 32 rows of the tile (from row r0) times the operand's 32 rows: lane (li, h) gets column li
-// (operand row) and tile rows r0 + 8 (i / 4) + 4 h + i % 4.
-template <int D>
-__device__ __forceinline__ f32x16 row_product(const uint16_t* lds, int r0, const RowOperand<D>& q, int lane) {
-    f32x16 acc = zero16();
+// Runs use(i, fragment i), i = 0 .. N - 1, with the next AHEAD fragments already on their way from LDS.
+// The order is held as it is written: left alone, the compiler moves each read to right before its use,
+// and every matrix instruction then waits for LDS.
+template <int N, int AHEAD, class Read, class Use>
+__device__ __forceinline__ void pipelined(Read read, Use use) {
+    bf16x8 f[AHEAD];
 #pragma unroll
-    for (int s = 0; s < D / 16; ++s) acc = mfma(Tile<D>::row_frag(lds, r0 + (lane & 31), s, lane >> 5), q.f[s], acc);
-    return acc;
+    for (int i = 0; i < AHEAD && i < N; ++i) f[i] = read(i);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const bf16x8 now = f[i % AHEAD];
+        if (i + AHEAD < N) f[i % AHEAD] = read(i + AHEAD);
+        __builtin_amdgcn_sched_barrier(kMayCross);
+        use(i, now);
+        __builtin_amdgcn_sched_barrier(kMayCross);
+    }
+}
+
+// 32 KT rows of the tile (from row r0) times the operand's 32 rows: lane (li, h) gets column li
+// (operand row) and, in acc[k], tile rows r0 + 32 k + 8 (i / 4) + 4 h + i % 4.
+template <int D, int KT>
+__device__ __forceinline__ void row_product(f32x16 (&acc)[KT], const uint16_t* lds, int r0, const RowOperand<D>& q, int lane) {
+    constexpr int kSteps = D / 16;
+#pragma unroll
+    for (int k = 0; k < KT; ++k) acc[k] = zero16();
+    pipelined<KT * kSteps, kAhead>(
+        [&](int i) { return Tile<D>::row_frag(lds, r0 + 32 * (i / kSteps) + (lane & 31), i % kSteps, lane >> 5); },
+        [&](int i, bf16x8 a) { acc[i / kSteps] = mfma(a, q.f[i % kSteps], acc[i / kSteps]); });
 }
 
 // Registers 8 s .. 8 s + 7 rounded to bf16 (nearest even): probabilities and score gradients are
@@ -149,16 +187,17 @@ __device__ __forceinline__ bf16x8 half_operand(const f32x16& x, int s) {
     return v;
 }
 
-// acc[t] += (columns 32 t .. of tile rows r0 .. r0 + 31)^T times x: lane li keeps its column of x,
+// acc[t] += (columns 32 t .. of tile rows r0 .. r0 + 32 KT - 1)^T times x: lane li keeps its column of x,
 // rows 32 t + 8 (i / 4) + 4 h + i % 4 of the tile's columns.
-template <int D>
-__device__ __forceinline__ void col_product(f32x16 (&acc)[D / 32], const uint16_t* lds, int r0, const f32x16& x, int lane) {
+template <int D, int KT>
+__device__ __forceinline__ void col_product(f32x16 (&acc)[D / 32], const uint16_t* lds, int r0, const f32x16 (&x)[KT], int lane) {
+    constexpr int kTiles = D / 32;
+    bf16x8 b[2 * KT];
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-        const bf16x8 b = half_operand(x, s);
-#pragma unroll
-        for (int t = 0; t < D / 32; ++t) acc[t] = mfma(Tile<D>::col_frag(lds, r0 + 16 * s, t, lane), b, acc[t]);
-    }
+    for (int s = 0; s < 2 * KT; ++s) b[s] = half_operand(x[s / 2], s % 2);
+    pipelined<2 * KT * kTiles, kAhead>(
+        [&](int i) { return Tile<D>::col_frag(lds, r0 + 16 * (i / kTiles), i % kTiles, lane); },
+        [&](int i, bf16x8 a) { acc[i % kTiles] = mfma(a, b[i / kTiles], acc[i % kTiles]); });
 }
 
 // Value of the other half of the wave (lanes l and l + 32 exchanged).
@@ -195,8 +234,11 @@ __device__ __forceinline__ void store_row(uint16_t* row, bool live, const f32x16
     for (int t = 0; t < D / 32; ++t) store_block(row, live, acc[t], f, t, h, chunks);
 }
 
-// Barrier that orders the workgroup's LDS accesses and leaves loads from memory in flight.
-__device__ __forceinline__ void lds_barrier() {
+// Barrier after which the tiles that were begun and ended before it are visible to the workgroup, and no
+// wave reads the ones before.  What is still on its way straight to LDS is waited for.
+template <bool DIRECT>
+__device__ __forceinline__ void tile_barrier() {
+    if constexpr (DIRECT) __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");

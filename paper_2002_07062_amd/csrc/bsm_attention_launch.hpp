@@ -41,6 +41,8 @@ struct SequenceArgs {
     float scale;
 };
 
+bool aligned_pieces(const Heads& t);  // 16-byte pieces on 16-byte boundaries
+
 hipError_t launch_attention(const SequenceArgs& a, const Unit* units, int64_t n, hipStream_t stream);
 // dq (and delta), then dk and dv, which read delta
 hipError_t launch_attention_backward(const SequenceArgs& a, const Unit* q_units, int64_t n_q, const Unit* kv_units,

@@ -89,36 +89,37 @@ __device__ __forceinline__ Place place_of(const PagedArgs& a, int64_t w) {
 
 // The rows of K and V that a thread stages: tile row i is key j0 + i of the request.  Keys past its
 // end, and keys of table entries that name no page, are zeros.
-template <int D, int ROWS, int THREADS>
+template <int D, int ROWS, int THREADS, bool DIRECT>
 struct PagedStage {
-    using S = Stage<D, ROWS, THREADS>;
+    using S = Stage<D, ROWS, THREADS, DIRECT>;
     S k, v;
     int page[S::kN];
-    __device__ __forceinline__ static int divide(const PagedArgs& a, int j) { return j / a.cache.page_size; }
     // table entries of the tile at j0 (-1: none); the request has keys 0 .. end - 1
     __device__ __forceinline__ void find(const PagedArgs& a, const int32_t* table, int tid, int j0, int end) {
 #pragma unroll
         for (int n = 0; n < S::kN; ++n) {
-            const int j = j0 + S::row(tid, n), entry = table[divide(a, min(j, end - 1))];
+            const int j = j0 + S::row(tid, n), entry = table[min(j, end - 1) / a.cache.page_size];
             page[n] = j < end && entry < a.cache.n_pages ? entry : -1;
         }
     }
-    __device__ __forceinline__ void load(const PagedArgs& a, int head, int tid, int j0, int chunks) {
-        const int c = S::chunk(tid);
+    __device__ __forceinline__ void begin(const PagedArgs& a, int head, int tid, int j0, int chunks, uint16_t* lds_k, uint16_t* lds_v) {
 #pragma unroll
         for (int n = 0; n < S::kN; ++n) {
-            const int j = j0 + S::row(tid, n);
+            const int j = j0 + S::row(tid, n), c = S::chunk(tid, n);
             const bool live = page[n] >= 0 && c < chunks;
-            const int64_t at = page[n] * a.cache.page + (j - divide(a, j) * a.cache.page_size) * a.cache.row +
-                               head * a.cache.head + 8 * c;
-            k.r[n] = load_or_zero(a.cache.k + at, live);
-            v.r[n] = load_or_zero(a.cache.v + at, live);
+            const int64_t from = page[n] * a.cache.page + j % a.cache.page_size * a.cache.row + head * a.cache.head + 8 * c;
+            k.piece(tid, n, lds_k, a.cache.k + from, live);
+            v.piece(tid, n, lds_v, a.cache.v + from, live);
         }
+    }
+    __device__ __forceinline__ void end(int tid, uint16_t* lds_k, uint16_t* lds_v) const {
+        k.end(tid, lds_k);
+        v.end(tid, lds_v);
     }
 };
 
 // Many rows (chunks of prompts): a tile has 128 rows, 32 per wave, and the waves share the staged keys.
-template <int D>
+template <int D, bool DIRECT>
 __global__ __launch_bounds__(kThreads, 2) void paged_kernel(const PagedArgs a) {
     constexpr int kKeys = 64, kTileElems = kKeys * D;
     __shared__ __align__(16) uint16_t lds[2][2][kTileElems];  // buffer, K or V
@@ -150,37 +151,33 @@ __global__ __launch_bounds__(kThreads, 2) void paged_kernel(const PagedArgs a) {
     Online<D> st;
     st.init();
     const float c = a.scale * kLog2e;
-    PagedStage<D, kKeys, kThreads> stage;
+    PagedStage<D, kKeys, kThreads, DIRECT> stage;
     if (begin < end) {
         stage.find(a, table, tid, begin, r.kv_len);
-        stage.load(a, r.head, tid, begin, chunks);
+        stage.begin(a, r.head, tid, begin, chunks, lds[0][0], lds[0][1]);
         stage.find(a, table, tid, begin + kKeys, r.kv_len);
-        stage.k.store(tid, lds[0][0]);
-        stage.v.store(tid, lds[0][1]);
+        stage.end(tid, lds[0][0], lds[0][1]);
     }
     int buf = 0;
     for (int j0 = begin; j0 < end; j0 += kKeys, buf ^= 1) {
         const int next = j0 + kKeys;
-        lds_barrier();
+        tile_barrier<DIRECT>();
         if (next < end) {
-            stage.load(a, r.head, tid, next, chunks);
+            stage.begin(a, r.head, tid, next, chunks, lds[buf ^ 1][0], lds[buf ^ 1][1]);
             stage.find(a, table, tid, next + kKeys, r.kv_len);
         }
         if (any_row && j0 <= w1.hi && next > w0.lo) {
             f32x16 s[kKeys / 32];
-#pragma unroll
-            for (int k = 0; k < kKeys / 32; ++k) s[k] = row_product<D>(lds[buf][0], 32 * k, q, lane);
+            row_product<D>(s, lds[buf][0], 0, q, lane);
             if (j0 < w1.lo || next - 1 > w0.hi || end < next) {
 #pragma unroll
                 for (int k = 0; k < kKeys / 32; ++k) mask_block(s[k], j0 + 32 * k, h, mine.lo, min(mine.hi, end - 1));
             }
             st.weigh(s, c);
-#pragma unroll
-            for (int k = 0; k < kKeys / 32; ++k) col_product<D>(st.o, lds[buf][1], 32 * k, s[k], lane);
+            col_product<D>(st.o, lds[buf][1], 0, s, lane);
         }
         if (next < end) {
-            stage.k.store(tid, lds[buf ^ 1][0]);
-            stage.v.store(tid, lds[buf ^ 1][1]);
+            stage.end(tid, lds[buf ^ 1][0], lds[buf ^ 1][1]);
         }
     }
     const float total = st.row_sum();
@@ -650,7 +647,9 @@ hipError_t launch_paged(const PagedArgs& a, hipStream_t stream) {
     const unsigned grid = static_cast<unsigned>(tiles * a.splits);
     if (a.tile_rows == 16) paged_few_kernel<D, 1><<<grid, kThreads, 0, stream>>>(a);
     else if (a.tile_rows == 32) paged_few_kernel<D, 2><<<grid, kThreads, 0, stream>>>(a);
-    else paged_kernel<D><<<grid, kThreads, 0, stream>>>(a);
+    else if (aligned_pieces({a.cache.k, a.cache.page, a.cache.row, a.cache.head}) && reinterpret_cast<uintptr_t>(a.cache.v) % 16 == 0)
+        paged_kernel<D, true><<<grid, kThreads, 0, stream>>>(a);
+    else paged_kernel<D, false><<<grid, kThreads, 0, stream>>>(a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;
     paged_join_kernel<D><<<static_cast<unsigned>(tiles), kThreads, 0, stream>>>(a);
