@@ -53,35 +53,40 @@ __global__ __launch_bounds__(kThreads, 2) void attention_kernel(const SequenceAr
     Online<D> st;
     st.init();
     const float c = a.scale * kLog2e;
+    sk.init(tid, a.k.row, chunks);
+    sv.init(tid, a.v.row, chunks);
     if (begin < end) {
         sk.begin(tid, lds[0][0], kp + begin * a.k.row, a.k.row, 0, u.kv_len - begin, chunks);
         sv.begin(tid, lds[0][1], vp + begin * a.v.row, a.v.row, 0, u.kv_len - begin, chunks);
         sk.end(tid, lds[0][0]);
         sv.end(tid, lds[0][1]);
     }
-    int buf = 0;
-    for (int j0 = begin; j0 < end; j0 += kKeys, buf ^= 1) {
+    const Frags<D> at_lane(lane);
+    // the tiles read and the tiles written in a step are apart
+    auto step = [&](int j0, uint16_t* __restrict__ next_k, uint16_t* __restrict__ next_v, const uint16_t* __restrict__ now_k,
+                    const uint16_t* __restrict__ now_v) __attribute__((always_inline)) {
         tile_barrier<DIRECT>();
         const int next = j0 + kKeys;
         if (next < end) {
-            sk.begin(tid, lds[buf ^ 1][0], kp + next * a.k.row, a.k.row, 0, u.kv_len - next, chunks);
-            sv.begin(tid, lds[buf ^ 1][1], vp + next * a.v.row, a.v.row, 0, u.kv_len - next, chunks);
+            sk.begin(tid, next_k, kp + next * a.k.row, a.k.row, 0, u.kv_len - next, chunks);
+            sv.begin(tid, next_v, vp + next * a.v.row, a.v.row, 0, u.kv_len - next, chunks);
         }
         if (any_row && j0 <= w1.hi && next > w0.lo) {
             f32x16 s[kKeys / 32];
-            row_product<D>(s, lds[buf][0], 0, q, lane);
+            row_product<D>(s, at_lane, now_k, 0, q);
             if (j0 < w1.lo || next - 1 > w0.hi) {
 #pragma unroll
                 for (int k = 0; k < kKeys / 32; ++k) mask_block(s[k], j0 + 32 * k, h, mine.lo, mine.hi);
             }
             st.weigh(s, c);
-            col_product<D>(st.o, lds[buf][1], 0, s, lane);
+            col_product<D>(st.o, at_lane, now_v, 0, s);
         }
         if (next < end) {
-            sk.end(tid, lds[buf ^ 1][0]);
-            sv.end(tid, lds[buf ^ 1][1]);
+            sk.end(tid, next_k);
+            sv.end(tid, next_v);
         }
-    }
+    };
+    in_turn(begin, end, kKeys, [&](int j0, auto buf) { step(j0, lds[1 - buf][0], lds[1 - buf][1], lds[buf][0], lds[buf][1]); });
     const float total = st.row_sum();
     // a row that sees nothing, or only scores of -inf, is zero
     const float f = total == 0.0f ? 0.0f : 1.0f / total;
@@ -118,7 +123,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(const Sequenc
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 delta = __builtin_fmaf(static_cast<float>(o.f[s][e]), static_cast<float>(dout.f[s][e]), delta);
-        delta += other_half(delta);
+        delta = half_sum(delta);
         const int64_t r = u.head * a.total_q + u.lse_row + i;
         if (live) {
             lse = a.lse[r];
@@ -139,27 +144,30 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(const Sequenc
 #pragma unroll
     for (int t = 0; t < D / 32; ++t) dq[t] = zero16();
     const float c = a.scale * kLog2e;
+    sk.init(tid, a.k.row, chunks);
+    sv.init(tid, a.v.row, chunks);
     if (begin < end) {
         sk.begin(tid, lds[0][0], kp + begin * a.k.row, a.k.row, 0, u.kv_len - begin, chunks);
         sv.begin(tid, lds[0][1], vp + begin * a.v.row, a.v.row, 0, u.kv_len - begin, chunks);
         sk.end(tid, lds[0][0]);
         sv.end(tid, lds[0][1]);
     }
-    int buf = 0;
-    for (int j0 = begin; j0 < end; j0 += kKeys, buf ^= 1) {
+    const Frags<D> at_lane(lane);
+    auto step = [&](int j0, uint16_t* __restrict__ next_k, uint16_t* __restrict__ next_v, const uint16_t* __restrict__ now_k,
+                    const uint16_t* __restrict__ now_v) __attribute__((always_inline)) {
         tile_barrier<DIRECT>();
         const int next = j0 + kKeys;
         if (next < end) {
-            sk.begin(tid, lds[buf ^ 1][0], kp + next * a.k.row, a.k.row, 0, u.kv_len - next, chunks);
-            sv.begin(tid, lds[buf ^ 1][1], vp + next * a.v.row, a.v.row, 0, u.kv_len - next, chunks);
+            sk.begin(tid, next_k, kp + next * a.k.row, a.k.row, 0, u.kv_len - next, chunks);
+            sv.begin(tid, next_v, vp + next * a.v.row, a.v.row, 0, u.kv_len - next, chunks);
         }
         if (any_row && j0 <= w1.hi && next > w0.lo) {
             const bool masked = j0 < w1.lo || next - 1 > w0.hi;
 #pragma unroll
             for (int k = 0; k < kKeys / 32; ++k) {
                 f32x16 s[1], dp[1];
-                row_product<D>(s, lds[buf][0], 32 * k, q, lane);
-                row_product<D>(dp, lds[buf][1], 32 * k, dout, lane);
+                row_product<D>(s, at_lane, now_k, 32 * k, q);
+                row_product<D>(dp, at_lane, now_v, 32 * k, dout);
                 if (masked) mask_block(s[0], j0 + 32 * k, h, mine.lo, mine.hi);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
@@ -168,14 +176,15 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(const Sequenc
                     // a masked score contributes nothing, whatever v holds there
                     s[0][e] = masked && s[0][e] == -kInf ? 0.0f : ds;
                 }
-                col_product<D>(dq, lds[buf][0], 32 * k, s, lane);
+                col_product<D>(dq, at_lane, now_k, 32 * k, s);
             }
         }
         if (next < end) {
-            sk.end(tid, lds[buf ^ 1][0]);
-            sv.end(tid, lds[buf ^ 1][1]);
+            sk.end(tid, next_k);
+            sv.end(tid, next_v);
         }
-    }
+    };
+    in_turn(begin, end, kKeys, [&](int j0, auto buf) { step(j0, lds[1 - buf][0], lds[1 - buf][1], lds[buf][0], lds[buf][1]); });
     if (lse == -kInf) {  // the row saw nothing: no gradient, whatever dout holds
 #pragma unroll
         for (int t = 0; t < D / 32; ++t) dq[t] = zero16();
@@ -190,7 +199,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(const Sequenc
 template <int D, bool DIRECT>
 __global__ __launch_bounds__(kThreads, 1) void attention_dkv_kernel(const SequenceArgs a, const Unit* __restrict__ units) {
     __shared__ __align__(16) uint16_t lds[2][2][kKeys * D];  // buffer, q or dout
-    __shared__ __align__(16) float stat[2][2][kKeys];        // buffer, reference or delta
+    __shared__ __align__(16) float stat[2][2 * kKeys];       // buffer; references, then deltas
     const Unit u = units[blockIdx.x];
     if (u.rows <= 0) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, li = lane & 31, h = lane >> 5;
@@ -220,10 +229,12 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dkv_kernel(const Sequen
 
     Stage<D, kKeys, kThreads, DIRECT> sq, sd;
     float ref = kInf, delta = 0.0f;  // of row `tid` of the step, threads 0 .. kKeys - 1
-    auto fetch = [&](int g, int r0, int buf) {
+    sq.init(tid, a.q.row, chunks);
+    sd.init(tid, a.dout.row, chunks);
+    auto fetch = [&](int g, int r0, uint16_t* to_q, uint16_t* to_d) __attribute__((always_inline)) {
         const int head = u.head * a.group + g;
-        sq.begin(tid, lds[buf][0], at(a.q, u, u.q_start + r0, head), a.q.row, dead - r0, end - r0, chunks);
-        sd.begin(tid, lds[buf][1], at(a.dout, u, u.q_start + r0, head), a.dout.row, dead - r0, end - r0, chunks);
+        sq.begin(tid, to_q, at(a.q, u, u.q_start + r0, head), a.q.row, dead - r0, end - r0, chunks);
+        sd.begin(tid, to_d, at(a.dout, u, u.q_start + r0, head), a.dout.row, dead - r0, end - r0, chunks);
         if (tid < kKeys) {
             const int64_t r = head * a.total_q + u.lse_row + min(r0 + tid, end - 1);
             ref = reference(a.lse[r]);
@@ -234,27 +245,30 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dkv_kernel(const Sequen
             }
         }
     };
-    auto put = [&](int buf) {
-        sq.end(tid, lds[buf][0]);
-        sd.end(tid, lds[buf][1]);
+    auto put = [&](uint16_t* to_q, uint16_t* to_d, float* to_stat) __attribute__((always_inline)) {
+        sq.end(tid, to_q);
+        sd.end(tid, to_d);
         if (tid < kKeys) {
-            stat[buf][0][tid] = ref;
-            stat[buf][1][tid] = delta;
+            to_stat[tid] = ref;
+            to_stat[kKeys + tid] = delta;
         }
     };
     if (total > 0) {
-        fetch(0, begin, 0);
-        put(0);
+        fetch(0, begin, lds[0][0], lds[0][1]);
+        put(lds[0][0], lds[0][1], stat[0]);
     }
-    int buf = 0, r0 = begin, g = 0;
-    for (int64_t n = 0; n < total; ++n, buf ^= 1) {
+    int r0 = begin, g = 0;
+    const Frags<D> at_lane(lane);
+    auto step = [&](int64_t n, uint16_t* __restrict__ next_q, uint16_t* __restrict__ next_d, float* __restrict__ next_stat,
+                    const uint16_t* __restrict__ now_q, const uint16_t* __restrict__ now_d, const float* __restrict__ now_stat)
+                    __attribute__((always_inline)) {
         tile_barrier<DIRECT>();
         int next_r0 = r0 + kKeys, next_g = g;
         if (next_r0 >= end) {
             next_r0 = begin;
             ++next_g;
         }
-        if (n + 1 < total) fetch(next_g, next_r0, buf ^ 1);
+        if (n + 1 < total) fetch(next_g, next_r0, next_q, next_d);
         // whether the mask hides some pair, or every pair, of these query rows and the wave's keys
         bool masked = false, none = !any_row;
         if (a.mask.causal) {
@@ -270,12 +284,12 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dkv_kernel(const Sequen
 #pragma unroll
             for (int b = 0; b < kKeys / 32; ++b) {
                 f32x16 p[1], ds[1];
-                row_product<D>(p, lds[buf][0], 32 * b, k, lane);
-                row_product<D>(ds, lds[buf][1], 32 * b, v, lane);
+                row_product<D>(p, at_lane, now_q, 32 * b, k);
+                row_product<D>(ds, at_lane, now_d, 32 * b, v);
 #pragma unroll
                 for (int e4 = 0; e4 < 4; ++e4) {
-                    const f32x4 rr = *reinterpret_cast<const f32x4*>(&stat[buf][0][32 * b + 8 * e4 + 4 * h]);
-                    const f32x4 dd = *reinterpret_cast<const f32x4*>(&stat[buf][1][32 * b + 8 * e4 + 4 * h]);
+                    const f32x4 rr = *reinterpret_cast<const f32x4*>(now_stat + 32 * b + 8 * e4 + 4 * h);
+                    const f32x4 dd = *reinterpret_cast<const f32x4*>(now_stat + kKeys + 32 * b + 8 * e4 + 4 * h);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int x = 4 * e4 + e;
@@ -291,14 +305,17 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dkv_kernel(const Sequen
                         ds[0][x] = dv_;
                     }
                 }
-                col_product<D>(dv, lds[buf][1], 32 * b, p, lane);
-                col_product<D>(dk, lds[buf][0], 32 * b, ds, lane);
+                col_product<D>(dv, at_lane, now_d, 32 * b, p);
+                col_product<D>(dk, at_lane, now_q, 32 * b, ds);
             }
         }
-        if (n + 1 < total) put(buf ^ 1);
+        if (n + 1 < total) put(next_q, next_d, next_stat);
         r0 = next_r0;
         g = next_g;
-    }
+    };
+    in_turn(0, total, 1, [&](int64_t n, auto buf) {
+        step(n, lds[1 - buf][0], lds[1 - buf][1], stat[1 - buf], lds[buf][0], lds[buf][1], stat[buf]);
+    });
     const int64_t row = u.kv_start + j;
     store_row<D>(a.dk.p + u.seq * a.dk.seq + row * a.dk.row + u.head * a.dk.head, live, dk, a.scale, h, chunks);
     store_row<D>(a.dv.p + u.seq * a.dv.seq + row * a.dv.row + u.head * a.dv.head, live, dv, 1.0f, h, chunks);

@@ -15,6 +15,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "bsm_attention_launch.hpp"
 
@@ -54,24 +55,41 @@ struct Tile {
         const int f = D == 128 ? ((row & 3) << 2) | ((row >> 2) & 3) : (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
         return row * kChunks + (chunk ^ f);
     }
-    // lane (li, h): element 16 step + 8 h .. + 7 of `row`
-    __device__ static __forceinline__ bf16x8 row_frag(const uint16_t* lds, int row, int step, int h) {
-        return *reinterpret_cast<const bf16x8*>(lds + 8 * place(row, 2 * step + h));
+    static constexpr int kRowBytes = 2 * D;
+};
+
+// Where a lane's fragments lie, in bytes from the start of a tile: the same for every 16 rows, so that what
+// changes from read to read is a constant of the instruction.
+template <int D>
+struct Frags {
+    int row[D / 16];     // row li, elements 16 s + 8 h .. + 7
+    int col[2][D / 32];  // see col_frag
+    __device__ __forceinline__ explicit Frags(int lane) {
+        const int li = lane & 31, h = lane >> 5, g = lane >> 4, s = lane & 15;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) row[i] = 16 * Tile<D>::place(li, 2 * i + h);
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t) {
+            const int r = 4 * (g >> 1) + (s >> 2), c = 32 * t + 16 * (g & 1) + 4 * (s & 3);
+            col[0][t] = 16 * Tile<D>::place(r, c >> 3) + 2 * (c & 7);
+            col[1][t] = 16 * Tile<D>::place(r + 8, c >> 3) + 2 * (c & 7);
+        }
+    }
+    // lane (li, h): elements 16 s + 8 h .. + 7 of row r0 + li; r0 a multiple of 16
+    __device__ __forceinline__ bf16x8 row_frag(const uint16_t* lds, int r0, int s) const {
+        return *reinterpret_cast<const bf16x8*>(reinterpret_cast<const char*>(lds) + row[s] + r0 * Tile<D>::kRowBytes);
     }
     // lane (li, h): column 32 t + li of rows r0 + 4 h + {0..3} and r0 + 8 + 4 h + {0..3}; r0 a
     // multiple of 16.  ds_read_b64_tr_b16 works in groups of 16 lanes: lane s points at row s / 4,
     // columns 4 (s % 4) .. + 3 of a 4 x 16 block and receives the block's column s.
-    __device__ static __forceinline__ bf16x8 col_frag(const uint16_t* lds, int r0, int t, int lane) {
-        const int g = lane >> 4, s = lane & 15;
-        const int row = r0 + 4 * (g >> 1) + (s >> 2), col = 32 * t + 16 * (g & 1) + 4 * (s & 3);
-        const uint16_t* p0 = lds + 8 * place(row, col >> 3) + (col & 7);
-        const uint16_t* p1 = lds + 8 * place(row + 8, col >> 3) + (col & 7);
+    __device__ __forceinline__ bf16x8 col_frag(const uint16_t* lds, int r0, int t) const {
+        const char* p = reinterpret_cast<const char*>(lds) + r0 * Tile<D>::kRowBytes;
         union {
             i16x4 half[2];
             bf16x8 all;
         } u;
-        u.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)p0);
-        u.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)p1);
+        u.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(p + col[0][t]));
+        u.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(p + col[1][t]));
         return u.all;
     }
 };
@@ -94,15 +112,25 @@ struct Stage {
     static constexpr int kN = ROWS * Tile<D>::kChunks / THREADS;
     static_assert(kN >= 1 && ROWS * Tile<D>::kChunks % THREADS == 0, "");
     u32x4 r[DIRECT ? 1 : kN];
+    uint32_t off[DIRECT ? kN : 1];  // bytes from the tile's first row, for whole tiles
+    bool near;                      // the offsets fit
     __device__ static __forceinline__ int row(int tid, int j) { return (tid + THREADS * j) / Tile<D>::kChunks; }
     __device__ static __forceinline__ int chunk(int tid, int j) {
         const int c = tid % Tile<D>::kChunks;
         return DIRECT ? Tile<D>::place(row(tid, j), c) % Tile<D>::kChunks : c;
     }
+    // `stride` of the rows of all the tiles to come
+    __device__ __forceinline__ void init(int tid, int64_t stride, int chunks) {
+        if constexpr (DIRECT) {
+            near = chunks == Tile<D>::kChunks && stride < (int64_t{1} << 24);
+#pragma unroll
+            for (int j = 0; j < kN; ++j) off[j] = static_cast<uint32_t>(2 * (row(tid, j) * stride + 8 * chunk(tid, j)));
+        }
+    }
     __device__ __forceinline__ void piece(int tid, int j, uint16_t* lds, const uint16_t* p, bool live) {
         const uint16_t* from = live ? p : kZeros;
         if constexpr (DIRECT) {
-            uint16_t* to = lds + 8 * ((tid & ~63) + THREADS * j);
+            uint16_t* to = lds + 8 * (64 * __builtin_amdgcn_readfirstlane(tid >> 6) + THREADS * j);
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
                                              (__attribute__((address_space(3))) void*)to, 16, 0, 0);
         } else {
@@ -110,6 +138,17 @@ struct Stage {
         }
     }
     __device__ __forceinline__ void begin(int tid, uint16_t* lds, const uint16_t* p, int64_t stride, int lo, int hi, int chunks) {
+        if constexpr (DIRECT) {
+            if (near && lo <= 0 && hi >= ROWS) {  // nothing to leave out: one base, offsets as they are
+#pragma unroll
+                for (int j = 0; j < kN; ++j)
+                    __builtin_amdgcn_global_load_lds(
+                        (const __attribute__((address_space(1))) void*)(reinterpret_cast<const char*>(p) + off[j]),
+                        (__attribute__((address_space(3))) void*)(lds + 8 * (64 * __builtin_amdgcn_readfirstlane(tid >> 6) + THREADS * j)),
+                        16, 0, 0);
+                return;
+            }
+        }
 #pragma unroll
         for (int j = 0; j < kN; ++j) {
             const int i = row(tid, j), c = chunk(tid, j);
@@ -169,12 +208,12 @@ __device__ __forceinline__ void pipelined(Read read, Use use) {
 // 32 KT rows of the tile (from row r0) times the operand's 32 rows: lane (li, h) gets column li
 // (operand row) and, in acc[k], tile rows r0 + 32 k + 8 (i / 4) + 4 h + i % 4.
 template <int D, int KT>
-__device__ __forceinline__ void row_product(f32x16 (&acc)[KT], const uint16_t* lds, int r0, const RowOperand<D>& q, int lane) {
+__device__ __forceinline__ void row_product(f32x16 (&acc)[KT], const Frags<D>& at, const uint16_t* lds, int r0, const RowOperand<D>& q) {
     constexpr int kSteps = D / 16;
 #pragma unroll
     for (int k = 0; k < KT; ++k) acc[k] = zero16();
     pipelined<KT * kSteps, kAhead>(
-        [&](int i) { return Tile<D>::row_frag(lds, r0 + 32 * (i / kSteps) + (lane & 31), i % kSteps, lane >> 5); },
+        [&](int i) { return at.row_frag(lds, r0 + 32 * (i / kSteps), i % kSteps); },
         [&](int i, bf16x8 a) { acc[i / kSteps] = mfma(a, q.f[i % kSteps], acc[i / kSteps]); });
 }
 
@@ -190,19 +229,31 @@ __device__ __forceinline__ bf16x8 half_operand(const f32x16& x, int s) {
 // acc[t] += (columns 32 t .. of tile rows r0 .. r0 + 32 KT - 1)^T times x: lane li keeps its column of x,
 // rows 32 t + 8 (i / 4) + 4 h + i % 4 of the tile's columns.
 template <int D, int KT>
-__device__ __forceinline__ void col_product(f32x16 (&acc)[D / 32], const uint16_t* lds, int r0, const f32x16 (&x)[KT], int lane) {
+__device__ __forceinline__ void col_product(f32x16 (&acc)[D / 32], const Frags<D>& at, const uint16_t* lds, int r0, const f32x16 (&x)[KT]) {
     constexpr int kTiles = D / 32;
     bf16x8 b[2 * KT];
 #pragma unroll
     for (int s = 0; s < 2 * KT; ++s) b[s] = half_operand(x[s / 2], s % 2);
     pipelined<2 * KT * kTiles, kAhead>(
-        [&](int i) { return Tile<D>::col_frag(lds, r0 + 16 * (i / kTiles), i % kTiles, lane); },
+        [&](int i) { return at.col_frag(lds, r0 + 16 * (i / kTiles), i % kTiles); },
         [&](int i, bf16x8 a) { acc[i % kTiles] = mfma(a, b[i / kTiles], acc[i % kTiles]); });
 }
 
-// Value of the other half of the wave (lanes l and l + 32 exchanged).
-__device__ __forceinline__ float other_half(float v) {
-    return __shfl_xor(v, 32, 64);
+// f(v of lane l, v of lane l ^ 32), the same in both: v_permlane32_swap exchanges the upper half of one
+// register with the lower half of another.  Written out because the compiler, given the builtin with two
+// copies of one value, uses one of its two results twice; the s_nop is the distance that the
+// instruction keeps from the one that wrote its operand.
+template <class F>
+__device__ __forceinline__ float both_halves(float v, F f) {
+    float x = v, y = v;
+    asm volatile("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(x), "+v"(y));
+    return f(x, y);
+}
+__device__ __forceinline__ float half_sum(float v) {
+    return both_halves(v, [](float x, float y) { return x + y; });
+}
+__device__ __forceinline__ float half_max(float v) {
+    return both_halves(v, [](float x, float y) { return fmaxf(x, y); });
 }
 
 // Index along the tile's rows of register i in half h.
@@ -244,6 +295,15 @@ __device__ __forceinline__ void tile_barrier() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+// Runs step(x, buffer) for x = begin, begin + by, ..., the buffers 0 and 1 in turn and known to the compiler.
+template <class Step>
+__device__ __forceinline__ void in_turn(int64_t begin, int64_t end, int by, Step step) {
+    for (int64_t x = begin; x < end; x += 2 * by) {
+        step(x, std::integral_constant<int, 0>{});
+        if (x + by < end) step(x + by, std::integral_constant<int, 1>{});
+    }
+}
+
 // ------------------------------------------------------------------------- online softmax
 // One pass over the keys for 32 query rows, row li in lanes li and li + 32: m is the reference
 // that the exponents of a row are taken from, in log2 units of the scaled scores, l the lane's
@@ -273,7 +333,7 @@ struct Online {
         for (int k = 0; k < KT; ++k)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, s[k][i]);
-        top = fmaxf(top, other_half(top)) * c;
+        top = half_max(top) * c;
         // (also where m is still -inf; a NaN leaves m as it is and reaches l below)
         if (__any(top > m + kSlack)) {
             const float next = fmaxf(m, top);
@@ -296,7 +356,7 @@ struct Online {
             }
         l += sum;
     }
-    __device__ __forceinline__ float row_sum() const { return l + other_half(l); }
+    __device__ __forceinline__ float row_sum() const { return half_sum(l); }
     // natural-log statistic of a row with sum `total`
     __device__ __forceinline__ float statistic(float total) const {
         return total == 0.0f ? -kInf : (m + __builtin_amdgcn_logf(total)) * kLn2;

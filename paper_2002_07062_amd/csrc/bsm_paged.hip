@@ -158,28 +158,29 @@ __global__ __launch_bounds__(kThreads, 2) void paged_kernel(const PagedArgs a) {
         stage.find(a, table, tid, begin + kKeys, r.kv_len);
         stage.end(tid, lds[0][0], lds[0][1]);
     }
-    int buf = 0;
-    for (int j0 = begin; j0 < end; j0 += kKeys, buf ^= 1) {
+    const Frags<D> at_lane(lane);
+    // the tiles read and the tiles written in a step are apart
+    auto step = [&](int j0, uint16_t* __restrict__ next_k, uint16_t* __restrict__ next_v, const uint16_t* __restrict__ now_k,
+                    const uint16_t* __restrict__ now_v) __attribute__((always_inline)) {
         const int next = j0 + kKeys;
         tile_barrier<DIRECT>();
         if (next < end) {
-            stage.begin(a, r.head, tid, next, chunks, lds[buf ^ 1][0], lds[buf ^ 1][1]);
+            stage.begin(a, r.head, tid, next, chunks, next_k, next_v);
             stage.find(a, table, tid, next + kKeys, r.kv_len);
         }
         if (any_row && j0 <= w1.hi && next > w0.lo) {
             f32x16 s[kKeys / 32];
-            row_product<D>(s, lds[buf][0], 0, q, lane);
+            row_product<D>(s, at_lane, now_k, 0, q);
             if (j0 < w1.lo || next - 1 > w0.hi || end < next) {
 #pragma unroll
                 for (int k = 0; k < kKeys / 32; ++k) mask_block(s[k], j0 + 32 * k, h, mine.lo, min(mine.hi, end - 1));
             }
             st.weigh(s, c);
-            col_product<D>(st.o, lds[buf][1], 0, s, lane);
+            col_product<D>(st.o, at_lane, now_v, 0, s);
         }
-        if (next < end) {
-            stage.end(tid, lds[buf ^ 1][0], lds[buf ^ 1][1]);
-        }
-    }
+        if (next < end) stage.end(tid, next_k, next_v);
+    };
+    in_turn(begin, end, kKeys, [&](int j0, auto buf) { step(j0, lds[1 - buf][0], lds[1 - buf][1], lds[buf][0], lds[buf][1]); });
     const float total = st.row_sum();
     if (ps.first == ps.last) {
         uint16_t* out = a.o.p + q_row * a.o.row + q_head * a.o.head;
