@@ -9,7 +9,10 @@ passed transposed). Nothing is copied or computed here.
 from __future__ import annotations
 
 import ctypes
+import itertools
 import math
+import struct
+import threading
 
 import numpy as np
 import torch
@@ -47,7 +50,7 @@ def _load() -> ctypes.CDLL:
         return _lib
     lib = _b.load()
     P = ctypes.POINTER
-    H = P(bsm_heads)
+    H = _vp  # bsm_heads, as _refs makes them
     c_int = ctypes.c_int
     sig = {
         "bsm_attention_plan_create": [P(_vp), P(_i32), P(_i32), P(_i64), P(_i64), _i64, _i32, _i32,
@@ -72,38 +75,80 @@ def _load() -> ctypes.CDLL:
     return lib
 
 
-def _same_device(device, *tensors) -> None:
-    for t in tensors:
-        if t is not None and t.device != device:
-            raise ValueError(f"expected tensors on {device}, got one on {t.device}")
+# The stream's handle without a Stream object around it (a call of these is mostly launch time).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _contiguous(t, dtype, n, name) -> int:
-    """Pointer of a contiguous GPU tensor of `dtype` with at least n elements."""
-    if t.dtype != dtype:
+def _stream(index, stream):
+    if stream is not None:
+        return _stream_of(None, stream)
+    if _raw_stream is not None:
+        return _raw_stream(index)
+    return torch.cuda.current_stream(index).cuda_stream
+
+
+def _call(index, fn, *args) -> None:
+    """Calls a C entry point with GPU `index` as the current device."""
+    if torch.cuda.current_device() == index:
+        status = fn(*args)
+    else:
+        with torch.cuda.device(index):
+            status = fn(*args)
+    if status:
+        _check(status)
+
+
+def _contiguous(t, dtype, n, name, index) -> int:
+    """Pointer of a contiguous tensor of `dtype` on GPU `index` with at least n elements."""
+    if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous GPU tensor")
+    if t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous tensor on cuda:{index}")
     if t.numel() < n:
         raise ValueError(f"{name} has {t.numel()} elements, needs {n}")
     return t.data_ptr()
 
 
-def _operand(t, rows, batch, heads, dim, name) -> bsm_heads:
-    """`t` as (tokens, heads, dim) with at least `rows` tokens, or (batch, rows, heads, dim)."""
-    if t.dtype != torch.bfloat16:
+def _operand(t, rows, batch, heads, dim, name, index):
+    """The fields of a bsm_heads for `t`: (tokens, heads, dim) with at least `rows` tokens, or
+    (batch, rows, heads, dim), on GPU `index`."""
+    shape = t.shape
+    n = len(shape)
+    if t.dtype is not torch.bfloat16:
         raise TypeError(f"{name} must be bfloat16, got {t.dtype}")
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a GPU tensor")
-    if t.dim() not in (3, 4) or t.shape[-2] != heads or t.shape[-1] != dim:
-        raise ValueError(f"{name} of shape {tuple(t.shape)} is no (tokens, {heads}, {dim}) or "
+    if t.get_device() != index or index < 0:
+        raise ValueError(f"{name} must be a tensor on cuda:{index}, got one on {t.device}")
+    if n not in (3, 4) or shape[-2] != heads or shape[-1] != dim:
+        raise ValueError(f"{name} of shape {tuple(shape)} is no (tokens, {heads}, {dim}) or "
                          f"(batch, rows, {heads}, {dim})")
-    if t.stride(-1) != 1 and dim > 1:
+    stride = t.stride()
+    if stride[-1] != 1 and dim > 1:
         raise ValueError(f"{name}: the last dimension must be contiguous")
-    if t.shape[-3] < rows or (t.dim() == 4 and t.shape[0] < batch):
-        raise ValueError(f"{name} of shape {tuple(t.shape)} is shorter than the sequences "
+    if shape[-3] < rows or (n == 4 and shape[0] < batch):
+        raise ValueError(f"{name} of shape {tuple(shape)} is shorter than the sequences "
                          f"({batch} sequences, rows up to {rows})")
-    return bsm_heads(t.data_ptr(), t.stride(0) if t.dim() == 4 else 0, t.stride(-3), t.stride(-2))
+    if n == 3:
+        return t.data_ptr(), 0, stride[0], stride[1]
+    return t.data_ptr(), *stride[:3]
+
+
+class _Scratch(threading.local):
+    """A thread's memory for the bsm_heads of a call, which the library reads before it returns."""
+
+    def __init__(self):
+        self.memory = (_i64 * 32)()
+        self.at = ctypes.addressof(self.memory)
+
+
+_scratch = _Scratch()
+_FIELDS = {n: struct.Struct(f"{4 * n}q") for n in (2, 4, 8)}
+
+
+def _refs(*operands):
+    """Addresses of a bsm_heads for each operand's fields, good until the thread's next call."""
+    n, at = len(operands), _scratch.at
+    _FIELDS[n].pack_into(_scratch.memory, 0, *itertools.chain.from_iterable(operands))
+    return range(at, at + 32 * n, 32)
 
 
 def _ref(x):
@@ -142,10 +187,10 @@ class AttentionPlan:
             pass
 
     def _q(self, t, name):
-        return _operand(t, self.q_end, self.batch, self.heads_q, self.head_dim, name)
+        return _operand(t, self.q_end, self.batch, self.heads_q, self.head_dim, name, self.device)
 
     def _kv(self, t, name):
-        return _operand(t, self.kv_end, self.batch, self.heads_kv, self.head_dim, name)
+        return _operand(t, self.kv_end, self.batch, self.heads_kv, self.head_dim, name, self.device)
 
 
 def _lengths(a, n=None):
@@ -212,14 +257,11 @@ def bsm_attention_execute(plan: AttentionPlan, q, k, v, o, lse=None, scale=None,
     """o = attention of q over k and v under the plan (see bsm.h); lse: None or a float32 tensor
     of heads_q * total_q elements for the rows' log-sum-exp, which the backward pass needs.
     scale: default 1 / sqrt(head_dim). Returns o."""
-    lib = _load()
-    a = [plan._q(q, "q"), plan._kv(k, "k"), plan._kv(v, "v"), plan._q(o, "o")]
-    lp = None if lse is None else _contiguous(lse, torch.float32, plan.lse_elems, "lse")
-    dev = torch.device("cuda", plan.device)
-    _same_device(dev, q, k, v, o, lse)
-    with torch.cuda.device(dev):
-        _check(lib.bsm_attention_execute(plan.handle, *map(_ref, a), lp,
-                                         _scale_of(scale, plan.head_dim), _stream_of(q, stream)))
+    fn = _load().bsm_attention_execute
+    refs = _refs(plan._q(q, "q"), plan._kv(k, "k"), plan._kv(v, "v"), plan._q(o, "o"))
+    dev = plan.device
+    lp = None if lse is None else _contiguous(lse, torch.float32, plan.lse_elems, "lse", dev)
+    _call(dev, fn, plan.handle, *refs, lp, _scale_of(scale, plan.head_dim), _stream(dev, stream))
     return o
 
 
@@ -228,42 +270,44 @@ def bsm_attention_backward(plan: AttentionPlan, q, k, v, o, lse, dout, dq, dk, d
     """Gradients of bsm_attention_execute: dq, dk and dv from q, k, v, its o and lse, and dout
     (see bsm.h). workspace: None (allocated for the call on the current stream) or a tensor of
     plan.workspace_bytes bytes. Returns (dq, dk, dv)."""
-    lib = _load()
-    a = [plan._q(q, "q"), plan._kv(k, "k"), plan._kv(v, "v"), plan._q(o, "o")]
-    g = [plan._q(dout, "dout"), plan._q(dq, "dq"), plan._kv(dk, "dk"), plan._kv(dv, "dv")]
-    lp = _contiguous(lse, torch.float32, plan.lse_elems, "lse")
-    dev = torch.device("cuda", plan.device)
-    _same_device(dev, q, k, v, o, lse, dout, dq, dk, dv, workspace)
-    if workspace is None:
-        if stream is not None:
-            raise ValueError("a call on a stream of its own needs its own workspace")
-        with torch.cuda.device(dev):
-            workspace = torch.empty(plan.workspace_bytes, dtype=torch.uint8, device=dev)
-    elif not workspace.is_contiguous():
-        raise ValueError("workspace must be contiguous")
-    with torch.cuda.device(dev):
-        _check(lib.bsm_attention_backward(
-            plan.handle, *map(_ref, a), lp, *map(_ref, g), _scale_of(scale, plan.head_dim),
-            workspace.data_ptr(), workspace.numel() * workspace.element_size(),
-            _stream_of(q, stream)))
+    fn = _load().bsm_attention_backward
+    dev = plan.device
+    refs = _refs(plan._q(q, "q"), plan._kv(k, "k"), plan._kv(v, "v"), plan._q(o, "o"),
+                 plan._q(dout, "dout"), plan._q(dq, "dq"), plan._kv(dk, "dk"), plan._kv(dv, "dv"))
+    lp = _contiguous(lse, torch.float32, plan.lse_elems, "lse", dev)
+    wp, wn, workspace = _workspace(workspace, lambda: plan.workspace_bytes, dev, stream)
+    _call(dev, fn, plan.handle, *refs[:4], lp, *refs[4:], _scale_of(scale, plan.head_dim), wp, wn,
+          _stream(dev, stream))
     return dq, dk, dv
 
 
+def _workspace(workspace, needed, index, stream):
+    """(pointer, bytes, tensor) of the caller's workspace, or of one allocated for the call on the
+    current stream."""
+    if workspace is None:
+        if stream is not None:
+            raise ValueError("a call on a stream of its own needs its own workspace")
+        workspace = torch.empty(needed(), dtype=torch.uint8, device=torch.device("cuda", index))
+    elif workspace.get_device() != index or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous tensor on cuda:{index}")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
+
+
 # ------------------------------------------------------------------------------ paged cache
-def _cache_of(k_cache, v_cache) -> bsm_cache:
-    """k_cache, v_cache: bfloat16 GPU tensors (pages, page size, heads, dim) of the same strides."""
-    for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
-        if t.dtype != torch.bfloat16:
-            raise TypeError(f"{name} must be bfloat16, got {t.dtype}")
-        if not t.is_cuda or t.dim() != 4:
-            raise ValueError(f"{name} must be a GPU tensor (pages, page size, heads, dim)")
-        if t.stride(3) != 1 and t.shape[3] > 1:
-            raise ValueError(f"{name}: the last dimension must be contiguous")
-    if k_cache.shape != v_cache.shape or k_cache.stride() != v_cache.stride():
+def _cache_of(k_cache, v_cache) -> tuple[bsm_cache, int]:
+    """k_cache, v_cache: bfloat16 tensors (pages, page size, heads, dim) of the same strides on one
+    GPU, whose index is returned beside the cache."""
+    shape, stride, index = k_cache.shape, k_cache.stride(), k_cache.get_device()
+    if k_cache.dtype is not torch.bfloat16 or v_cache.dtype is not torch.bfloat16:
+        raise TypeError(f"k_cache and v_cache must be bfloat16, got {k_cache.dtype} and {v_cache.dtype}")
+    if index < 0 or v_cache.get_device() != index or len(shape) != 4:
+        raise ValueError("k_cache and v_cache must be (pages, page size, heads, dim) on one GPU")
+    if stride[3] != 1 and shape[3] > 1:
+        raise ValueError("k_cache and v_cache: the last dimension must be contiguous")
+    if shape != v_cache.shape or stride != v_cache.stride():
         raise ValueError("k_cache and v_cache must have the same shape and strides")
-    n, page, heads, dim = k_cache.shape
-    return bsm_cache(k_cache.data_ptr(), v_cache.data_ptr(), n, *k_cache.stride()[:3], page,
-                     heads, dim, 0)
+    return bsm_cache(k_cache.data_ptr(), v_cache.data_ptr(), shape[0], *stride[:3], *shape[1:],
+                     0), index
 
 
 def bsm_cache_slots(cached, fresh, page_size, n_pages, table, free_pages, n_free, q_start, kv_len,
@@ -271,38 +315,35 @@ def bsm_cache_slots(cached, fresh, page_size, n_pages, table, free_pages, n_free
     """Block table and slot map of a step from the requests' lengths (see bsm.h). int32 tensors on
     one GPU: cached, fresh, kv_len (batch), table (batch, width), free_pages, n_free (1),
     q_start (batch + 1), taken (2); slots: int64, as many as the step has room for tokens."""
-    lib = _load()
-    batch = cached.numel()
+    fn = _load().bsm_cache_slots
+    batch, dev = cached.numel(), cached.get_device()
+    if dev < 0:
+        raise ValueError("cached must be a GPU tensor")
     if table.dim() != 2 or table.shape[0] < batch:
         raise ValueError(f"table of shape {tuple(table.shape)} has no row for each of {batch}")
     i32 = torch.int32
-    p = [_contiguous(cached, i32, batch, "cached"), _contiguous(fresh, i32, batch, "fresh")]
-    dev = cached.device
-    _same_device(dev, fresh, table, free_pages, n_free, q_start, kv_len, slots, taken)
-    with torch.cuda.device(dev):
-        _check(lib.bsm_cache_slots(
-            *p, batch, int(page_size), int(n_pages), _contiguous(table, i32, 0, "table"),
-            table.shape[1], _contiguous(free_pages, i32, 0, "free_pages"), free_pages.numel(),
-            _contiguous(n_free, i32, 1, "n_free"), _contiguous(q_start, i32, batch + 1, "q_start"),
-            _contiguous(kv_len, i32, batch, "kv_len"),
-            _contiguous(slots, torch.int64, 0, "slots"), slots.numel(),
-            _contiguous(taken, i32, 2, "taken"), _stream_of(cached, stream)))
+    _call(dev, fn, _contiguous(cached, i32, batch, "cached", dev),
+          _contiguous(fresh, i32, batch, "fresh", dev), batch, int(page_size), int(n_pages),
+          _contiguous(table, i32, 0, "table", dev), table.shape[1],
+          _contiguous(free_pages, i32, 0, "free_pages", dev), free_pages.numel(),
+          _contiguous(n_free, i32, 1, "n_free", dev),
+          _contiguous(q_start, i32, batch + 1, "q_start", dev),
+          _contiguous(kv_len, i32, batch, "kv_len", dev),
+          _contiguous(slots, torch.int64, 0, "slots", dev), slots.numel(),
+          _contiguous(taken, i32, 2, "taken", dev), _stream(dev, stream))
 
 
 def bsm_cache_append(k, v, slots, k_cache, v_cache, stream=None):
     """Writes the tokens of k and v (tokens, heads, dim) to their slots of the cache."""
-    lib = _load()
-    cache = _cache_of(k_cache, v_cache)
+    fn = _load().bsm_cache_append
+    cache, dev = _cache_of(k_cache, v_cache)
     tokens = slots.numel()
     if k.dim() != 3 or v.dim() != 3:
         raise ValueError("k and v must be (tokens, heads, dim)")
-    kh = _operand(k, tokens, 1, cache.heads, cache.head_dim, "k")
-    vh = _operand(v, tokens, 1, cache.heads, cache.head_dim, "v")
-    sp = _contiguous(slots, torch.int64, 0, "slots")
-    _same_device(k_cache.device, v_cache, k, v, slots)
-    with torch.cuda.device(k_cache.device):
-        _check(lib.bsm_cache_append(_ref(cache), _ref(kh), _ref(vh), sp, tokens,
-                                    _stream_of(k_cache, stream)))
+    kr, vr = _refs(_operand(k, tokens, 1, cache.heads, cache.head_dim, "k", dev),
+                   _operand(v, tokens, 1, cache.heads, cache.head_dim, "v", dev))
+    _call(dev, fn, _ref(cache), kr, vr, _contiguous(slots, torch.int64, 0, "slots", dev), tokens,
+          _stream(dev, stream))
 
 
 def bsm_attention_paged_workspace(batch, tokens, heads_q, heads_kv, head_dim, max_q, max_kv,
@@ -322,36 +363,24 @@ def bsm_attention_paged(q, k_cache, v_cache, table, q_start, kv_len, o, max_q, m
     (batch). max_q, max_kv: host bounds on a chunk and on kv_len (default: the table's width).
     workspace: None (allocated for the call on the current stream) or a tensor of
     bsm_attention_paged_workspace bytes. Returns o."""
-    lib = _load()
-    cache = _cache_of(k_cache, v_cache)
+    fn = _load().bsm_attention_paged
+    cache, dev = _cache_of(k_cache, v_cache)
     if q.dim() != 3 or o.dim() != 3:
         raise ValueError("q and o must be (tokens, heads, dim)")
-    tokens, heads_q = q.shape[0], q.shape[1]
-    batch = kv_len.numel()
+    tokens, heads_q, _ = q.shape
+    batch, dim = kv_len.numel(), cache.head_dim
     if table.dim() != 2 or table.shape[0] < batch:
         raise ValueError(f"table of shape {tuple(table.shape)} has no row for each of {batch}")
-    qh = _operand(q, tokens, 1, heads_q, cache.head_dim, "q")
-    oh = _operand(o, tokens, 1, heads_q, cache.head_dim, "o")
-    i32 = torch.int32
-    tp = _contiguous(table, i32, 0, "table")
-    sp = _contiguous(q_start, i32, batch + 1, "q_start")
-    lp = _contiguous(kv_len, i32, 0, "kv_len")
-    dev = q.device
-    _same_device(dev, k_cache, v_cache, table, q_start, kv_len, o, workspace)
-    width = table.shape[1]
+    qr, orr = _refs(_operand(q, tokens, 1, heads_q, dim, "q", dev),
+                    _operand(o, tokens, 1, heads_q, dim, "o", dev))
+    i32, width = torch.int32, table.shape[1]
+    tp = _contiguous(table, i32, 0, "table", dev)
+    sp = _contiguous(q_start, i32, batch + 1, "q_start", dev)
+    lp = _contiguous(kv_len, i32, 0, "kv_len", dev)
     max_kv = width * cache.page_size if max_kv is None else int(max_kv)
-    with torch.cuda.device(dev):
-        if workspace is None:
-            if stream is not None:
-                raise ValueError("a call on a stream of its own needs its own workspace")
-            workspace = torch.empty(
-                bsm_attention_paged_workspace(batch, tokens, heads_q, cache.heads, cache.head_dim,
-                                              max_q, max_kv, dev.index),
-                dtype=torch.uint8, device=dev)
-        elif not workspace.is_contiguous():
-            raise ValueError("workspace must be contiguous")
-        _check(lib.bsm_attention_paged(
-            _ref(cache), _ref(qh), _ref(oh), tp, width, sp, lp, batch, tokens, heads_q, int(max_q),
-            max_kv, int(window), _scale_of(scale, cache.head_dim), workspace.data_ptr(),
-            workspace.numel() * workspace.element_size(), _stream_of(q, stream)))
+    wp, wn, workspace = _workspace(
+        workspace, lambda: bsm_attention_paged_workspace(batch, tokens, heads_q, cache.heads, dim,
+                                                         max_q, max_kv, dev), dev, stream)
+    _call(dev, fn, _ref(cache), qr, orr, tp, width, sp, lp, batch, tokens, heads_q, int(max_q),
+          max_kv, int(window), _scale_of(scale, dim), wp, wn, _stream(dev, stream))
     return o

@@ -89,49 +89,51 @@ struct Span {
 };
 bool overlap(const Span& a, const Span& b) { return a.from < b.to && b.from < a.to; }
 
-// An operand with `heads` heads whose rows end before `end` (in sequence b: starts[b] + lens[b]);
-// `shared`: two sequences have a row in common.  A written one must have a place for each row.
-bsm_status take(const char* name, const bsm_heads* h, const std::vector<int64_t>& starts, const std::vector<int32_t>& lens,
-                int64_t end, bool shared, int64_t heads, int64_t dim, bool written, Heads* out, Span* span) {
+// Rows of an operand: of every sequence b, [start[b], start[b] + len[b]).
+struct Rows {
+    const std::vector<int64_t>* start = nullptr;  // null: one sequence of rows 0 .. end - 1
+    const std::vector<int32_t>* len = nullptr;
+    int64_t end = 0, longest = 0;  // largest row + 1, rows of the longest sequence
+    bool shared = false;           // two sequences have a row in common
+    bool in_order = true;          // no sequence starts before the one before it
+};
+
+// An operand with `heads` heads.  A written one must have a place of its own for each row.
+bsm_status take(const char* name, const bsm_heads* h, const Rows& r, int64_t heads, int64_t dim, bool written, Heads* out, Span* span) {
     if (!h) return fail(BSM_ERR_INVALID_ARG, "%s is NULL", name);
     *span = {};
     *out = {static_cast<uint16_t*>(h->data), h->seq, h->row, h->head};
     if (h->seq < 0 || h->row < 0 || h->head < 0 || h->seq > kMostStride || h->row > kMostStride || h->head > kMostStride)
         return fail(BSM_ERR_INVALID_ARG, "%s: strides must be in 0 .. 2^40", name);
-    if (end == 0) return BSM_OK;  // no rows
+    if (r.end == 0) return BSM_OK;  // no rows
     if (!h->data) return fail(BSM_ERR_INVALID_ARG, "%s: data is NULL", name);
     if (reinterpret_cast<uintptr_t>(h->data) % 2 != 0)
         return fail(BSM_ERR_INVALID_ARG, "%s: data is not aligned to the element size", name);
-    double far = 0.0;
-    int64_t longest = 0, last = 0, most = 0, batch = static_cast<int64_t>(lens.size());
-    for (int64_t b = 0; b < batch; ++b) {
-        if (lens[b] == 0) continue;
-        const double d = static_cast<double>(b) * h->seq + static_cast<double>(starts[b] + lens[b]) * h->row;
-        if (d > 1.0e18) return fail(BSM_ERR_INVALID_ARG, "%s: rows too far apart", name);
-        const int64_t e = b * h->seq + (starts[b] + lens[b] - 1) * h->row;
-        far = std::max(far, d);
-        last = std::max(last, e);
-        longest = std::max<int64_t>(longest, lens[b]);
-        most = std::max(most, starts[b] + lens[b]);
+    const int64_t batch = r.start ? static_cast<int64_t>(r.start->size()) : 1;
+    const double far = static_cast<double>(batch) * h->seq + static_cast<double>(r.end) * h->row + static_cast<double>(heads) * h->head;
+    if (far > 1.0e18) return fail(BSM_ERR_INVALID_ARG, "%s: rows too far apart", name);
+    int64_t last = (r.end - 1) * h->row;  // of the rows' elements
+    if (h->seq != 0 && r.start) {
+        last = 0;
+        for (int64_t b = 0; b < batch; ++b)
+            if ((*r.len)[b] > 0) last = std::max(last, b * h->seq + ((*r.start)[b] + (*r.len)[b] - 1) * h->row);
     }
-    if (static_cast<double>(heads) * h->head + far > 1.0e18) return fail(BSM_ERR_INVALID_ARG, "%s: rows too far apart", name);
     span->from = reinterpret_cast<uintptr_t>(h->data);
     span->to = span->from + 2 * static_cast<uintptr_t>(last + (heads - 1) * h->head + dim);
     if (!written) return BSM_OK;
     // within a sequence: heads inside a row, or rows inside a head
-    const int64_t rows = h->seq == 0 ? most : longest;
+    const int64_t rows = h->seq == 0 ? r.end : r.longest;
     const bool heads_inside = (heads == 1 || h->head >= dim) && (rows == 1 || h->row >= (heads - 1) * h->head + dim);
     const bool rows_inside = (rows == 1 || h->row >= dim) && (heads == 1 || h->head >= (rows - 1) * h->row + dim);
     bool apart = heads_inside || rows_inside;
-    // between sequences: disjoint rows of one numbering, or blocks that follow each other
+    // between sequences: disjoint rows of one numbering, or blocks that follow each other (packed rows on
+    // top of a sequence stride only move the sequences further apart)
     if (h->seq == 0) {
-        apart = apart && !shared;
+        apart = apart && !r.shared;
     } else if (batch > 1) {
-        const int64_t block = (most - 1) * h->row + (heads - 1) * h->head + dim;
-        bool in_order = true;  // packed rows on top of a sequence stride move sequences further apart
-        for (int64_t b = 1; b < batch; ++b) in_order = in_order && starts[b] >= starts[b - 1];
-        const int64_t own = (longest - 1) * h->row + (heads - 1) * h->head + dim;
-        apart = apart && (h->seq >= block || (in_order && h->seq >= own));
+        const int64_t block = (r.end - 1) * h->row + (heads - 1) * h->head + dim;
+        const int64_t own = (r.longest - 1) * h->row + (heads - 1) * h->head + dim;
+        apart = apart && (h->seq >= block || (r.in_order && h->seq >= own));
     }
     if (!apart) return fail(BSM_ERR_INVALID_ARG, "%s: rows overlap each other", name);
     return BSM_OK;
@@ -142,8 +144,13 @@ bsm_status take_rows(const char* name, const bsm_heads* h, int64_t tokens, int64
                      Span* span) {
     if (!h) return fail(BSM_ERR_INVALID_ARG, "%s is NULL", name);
     const bsm_heads one = {h->data, 0, h->row, h->head};
-    return take(name, &one, {0}, {static_cast<int32_t>(tokens)}, tokens, false, heads, dim, written, out, span);
+    Rows r;
+    r.end = r.longest = tokens;
+    return take(name, &one, r, heads, dim, written, out, span);
 }
+
+Rows q_rows(const bsm_att::Sequences& s) { return {&s.q_start, &s.q_len, s.q_end, s.q_longest, s.q_shared, s.q_in_order}; }
+Rows kv_rows(const bsm_att::Sequences& s) { return {&s.kv_start, &s.kv_len, s.kv_end, s.kv_longest, s.kv_shared, s.kv_in_order}; }
 
 Span bytes_at(const void* p, int64_t bytes) {
     const uintptr_t a = reinterpret_cast<uintptr_t>(p);
@@ -258,12 +265,13 @@ bsm_status forward(bsm_attention_plan p, const bsm_heads* q, const bsm_heads* k,
     if (st != BSM_OK) return st;
     if ((st = check_scale(scale)) != BSM_OK) return st;
     const bsm_att::Sequences& s = p->seqs;
+    const Rows qr = q_rows(s), kr = kv_rows(s);
     bsm_att::SequenceArgs a{};
     Span sq, sk, sv, so;
-    if ((st = take("q", q, s.q_start, s.q_len, s.q_end, false, s.heads_q, s.dim, false, &a.q, &sq)) != BSM_OK ||
-        (st = take("k", k, s.kv_start, s.kv_len, s.kv_end, false, s.heads_kv, s.dim, false, &a.k, &sk)) != BSM_OK ||
-        (st = take("v", v, s.kv_start, s.kv_len, s.kv_end, false, s.heads_kv, s.dim, false, &a.v, &sv)) != BSM_OK ||
-        (st = take("o", o, s.q_start, s.q_len, s.q_end, s.q_shared, s.heads_q, s.dim, true, &a.o, &so)) != BSM_OK)
+    if ((st = take("q", q, qr, s.heads_q, s.dim, false, &a.q, &sq)) != BSM_OK ||
+        (st = take("k", k, kr, s.heads_kv, s.dim, false, &a.k, &sk)) != BSM_OK ||
+        (st = take("v", v, kr, s.heads_kv, s.dim, false, &a.v, &sv)) != BSM_OK ||
+        (st = take("o", o, qr, s.heads_q, s.dim, true, &a.o, &so)) != BSM_OK)
         return st;
     const Span sl = lse ? bytes_at(lse, 4 * s.heads_q * s.total_q) : Span{};
     if (overlap(so, sq) || overlap(so, sk) || overlap(so, sv)) return fail(BSM_ERR_ALIAS, "o overlaps an operand");
@@ -294,16 +302,17 @@ bsm_status backward(bsm_attention_plan p, const bsm_heads* q, const bsm_heads* k
     if (st != BSM_OK) return st;
     if ((st = check_scale(scale)) != BSM_OK) return st;
     const bsm_att::Sequences& s = p->seqs;
+    const Rows qr = q_rows(s), kr = kv_rows(s);
     bsm_att::SequenceArgs a{};
     Span in[7], out[4];
-    if ((st = take("q", q, s.q_start, s.q_len, s.q_end, false, s.heads_q, s.dim, false, &a.q, &in[0])) != BSM_OK ||
-        (st = take("k", k, s.kv_start, s.kv_len, s.kv_end, false, s.heads_kv, s.dim, false, &a.k, &in[1])) != BSM_OK ||
-        (st = take("v", v, s.kv_start, s.kv_len, s.kv_end, false, s.heads_kv, s.dim, false, &a.v, &in[2])) != BSM_OK ||
-        (st = take("o", o, s.q_start, s.q_len, s.q_end, false, s.heads_q, s.dim, false, &a.o, &in[3])) != BSM_OK ||
-        (st = take("dout", dout, s.q_start, s.q_len, s.q_end, false, s.heads_q, s.dim, false, &a.dout, &in[4])) != BSM_OK ||
-        (st = take("dq", dq, s.q_start, s.q_len, s.q_end, s.q_shared, s.heads_q, s.dim, true, &a.dq, &out[0])) != BSM_OK ||
-        (st = take("dk", dk, s.kv_start, s.kv_len, s.kv_end, s.kv_shared, s.heads_kv, s.dim, true, &a.dk, &out[1])) != BSM_OK ||
-        (st = take("dv", dv, s.kv_start, s.kv_len, s.kv_end, s.kv_shared, s.heads_kv, s.dim, true, &a.dv, &out[2])) != BSM_OK)
+    if ((st = take("q", q, qr, s.heads_q, s.dim, false, &a.q, &in[0])) != BSM_OK ||
+        (st = take("k", k, kr, s.heads_kv, s.dim, false, &a.k, &in[1])) != BSM_OK ||
+        (st = take("v", v, kr, s.heads_kv, s.dim, false, &a.v, &in[2])) != BSM_OK ||
+        (st = take("o", o, qr, s.heads_q, s.dim, false, &a.o, &in[3])) != BSM_OK ||
+        (st = take("dout", dout, qr, s.heads_q, s.dim, false, &a.dout, &in[4])) != BSM_OK ||
+        (st = take("dq", dq, qr, s.heads_q, s.dim, true, &a.dq, &out[0])) != BSM_OK ||
+        (st = take("dk", dk, kr, s.heads_kv, s.dim, true, &a.dk, &out[1])) != BSM_OK ||
+        (st = take("dv", dv, kr, s.heads_kv, s.dim, true, &a.dv, &out[2])) != BSM_OK)
         return st;
     const int64_t need = workspace_of(s);
     if (need > 0 && (!lse || !workspace)) return fail(BSM_ERR_INVALID_ARG, "lse or workspace is NULL");

@@ -18,14 +18,18 @@ bool any_shared(const std::vector<int64_t>& start, const std::vector<int32_t>& l
     return false;
 }
 
-int64_t fill(const int64_t* given, const std::vector<int32_t>& len, std::vector<int64_t>* start, int64_t* end, bool* shared) {
+int64_t fill(const int64_t* given, const std::vector<int32_t>& len, std::vector<int64_t>* start, int64_t* end, int64_t* longest,
+             bool* shared, bool* in_order) {
     int64_t total = 0;
-    *end = 0;
+    *end = *longest = 0;
+    *in_order = true;
     start->resize(len.size());
     for (size_t b = 0; b < len.size(); ++b) {
         (*start)[b] = given ? given[b] : total;
         total += len[b];
         if (len[b] > 0) *end = std::max(*end, (*start)[b] + len[b]);
+        *longest = std::max<int64_t>(*longest, len[b]);
+        if (b > 0 && (*start)[b] < (*start)[b - 1]) *in_order = false;
     }
     *shared = given && any_shared(*start, len);
     return total;
@@ -108,8 +112,8 @@ std::vector<Unit> order(std::vector<Costed>& units, bsm_schedule schedule, int n
 }  // namespace
 
 void finish_sequences(Sequences* s, const int64_t* q_start, const int64_t* kv_start) {
-    s->total_q = fill(q_start, s->q_len, &s->q_start, &s->q_end, &s->q_shared);
-    s->total_kv = fill(kv_start, s->kv_len, &s->kv_start, &s->kv_end, &s->kv_shared);
+    s->total_q = fill(q_start, s->q_len, &s->q_start, &s->q_end, &s->q_longest, &s->q_shared, &s->q_in_order);
+    s->total_kv = fill(kv_start, s->kv_len, &s->kv_start, &s->kv_end, &s->kv_longest, &s->kv_shared, &s->kv_in_order);
     s->pairs = 0;
     for (int64_t b = 0; b < s->batch; ++b) s->pairs += visible(s->q_len[b], s->kv_len[b], s->mask);
 }

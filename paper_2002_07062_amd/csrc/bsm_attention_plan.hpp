@@ -18,6 +18,8 @@ struct Sequences {
     Mask mask{0, 0};
     int64_t total_q = 0, total_kv = 0;
     int64_t q_end = 0, kv_end = 0;           // largest row + 1
+    int64_t q_longest = 0, kv_longest = 0;   // rows of the longest sequence
+    bool q_in_order = true, kv_in_order = true;  // no sequence starts before the one before it
     bool q_shared = false, kv_shared = false;  // some row belongs to two sequences
     int64_t pairs = 0;
 };
