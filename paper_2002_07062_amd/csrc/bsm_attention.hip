@@ -61,7 +61,8 @@ __global__ __launch_bounds__(kThreads, 2) void attention_kernel(const SequenceAr
         sk.end(tid, lds[0][0]);
         sv.end(tid, lds[0][1]);
     }
-    const Frags<D> at_lane(lane);
+    const RowFrags<D> rows_at(lane);
+    const ColFrags<D> cols_at(lane);
     // the tiles read and the tiles written in a step are apart
     auto step = [&](int j0, uint16_t* __restrict__ next_k, uint16_t* __restrict__ next_v, const uint16_t* __restrict__ now_k,
                     const uint16_t* __restrict__ now_v) __attribute__((always_inline)) {
@@ -73,13 +74,15 @@ __global__ __launch_bounds__(kThreads, 2) void attention_kernel(const SequenceAr
         }
         if (any_row && j0 <= w1.hi && next > w0.lo) {
             f32x16 s[kKeys / 32];
-            row_product<D>(s, at_lane, now_k, 0, q);
+            row_product<D>(s, rows_at, now_k, 0, q);
             if (j0 < w1.lo || next - 1 > w0.hi) {
 #pragma unroll
                 for (int k = 0; k < kKeys / 32; ++k) mask_block(s[k], j0 + 32 * k, h, mine.lo, mine.hi);
             }
             st.weigh(s, c);
-            col_product<D>(st.o, at_lane, now_v, 0, s);
+            bf16x8 p[kKeys / 16];
+            to_operands(p, s);
+            col_product(st.o, cols_at, now_v, 0, p);
         }
         if (next < end) {
             sk.end(tid, next_k);
@@ -152,7 +155,8 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(const Sequenc
         sk.end(tid, lds[0][0]);
         sv.end(tid, lds[0][1]);
     }
-    const Frags<D> at_lane(lane);
+    const RowFrags<D> rows_at(lane);
+    const ColFrags<D> cols_at(lane);
     auto step = [&](int j0, uint16_t* __restrict__ next_k, uint16_t* __restrict__ next_v, const uint16_t* __restrict__ now_k,
                     const uint16_t* __restrict__ now_v) __attribute__((always_inline)) {
         tile_barrier<DIRECT>();
@@ -166,8 +170,8 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(const Sequenc
 #pragma unroll
             for (int k = 0; k < kKeys / 32; ++k) {
                 f32x16 s[1], dp[1];
-                row_product<D>(s, at_lane, now_k, 32 * k, q);
-                row_product<D>(dp, at_lane, now_v, 32 * k, dout);
+                row_product<D>(s, rows_at, now_k, 32 * k, q);
+                row_product<D>(dp, rows_at, now_v, 32 * k, dout);
                 if (masked) mask_block(s[0], j0 + 32 * k, h, mine.lo, mine.hi);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
@@ -176,7 +180,9 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(const Sequenc
                     // a masked score contributes nothing, whatever v holds there
                     s[0][e] = masked && s[0][e] == -kInf ? 0.0f : ds;
                 }
-                col_product<D>(dq, at_lane, now_k, 32 * k, s);
+                bf16x8 ds[2];
+                to_operands(ds, s);
+                col_product(dq, cols_at, now_k, 32 * k, ds);
             }
         }
         if (next < end) {
@@ -194,24 +200,39 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(const Sequenc
 }
 
 // dv_j = sum_i P_ij do_i and dk_j = scale * sum_i dS_ij q_i over the rows of all query heads that
-// share the key/value head: a wave keeps 32 keys (k, v and both sums in registers), the query
-// rows stream through LDS.  No sum crosses a workgroup, so the result does not depend on timing.
+// share the key/value head: k, v and both sums stay in registers, the query rows stream through LDS, 64
+// at a time.  No sum crosses a workgroup, so the result does not depend on timing.
+// Two waves share 32 keys: wave x of the pair forms P and dS for the 32 query rows of block x, the pair
+// exchanges them through LDS as operands, and each adds up half of the head dimension over both blocks.
+// That keeps a wave's sums at 64 registers, so that two waves fit a SIMD and one's exponentials run beside
+// the other's products (a wave that held whole sums took 400 registers and ran alone: 735 us against
+// 567 us on six ragged causal sequences of 700 .. 4001 tokens, 32 / 8 heads of 128).
+constexpr int kPairThreads = 512;
+
 template <int D, bool DIRECT>
-__global__ __launch_bounds__(kThreads, 1) void attention_dkv_kernel(const SequenceArgs a, const Unit* __restrict__ units) {
-    __shared__ __align__(16) uint16_t lds[2][2][kKeys * D];  // buffer, q or dout
-    __shared__ __align__(16) float stat[2][2 * kKeys];       // buffer; references, then deltas
+__global__ __launch_bounds__(kPairThreads, 2) void attention_dkv_kernel(const SequenceArgs a, const Unit* __restrict__ units) {
+    constexpr int kTiles = D / 64;  // blocks of 32 columns of a wave
+    // One array: of several, the compiler forgets which tiles a step reads and writes, and waits for the
+    // loads on their way before every read of LDS.
+    struct Shared {
+        uint16_t tile[2][2][kKeys * D];    // buffer, q or dout
+        float stat[2][2 * kKeys];          // buffer; references, then deltas
+        bf16x8 exchange[4][2][4][kWave];   // pair, block; P and dS of 16 rows
+    };
+    __shared__ __align__(16) Shared lds;
     const Unit u = units[blockIdx.x];
     if (u.rows <= 0) return;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, li = lane & 31, h = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), li = lane & 31, h = lane >> 5;
+    const int pair = wave >> 1, x = wave & 1;
     const int chunks = a.dim / 8;
-    const int j0 = u.first + kRows * wave, j = j0 + li;
+    const int j0 = u.first + kRows * pair, j = j0 + li;
     const bool live = j < u.first + u.rows;
     RowOperand<D> k, v;
     k.load(at(a.k, u, u.kv_start + j, u.head), live, h, chunks);
     v.load(at(a.v, u, u.kv_start + j, u.head), live, h, chunks);
-    f32x16 dk[D / 32], dv[D / 32];
+    f32x16 dk[kTiles], dv[kTiles];
 #pragma unroll
-    for (int t = 0; t < D / 32; ++t) dk[t] = dv[t] = zero16();
+    for (int t = 0; t < kTiles; ++t) dk[t] = dv[t] = zero16();
     const float c = a.scale * kLog2e;
     // Query rows that see a key of the unit: i + off >= j, and i + off < j + window.  Rows before the
     // first key (`dead` of them, where there are more queries than keys) count as zeros, whatever they hold.
@@ -227,38 +248,43 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dkv_kernel(const Sequen
     const int64_t total = static_cast<int64_t>(steps) * a.group;
     const bool any_row = j0 <= last;
 
-    Stage<D, kKeys, kThreads, DIRECT> sq, sd;
-    float ref = kInf, delta = 0.0f;  // of row `tid` of the step, threads 0 .. kKeys - 1
+    Stage<D, kKeys, kPairThreads, DIRECT> sq, sd;
+    float lse = 0.0f, delta = 0.0f;  // of row `tid` % kKeys of the step to come
+    int rows_left = 0;
     sq.init(tid, a.q.row, chunks);
     sd.init(tid, a.dout.row, chunks);
-    auto fetch = [&](int g, int r0, uint16_t* to_q, uint16_t* to_d) __attribute__((always_inline)) {
-        const int head = u.head * a.group + g;
-        sq.begin(tid, to_q, at(a.q, u, u.q_start + r0, head), a.q.row, dead - r0, end - r0, chunks);
-        sd.begin(tid, to_d, at(a.dout, u, u.q_start + r0, head), a.dout.row, dead - r0, end - r0, chunks);
-        if (tid < kKeys) {
-            const int64_t r = head * a.total_q + u.lse_row + min(r0 + tid, end - 1);
-            ref = reference(a.lse[r]);
-            delta = a.delta[r];
-            if (r0 + tid >= end || ref == kInf) {
-                ref = kInf;
-                delta = 0.0f;
-            }
-        }
+    auto fetch_stat = [&](int g, int r0) __attribute__((always_inline)) {
+        const int64_t r = static_cast<int64_t>(u.head * a.group + g) * a.total_q + u.lse_row + min(r0 + tid % kKeys, end - 1);
+        lse = a.lse[r];
+        delta = a.delta[r];
+        rows_left = end - r0;
     };
     auto put = [&](uint16_t* to_q, uint16_t* to_d, float* to_stat) __attribute__((always_inline)) {
         sq.end(tid, to_q);
         sd.end(tid, to_d);
         if (tid < kKeys) {
+            const float ref = tid < rows_left ? reference(lse) : kInf;
             to_stat[tid] = ref;
-            to_stat[kKeys + tid] = delta;
+            to_stat[kKeys + tid] = ref == kInf ? 0.0f : delta;
         }
     };
     if (total > 0) {
-        fetch(0, begin, lds[0][0], lds[0][1]);
-        put(lds[0][0], lds[0][1], stat[0]);
+        const int head = u.head * a.group;
+        sq.begin(tid, lds.tile[0][0], at(a.q, u, u.q_start + begin, head), a.q.row, dead - begin, end - begin, chunks);
+        sd.begin(tid, lds.tile[0][1], at(a.dout, u, u.q_start + begin, head), a.dout.row, dead - begin, end - begin, chunks);
+        fetch_stat(0, begin);
+        put(lds.tile[0][0], lds.tile[0][1], lds.stat[0]);
     }
     int r0 = begin, g = 0;
-    const Frags<D> at_lane(lane);
+    constexpr int kBlockBytes = 32 * Tile<D>::kRowBytes;
+    const RowFrags<D> rows_at(lane, x * kBlockBytes);
+    const ColFrags<D, kTiles> mine_at(lane, x * kTiles, x * kBlockBytes), other_at(lane, x * kTiles, (1 - x) * kBlockBytes);
+    // whether the mask hides every pair of query rows p0 .. p1 (as positions) and the pair's keys
+    auto none = [&](int p0, int p1) {
+        if (!any_row || p1 < p0) return true;
+        if (!a.mask.causal) return false;
+        return p1 < j0 || (a.mask.window > 0 && static_cast<int64_t>(p0) - a.mask.window >= j0 + kRows - 1);
+    };
     auto step = [&](int64_t n, uint16_t* __restrict__ next_q, uint16_t* __restrict__ next_d, float* __restrict__ next_stat,
                     const uint16_t* __restrict__ now_q, const uint16_t* __restrict__ now_d, const float* __restrict__ now_stat)
                     __attribute__((always_inline)) {
@@ -268,57 +294,78 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dkv_kernel(const Sequen
             next_r0 = begin;
             ++next_g;
         }
-        if (n + 1 < total) fetch(next_g, next_r0, next_q, next_d);
-        // whether the mask hides some pair, or every pair, of these query rows and the wave's keys
-        bool masked = false, none = !any_row;
-        if (a.mask.causal) {
-            const int p0 = r0 + off, p1 = min(r0 + kKeys, end) - 1 + off;
-            masked = p0 < j0 + kRows - 1;
-            none = none || p1 < j0;
-            if (a.mask.window > 0) {
-                masked = masked || static_cast<int64_t>(p1) - a.mask.window >= j0;
-                none = none || static_cast<int64_t>(p0) - a.mask.window >= j0 + kRows - 1;
+        if (n + 1 < total) {
+            const int head = u.head * a.group + next_g;
+            sq.begin(tid, next_q, at(a.q, u, u.q_start + next_r0, head), a.q.row, dead - next_r0, end - next_r0, chunks);
+            sd.begin(tid, next_d, at(a.dout, u, u.q_start + next_r0, head), a.dout.row, dead - next_r0, end - next_r0, chunks);
+            fetch_stat(next_g, next_r0);
+        }
+        const int b0 = r0 + 32 * x + off, b1 = min(r0 + 32 * x + 32, end) - 1 + off;              // positions of the wave's block
+        const int c0 = r0 + 32 * (1 - x) + off, c1 = min(r0 + 32 * (1 - x) + 32, end) - 1 + off;  // and of the other's
+        const bool mine = !none(b0, b1), other = !none(c0, c1);
+        bf16x8 po[2], so[2];
+        if (mine) {
+            f32x16 p[1], ds[1];
+            row_product<D>(p, rows_at, now_q, 0, k);
+            row_product<D>(ds, rows_at, now_d, 0, v);
+            const bool masked = a.mask.causal && (b0 < j0 + kRows - 1 || (a.mask.window > 0 && static_cast<int64_t>(b1) - a.mask.window >= j0));
+#pragma unroll
+            for (int e4 = 0; e4 < 4; ++e4) {
+                const f32x4 rr = *reinterpret_cast<const f32x4*>(now_stat + 32 * x + 8 * e4 + 4 * h);
+                const f32x4 dd = *reinterpret_cast<const f32x4*>(now_stat + kKeys + 32 * x + 8 * e4 + 4 * h);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int y = 4 * e4 + e;
+                    p[0][y] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[0][y], c, -rr[e]));
+                    ds[0][y] = p[0][y] * (ds[0][y] - dd[e]);
+                }
+            }
+            if (masked) {
+#pragma unroll
+                for (int y = 0; y < 16; ++y) {
+                    const Seen s = seen_keys(r0 + 32 * x + 4 * h + reg_row(y), u.q_len, u.kv_len, a.mask);
+                    const bool sees = j >= s.lo && j <= s.hi;
+                    p[0][y] = sees ? p[0][y] : 0.0f;
+                    ds[0][y] = sees ? ds[0][y] : 0.0f;
+                }
+            }
+            to_operands(po, p);
+            to_operands(so, ds);
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                lds.exchange[pair][x][s][lane] = po[s];
+                lds.exchange[pair][x][2 + s][lane] = so[s];
             }
         }
-        if (!none) {
+        lds_barrier();
+        if (mine) {
+            col_product(dv, mine_at, now_d, 0, po);
+            col_product(dk, mine_at, now_q, 0, so);
+        }
+        if (other) {
 #pragma unroll
-            for (int b = 0; b < kKeys / 32; ++b) {
-                f32x16 p[1], ds[1];
-                row_product<D>(p, at_lane, now_q, 32 * b, k);
-                row_product<D>(ds, at_lane, now_d, 32 * b, v);
-#pragma unroll
-                for (int e4 = 0; e4 < 4; ++e4) {
-                    const f32x4 rr = *reinterpret_cast<const f32x4*>(now_stat + 32 * b + 8 * e4 + 4 * h);
-                    const f32x4 dd = *reinterpret_cast<const f32x4*>(now_stat + kKeys + 32 * b + 8 * e4 + 4 * h);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int x = 4 * e4 + e;
-                        float pv = __builtin_amdgcn_exp2f(__builtin_fmaf(p[0][x], c, -rr[e]));
-                        float dv_ = pv * (ds[0][x] - dd[e]);
-                        if (masked) {
-                            const Seen s = seen_keys(r0 + 32 * b + 8 * e4 + 4 * h + e, u.q_len, u.kv_len, a.mask);
-                            const bool sees = j >= s.lo && j <= s.hi;
-                            pv = sees ? pv : 0.0f;
-                            dv_ = sees ? dv_ : 0.0f;
-                        }
-                        p[0][x] = pv;
-                        ds[0][x] = dv_;
-                    }
-                }
-                col_product<D>(dv, at_lane, now_d, 32 * b, p);
-                col_product<D>(dk, at_lane, now_q, 32 * b, ds);
+            for (int s = 0; s < 2; ++s) {
+                po[s] = lds.exchange[pair][1 - x][s][lane];
+                so[s] = lds.exchange[pair][1 - x][2 + s][lane];
             }
+            col_product(dv, other_at, now_d, 0, po);
+            col_product(dk, other_at, now_q, 0, so);
         }
         if (n + 1 < total) put(next_q, next_d, next_stat);
         r0 = next_r0;
         g = next_g;
     };
     in_turn(0, total, 1, [&](int64_t n, auto buf) {
-        step(n, lds[1 - buf][0], lds[1 - buf][1], stat[1 - buf], lds[buf][0], lds[buf][1], stat[buf]);
+        step(n, lds.tile[1 - buf][0], lds.tile[1 - buf][1], lds.stat[1 - buf], lds.tile[buf][0], lds.tile[buf][1], lds.stat[buf]);
     });
     const int64_t row = u.kv_start + j;
-    store_row<D>(a.dk.p + u.seq * a.dk.seq + row * a.dk.row + u.head * a.dk.head, live, dk, a.scale, h, chunks);
-    store_row<D>(a.dv.p + u.seq * a.dv.seq + row * a.dv.row + u.head * a.dv.head, live, dv, 1.0f, h, chunks);
+    uint16_t* to_k = a.dk.p + u.seq * a.dk.seq + row * a.dk.row + u.head * a.dk.head;
+    uint16_t* to_v = a.dv.p + u.seq * a.dv.seq + row * a.dv.row + u.head * a.dv.head;
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+        store_block(to_k, live, dk[t], a.scale, x * kTiles + t, h, chunks);
+        store_block(to_v, live, dv[t], 1.0f, x * kTiles + t, h, chunks);
+    }
 }
 
 }  // namespace
@@ -354,10 +401,10 @@ hipError_t launch_attention_backward(const SequenceArgs& a, const Unit* q_units,
     if (n_kv > 0) {
         const bool direct = aligned_pieces(a.q) && aligned_pieces(a.dout);
         const unsigned grid = static_cast<unsigned>(n_kv);
-        if (a.dim <= 64 && direct) attention_dkv_kernel<64, true><<<grid, kThreads, 0, stream>>>(a, kv_units);
-        else if (a.dim <= 64) attention_dkv_kernel<64, false><<<grid, kThreads, 0, stream>>>(a, kv_units);
-        else if (direct) attention_dkv_kernel<128, true><<<grid, kThreads, 0, stream>>>(a, kv_units);
-        else attention_dkv_kernel<128, false><<<grid, kThreads, 0, stream>>>(a, kv_units);
+        if (a.dim <= 64 && direct) attention_dkv_kernel<64, true><<<grid, kPairThreads, 0, stream>>>(a, kv_units);
+        else if (a.dim <= 64) attention_dkv_kernel<64, false><<<grid, kPairThreads, 0, stream>>>(a, kv_units);
+        else if (direct) attention_dkv_kernel<128, true><<<grid, kPairThreads, 0, stream>>>(a, kv_units);
+        else attention_dkv_kernel<128, false><<<grid, kPairThreads, 0, stream>>>(a, kv_units);
         return hipGetLastError();
     }
     return hipSuccess;

@@ -59,37 +59,43 @@ struct Tile {
 };
 
 // Where a lane's fragments lie, in bytes from the start of a tile: the same for every 16 rows, so that what
-// changes from read to read is a constant of the instruction.
+// changes from read to read is a constant of the instruction.  `base`: bytes added to all of them.
 template <int D>
-struct Frags {
-    int row[D / 16];     // row li, elements 16 s + 8 h .. + 7
-    int col[2][D / 32];  // see col_frag
-    __device__ __forceinline__ explicit Frags(int lane) {
-        const int li = lane & 31, h = lane >> 5, g = lane >> 4, s = lane & 15;
+struct RowFrags {
+    int at[D / 16];
+    __device__ __forceinline__ explicit RowFrags(int lane, int base = 0) {
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) row[i] = 16 * Tile<D>::place(li, 2 * i + h);
-#pragma unroll
-        for (int t = 0; t < D / 32; ++t) {
-            const int r = 4 * (g >> 1) + (s >> 2), c = 32 * t + 16 * (g & 1) + 4 * (s & 3);
-            col[0][t] = 16 * Tile<D>::place(r, c >> 3) + 2 * (c & 7);
-            col[1][t] = 16 * Tile<D>::place(r + 8, c >> 3) + 2 * (c & 7);
-        }
+        for (int i = 0; i < D / 16; ++i) at[i] = base + 16 * Tile<D>::place(lane & 31, 2 * i + (lane >> 5));
     }
     // lane (li, h): elements 16 s + 8 h .. + 7 of row r0 + li; r0 a multiple of 16
-    __device__ __forceinline__ bf16x8 row_frag(const uint16_t* lds, int r0, int s) const {
-        return *reinterpret_cast<const bf16x8*>(reinterpret_cast<const char*>(lds) + row[s] + r0 * Tile<D>::kRowBytes);
+    __device__ __forceinline__ bf16x8 read(const uint16_t* lds, int r0, int s) const {
+        return *reinterpret_cast<const bf16x8*>(reinterpret_cast<const char*>(lds) + at[s] + r0 * Tile<D>::kRowBytes);
     }
-    // lane (li, h): column 32 t + li of rows r0 + 4 h + {0..3} and r0 + 8 + 4 h + {0..3}; r0 a
+};
+// Column blocks t0 .. t0 + TILES - 1 of 32.
+template <int D, int TILES = D / 32>
+struct ColFrags {
+    int at[2][TILES];
+    __device__ __forceinline__ explicit ColFrags(int lane, int t0 = 0, int base = 0) {
+        const int g = lane >> 4, s = lane & 15;
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) {
+            const int r = 4 * (g >> 1) + (s >> 2), c = 32 * (t0 + t) + 16 * (g & 1) + 4 * (s & 3);
+            at[0][t] = base + 16 * Tile<D>::place(r, c >> 3) + 2 * (c & 7);
+            at[1][t] = base + 16 * Tile<D>::place(r + 8, c >> 3) + 2 * (c & 7);
+        }
+    }
+    // lane (li, h): column 32 (t0 + t) + li of rows r0 + 4 h + {0..3} and r0 + 8 + 4 h + {0..3}; r0 a
     // multiple of 16.  ds_read_b64_tr_b16 works in groups of 16 lanes: lane s points at row s / 4,
     // columns 4 (s % 4) .. + 3 of a 4 x 16 block and receives the block's column s.
-    __device__ __forceinline__ bf16x8 col_frag(const uint16_t* lds, int r0, int t) const {
+    __device__ __forceinline__ bf16x8 read(const uint16_t* lds, int r0, int t) const {
         const char* p = reinterpret_cast<const char*>(lds) + r0 * Tile<D>::kRowBytes;
         union {
             i16x4 half[2];
             bf16x8 all;
         } u;
-        u.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(p + col[0][t]));
-        u.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(p + col[1][t]));
+        u.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(p + at[0][t]));
+        u.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(p + at[1][t]));
         return u.all;
     }
 };
@@ -208,35 +214,32 @@ __device__ __forceinline__ void pipelined(Read read, Use use) {
 // 32 KT rows of the tile (from row r0) times the operand's 32 rows: lane (li, h) gets column li
 // (operand row) and, in acc[k], tile rows r0 + 32 k + 8 (i / 4) + 4 h + i % 4.
 template <int D, int KT>
-__device__ __forceinline__ void row_product(f32x16 (&acc)[KT], const Frags<D>& at, const uint16_t* lds, int r0, const RowOperand<D>& q) {
+__device__ __forceinline__ void row_product(f32x16 (&acc)[KT], const RowFrags<D>& at, const uint16_t* lds, int r0, const RowOperand<D>& q) {
     constexpr int kSteps = D / 16;
 #pragma unroll
     for (int k = 0; k < KT; ++k) acc[k] = zero16();
     pipelined<KT * kSteps, kAhead>(
-        [&](int i) { return at.row_frag(lds, r0 + 32 * (i / kSteps), i % kSteps); },
+        [&](int i) { return at.read(lds, r0 + 32 * (i / kSteps), i % kSteps); },
         [&](int i, bf16x8 a) { acc[i / kSteps] = mfma(a, q.f[i % kSteps], acc[i / kSteps]); });
 }
 
-// Registers 8 s .. 8 s + 7 rounded to bf16 (nearest even): probabilities and score gradients are
-// rounded once, as operands of the next product, whose sums stay in fp32.
-__device__ __forceinline__ bf16x8 half_operand(const f32x16& x, int s) {
-    bf16x8 v;
+// Blocks of 32 x 32 as operands of 16 rows, rounded to bf16 (nearest even): probabilities and score
+// gradients are rounded once, as operands of the next product, whose sums stay in fp32.
+template <int KT>
+__device__ __forceinline__ void to_operands(bf16x8 (&b)[2 * KT], const f32x16 (&x)[KT]) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = static_cast<__bf16>(x[8 * s + e]);
-    return v;
+    for (int s = 0; s < 2 * KT; ++s)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) b[s][e] = static_cast<__bf16>(x[s / 2][8 * (s % 2) + e]);
 }
 
-// acc[t] += (columns 32 t .. of tile rows r0 .. r0 + 32 KT - 1)^T times x: lane li keeps its column of x,
-// rows 32 t + 8 (i / 4) + 4 h + i % 4 of the tile's columns.
-template <int D, int KT>
-__device__ __forceinline__ void col_product(f32x16 (&acc)[D / 32], const Frags<D>& at, const uint16_t* lds, int r0, const f32x16 (&x)[KT]) {
-    constexpr int kTiles = D / 32;
-    bf16x8 b[2 * KT];
-#pragma unroll
-    for (int s = 0; s < 2 * KT; ++s) b[s] = half_operand(x[s / 2], s % 2);
-    pipelined<2 * KT * kTiles, kAhead>(
-        [&](int i) { return at.col_frag(lds, r0 + 16 * (i / kTiles), i % kTiles); },
-        [&](int i, bf16x8 a) { acc[i % kTiles] = mfma(a, b[i / kTiles], acc[i % kTiles]); });
+// acc[t] += (columns of block t of tile rows r0 .. r0 + 16 N - 1)^T times N operands of 16 rows each: lane li
+// keeps its column of them, rows 8 (i / 4) + 4 h + i % 4 of the block's columns.
+template <int D, int TILES, int N>
+__device__ __forceinline__ void col_product(f32x16 (&acc)[TILES], const ColFrags<D, TILES>& at, const uint16_t* lds, int r0,
+                                            const bf16x8 (&b)[N]) {
+    pipelined<N * TILES, kAhead>([&](int i) { return at.read(lds, r0 + 16 * (i / TILES), i % TILES); },
+                                 [&](int i, bf16x8 a) { acc[i % TILES] = mfma(a, b[i / TILES], acc[i % TILES]); });
 }
 
 // f(v of lane l, v of lane l ^ 32), the same in both: v_permlane32_swap exchanges the upper half of one
@@ -285,14 +288,18 @@ __device__ __forceinline__ void store_row(uint16_t* row, bool live, const f32x16
     for (int t = 0; t < D / 32; ++t) store_block(row, live, acc[t], f, t, h, chunks);
 }
 
+// Barrier that orders the workgroup's LDS accesses and leaves loads from memory in flight.
+__device__ __forceinline__ void lds_barrier() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
 // Barrier after which the tiles that were begun and ended before it are visible to the workgroup, and no
 // wave reads the ones before.  What is still on its way straight to LDS is waited for.
 template <bool DIRECT>
 __device__ __forceinline__ void tile_barrier() {
     if constexpr (DIRECT) __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-    __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+    lds_barrier();
 }
 
 // Runs step(x, buffer) for x = begin, begin + by, ..., the buffers 0 and 1 in turn and known to the compiler.

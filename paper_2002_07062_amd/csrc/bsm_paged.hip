@@ -158,7 +158,8 @@ __global__ __launch_bounds__(kThreads, 2) void paged_kernel(const PagedArgs a) {
         stage.find(a, table, tid, begin + kKeys, r.kv_len);
         stage.end(tid, lds[0][0], lds[0][1]);
     }
-    const Frags<D> at_lane(lane);
+    const RowFrags<D> rows_at(lane);
+    const ColFrags<D> cols_at(lane);
     // the tiles read and the tiles written in a step are apart
     auto step = [&](int j0, uint16_t* __restrict__ next_k, uint16_t* __restrict__ next_v, const uint16_t* __restrict__ now_k,
                     const uint16_t* __restrict__ now_v) __attribute__((always_inline)) {
@@ -170,13 +171,15 @@ __global__ __launch_bounds__(kThreads, 2) void paged_kernel(const PagedArgs a) {
         }
         if (any_row && j0 <= w1.hi && next > w0.lo) {
             f32x16 s[kKeys / 32];
-            row_product<D>(s, at_lane, now_k, 0, q);
+            row_product<D>(s, rows_at, now_k, 0, q);
             if (j0 < w1.lo || next - 1 > w0.hi || end < next) {
 #pragma unroll
                 for (int k = 0; k < kKeys / 32; ++k) mask_block(s[k], j0 + 32 * k, h, mine.lo, min(mine.hi, end - 1));
             }
             st.weigh(s, c);
-            col_product<D>(st.o, at_lane, now_v, 0, s);
+            bf16x8 p[kKeys / 16];
+            to_operands(p, s);
+            col_product(st.o, cols_at, now_v, 0, p);
         }
         if (next < end) stage.end(tid, next_k, next_v);
     };
