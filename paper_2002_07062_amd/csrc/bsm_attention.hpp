@@ -102,7 +102,7 @@ struct ColFrags {
 
 // Where rows and chunks that do not exist are read: a load that is always done, from one place or the
 // other, stays in flight; one inside a branch is waited for at the branch's end.
-static __device__ __attribute__((aligned(16))) const uint16_t kZeros[8] = {};
+static __device__ __attribute__((aligned(16))) const uint16_t kZeros[128] = {};
 __device__ __forceinline__ u32x4 load_or_zero(const uint16_t* p, bool live) {
     return *reinterpret_cast<const u32x4_any*>(live ? p : kZeros);
 }

@@ -157,14 +157,16 @@ PagedCut cut_paged(int64_t batch, int64_t tokens, int32_t heads_kv, int32_t grou
     const int64_t rows = std::min<int64_t>(max_q, tokens) * group;
     c.tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : kTileRows;
     c.tiles = static_cast<int32_t>(std::max<int64_t>(1, (rows + c.tile_rows - 1) / c.tile_rows));
-    // Two workgroups fit a CU.  With few rows, pieces for eight rounds of them where the axis is long
-    // enough: requests differ in length, and short pieces even that out.  With many, a piece's rows cost
-    // a write and a read of their own, so there are no more pieces than fill the CUs twice.
+    // Two or three workgroups fit a CU.  Pieces of the key axis fill the CUs, in as many rounds as pieces of
+    // 1024 keys give, at most eight: requests differ in length, and more rounds even that out, but a piece
+    // also has to find its request and its first page before it reads any key.  With many rows a
+    // piece's rows cost a write and a read of their own, so there are no more pieces than fill the CUs twice.
     const int64_t units = std::max<int64_t>(1, batch * heads_kv * c.tiles);
-    const int64_t rounds = c.tile_rows == kTileRows ? 2 : 8;
-    const int64_t want = (rounds * 2 * static_cast<int64_t>(n_cu) + units - 1) / units;
-    const int64_t keys = std::max<int64_t>(1, max_kv), most = (keys + 255) / 256;
-    const int64_t splits = std::max<int64_t>(1, std::min(want, most));
+    const int64_t keys = std::max<int64_t>(1, max_kv), slots = 2 * static_cast<int64_t>(n_cu);
+    const int64_t once = (slots + units - 1) / units;  // pieces that fill the CUs
+    int64_t splits = c.tile_rows == kTileRows ? (2 * slots + units - 1) / units
+                                              : std::min((8 * slots + units - 1) / units, std::max(once, keys / 1024));
+    splits = std::max<int64_t>(1, std::min(splits, (keys + 255) / 256));
     const int64_t each = ((keys + splits - 1) / splits + kKeyTile - 1) / kKeyTile * kKeyTile;
     c.split_keys = static_cast<int32_t>(each);
     c.splits = static_cast<int32_t>((keys + each - 1) / each);

@@ -212,8 +212,9 @@ __global__ __launch_bounds__(kThreads, 2) void paged_kernel(const PagedArgs a) {
 // registers are the next operand: keys 4 quad + i and 16 + 4 quad + i of a block.
 // A lane reads two keys' rows, n and n + 16, of K and of V.  K goes to the matrix cores as it comes; V is
 // turned in LDS.  The next block's loads are issued when the scores have left K's registers.
-template <int D, int NQ>
-__global__ __launch_bounds__(kThreads, 2) void paged_few_kernel(const PagedArgs a) {
+// FULL: the head dimension is D, so that a row is read from one address or from zeros as a whole.
+template <int D, int NQ, bool FULL>
+__global__ __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) void paged_few_kernel(const PagedArgs a) {
     constexpr int kKeys = 32, kSteps = D / 32, kTiles = D / 16;
     constexpr int kRegs = NQ * kTiles * 4;  // outputs of a lane
     constexpr int kBytes = kWaves * (kRegs * kWave * 4 > kKeys * D * 2 ? kRegs * kWave * 4 : kKeys * D * 2);
@@ -249,7 +250,17 @@ __global__ __launch_bounds__(kThreads, 2) void paged_few_kernel(const PagedArgs 
     const int end = piece == a.splits - 1 ? ps.keys.hi + 1 : min(ps.keys.hi + 1, (piece + 1) * a.split_keys);
     const int begin = from / kKeys * kKeys + wave * kKeys;
     const int32_t* table = a.table + static_cast<int64_t>(r.b) * a.width;
-    uint16_t* mem = reinterpret_cast<uint16_t*>(lds) + wave * kKeys * D;
+    // the wave's V block: places do not depend on a multiple of 16 of the row
+    unsigned char* turned = lds + wave * kKeys * D * 2;
+    int put_at[kSteps], col_at[kTiles];
+#pragma unroll
+    for (int e = 0; e < kSteps; ++e) put_at[e] = 16 * Tile<D>::place(n, 4 * e + quad);
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+        // lane (n, quad): column 16 t + n of rows 4 quad + {0..3} (and of those 16 further)
+        const int row = 4 * quad + (n >> 2), col = 16 * t + 4 * (n & 3);
+        col_at[t] = 16 * Tile<D>::place(row, col >> 3) + 2 * (col & 7);
+    }
 
     f32x4 o[NQ][kTiles];
     float m[NQ], l[NQ];
@@ -276,10 +287,12 @@ __global__ __launch_bounds__(kThreads, 2) void paged_few_kernel(const PagedArgs 
             const int j = j0 + 16 * y + n;
             const bool live = page[y] >= 0;
             const int64_t from = page[y] * a.cache.page + (j % a.cache.page_size) * a.cache.row + r.head * a.cache.head + 8 * quad;
+            const uint16_t* kp = live ? a.cache.k + from : kZeros + 8 * quad;
+            const uint16_t* vp = live ? a.cache.v + from : kZeros + 8 * quad;
 #pragma unroll
             for (int s = 0; s < kSteps; ++s) {
-                k[y][s] = load_or_zero(a.cache.k + from + 32 * s, live && 4 * s + quad < chunks);
-                v[y][s] = load_or_zero(a.cache.v + from + 32 * s, live && 4 * s + quad < chunks);
+                k[y][s] = load_or_zero(kp + 32 * s, FULL || 4 * s + quad < chunks);
+                v[y][s] = load_or_zero(vp + 32 * s, FULL || 4 * s + quad < chunks);
             }
         }
     };
@@ -304,7 +317,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_few_kernel(const PagedArgs 
         for (int y = 0; y < 2; ++y)
 #pragma unroll
             for (int e = 0; e < kSteps; ++e)
-                *reinterpret_cast<u32x4*>(mem + 8 * Tile<D>::place(16 * y + n, 4 * e + quad)) = v[y][e];
+                *reinterpret_cast<u32x4*>(turned + put_at[e] + 16 * y * Tile<D>::kRowBytes) = v[y][e];
         const int next = j0 + step;
         if (next < end) {
             load(next);
@@ -354,14 +367,12 @@ __global__ __launch_bounds__(kThreads, 2) void paged_few_kernel(const PagedArgs 
                 }
 #pragma unroll
             for (int t = 0; t < kTiles; ++t) {
-                // lane (n, quad): column 16 t + n of rows 4 quad + {0..3} and 16 + 4 quad + {0..3}
-                const int row = 4 * quad + (n >> 2), col = 16 * t + 4 * (n & 3);
                 union {
                     i16x4 half[2];
                     bf16x8 all;
                 } u;
-                u.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(mem + 8 * Tile<D>::place(row, col >> 3) + (col & 7)));
-                u.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(mem + 8 * Tile<D>::place(row + 16, col >> 3) + (col & 7)));
+                u.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(turned + col_at[t]));
+                u.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(turned + col_at[t] + 16 * Tile<D>::kRowBytes));
                 o[x][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(u.all, p, o[x][t], 0, 0, 0);
             }
         }
@@ -649,8 +660,11 @@ template <int D>
 hipError_t launch_paged(const PagedArgs& a, hipStream_t stream) {
     const int64_t tiles = a.batch * a.cache.heads * a.tiles;
     const unsigned grid = static_cast<unsigned>(tiles * a.splits);
-    if (a.tile_rows == 16) paged_few_kernel<D, 1><<<grid, kThreads, 0, stream>>>(a);
-    else if (a.tile_rows == 32) paged_few_kernel<D, 2><<<grid, kThreads, 0, stream>>>(a);
+    const bool full = a.cache.dim == D;
+    if (a.tile_rows == 16 && full) paged_few_kernel<D, 1, true><<<grid, kThreads, 0, stream>>>(a);
+    else if (a.tile_rows == 16) paged_few_kernel<D, 1, false><<<grid, kThreads, 0, stream>>>(a);
+    else if (a.tile_rows == 32 && full) paged_few_kernel<D, 2, true><<<grid, kThreads, 0, stream>>>(a);
+    else if (a.tile_rows == 32) paged_few_kernel<D, 2, false><<<grid, kThreads, 0, stream>>>(a);
     else if (aligned_pieces({a.cache.k, a.cache.page, a.cache.row, a.cache.head}) && reinterpret_cast<uintptr_t>(a.cache.v) % 16 == 0)
         paged_kernel<D, true><<<grid, kThreads, 0, stream>>>(a);
     else paged_kernel<D, false><<<grid, kThreads, 0, stream>>>(a);
