@@ -103,9 +103,12 @@ struct ColFrags {
 // Where rows and chunks that do not exist are read: a load that is always done, from one place or the
 // other, stays in flight; one inside a branch is waited for at the branch's end.
 static __device__ __attribute__((aligned(16))) const uint16_t kZeros[128] = {};
-__device__ __forceinline__ u32x4 load_or_zero(const uint16_t* p, bool live) {
-    return *reinterpret_cast<const u32x4_any*>(live ? p : kZeros);
+// (Through the address space of device memory: a pointer chosen between two would be read by flat loads,
+// which also wait in line with LDS.)
+__device__ __forceinline__ u32x4 load_global(const uint16_t* p) {
+    return *(const __attribute__((address_space(1))) u32x4_any*)(p);
 }
+__device__ __forceinline__ u32x4 load_or_zero(const uint16_t* p, bool live) { return load_global(live ? p : kZeros); }
 
 // Carries a ROWS x D tile from memory to LDS, 16 bytes at a time: `begin` starts the loads of the tile
 // whose first row is at p and of which rows lo .. hi - 1 exist, `end` leaves them in LDS; then a
@@ -140,7 +143,7 @@ struct Stage {
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
                                              (__attribute__((address_space(3))) void*)to, 16, 0, 0);
         } else {
-            r[j] = *reinterpret_cast<const u32x4_any*>(from);
+            r[j] = load_global(from);
         }
     }
     __device__ __forceinline__ void begin(int tid, uint16_t* lds, const uint16_t* p, int64_t stride, int lo, int hi, int chunks) {

@@ -394,7 +394,7 @@ bsm_status check_paged_sizes(int64_t batch, int64_t tokens, int64_t heads_q, int
 bsm_status paged_cut(int64_t batch, int64_t tokens, int32_t heads_q, int32_t heads_kv, int32_t dim, int32_t max_q, int32_t max_kv,
                      int n_cu, bsm_att::PagedCut* cut) {
     *cut = bsm_att::cut_paged(batch, tokens, heads_kv, heads_q / heads_kv, dim, max_q, max_kv, n_cu);
-    if (static_cast<double>(batch) * heads_kv * cut->tiles * cut->splits > kMostWorkgroups)
+    if (cut->grid > kMostWorkgroups)
         return fail(BSM_ERR_INVALID_ARG, "batch %lld with max_q %d is too large for one call", static_cast<long long>(batch), max_q);
     return BSM_OK;
 }
@@ -449,6 +449,8 @@ bsm_status paged(const bsm_cache* cache, const bsm_heads* q, const bsm_heads* o,
     a.window = window;
     a.scale = scale;
     a.tile_rows = cut.tile_rows;
+    a.shares = cut.shares;
+    a.least_share = cut.least_share;
     a.tiles = cut.tiles;
     a.splits = cut.splits;
     a.split_keys = cut.split_keys;

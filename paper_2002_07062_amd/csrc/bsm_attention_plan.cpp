@@ -156,22 +156,32 @@ PagedCut cut_paged(int64_t batch, int64_t tokens, int32_t heads_kv, int32_t grou
     PagedCut c{};
     const int64_t rows = std::min<int64_t>(max_q, tokens) * group;
     c.tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : kTileRows;
+    const int padded = dim <= 64 ? 64 : 128;
+    const int64_t keys = std::max<int64_t>(1, max_kv);
+    if (c.tile_rows < kTileRows) {
+        c.tiles = c.splits = 1;
+        c.grid = batch * heads_kv;
+        // Up to eight rounds of a workgroup's 128 keys, a join would cost more than it saves.
+        if (keys <= 1024) return c;
+        // Shares for eight rounds of two workgroups on a CU, of 2048 keys at least: CUs do not read equally
+        // fast (one round of equal shares left them idle for 30% of the time), but a workgroup also has to
+        // count the stream and find its first page before it reads any key.
+        c.shares = static_cast<int32_t>(std::max(1, 16 * n_cu / heads_kv));
+        c.least_share = 16;
+        c.grid = std::max(c.grid, static_cast<int64_t>(c.shares) * heads_kv);
+        c.part_floats = 2 * static_cast<int64_t>(c.shares) * heads_kv * c.tile_rows * (padded + 2);
+        return c;
+    }
     c.tiles = static_cast<int32_t>(std::max<int64_t>(1, (rows + c.tile_rows - 1) / c.tile_rows));
-    // Two or three workgroups fit a CU.  Pieces of the key axis fill the CUs, in as many rounds as pieces of
-    // 1024 keys give, at most eight: requests differ in length, and more rounds even that out, but a piece
-    // also has to find its request and its first page before it reads any key.  With many rows a
-    // piece's rows cost a write and a read of their own, so there are no more pieces than fill the CUs twice.
-    const int64_t units = std::max<int64_t>(1, batch * heads_kv * c.tiles);
-    const int64_t keys = std::max<int64_t>(1, max_kv), slots = 2 * static_cast<int64_t>(n_cu);
-    const int64_t once = (slots + units - 1) / units;  // pieces that fill the CUs
-    int64_t splits = c.tile_rows == kTileRows ? (2 * slots + units - 1) / units
-                                              : std::min((8 * slots + units - 1) / units, std::max(once, keys / 1024));
-    splits = std::max<int64_t>(1, std::min(splits, (keys + 255) / 256));
+    // Two workgroups fit a CU.  A piece's rows cost a write and a read of their own, so there are no more
+    // pieces than fill the CUs twice.
+    const int64_t units = std::max<int64_t>(1, batch * heads_kv * c.tiles), slots = 2 * static_cast<int64_t>(n_cu);
+    const int64_t splits = std::max<int64_t>(1, std::min((2 * slots + units - 1) / units, (keys + 255) / 256));
     const int64_t each = ((keys + splits - 1) / splits + kKeyTile - 1) / kKeyTile * kKeyTile;
     c.split_keys = static_cast<int32_t>(each);
     c.splits = static_cast<int32_t>((keys + each - 1) / each);
-    const int padded = dim <= 64 ? 64 : 128;
     c.part_floats = c.splits > 1 ? units * c.splits * c.tile_rows * (padded + 2) : 0;
+    c.grid = units * c.splits;
     return c;
 }
 

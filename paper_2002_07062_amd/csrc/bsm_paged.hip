@@ -8,6 +8,40 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = 4;
 
+// Sums of tokens and pages over the requests before a thread's, and the chunk's totals.
+struct Two {
+    int64_t tokens, pages;
+};
+__device__ __forceinline__ Two scan(Two mine, Two* total, int64_t (*mem)[2]) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    Two x = mine;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int64_t t = __shfl_up(x.tokens, d, 64), p = __shfl_up(x.pages, d, 64);
+        if (lane >= d) {
+            x.tokens += t;
+            x.pages += p;
+        }
+    }
+    if (lane == 63) {
+        mem[wave][0] = x.tokens;
+        mem[wave][1] = x.pages;
+    }
+    __syncthreads();
+    Two before = {0, 0};
+    *total = {0, 0};
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        if (w < wave) {
+            before.tokens += mem[w][0];
+            before.pages += mem[w][1];
+        }
+        total->tokens += mem[w][0];
+        total->pages += mem[w][1];
+    }
+    return {before.tokens + x.tokens - mine.tokens, before.pages + x.pages - mine.pages};
+}
+
 // ---------------------------------------------------------------------------------- attention
 // One request and key/value head: the rows are (new token, query head of the group) pairs, token
 // after token, so that the query heads that share a key/value head read it once.
@@ -63,29 +97,50 @@ __device__ __forceinline__ Pieces pieces(const PagedArgs& a, const Request& r, i
     return p;
 }
 
+// Element of row `row` of the request and head in q or o.
+__device__ __forceinline__ int64_t row_at(const PagedArgs& a, const Request& r, const Heads& t, int row) {
+    return (r.q0 + row / a.group) * t.row + (r.head * a.group + row % a.group) * t.head;
+}
+
 // Floats of one piece's part: its rows' outputs, then their references and sums.
 __device__ __forceinline__ int64_t part_at(const PagedArgs& a, int D, const Request& r, int tile, int piece) {
     return (((static_cast<int64_t>(r.b) * a.cache.heads + r.head) * a.tiles + tile) * a.splits + piece) * a.tile_rows * (D + 2);
 }
 
-// What workgroup w does.  The workgroups of all requests and heads follow each other, tile after tile,
-// piece after piece, so the tiles that read the same keys run on one XCD (w mod 8 where requests times
-// heads is a multiple of 8).  The heads are rotated from request to request and piece to piece: a page
-// has its heads side by side, and an XCD that only ever read one of 8 heads of 128 would use 2 of its 16
-// L2 channels, which lie 256 bytes apart.
+// What workgroup w does.  The requests follow each other, the one with the most keys first (with more
+// than kThreads of them, as they come), so that the CUs end together; of each its tiles, pieces and heads, the
+// heads side by side.  They are rotated from request to request: a page has its heads side by side, and
+// an XCD that only ever read one of 8 heads of 128 (workgroups go to the 8 XCDs in turn) would use 2 of
+// its 16 L2 channels, which lie 256 bytes apart.
 struct Place {
     int64_t b;
     int head, tile, piece;
 };
-__device__ __forceinline__ Place place_of(const PagedArgs& a, int64_t w) {
-    const int64_t units = a.batch * a.cache.heads, unit = w % units, rest = w / units;
+__device__ __forceinline__ Place place_of(const PagedArgs& a, int64_t w, int* mem) {
+    const int64_t per = static_cast<int64_t>(a.tiles) * a.splits, unit = w / a.cache.heads;
     Place p;
-    p.tile = static_cast<int>(rest % a.tiles);
-    p.piece = static_cast<int>(rest / a.tiles);
-    p.b = unit / a.cache.heads;
-    p.head = static_cast<int>((unit + p.b + p.piece) % a.cache.heads);
+    p.b = unit / per;
+    p.tile = static_cast<int>(unit % per) / a.splits;
+    p.piece = static_cast<int>(unit % per) % a.splits;
+    p.head = static_cast<int>((w + p.b) % a.cache.heads);
+    if (a.batch <= kThreads) {
+        const int i = threadIdx.x, n = static_cast<int>(a.batch);
+        if (i < n) {
+            const int mine = a.kv_len[i];
+            int rank = 0;
+            for (int j = 0; j < n; ++j) {
+                const int other = a.kv_len[j];
+                rank += other > mine || (other == mine && j < i) ? 1 : 0;
+            }
+            if (rank == p.b) *mem = i;
+        }
+        __syncthreads();
+        p.b = __builtin_amdgcn_readfirstlane(*mem);
+    }
     return p;
 }
+
+__device__ __forceinline__ bool names_page(const PagedArgs& a, int entry) { return entry >= 0 && entry < a.cache.n_pages; }
 
 // The rows of K and V that a thread stages: tile row i is key j0 + i of the request.  Keys past its
 // end, and keys of table entries that name no page, are zeros.
@@ -93,20 +148,19 @@ template <int D, int ROWS, int THREADS, bool DIRECT>
 struct PagedStage {
     using S = Stage<D, ROWS, THREADS, DIRECT>;
     S k, v;
-    int page[S::kN];
-    // table entries of the tile at j0 (-1: none); the request has keys 0 .. end - 1
+    int page[S::kN];  // table entries, looked at when they are used: they are loaded behind a tile's loads
+    // table entries of the tile at j0; the request has keys 0 .. end - 1
     __device__ __forceinline__ void find(const PagedArgs& a, const int32_t* table, int tid, int j0, int end) {
 #pragma unroll
         for (int n = 0; n < S::kN; ++n) {
-            const int j = j0 + S::row(tid, n), entry = table[min(j, end - 1) / a.cache.page_size];
-            page[n] = j < end && entry < a.cache.n_pages ? entry : -1;
+            page[n] = table[min(j0 + S::row(tid, n), end - 1) / a.cache.page_size];
         }
     }
-    __device__ __forceinline__ void begin(const PagedArgs& a, int head, int tid, int j0, int chunks, uint16_t* lds_k, uint16_t* lds_v) {
+    __device__ __forceinline__ void begin(const PagedArgs& a, int head, int tid, int j0, int end, int chunks, uint16_t* lds_k, uint16_t* lds_v) {
 #pragma unroll
         for (int n = 0; n < S::kN; ++n) {
             const int j = j0 + S::row(tid, n), c = S::chunk(tid, n);
-            const bool live = page[n] >= 0 && c < chunks;
+            const bool live = j < end && names_page(a, page[n]) && c < chunks;
             const int64_t from = page[n] * a.cache.page + j % a.cache.page_size * a.cache.row + head * a.cache.head + 8 * c;
             k.piece(tid, n, lds_k, a.cache.k + from, live);
             v.piece(tid, n, lds_v, a.cache.v + from, live);
@@ -122,8 +176,14 @@ struct PagedStage {
 template <int D, bool DIRECT>
 __global__ __launch_bounds__(kThreads, 2) void paged_kernel(const PagedArgs a) {
     constexpr int kKeys = 64, kTileElems = kKeys * D;
-    __shared__ __align__(16) uint16_t lds[2][2][kTileElems];  // buffer, K or V
-    const Place at = place_of(a, blockIdx.x);
+    // One array: of several, the compiler forgets which tiles a step reads and writes, and waits for the
+    // loads on their way before every read of LDS.
+    struct Shared {
+        uint16_t tile[2][2][kTileElems];  // buffer, K or V
+        int place;
+    };
+    __shared__ __align__(16) Shared lds;
+    const Place at = place_of(a, blockIdx.x, &lds.place);
     const int tile = at.tile, piece = at.piece;
     const Request r = request(a, at.b, at.head);
     const int tile0 = tile * a.tile_rows;
@@ -154,9 +214,9 @@ __global__ __launch_bounds__(kThreads, 2) void paged_kernel(const PagedArgs a) {
     PagedStage<D, kKeys, kThreads, DIRECT> stage;
     if (begin < end) {
         stage.find(a, table, tid, begin, r.kv_len);
-        stage.begin(a, r.head, tid, begin, chunks, lds[0][0], lds[0][1]);
+        stage.begin(a, r.head, tid, begin, r.kv_len, chunks, lds.tile[0][0], lds.tile[0][1]);
         stage.find(a, table, tid, begin + kKeys, r.kv_len);
-        stage.end(tid, lds[0][0], lds[0][1]);
+        stage.end(tid, lds.tile[0][0], lds.tile[0][1]);
     }
     const RowFrags<D> rows_at(lane);
     const ColFrags<D> cols_at(lane);
@@ -166,7 +226,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_kernel(const PagedArgs a) {
         const int next = j0 + kKeys;
         tile_barrier<DIRECT>();
         if (next < end) {
-            stage.begin(a, r.head, tid, next, chunks, next_k, next_v);
+            stage.begin(a, r.head, tid, next, r.kv_len, chunks, next_k, next_v);
             stage.find(a, table, tid, next + kKeys, r.kv_len);
         }
         if (any_row && j0 <= w1.hi && next > w0.lo) {
@@ -183,7 +243,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_kernel(const PagedArgs a) {
         }
         if (next < end) stage.end(tid, next_k, next_v);
     };
-    in_turn(begin, end, kKeys, [&](int j0, auto buf) { step(j0, lds[1 - buf][0], lds[1 - buf][1], lds[buf][0], lds[buf][1]); });
+    in_turn(begin, end, kKeys, [&](int j0, auto buf) { step(j0, lds.tile[1 - buf][0], lds.tile[1 - buf][1], lds.tile[buf][0], lds.tile[buf][1]); });
     const float total = st.row_sum();
     if (ps.first == ps.last) {
         uint16_t* out = a.o.p + q_row * a.o.row + q_head * a.o.head;
@@ -213,322 +273,396 @@ __global__ __launch_bounds__(kThreads, 2) void paged_kernel(const PagedArgs a) {
 // A lane reads two keys' rows, n and n + 16, of K and of V.  K goes to the matrix cores as it comes; V is
 // turned in LDS.  The next block's loads are issued when the scores have left K's registers.
 // FULL: the head dimension is D, so that a row is read from one address or from zeros as a whole.
+//
+// The work is one stream: request after request, the blocks of kFewKeys keys that its rows see.  Its
+// equal shares go to one workgroup for each key/value head, wherever they begin and end, so requests of
+// any lengths keep all CUs busy to the end; a request whose blocks lie in several shares is joined
+// afterwards.  The workgroups of a share run side by side, and with them the reads of a page's heads, which
+// lie side by side too.  Each workgroup counts the stream itself, 8 bytes a request from the cache.
+constexpr int kFewKeys = 128;
+
+// Blocks of one head of a request; one without keys has a block that writes zeros.
+struct Blocks {
+    Keys keys;
+    int first, n;
+};
+__device__ __forceinline__ Blocks blocks_of(const PagedArgs& a, const Request& r) {
+    Blocks x = {{0, -1}, 0, 0};
+    if (r.rows == 0) return x;
+    x.keys.lo = seen_keys(a, r, 0).lo;
+    x.keys.hi = seen_keys(a, r, (r.rows - 1) / a.group).hi;
+    x.n = 1;
+    if (x.keys.hi >= x.keys.lo) {
+        x.first = x.keys.lo / kFewKeys;
+        x.n = x.keys.hi / kFewKeys - x.first + 1;
+    }
+    return x;
+}
+
+// A value that all lanes hold, as one that the compiler knows to be the same in all of them.
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+    const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(x)), hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(x >> 32));
+    return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
+}
+
+// Sum over the workgroup's threads.
+__device__ __forceinline__ int64_t sum_of_threads(int64_t x, int64_t* mem) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) x += __shfl_xor(x, d, 64);
+    __syncthreads();
+    if (lane == 0) mem[wave] = x;
+    __syncthreads();
+    int64_t all = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) all += mem[w];
+    return uniform(all);
+}
+
+// Blocks of the requests before b, of one head.
+__device__ __forceinline__ int64_t blocks_before(const PagedArgs& a, int64_t b, int64_t* mem) {
+    int64_t x = 0;
+    for (int64_t i = threadIdx.x; i < b; i += kThreads) x += blocks_of(a, request(a, i, 0)).n;
+    return sum_of_threads(x, mem);
+}
+__device__ __forceinline__ int64_t share_of(const PagedArgs& a, int64_t blocks) {
+    const int64_t even = (blocks + a.shares - 1) / a.shares;
+    return even > a.least_share ? even : a.least_share;
+}
+__device__ __forceinline__ int64_t few_part_at(const PagedArgs& a, int D, int64_t part) {
+    return part * a.tile_rows * (D + 2);
+}
+
 template <int D, int NQ, bool FULL>
-__global__ __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) void paged_few_kernel(const PagedArgs a) {
+__global__ __launch_bounds__(kThreads, 2) void paged_few_kernel(const PagedArgs a) {
     constexpr int kKeys = 32, kSteps = D / 32, kTiles = D / 16;
+    static_assert(kKeys * kWaves == kFewKeys, "");
     constexpr int kRegs = NQ * kTiles * 4;  // outputs of a lane
     constexpr int kBytes = kWaves * (kRegs * kWave * 4 > kKeys * D * 2 ? kRegs * kWave * 4 : kKeys * D * 2);
     __shared__ __align__(16) unsigned char lds[kBytes];
     __shared__ float stat[2][kWaves][16 * NQ];
-    const Place at = place_of(a, blockIdx.x);
-    const int tile = at.tile, piece = at.piece;
-    const Request r = request(a, at.b, at.head);
-    const int tile0 = tile * a.tile_rows;
-    if (tile0 >= r.rows) return;
-    const Pieces ps = pieces(a, r, tile0);
-    if (piece < ps.first || piece > ps.last) return;
-
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, quad = lane >> 4;
+    __shared__ int64_t mem[kWaves], s_at[2];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, quad = lane >> 4;
     const int chunks = a.cache.dim / 8;
-    bf16x8 q[NQ][kSteps];
-    Keys mine[NQ];
-    uint16_t* out[NQ];
-#pragma unroll
-    for (int x = 0; x < NQ; ++x) {
-        const int row = tile0 + 16 * x + n, token = row / a.group, head = r.head * a.group + row % a.group;
-        mine[x] = seen_keys(a, r, token);
-        out[x] = row < r.rows ? a.o.p + (r.q0 + token) * a.o.row + head * a.o.head : nullptr;
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            const uint16_t* from = a.q.p + (r.q0 + token) * a.q.row + head * a.q.head + 8 * (4 * s + quad);
-            q[x][s] = __builtin_bit_cast(bf16x8, load_or_zero(from, row < r.rows && 4 * s + quad < chunks));
-        }
-    }
-    // keys that every row of the tile sees
-    const int all_lo = seen_keys(a, r, min(tile0 + a.tile_rows, r.rows) / a.group).lo, all_hi = seen_keys(a, r, tile0 / a.group).hi;
-    const int from = max(ps.keys.lo, piece * a.split_keys);
-    const int end = piece == a.splits - 1 ? ps.keys.hi + 1 : min(ps.keys.hi + 1, (piece + 1) * a.split_keys);
-    const int begin = from / kKeys * kKeys + wave * kKeys;
-    const int32_t* table = a.table + static_cast<int64_t>(r.b) * a.width;
-    // the wave's V block: places do not depend on a multiple of 16 of the row
-    unsigned char* turned = lds + wave * kKeys * D * 2;
-    int put_at[kSteps], col_at[kTiles];
-#pragma unroll
-    for (int e = 0; e < kSteps; ++e) put_at[e] = 16 * Tile<D>::place(n, 4 * e + quad);
-#pragma unroll
-    for (int t = 0; t < kTiles; ++t) {
-        // lane (n, quad): column 16 t + n of rows 4 quad + {0..3} (and of those 16 further)
-        const int row = 4 * quad + (n >> 2), col = 16 * t + 4 * (n & 3);
-        col_at[t] = 16 * Tile<D>::place(row, col >> 3) + 2 * (col & 7);
-    }
 
-    f32x4 o[NQ][kTiles];
-    float m[NQ], l[NQ];
-#pragma unroll
-    for (int x = 0; x < NQ; ++x) {
-        m[x] = -kInf;
-        l[x] = 0.0f;
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t) o[x][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    // the share: `left` blocks from block `block` of request b
+    const int64_t w = blockIdx.x / a.cache.heads;
+    const int head = static_cast<int>((blockIdx.x + w) % a.cache.heads);  // rotated, see place_of
+    int64_t b = 0, left = 0;
+    int block = 0;
+    if (a.shares == 0) {  // one request each
+        b = w;
+        left = blocks_of(a, request(a, b, 0)).n;
+    } else {
+        const int64_t blocks = blocks_before(a, a.batch, mem), share = share_of(a, blocks), start = w * share;
+        left = min(share, blocks - start);
+        if (left > 0) {
+            int64_t before = 0;
+            for (int64_t b0 = 0; b0 < a.batch && before <= start; b0 += kThreads) {
+                const int64_t mine = b0 + tid < a.batch ? blocks_of(a, request(a, b0 + tid, 0)).n : 0;
+                Two total;
+                const int64_t at = before + scan({mine, 0}, &total, reinterpret_cast<int64_t(*)[2]>(lds)).tokens;
+                if (start >= at && start < at + mine) {
+                    s_at[0] = b0 + tid;
+                    s_at[1] = start - at;
+                }
+                before = uniform(before + total.tokens);
+                __syncthreads();
+            }
+            b = uniform(s_at[0]);
+            block = static_cast<int>(uniform(s_at[1]));
+        }
     }
+    bool at_start = true;  // nothing of the share is done
+    // The wave's V block.  A place does not depend on a multiple of 16 of the row, and chunk x ^ y lies at an
+    // exclusive or of 16 y with the place of chunk x: one address each for writing and for reading.
+    unsigned char* turned = lds + wave * kKeys * D * 2;
+    int put_at = 16 * Tile<D>::place(n, quad);  // row n, chunk quad; chunk 4 e + quad is 64 e away
+    // lane (n, quad): column n of rows 4 quad + {0..3} (and of those 16 further); column 16 t + n is 32 t away
+    int col_at = 16 * Tile<D>::place(4 * quad + (n >> 2), (n & 3) >> 1) + 8 * (n & 1);
     const float c = a.scale * kLog2e;
-    u32x4 k[2][kSteps], v[2][kSteps];
-    int page[2];
-    auto find = [&](int j0) {
+    for (; left > 0; ++b, block = 0) {
+        const Request r = request(a, b, head);
+        const Blocks bl = blocks_of(a, r);
+        if (block < bl.n) {
+            const int first = block, count = static_cast<int>(min(static_cast<int64_t>(bl.n - first), left));
+            const bool whole = count == bl.n;
+            const int64_t part_index = 2 * (w * a.cache.heads + head) + (first == 0 && !at_start ? 1 : 0);
+            left -= count;
+            at_start = false;
+            // keys of the unit's blocks that some row sees
+            const int from = (bl.first + first) * kFewKeys, end = min(bl.keys.hi + 1, from + count * kFewKeys);
+            bf16x8 q[NQ][kSteps];
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
-            const int j = j0 + 16 * y + n, entry = table[min(j, r.kv_len - 1) / a.cache.page_size];
-            page[y] = j < r.kv_len && entry < a.cache.n_pages ? entry : -1;
-        }
-    };
-    auto load = [&](int j0) {
+            for (int x = 0; x < NQ; ++x) {
+                const int row = 16 * x + n;
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
-            const int j = j0 + 16 * y + n;
-            const bool live = page[y] >= 0;
-            const int64_t from = page[y] * a.cache.page + (j % a.cache.page_size) * a.cache.row + r.head * a.cache.head + 8 * quad;
-            const uint16_t* kp = live ? a.cache.k + from : kZeros + 8 * quad;
-            const uint16_t* vp = live ? a.cache.v + from : kZeros + 8 * quad;
-#pragma unroll
-            for (int s = 0; s < kSteps; ++s) {
-                k[y][s] = load_or_zero(kp + 32 * s, FULL || 4 * s + quad < chunks);
-                v[y][s] = load_or_zero(vp + 32 * s, FULL || 4 * s + quad < chunks);
+                for (int s = 0; s < kSteps; ++s) {
+                    const uint16_t* from_q = a.q.p + row_at(a, r, a.q, row) + 8 * (4 * s + quad);
+                    q[x][s] = __builtin_bit_cast(bf16x8, load_or_zero(from_q, row < r.rows && 4 * s + quad < chunks));
+                }
             }
-        }
-    };
-    constexpr int step = kKeys * kWaves;
-    if (begin < end) {
-        find(begin);
-        load(begin);
-        find(begin + step);
-    }
-    for (int j0 = begin; j0 < end; j0 += step) {
-        f32x4 s[NQ][2];
+            // keys that every row sees
+            const int all_lo = seen_keys(a, r, (r.rows - 1) / a.group).lo, all_hi = seen_keys(a, r, 0).hi;
+            const int begin = from + wave * kKeys;
+            const int32_t* table = a.table + static_cast<int64_t>(r.b) * a.width;
+
+            f32x4 o[NQ][kTiles];
+            float m[NQ], l[NQ];
 #pragma unroll
-        for (int x = 0; x < NQ; ++x)
+            for (int x = 0; x < NQ; ++x) {
+                m[x] = -kInf;
+                l[x] = 0.0f;
 #pragma unroll
-            for (int y = 0; y < 2; ++y) {
-                s[x][y] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                for (int e = 0; e < kSteps; ++e)
-                    s[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[y][e]), q[x][e], s[x][y], 0, 0, 0);
+                for (int t = 0; t < kTiles; ++t) o[x][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
             }
+            u32x4 k[2][kSteps], v[2][kSteps];
+            int page[2];
+            auto find = [&](int j0) {
 #pragma unroll
-        for (int y = 0; y < 2; ++y)
+                for (int y = 0; y < 2; ++y) {
+                    page[y] = table[min(j0 + 16 * y + n, r.kv_len - 1) / a.cache.page_size];
+                }
+            };
+            auto load = [&](int j0) {
 #pragma unroll
-            for (int e = 0; e < kSteps; ++e)
-                *reinterpret_cast<u32x4*>(turned + put_at[e] + 16 * y * Tile<D>::kRowBytes) = v[y][e];
-        const int next = j0 + step;
-        if (next < end) {
-            load(next);
-            find(next + step);
-        }
-        // the wave's own writes, before its lanes read each other's
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup", "local");
-        __builtin_amdgcn_wave_barrier();
-        const bool masked = j0 < all_lo || j0 + kKeys - 1 > all_hi || j0 + kKeys > end;
+                for (int y = 0; y < 2; ++y) {
+                    const int j = j0 + 16 * y + n;
+                    const bool live = j < r.kv_len && names_page(a, page[y]);
+                    const int64_t at = page[y] * a.cache.page + (j % a.cache.page_size) * a.cache.row + r.head * a.cache.head + 8 * quad;
+                    const uint16_t* kp = live ? a.cache.k + at : kZeros + 8 * quad;
+                    const uint16_t* vp = live ? a.cache.v + at : kZeros + 8 * quad;
 #pragma unroll
-        for (int x = 0; x < NQ; ++x) {
-            if (masked) {
+                    for (int s = 0; s < kSteps; ++s) {
+                        k[y][s] = load_or_zero(kp + 32 * s, FULL || 4 * s + quad < chunks);
+                        v[y][s] = load_or_zero(vp + 32 * s, FULL || 4 * s + quad < chunks);
+                    }
+                }
+            };
+            constexpr int step = kKeys * kWaves;
+            if (begin < end) {
+                find(begin);
+                load(begin);
+                find(begin + step);
+            }
+            for (int j0 = begin; j0 < end; j0 += step) {
+                // kept as one register each, not as one for every e and t
+                asm volatile("" : "+v"(put_at), "+v"(col_at));
+                f32x4 s[NQ][2];
+#pragma unroll
+                for (int x = 0; x < NQ; ++x)
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        s[x][y] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                        for (int e = 0; e < kSteps; ++e)
+                            s[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[y][e]), q[x][e], s[x][y], 0, 0, 0);
+                    }
 #pragma unroll
                 for (int y = 0; y < 2; ++y)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int j = j0 + 16 * y + 4 * quad + i;
-                        s[x][y][i] = j >= mine[x].lo && j <= mine[x].hi && j < end ? s[x][y][i] : -kInf;
+                    for (int e = 0; e < kSteps; ++e)
+                        *reinterpret_cast<u32x4*>(turned + (put_at ^ 64 * e) + 16 * y * Tile<D>::kRowBytes) = v[y][e];
+                const int next = j0 + step;
+                if (next < end) {
+                    load(next);
+                    find(next + step);
+                }
+                // the wave's own writes, before its lanes read each other's
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup", "local");
+                __builtin_amdgcn_wave_barrier();
+                const bool masked = j0 < all_lo || j0 + kKeys - 1 > all_hi || j0 + kKeys > end;
+#pragma unroll
+                for (int x = 0; x < NQ; ++x) {
+                    if (masked) {
+                        const Keys mine = seen_keys(a, r, (16 * x + n) / a.group);
+#pragma unroll
+                        for (int y = 0; y < 2; ++y)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const int j = j0 + 16 * y + 4 * quad + i;
+                                s[x][y][i] = j >= mine.lo && j <= mine.hi && j < end ? s[x][y][i] : -kInf;
+                            }
                     }
+                    float top = s[x][0][0];
+#pragma unroll
+                    for (int y = 0; y < 2; ++y)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) top = fmaxf(top, s[x][y][i]);
+                    top = fmaxf(top, __shfl_xor(top, 16, 64));
+                    top = fmaxf(top, __shfl_xor(top, 32, 64)) * c;
+                    if (__any(top > m[x] + kSlack)) {
+                        const float to = fmaxf(m[x], top);
+                        const float f = to == -kInf ? 1.0f : __builtin_amdgcn_exp2f(m[x] - to);
+                        m[x] = to;
+                        l[x] *= f;
+#pragma unroll
+                        for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) o[x][t][i] *= f;
+                    }
+                    const float ref = m[x] == -kInf ? 0.0f : m[x];
+                    bf16x8 p;
+#pragma unroll
+                    for (int y = 0; y < 2; ++y)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][y][i], c, -ref));
+                            l[x] += e;
+                            p[4 * y + i] = static_cast<__bf16>(e);
+                        }
+#pragma unroll
+                    for (int t = 0; t < kTiles; ++t) {
+                        union {
+                            i16x4 half[2];
+                            bf16x8 all;
+                        } u;
+                        u.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(turned + (col_at ^ 32 * t)));
+                        u.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(turned + (col_at ^ 32 * t) + 16 * Tile<D>::kRowBytes));
+                        o[x][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(u.all, p, o[x][t], 0, 0, 0);
+                    }
+                }
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup", "local");
+                __builtin_amdgcn_wave_barrier();
             }
-            float top = s[x][0][0];
+
+            // join the four waves' rows
+            float* sums = reinterpret_cast<float*>(lds);  // [wave][register][lane]
 #pragma unroll
-            for (int y = 0; y < 2; ++y)
+            for (int x = 0; x < NQ; ++x) {
+                l[x] += __shfl_xor(l[x], 16, 64);
+                l[x] += __shfl_xor(l[x], 32, 64);
+                if (quad == 0) {
+                    stat[0][wave][16 * x + n] = m[x];
+                    stat[1][wave][16 * x + n] = l[x];
+                }
+            }
+            __syncthreads();
+            float top[NQ], total[NQ];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) top = fmaxf(top, s[x][y][i]);
-            top = fmaxf(top, __shfl_xor(top, 16, 64));
-            top = fmaxf(top, __shfl_xor(top, 32, 64)) * c;
-            if (__any(top > m[x] + kSlack)) {
-                const float to = fmaxf(m[x], top);
-                const float f = to == -kInf ? 1.0f : __builtin_amdgcn_exp2f(m[x] - to);
-                m[x] = to;
-                l[x] *= f;
+            for (int x = 0; x < NQ; ++x) {
+                top[x] = -kInf;
+                total[x] = 0.0f;
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w) top[x] = fmaxf(top[x], stat[0][w][16 * x + n]);
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w) {
+                    const float mw = stat[0][w][16 * x + n], lw = stat[1][w][16 * x + n];
+                    total[x] += mw == -kInf ? lw : lw * __builtin_amdgcn_exp2f(mw - top[x]);
+                }
+                const float f = m[x] == -kInf ? 1.0f : __builtin_amdgcn_exp2f(m[x] - top[x]);
 #pragma unroll
                 for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) o[x][t][i] *= f;
+                    for (int i = 0; i < 4; ++i) sums[(wave * kRegs + (x * kTiles + t) * 4 + i) * kWave + lane] = o[x][t][i] * f;
             }
-            const float ref = m[x] == -kInf ? 0.0f : m[x];
-            bf16x8 p;
+            __syncthreads();
+            float* part = whole ? nullptr : a.part + few_part_at(a, D, part_index);
 #pragma unroll
-            for (int y = 0; y < 2; ++y)
+            for (int x = 0; x < NQ; ++x) {
+                if (16 * x + n >= r.rows) continue;
+                uint16_t* out = a.o.p + row_at(a, r, a.o, 16 * x + n);
+                const float inv = total[x] == 0.0f ? 0.0f : 1.0f / total[x];
+                for (int t = wave; t < kTiles; t += kWaves) {
+                    f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][y][i], c, -ref));
-                    l[x] += e;
-                    p[4 * y + i] = static_cast<__bf16>(e);
+                    for (int w = 0; w < kWaves; ++w)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) y[i] += sums[(w * kRegs + (x * kTiles + t) * 4 + i) * kWave + lane];
+                    const int d = 16 * t + 4 * quad;
+                    if (!whole) {
+                        *reinterpret_cast<f32x4*>(part + (16 * x + n) * D + d) = y;
+                    } else if (d < a.cache.dim) {
+                        const bf16x2 lo = {static_cast<__bf16>(y[0] * inv), static_cast<__bf16>(y[1] * inv)};
+                        const bf16x2 hi = {static_cast<__bf16>(y[2] * inv), static_cast<__bf16>(y[3] * inv)};
+                        *reinterpret_cast<u32x2_any*>(out + d) =
+                            u32x2{__builtin_bit_cast(unsigned int, lo), __builtin_bit_cast(unsigned int, hi)};
+                    }
                 }
-#pragma unroll
-            for (int t = 0; t < kTiles; ++t) {
-                union {
-                    i16x4 half[2];
-                    bf16x8 all;
-                } u;
-                u.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(turned + col_at[t]));
-                u.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(turned + col_at[t] + 16 * Tile<D>::kRowBytes));
-                o[x][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(u.all, p, o[x][t], 0, 0, 0);
+                if (!whole && wave == 0 && quad == 0) {
+                    part[a.tile_rows * D + 16 * x + n] = top[x];
+                    part[a.tile_rows * (D + 1) + 16 * x + n] = total[x];
+                }
             }
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup", "local");
-        __builtin_amdgcn_wave_barrier();
-    }
-
-    // join the four waves' rows
-    float* sums = reinterpret_cast<float*>(lds);  // [wave][register][lane]
-#pragma unroll
-    for (int x = 0; x < NQ; ++x) {
-        l[x] += __shfl_xor(l[x], 16, 64);
-        l[x] += __shfl_xor(l[x], 32, 64);
-        if (quad == 0) {
-            stat[0][wave][16 * x + n] = m[x];
-            stat[1][wave][16 * x + n] = l[x];
-        }
-    }
-    __syncthreads();
-    float top[NQ], total[NQ];
-#pragma unroll
-    for (int x = 0; x < NQ; ++x) {
-        top[x] = -kInf;
-        total[x] = 0.0f;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) top[x] = fmaxf(top[x], stat[0][w][16 * x + n]);
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            const float mw = stat[0][w][16 * x + n], lw = stat[1][w][16 * x + n];
-            total[x] += mw == -kInf ? lw : lw * __builtin_amdgcn_exp2f(mw - top[x]);
-        }
-        const float f = m[x] == -kInf ? 1.0f : __builtin_amdgcn_exp2f(m[x] - top[x]);
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sums[(wave * kRegs + (x * kTiles + t) * 4 + i) * kWave + lane] = o[x][t][i] * f;
-    }
-    __syncthreads();
-    const bool whole = ps.first == ps.last;
-    float* part = whole ? nullptr : a.part + part_at(a, D, r, tile, piece);
-#pragma unroll
-    for (int x = 0; x < NQ; ++x) {
-        if (!out[x]) continue;
-        const float inv = total[x] == 0.0f ? 0.0f : 1.0f / total[x];
-        for (int t = wave; t < kTiles; t += kWaves) {
-            f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int w = 0; w < kWaves; ++w)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) y[i] += sums[(w * kRegs + (x * kTiles + t) * 4 + i) * kWave + lane];
-            const int d = 16 * t + 4 * quad;
-            if (!whole) {
-                *reinterpret_cast<f32x4*>(part + (16 * x + n) * D + d) = y;
-            } else if (d < a.cache.dim) {
-                const bf16x2 lo = {static_cast<__bf16>(y[0] * inv), static_cast<__bf16>(y[1] * inv)};
-                const bf16x2 hi = {static_cast<__bf16>(y[2] * inv), static_cast<__bf16>(y[3] * inv)};
-                *reinterpret_cast<u32x2_any*>(out[x] + d) =
-                    u32x2{__builtin_bit_cast(unsigned int, lo), __builtin_bit_cast(unsigned int, hi)};
-            }
-        }
-        if (!whole && wave == 0 && quad == 0) {
-            part[a.tile_rows * D + 16 * x + n] = top[x];
-            part[a.tile_rows * (D + 1) + 16 * x + n] = total[x];
+            __syncthreads();  // the next unit writes where this one's sums were
         }
     }
 }
 
-// Joins the pieces of the rows that more than one piece holds: one wave per row, a lane per piece for
-// the statistics, then a lane per D / 64 columns.
+// Joins n parts of a row, one wave: a lane per part for the statistics, then a lane per D / 64 columns.  part(p)
+// is the p-th part's first float.
+template <int D, class Part>
+__device__ __forceinline__ void join_row(const PagedArgs& a, const Request& r, int row, int i, int n, Part part) {
+    constexpr int kPer = D / 64;
+    const int lane = threadIdx.x & 63;
+    float m = -kInf, total = 0.0f, acc[kPer];
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) acc[e] = 0.0f;
+    for (int p0 = 0; p0 < n; p0 += kWave) {
+        const bool mine = p0 + lane < n;
+        const float* stat = part(mine ? p0 + lane : 0) + a.tile_rows * D + i;
+        const float mp = mine ? stat[0] : -kInf, lp = mine ? stat[a.tile_rows] : 0.0f;
+        float top = fmaxf(m, mp);
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d, 64));
+        const float f = mp == -kInf ? 1.0f : __builtin_amdgcn_exp2f(mp - top);
+        const float old = m == -kInf ? 1.0f : __builtin_amdgcn_exp2f(m - top);
+        float sum = f * lp;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d, 64);
+        total = total * old + sum;
+        m = top;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) acc[e] *= old;
+        const int count = min(n - p0, kWave);
+        for (int p = 0; p < count; ++p) {
+            const float fp = __shfl(f, p, 64);
+            const float* from = part(p0 + p) + i * D + kPer * lane;
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) acc[e] += fp * from[e];
+        }
+    }
+    const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+    const int d = kPer * lane;
+    uint16_t* out = a.o.p + (r.q0 + row / a.group) * a.o.row + (r.head * a.group + row % a.group) * a.o.head + d;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e)
+        if (d + e < a.cache.dim) out[e] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(acc[e] * inv));
+}
+
+// Joins the pieces of the rows that more than one piece holds: a workgroup per tile and head.
 template <int D>
 __global__ __launch_bounds__(kThreads) void paged_join_kernel(const PagedArgs a) {
-    const Place at = place_of(a, blockIdx.x);
-    const int tile = at.tile;
-    const Request r = request(a, at.b, at.head);
-    const int tile0 = tile * a.tile_rows;
+    const int64_t unit = blockIdx.x / a.cache.heads;
+    const Request r = request(a, unit / a.tiles, static_cast<int>(blockIdx.x % a.cache.heads));
+    const int tile = static_cast<int>(unit % a.tiles), tile0 = tile * a.tile_rows;
     if (tile0 >= r.rows) return;
     const Pieces ps = pieces(a, r, tile0);
     if (ps.first == ps.last) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = ps.last - ps.first + 1;
-    constexpr int kPer = D / 64;
+    const float* first = a.part + part_at(a, D, r, tile, ps.first);
     const int64_t piece_floats = static_cast<int64_t>(a.tile_rows) * (D + 2);
-    for (int i = wave; i < a.tile_rows && tile0 + i < r.rows; i += kWaves) {
-        const float* part = a.part + part_at(a, D, r, tile, ps.first);
-        const float* m_at = part + a.tile_rows * D + i;
-        const float* l_at = m_at + a.tile_rows;
-        float m = -kInf, total = 0.0f, acc[kPer];
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) acc[e] = 0.0f;
-        for (int p0 = 0; p0 < n; p0 += kWave) {
-            const bool mine = p0 + lane < n;
-            const float mp = mine ? m_at[(p0 + lane) * piece_floats] : -kInf;
-            const float lp = mine ? l_at[(p0 + lane) * piece_floats] : 0.0f;
-            float top = fmaxf(m, mp);
-#pragma unroll
-            for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d, 64));
-            const float f = mp == -kInf ? 1.0f : __builtin_amdgcn_exp2f(mp - top);
-            const float old = m == -kInf ? 1.0f : __builtin_amdgcn_exp2f(m - top);
-            float sum = f * lp;
-#pragma unroll
-            for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d, 64);
-            total = total * old + sum;
-            m = top;
-#pragma unroll
-            for (int e = 0; e < kPer; ++e) acc[e] *= old;
-            const int count = min(n - p0, kWave);
-            const float* from = part + p0 * piece_floats + i * D + kPer * lane;
-            for (int p = 0; p < count; ++p) {
-                const float fp = __shfl(f, p, 64);
-#pragma unroll
-                for (int e = 0; e < kPer; ++e) acc[e] += fp * from[p * piece_floats + e];
-            }
-        }
-        const float inv = total == 0.0f ? 0.0f : 1.0f / total;
-        const int row = tile0 + i, d = kPer * lane;
-        uint16_t* out = a.o.p + (r.q0 + row / a.group) * a.o.row + (r.head * a.group + row % a.group) * a.o.head + d;
-#pragma unroll
-        for (int e = 0; e < kPer; ++e)
-            if (d + e < a.cache.dim) out[e] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(acc[e] * inv));
-    }
+    for (int i = threadIdx.x >> 6; i < a.tile_rows && tile0 + i < r.rows; i += kWaves)
+        join_row<D>(a, r, tile0 + i, i, ps.last - ps.first + 1, [&](int p) { return first + p * piece_floats; });
+}
+
+// Joins the parts of the requests whose blocks lie in more than one share: a workgroup per request and head.
+template <int D>
+__global__ __launch_bounds__(kThreads) void paged_few_join_kernel(const PagedArgs a) {
+    __shared__ int64_t mem[kWaves];
+    const int64_t b = blockIdx.x / a.cache.heads;
+    const Request r = request(a, b, static_cast<int>(blockIdx.x % a.cache.heads));
+    const Blocks bl = blocks_of(a, r);
+    const int64_t start = blocks_before(a, b, mem), share = share_of(a, blocks_before(a, a.batch, mem));
+    const int64_t w0 = start / share;
+    const int count = static_cast<int>((start + bl.n - 1) / share - w0) + 1;
+    if (bl.n == 0 || count == 1) return;
+    for (int i = threadIdx.x >> 6; i < r.rows; i += kWaves)
+        join_row<D>(a, r, i, i, count, [&](int p) {
+            return a.part + few_part_at(a, D, 2 * ((w0 + p) * a.cache.heads + r.head) + (p == 0 && start % share != 0 ? 1 : 0));
+        });
 }
 
 // -------------------------------------------------------------------------------------- slots
-// Sums of tokens and pages over the requests before a thread's, and the chunk's totals.
-struct Two {
-    int64_t tokens, pages;
-};
-__device__ __forceinline__ Two scan(Two mine, Two* total, int64_t (*mem)[2]) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    Two x = mine;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const int64_t t = __shfl_up(x.tokens, d, 64), p = __shfl_up(x.pages, d, 64);
-        if (lane >= d) {
-            x.tokens += t;
-            x.pages += p;
-        }
-    }
-    if (lane == 63) {
-        mem[wave][0] = x.tokens;
-        mem[wave][1] = x.pages;
-    }
-    __syncthreads();
-    Two before = {0, 0};
-    *total = {0, 0};
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        if (w < wave) {
-            before.tokens += mem[w][0];
-            before.pages += mem[w][1];
-        }
-        total->tokens += mem[w][0];
-        total->pages += mem[w][1];
-    }
-    return {before.tokens + x.tokens - mine.tokens, before.pages + x.pages - mine.pages};
-}
-
 // Every workgroup takes the sums over all requests itself (8 bytes a request, from the cache) and
 // then writes the slots of its share of the tokens, so that one launch does it.  A request's new
 // pages are the next ones of the free list; the token that starts a page writes its table entry.
@@ -658,19 +792,27 @@ __global__ __launch_bounds__(kThreads) void append_kernel(const Cache c, const H
 
 template <int D>
 hipError_t launch_paged(const PagedArgs& a, hipStream_t stream) {
-    const int64_t tiles = a.batch * a.cache.heads * a.tiles;
-    const unsigned grid = static_cast<unsigned>(tiles * a.splits);
-    const bool full = a.cache.dim == D;
-    if (a.tile_rows == 16 && full) paged_few_kernel<D, 1, true><<<grid, kThreads, 0, stream>>>(a);
-    else if (a.tile_rows == 16) paged_few_kernel<D, 1, false><<<grid, kThreads, 0, stream>>>(a);
-    else if (a.tile_rows == 32 && full) paged_few_kernel<D, 2, true><<<grid, kThreads, 0, stream>>>(a);
-    else if (a.tile_rows == 32) paged_few_kernel<D, 2, false><<<grid, kThreads, 0, stream>>>(a);
-    else if (aligned_pieces({a.cache.k, a.cache.page, a.cache.row, a.cache.head}) && reinterpret_cast<uintptr_t>(a.cache.v) % 16 == 0)
+    const int64_t units = a.batch * a.cache.heads;
+    hipError_t e;
+    if (a.tile_rows < kTileRows) {
+        const bool full = a.cache.dim == D;
+        const unsigned grid = static_cast<unsigned>(a.shares > 0 ? a.shares * a.cache.heads : units);
+        if (a.tile_rows == 16 && full) paged_few_kernel<D, 1, true><<<grid, kThreads, 0, stream>>>(a);
+        else if (a.tile_rows == 16) paged_few_kernel<D, 1, false><<<grid, kThreads, 0, stream>>>(a);
+        else if (full) paged_few_kernel<D, 2, true><<<grid, kThreads, 0, stream>>>(a);
+        else paged_few_kernel<D, 2, false><<<grid, kThreads, 0, stream>>>(a);
+        e = hipGetLastError();
+        if (e != hipSuccess || a.shares == 0) return e;
+        paged_few_join_kernel<D><<<static_cast<unsigned>(units), kThreads, 0, stream>>>(a);
+        return hipGetLastError();
+    }
+    const unsigned tiles = static_cast<unsigned>(units * a.tiles), grid = tiles * a.splits;
+    if (aligned_pieces({a.cache.k, a.cache.page, a.cache.row, a.cache.head}) && reinterpret_cast<uintptr_t>(a.cache.v) % 16 == 0)
         paged_kernel<D, true><<<grid, kThreads, 0, stream>>>(a);
     else paged_kernel<D, false><<<grid, kThreads, 0, stream>>>(a);
-    const hipError_t e = hipGetLastError();
+    e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;
-    paged_join_kernel<D><<<static_cast<unsigned>(tiles), kThreads, 0, stream>>>(a);
+    paged_join_kernel<D><<<tiles, kThreads, 0, stream>>>(a);
     return hipGetLastError();
 }
 
