@@ -427,7 +427,7 @@ bsm_status paged(const bsm_cache* cache, const bsm_heads* q, const bsm_heads* o,
     if (e != hipSuccess) return hip_fail(e, "device query");
     bsm_att::PagedCut cut;
     if ((st = paged_cut(batch, tokens, heads_q, cache->heads, cache->head_dim, max_q, max_kv, n_cu, &cut)) != BSM_OK) return st;
-    const int64_t need = 4 * cut.part_floats;
+    const int64_t need = 4 * (cut.few_floats + cut.tile_floats);
     if (workspace_bytes < need || (need > 0 && !workspace))
         return fail(BSM_ERR_INVALID_ARG, "workspace of %lld bytes, %lld needed", static_cast<long long>(workspace_bytes),
                     static_cast<long long>(need));
@@ -448,13 +448,14 @@ bsm_status paged(const bsm_cache* cache, const bsm_heads* q, const bsm_heads* o,
     a.group = heads_q / cache->heads;
     a.window = window;
     a.scale = scale;
-    a.tile_rows = cut.tile_rows;
+    a.few_rows = cut.few_rows;
     a.shares = cut.shares;
     a.least_share = cut.least_share;
     a.tiles = cut.tiles;
     a.splits = cut.splits;
     a.split_keys = cut.split_keys;
-    a.part = static_cast<float*>(workspace);
+    a.few_part = static_cast<float*>(workspace);
+    a.tile_part = a.few_part + cut.few_floats;
     e = bsm_att::launch_attention_paged(a, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "kernel launch");
     return BSM_OK;
@@ -638,7 +639,7 @@ bsm_status bsm_attention_paged_workspace(int64_t batch, int64_t tokens, int32_t 
     if (e != hipSuccess) return hip_fail(e, "device query");
     bsm_att::PagedCut cut;
     if ((st = paged_cut(batch, tokens, heads_q, heads_kv, head_dim, max_q, max_kv, n_cu, &cut)) != BSM_OK) return st;
-    *bytes = 4 * cut.part_floats;
+    *bytes = 4 * (cut.few_floats + cut.tile_floats);
     return BSM_OK;
 }
 

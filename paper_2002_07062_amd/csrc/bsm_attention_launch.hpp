@@ -68,15 +68,13 @@ struct PagedArgs {
     int32_t window;
     float scale;
     // how the work is cut, from bounds on the lengths alone
-    int32_t tile_rows;        // 16 or 32 (all rows of a request and head; the waves take turns at the keys) or 128
-    // 16 or 32: equal shares of the requests' blocks of 128 keys, at least least_share blocks each; 0: one
-    // request each
-    int32_t shares, least_share;
-    // 128:
-    int32_t tiles;            // per request and key/value head
-    int32_t splits;           // pieces of the key axis
-    int32_t split_keys;       // keys of a piece, a multiple of kKeyTile
-    float* part;              // outputs and statistics of what has to be joined
+    // Requests of up to few_rows rows of a key/value head (16 or 32; 0: none) go by shares: equal shares of
+    // their blocks of 128 keys, at least least_share blocks each; shares 0: one request each.
+    int32_t few_rows, shares, least_share;
+    // The others go by tiles of kTileRows rows, `tiles` per request and key/value head (0: there are none),
+    // in `splits` pieces of the key axis of split_keys keys each, a multiple of kKeyTile.
+    int32_t tiles, splits, split_keys;
+    float *few_part, *tile_part;  // outputs and statistics of what has to be joined
 };
 
 constexpr int kKeyTile = 128;

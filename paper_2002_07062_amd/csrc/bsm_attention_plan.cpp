@@ -154,34 +154,39 @@ std::vector<Unit> key_units(const Sequences& s, bsm_schedule schedule, int n_xcd
 PagedCut cut_paged(int64_t batch, int64_t tokens, int32_t heads_kv, int32_t group, int32_t dim, int32_t max_q,
                    int32_t max_kv, int n_cu) {
     PagedCut c{};
-    const int64_t rows = std::min<int64_t>(max_q, tokens) * group;
-    c.tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : kTileRows;
+    const int64_t rows = std::min<int64_t>(max_q, tokens) * group, keys = std::max<int64_t>(1, max_kv);
     const int padded = dim <= 64 ? 64 : 128;
-    const int64_t keys = std::max<int64_t>(1, max_kv);
-    if (c.tile_rows < kTileRows) {
-        c.tiles = c.splits = 1;
+    // Few rows over many keys are bound by reading the cache, many rows by the products: each has a kernel.  A
+    // batch that may hold both launches both (one chunk of 512 tokens over 4096 and 63 single tokens over
+    // 5000, 8 kv heads: 732 us by tiles alone, 370 us by both); where no request is shorter than the
+    // longest chunk, or there is only one, the tiles do.
+    if (rows <= 32) c.few_rows = rows <= 16 ? 16 : 32;
+    else if (batch > 1 && group <= 32 && tokens < batch * max_q) c.few_rows = group <= 16 ? 16 : 32;
+    if (c.few_rows > 0) {
         c.grid = batch * heads_kv;
-        // Up to eight rounds of a workgroup's 128 keys, a join would cost more than it saves.
-        if (keys <= 1024) return c;
-        // Shares for eight rounds of two workgroups on a CU, of 2048 keys at least: CUs do not read equally
-        // fast (one round of equal shares left them idle for 30% of the time), but a workgroup also has to
-        // count the stream and find its first page before it reads any key.
-        c.shares = static_cast<int32_t>(std::max(1, 16 * n_cu / heads_kv));
-        c.least_share = 16;
-        c.grid = std::max(c.grid, static_cast<int64_t>(c.shares) * heads_kv);
-        c.part_floats = 2 * static_cast<int64_t>(c.shares) * heads_kv * c.tile_rows * (padded + 2);
-        return c;
+        if (keys > 1024) {  // up to eight rounds of a workgroup's 128 keys, a join would cost more than it saves
+            // Shares for eight rounds of two workgroups on a CU, of 2048 keys at least: CUs do not read equally
+            // fast (one round of equal shares left them idle for 30% of the time), but a workgroup also has
+            // to count the stream and find its first page before it reads any key.
+            c.shares = static_cast<int32_t>(std::max(1, 16 * n_cu / heads_kv));
+            c.least_share = 16;
+            c.grid = std::max(c.grid, static_cast<int64_t>(c.shares) * heads_kv);
+            c.few_floats = 2 * static_cast<int64_t>(c.shares) * heads_kv * c.few_rows * (padded + 2);
+        }
     }
-    c.tiles = static_cast<int32_t>(std::max<int64_t>(1, (rows + c.tile_rows - 1) / c.tile_rows));
-    // Two workgroups fit a CU.  A piece's rows cost a write and a read of their own, so there are no more
-    // pieces than fill the CUs twice.
-    const int64_t units = std::max<int64_t>(1, batch * heads_kv * c.tiles), slots = 2 * static_cast<int64_t>(n_cu);
-    const int64_t splits = std::max<int64_t>(1, std::min((2 * slots + units - 1) / units, (keys + 255) / 256));
-    const int64_t each = ((keys + splits - 1) / splits + kKeyTile - 1) / kKeyTile * kKeyTile;
-    c.split_keys = static_cast<int32_t>(each);
-    c.splits = static_cast<int32_t>((keys + each - 1) / each);
-    c.part_floats = c.splits > 1 ? units * c.splits * c.tile_rows * (padded + 2) : 0;
-    c.grid = units * c.splits;
+    if (rows > 32) {
+        c.tiles = static_cast<int32_t>((rows + kTileRows - 1) / kTileRows);
+        // Two workgroups fit a CU.  A piece's rows cost a write and a read of their own, so there are no more
+        // pieces than fill the CUs once (8 chunks of 512 tokens over 1k..8k, 8 kv heads, which fill them
+        // twice: 320 us, in two pieces 476 us).
+        const int64_t units = std::max<int64_t>(1, batch * heads_kv * c.tiles), slots = 2 * static_cast<int64_t>(n_cu);
+        const int64_t splits = std::max<int64_t>(1, std::min((slots + units - 1) / units, (keys + 255) / 256));
+        const int64_t each = ((keys + splits - 1) / splits + kKeyTile - 1) / kKeyTile * kKeyTile;
+        c.split_keys = static_cast<int32_t>(each);
+        c.splits = static_cast<int32_t>((keys + each - 1) / each);
+        c.tile_floats = c.splits > 1 ? units * c.splits * kTileRows * (padded + 2) : 0;
+        c.grid = std::max(c.grid, units * std::max(c.splits, 8));  // the join has 8 workgroups for each tile
+    }
     return c;
 }
 

@@ -34,9 +34,9 @@ std::vector<Unit> key_units(const Sequences& s, bsm_schedule schedule, int n_xcd
 
 // How attention over a paged cache is cut.
 struct PagedCut {
-    int32_t tile_rows, shares, least_share, tiles, splits, split_keys;
-    int64_t part_floats;
-    int64_t grid;  // workgroups of the largest launch
+    int32_t few_rows, shares, least_share, tiles, splits, split_keys;  // as in PagedArgs
+    int64_t few_floats, tile_floats;                                   // of the parts
+    int64_t grid;                                                      // workgroups of the largest launch
 };
 PagedCut cut_paged(int64_t batch, int64_t tokens, int32_t heads_kv, int32_t group, int32_t dim, int32_t max_q,
                    int32_t max_kv, int n_cu);

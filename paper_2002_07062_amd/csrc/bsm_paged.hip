@@ -49,9 +49,10 @@ struct Request {
     int b, head;       // request, key/value head
     int64_t q0;        // its first row in q and o
     int q_len, kv_len;
-    int rows;          // q_len (at most max_q) * group
+    int rows;          // q_len (at most max_q) * group; 0 where the other kernel takes the request
 };
 
+template <bool FEW>
 __device__ __forceinline__ Request request(const PagedArgs& a, int64_t b, int head) {
     Request r;
     r.b = static_cast<int>(b);
@@ -64,6 +65,7 @@ __device__ __forceinline__ Request request(const PagedArgs& a, int64_t b, int he
     const int kv = a.kv_len[r.b];
     r.kv_len = kv < 0 ? 0 : kv < most ? kv : static_cast<int>(most);
     r.rows = min(r.q_len, a.max_q) * a.group;
+    if (FEW != (r.rows <= a.few_rows)) r.rows = 0;
     return r;
 }
 
@@ -84,7 +86,7 @@ struct Pieces {
     int first, last;
 };
 __device__ __forceinline__ Pieces pieces(const PagedArgs& a, const Request& r, int r0) {
-    const int r1 = min(r0 + a.tile_rows, r.rows) - 1;
+    const int r1 = min(r0 + kTileRows, r.rows) - 1;
     Pieces p;
     p.keys.lo = seen_keys(a, r, r0 / a.group).lo;
     p.keys.hi = seen_keys(a, r, r1 / a.group).hi;
@@ -104,7 +106,7 @@ __device__ __forceinline__ int64_t row_at(const PagedArgs& a, const Request& r, 
 
 // Floats of one piece's part: its rows' outputs, then their references and sums.
 __device__ __forceinline__ int64_t part_at(const PagedArgs& a, int D, const Request& r, int tile, int piece) {
-    return (((static_cast<int64_t>(r.b) * a.cache.heads + r.head) * a.tiles + tile) * a.splits + piece) * a.tile_rows * (D + 2);
+    return (((static_cast<int64_t>(r.b) * a.cache.heads + r.head) * a.tiles + tile) * a.splits + piece) * kTileRows * (D + 2);
 }
 
 // What workgroup w does.  The requests follow each other, the one with the most keys first (with more
@@ -125,17 +127,21 @@ __device__ __forceinline__ Place place_of(const PagedArgs& a, int64_t w, int* me
     p.head = static_cast<int>((w + p.b) % a.cache.heads);
     if (a.batch <= kThreads) {
         const int i = threadIdx.x, n = static_cast<int>(a.batch);
+        int mine = -1;
         if (i < n) {
-            const int mine = a.kv_len[i];
-            int rank = 0;
-            for (int j = 0; j < n; ++j) {
-                const int other = a.kv_len[j];
-                rank += other > mine || (other == mine && j < i) ? 1 : 0;
-            }
-            if (rank == p.b) *mem = i;
+            const Request r = request<false>(a, i, 0);
+            mine = r.rows > 0 ? r.kv_len : -1;
+            mem[1 + i] = mine;
         }
         __syncthreads();
-        p.b = __builtin_amdgcn_readfirstlane(*mem);
+        if (i < n) {
+            int rank = 0;
+            for (int j = 0; j < n; ++j) rank += mem[1 + j] > mine || (mem[1 + j] == mine && j < i) ? 1 : 0;
+            if (rank == p.b) mem[0] = i;
+        }
+        __syncthreads();
+        p.b = __builtin_amdgcn_readfirstlane(mem[0]);
+        __syncthreads();
     }
     return p;
 }
@@ -176,17 +182,13 @@ struct PagedStage {
 template <int D, bool DIRECT>
 __global__ __launch_bounds__(kThreads, 2) void paged_kernel(const PagedArgs a) {
     constexpr int kKeys = 64, kTileElems = kKeys * D;
-    // One array: of several, the compiler forgets which tiles a step reads and writes, and waits for the
-    // loads on their way before every read of LDS.
-    struct Shared {
-        uint16_t tile[2][2][kTileElems];  // buffer, K or V
-        int place;
-    };
-    __shared__ __align__(16) Shared lds;
-    const Place at = place_of(a, blockIdx.x, &lds.place);
+    // (One array: of several, the compiler forgets which tiles a step reads and writes, and waits for the
+    // loads on their way before every read of LDS.)
+    __shared__ __align__(16) uint16_t lds[2][2][kTileElems];  // buffer, K or V
+    const Place at = place_of(a, blockIdx.x, reinterpret_cast<int*>(lds));
     const int tile = at.tile, piece = at.piece;
-    const Request r = request(a, at.b, at.head);
-    const int tile0 = tile * a.tile_rows;
+    const Request r = request<false>(a, at.b, at.head);
+    const int tile0 = tile * kTileRows;
     if (tile0 >= r.rows) return;
     const Pieces ps = pieces(a, r, tile0);
     if (piece < ps.first || piece > ps.last) return;
@@ -214,9 +216,9 @@ __global__ __launch_bounds__(kThreads, 2) void paged_kernel(const PagedArgs a) {
     PagedStage<D, kKeys, kThreads, DIRECT> stage;
     if (begin < end) {
         stage.find(a, table, tid, begin, r.kv_len);
-        stage.begin(a, r.head, tid, begin, r.kv_len, chunks, lds.tile[0][0], lds.tile[0][1]);
+        stage.begin(a, r.head, tid, begin, r.kv_len, chunks, lds[0][0], lds[0][1]);
         stage.find(a, table, tid, begin + kKeys, r.kv_len);
-        stage.end(tid, lds.tile[0][0], lds.tile[0][1]);
+        stage.end(tid, lds[0][0], lds[0][1]);
     }
     const RowFrags<D> rows_at(lane);
     const ColFrags<D> cols_at(lane);
@@ -243,13 +245,13 @@ __global__ __launch_bounds__(kThreads, 2) void paged_kernel(const PagedArgs a) {
         }
         if (next < end) stage.end(tid, next_k, next_v);
     };
-    in_turn(begin, end, kKeys, [&](int j0, auto buf) { step(j0, lds.tile[1 - buf][0], lds.tile[1 - buf][1], lds.tile[buf][0], lds.tile[buf][1]); });
+    in_turn(begin, end, kKeys, [&](int j0, auto buf) { step(j0, lds[1 - buf][0], lds[1 - buf][1], lds[buf][0], lds[buf][1]); });
     const float total = st.row_sum();
     if (ps.first == ps.last) {
         uint16_t* out = a.o.p + q_row * a.o.row + q_head * a.o.head;
         store_row<D>(out, live, st.o, total == 0.0f ? 0.0f : 1.0f / total, h, chunks);
     } else if (live) {
-        float* part = a.part + part_at(a, D, r, tile, piece);
+        float* part = a.tile_part + part_at(a, D, r, tile, piece);
         float* to = part + (row - tile0) * D + 4 * h;
 #pragma unroll
         for (int t = 0; t < D / 32; ++t)
@@ -258,8 +260,8 @@ __global__ __launch_bounds__(kThreads, 2) void paged_kernel(const PagedArgs a) {
                 *reinterpret_cast<f32x4*>(to + 32 * t + 8 * g) =
                     f32x4{st.o[t][4 * g], st.o[t][4 * g + 1], st.o[t][4 * g + 2], st.o[t][4 * g + 3]};
         if (h == 0) {
-            part[a.tile_rows * D + row - tile0] = st.m;
-            part[a.tile_rows * (D + 1) + row - tile0] = total;
+            part[kTileRows * D + row - tile0] = st.m;
+            part[kTileRows * (D + 1) + row - tile0] = total;
         }
     }
 }
@@ -322,7 +324,7 @@ __device__ __forceinline__ int64_t sum_of_threads(int64_t x, int64_t* mem) {
 // Blocks of the requests before b, of one head.
 __device__ __forceinline__ int64_t blocks_before(const PagedArgs& a, int64_t b, int64_t* mem) {
     int64_t x = 0;
-    for (int64_t i = threadIdx.x; i < b; i += kThreads) x += blocks_of(a, request(a, i, 0)).n;
+    for (int64_t i = threadIdx.x; i < b; i += kThreads) x += blocks_of(a, request<true>(a, i, 0)).n;
     return sum_of_threads(x, mem);
 }
 __device__ __forceinline__ int64_t share_of(const PagedArgs& a, int64_t blocks) {
@@ -330,7 +332,7 @@ __device__ __forceinline__ int64_t share_of(const PagedArgs& a, int64_t blocks) 
     return even > a.least_share ? even : a.least_share;
 }
 __device__ __forceinline__ int64_t few_part_at(const PagedArgs& a, int D, int64_t part) {
-    return part * a.tile_rows * (D + 2);
+    return part * a.few_rows * (D + 2);
 }
 
 template <int D, int NQ, bool FULL>
@@ -352,14 +354,14 @@ __global__ __launch_bounds__(kThreads, 2) void paged_few_kernel(const PagedArgs 
     int block = 0;
     if (a.shares == 0) {  // one request each
         b = w;
-        left = blocks_of(a, request(a, b, 0)).n;
+        left = blocks_of(a, request<true>(a, b, 0)).n;
     } else {
         const int64_t blocks = blocks_before(a, a.batch, mem), share = share_of(a, blocks), start = w * share;
         left = min(share, blocks - start);
         if (left > 0) {
             int64_t before = 0;
             for (int64_t b0 = 0; b0 < a.batch && before <= start; b0 += kThreads) {
-                const int64_t mine = b0 + tid < a.batch ? blocks_of(a, request(a, b0 + tid, 0)).n : 0;
+                const int64_t mine = b0 + tid < a.batch ? blocks_of(a, request<true>(a, b0 + tid, 0)).n : 0;
                 Two total;
                 const int64_t at = before + scan({mine, 0}, &total, reinterpret_cast<int64_t(*)[2]>(lds)).tokens;
                 if (start >= at && start < at + mine) {
@@ -382,7 +384,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_few_kernel(const PagedArgs 
     int col_at = 16 * Tile<D>::place(4 * quad + (n >> 2), (n & 3) >> 1) + 8 * (n & 1);
     const float c = a.scale * kLog2e;
     for (; left > 0; ++b, block = 0) {
-        const Request r = request(a, b, head);
+        const Request r = request<true>(a, b, head);
         const Blocks bl = blocks_of(a, r);
         if (block < bl.n) {
             const int first = block, count = static_cast<int>(min(static_cast<int64_t>(bl.n - first), left));
@@ -557,7 +559,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_few_kernel(const PagedArgs 
                     for (int i = 0; i < 4; ++i) sums[(wave * kRegs + (x * kTiles + t) * 4 + i) * kWave + lane] = o[x][t][i] * f;
             }
             __syncthreads();
-            float* part = whole ? nullptr : a.part + few_part_at(a, D, part_index);
+            float* part = whole ? nullptr : a.few_part + few_part_at(a, D, part_index);
 #pragma unroll
             for (int x = 0; x < NQ; ++x) {
                 if (16 * x + n >= r.rows) continue;
@@ -580,8 +582,8 @@ __global__ __launch_bounds__(kThreads, 2) void paged_few_kernel(const PagedArgs 
                     }
                 }
                 if (!whole && wave == 0 && quad == 0) {
-                    part[a.tile_rows * D + 16 * x + n] = top[x];
-                    part[a.tile_rows * (D + 1) + 16 * x + n] = total[x];
+                    part[a.few_rows * D + 16 * x + n] = top[x];
+                    part[a.few_rows * (D + 1) + 16 * x + n] = total[x];
                 }
             }
             __syncthreads();  // the next unit writes where this one's sums were
@@ -589,10 +591,10 @@ __global__ __launch_bounds__(kThreads, 2) void paged_few_kernel(const PagedArgs 
     }
 }
 
-// Joins n parts of a row, one wave: a lane per part for the statistics, then a lane per D / 64 columns.  part(p)
-// is the p-th part's first float.
+// Joins n parts of a row, row i of the `rows` that a part holds, one wave: a lane per part for the statistics,
+// then a lane per D / 64 columns.  part(p) is the p-th part's first float.
 template <int D, class Part>
-__device__ __forceinline__ void join_row(const PagedArgs& a, const Request& r, int row, int i, int n, Part part) {
+__device__ __forceinline__ void join_row(const PagedArgs& a, const Request& r, int rows, int row, int i, int n, Part part) {
     constexpr int kPer = D / 64;
     const int lane = threadIdx.x & 63;
     float m = -kInf, total = 0.0f, acc[kPer];
@@ -600,8 +602,8 @@ __device__ __forceinline__ void join_row(const PagedArgs& a, const Request& r, i
     for (int e = 0; e < kPer; ++e) acc[e] = 0.0f;
     for (int p0 = 0; p0 < n; p0 += kWave) {
         const bool mine = p0 + lane < n;
-        const float* stat = part(mine ? p0 + lane : 0) + a.tile_rows * D + i;
-        const float mp = mine ? stat[0] : -kInf, lp = mine ? stat[a.tile_rows] : 0.0f;
+        const float* stat = part(mine ? p0 + lane : 0) + rows * D + i;
+        const float mp = mine ? stat[0] : -kInf, lp = mine ? stat[rows] : 0.0f;
         float top = fmaxf(m, mp);
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d, 64));
@@ -630,19 +632,20 @@ __device__ __forceinline__ void join_row(const PagedArgs& a, const Request& r, i
         if (d + e < a.cache.dim) out[e] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(acc[e] * inv));
 }
 
-// Joins the pieces of the rows that more than one piece holds: a workgroup per tile and head.
+// Joins the pieces of the rows that more than one piece holds: a workgroup per 16 rows of a tile.
+constexpr int kJoinRows = 16;
 template <int D>
 __global__ __launch_bounds__(kThreads) void paged_join_kernel(const PagedArgs a) {
-    const int64_t unit = blockIdx.x / a.cache.heads;
-    const Request r = request(a, unit / a.tiles, static_cast<int>(blockIdx.x % a.cache.heads));
-    const int tile = static_cast<int>(unit % a.tiles), tile0 = tile * a.tile_rows;
-    if (tile0 >= r.rows) return;
+    const int64_t groups = kTileRows / kJoinRows, unit = blockIdx.x / groups / a.cache.heads;
+    const Request r = request<false>(a, unit / a.tiles, static_cast<int>(blockIdx.x / groups % a.cache.heads));
+    const int tile = static_cast<int>(unit % a.tiles), tile0 = tile * kTileRows, i0 = static_cast<int>(blockIdx.x % groups) * kJoinRows;
+    if (tile0 + i0 >= r.rows) return;
     const Pieces ps = pieces(a, r, tile0);
     if (ps.first == ps.last) return;
-    const float* first = a.part + part_at(a, D, r, tile, ps.first);
-    const int64_t piece_floats = static_cast<int64_t>(a.tile_rows) * (D + 2);
-    for (int i = threadIdx.x >> 6; i < a.tile_rows && tile0 + i < r.rows; i += kWaves)
-        join_row<D>(a, r, tile0 + i, i, ps.last - ps.first + 1, [&](int p) { return first + p * piece_floats; });
+    const float* first = a.tile_part + part_at(a, D, r, tile, ps.first);
+    const int64_t piece_floats = static_cast<int64_t>(kTileRows) * (D + 2);
+    for (int i = i0 + (threadIdx.x >> 6); i < i0 + kJoinRows && tile0 + i < r.rows; i += kWaves)
+        join_row<D>(a, r, kTileRows, tile0 + i, i, ps.last - ps.first + 1, [&](int p) { return first + p * piece_floats; });
 }
 
 // Joins the parts of the requests whose blocks lie in more than one share: a workgroup per request and head.
@@ -650,15 +653,15 @@ template <int D>
 __global__ __launch_bounds__(kThreads) void paged_few_join_kernel(const PagedArgs a) {
     __shared__ int64_t mem[kWaves];
     const int64_t b = blockIdx.x / a.cache.heads;
-    const Request r = request(a, b, static_cast<int>(blockIdx.x % a.cache.heads));
+    const Request r = request<true>(a, b, static_cast<int>(blockIdx.x % a.cache.heads));
     const Blocks bl = blocks_of(a, r);
     const int64_t start = blocks_before(a, b, mem), share = share_of(a, blocks_before(a, a.batch, mem));
     const int64_t w0 = start / share;
     const int count = static_cast<int>((start + bl.n - 1) / share - w0) + 1;
     if (bl.n == 0 || count == 1) return;
     for (int i = threadIdx.x >> 6; i < r.rows; i += kWaves)
-        join_row<D>(a, r, i, i, count, [&](int p) {
-            return a.part + few_part_at(a, D, 2 * ((w0 + p) * a.cache.heads + r.head) + (p == 0 && start % share != 0 ? 1 : 0));
+        join_row<D>(a, r, a.few_rows, i, i, count, [&](int p) {
+            return a.few_part + few_part_at(a, D, 2 * ((w0 + p) * a.cache.heads + r.head) + (p == 0 && start % share != 0 ? 1 : 0));
         });
 }
 
@@ -793,27 +796,32 @@ __global__ __launch_bounds__(kThreads) void append_kernel(const Cache c, const H
 template <int D>
 hipError_t launch_paged(const PagedArgs& a, hipStream_t stream) {
     const int64_t units = a.batch * a.cache.heads;
-    hipError_t e;
-    if (a.tile_rows < kTileRows) {
+    hipError_t e = hipSuccess;
+    if (a.tiles > 0) {
+        const unsigned tiles = static_cast<unsigned>(units * a.tiles), grid = tiles * a.splits;
+        if (aligned_pieces({a.cache.k, a.cache.page, a.cache.row, a.cache.head}) && reinterpret_cast<uintptr_t>(a.cache.v) % 16 == 0)
+            paged_kernel<D, true><<<grid, kThreads, 0, stream>>>(a);
+        else paged_kernel<D, false><<<grid, kThreads, 0, stream>>>(a);
+        e = hipGetLastError();
+        if (e == hipSuccess && a.splits > 1) {
+            paged_join_kernel<D><<<tiles * (kTileRows / kJoinRows), kThreads, 0, stream>>>(a);
+            e = hipGetLastError();
+        }
+    }
+    if (e == hipSuccess && a.few_rows > 0) {
         const bool full = a.cache.dim == D;
-        const unsigned grid = static_cast<unsigned>(a.shares > 0 ? a.shares * a.cache.heads : units);
-        if (a.tile_rows == 16 && full) paged_few_kernel<D, 1, true><<<grid, kThreads, 0, stream>>>(a);
-        else if (a.tile_rows == 16) paged_few_kernel<D, 1, false><<<grid, kThreads, 0, stream>>>(a);
+        const unsigned grid = static_cast<unsigned>(a.shares > 0 ? static_cast<int64_t>(a.shares) * a.cache.heads : units);
+        if (a.few_rows == 16 && full) paged_few_kernel<D, 1, true><<<grid, kThreads, 0, stream>>>(a);
+        else if (a.few_rows == 16) paged_few_kernel<D, 1, false><<<grid, kThreads, 0, stream>>>(a);
         else if (full) paged_few_kernel<D, 2, true><<<grid, kThreads, 0, stream>>>(a);
         else paged_few_kernel<D, 2, false><<<grid, kThreads, 0, stream>>>(a);
         e = hipGetLastError();
-        if (e != hipSuccess || a.shares == 0) return e;
-        paged_few_join_kernel<D><<<static_cast<unsigned>(units), kThreads, 0, stream>>>(a);
-        return hipGetLastError();
+        if (e == hipSuccess && a.shares > 0) {
+            paged_few_join_kernel<D><<<static_cast<unsigned>(units), kThreads, 0, stream>>>(a);
+            e = hipGetLastError();
+        }
     }
-    const unsigned tiles = static_cast<unsigned>(units * a.tiles), grid = tiles * a.splits;
-    if (aligned_pieces({a.cache.k, a.cache.page, a.cache.row, a.cache.head}) && reinterpret_cast<uintptr_t>(a.cache.v) % 16 == 0)
-        paged_kernel<D, true><<<grid, kThreads, 0, stream>>>(a);
-    else paged_kernel<D, false><<<grid, kThreads, 0, stream>>>(a);
-    e = hipGetLastError();
-    if (e != hipSuccess || a.splits == 1) return e;
-    paged_join_kernel<D><<<tiles, kThreads, 0, stream>>>(a);
-    return hipGetLastError();
+    return e;
 }
 
 }  // namespace

@@ -114,6 +114,26 @@ def test_paged_attention_matches_the_oracle(case):
         assert torch.isnan(o[tokens:]).all(), "rows behind the last request were written"
 
 
+@pytest.mark.parametrize("chunk,window", [(1, 0), (1, 700), (45, 0)])
+def test_paged_attention_of_hundreds_of_requests(chunk, window):
+    """More requests than a workgroup has threads, most of them short, some long, some without new
+    tokens, one with a chunk of its own."""
+    rng = np.random.default_rng(chunk)
+    new = rng.integers(0, 3, 300).tolist()
+    kv_len = [int(rng.integers(n, 40)) for n in new]
+    for b in (0, 17, 255, 256, 299):
+        kv_len[b] = int(rng.integers(1100, 2300))
+    new[256], new[299] = chunk, 1
+    cache = Cache(kv_len, 16, 1, 64, 5)
+    g = torch.Generator().manual_seed(6)
+    q = (2 * torch.randn((sum(new), 2, 64), generator=g)).to(torch.bfloat16).cuda()
+    o = torch.full_like(q, NAN)
+    bsm.bsm_attention_paged(q, cache.k, cache.v, cache.table, i32([0] + list(np.cumsum(new))), i32(kv_len), o,
+                            max_q=max(new), max_kv=max(kv_len), window=window)
+    torch.cuda.synchronize()
+    _check(o, q, cache, new, kv_len, 2, 0.125, window)
+
+
 def test_bounds_keep_bad_lengths_and_pages_inside():
     """Entries that name no page read as zeros, lengths past the table count up to it, starts past
     the tokens are clamped, rows past max_q are left alone."""
