@@ -202,28 +202,35 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(const Sequenc
 // dv_j = sum_i P_ij do_i and dk_j = scale * sum_i dS_ij q_i over the rows of all query heads that
 // share the key/value head: k, v and both sums stay in registers, the query rows stream through LDS, 64
 // at a time.  No sum crosses a workgroup, so the result does not depend on timing.
-// Two waves share 32 keys: wave x of the pair forms P and dS for the 32 query rows of block x, the pair
-// exchanges them through LDS as operands, and each adds up half of the head dimension over both blocks.
-// That keeps a wave's sums at 64 registers, so that two waves fit a SIMD and one's exponentials run beside
-// the other's products (a wave that held whole sums took 400 registers and ran alone: 735 us against
-// 567 us on six ragged causal sequences of 700 .. 4001 tokens, 32 / 8 heads of 128).
-constexpr int kPairThreads = 512;
+// D = 64: a wave keeps 32 keys.  D = 128: two waves share 32 keys (kPair): wave x of the pair forms P and
+// dS for the 32 query rows of block x, the pair exchanges them through LDS as operands, and each adds up
+// half of the head dimension over both blocks.  That keeps a wave's sums at 64 registers, so that two
+// waves fit a SIMD and one's exponentials run beside the other's products (a wave that held whole sums
+// took 400 registers and ran alone: 735 us against 500 us on six ragged causal sequences of 700 .. 4001
+// tokens, 32 / 8 heads of 128).
+template <int D>
+struct Dkv {
+    static constexpr bool kPair = D == 128;
+    static constexpr int kThreads = kPair ? 512 : 256;
+    static constexpr int kTiles = kPair ? D / 64 : D / 32;  // blocks of 32 columns that a wave adds up
+};
 
 template <int D, bool DIRECT>
-__global__ __launch_bounds__(kPairThreads, 2) void attention_dkv_kernel(const SequenceArgs a, const Unit* __restrict__ units) {
-    constexpr int kTiles = D / 64;  // blocks of 32 columns of a wave
-    // One array: of several, the compiler forgets which tiles a step reads and writes, and waits for the
-    // loads on their way before every read of LDS.
+__global__ __launch_bounds__(Dkv<D>::kThreads, 2) void attention_dkv_kernel(const SequenceArgs a, const Unit* __restrict__ units) {
+    constexpr bool kPair = Dkv<D>::kPair;
+    constexpr int kTiles = Dkv<D>::kTiles, kBlocks = kKeys / 32;
+    // (One array: of several, the compiler forgets which tiles a step reads and writes, and waits for the
+    // loads on their way before every read of LDS.)
     struct Shared {
-        uint16_t tile[2][2][kKeys * D];    // buffer, q or dout
-        float stat[2][2 * kKeys];          // buffer; references, then deltas
-        bf16x8 exchange[4][2][4][kWave];   // pair, block; P and dS of 16 rows
+        uint16_t tile[2][2][kKeys * D];                             // buffer, q or dout
+        float stat[2][2 * kKeys];                                   // buffer; references, then deltas
+        bf16x8 exchange[kPair ? 4 : 1][kBlocks][4][kPair ? kWave : 1];  // pair, block; P and dS of 16 rows
     };
     __shared__ __align__(16) Shared lds;
     const Unit u = units[blockIdx.x];
     if (u.rows <= 0) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), li = lane & 31, h = lane >> 5;
-    const int pair = wave >> 1, x = wave & 1;
+    const int pair = kPair ? wave >> 1 : wave, x = kPair ? wave & 1 : 0;
     const int chunks = a.dim / 8;
     const int j0 = u.first + kRows * pair, j = j0 + li;
     const bool live = j < u.first + u.rows;
@@ -248,7 +255,7 @@ __global__ __launch_bounds__(kPairThreads, 2) void attention_dkv_kernel(const Se
     const int64_t total = static_cast<int64_t>(steps) * a.group;
     const bool any_row = j0 <= last;
 
-    Stage<D, kKeys, kPairThreads, DIRECT> sq, sd;
+    Stage<D, kKeys, Dkv<D>::kThreads, DIRECT> sq, sd;
     float lse = 0.0f, delta = 0.0f;  // of row `tid` % kKeys of the step to come
     int rows_left = 0;
     sq.init(tid, a.q.row, chunks);
@@ -279,11 +286,42 @@ __global__ __launch_bounds__(kPairThreads, 2) void attention_dkv_kernel(const Se
     constexpr int kBlockBytes = 32 * Tile<D>::kRowBytes;
     const RowFrags<D> rows_at(lane, x * kBlockBytes);
     const ColFrags<D, kTiles> mine_at(lane, x * kTiles, x * kBlockBytes), other_at(lane, x * kTiles, (1 - x) * kBlockBytes);
-    // whether the mask hides every pair of query rows p0 .. p1 (as positions) and the pair's keys
-    auto none = [&](int p0, int p1) {
+    // whether the mask hides every pair of the step's query rows i0 .. i0 + 31 and the wave's keys
+    auto none = [&](int i0) __attribute__((always_inline)) {
+        const int p0 = i0 + off, p1 = min(i0 + 32, end) - 1 + off;  // positions
         if (!any_row || p1 < p0) return true;
         if (!a.mask.causal) return false;
         return p1 < j0 || (a.mask.window > 0 && static_cast<int64_t>(p0) - a.mask.window >= j0 + kRows - 1);
+    };
+    // P and dS of query rows i0 .. i0 + 31, rows `first` .. of the tiles at rows_at
+    auto block = [&](int i0, int first, int first_stat, const uint16_t* now_q, const uint16_t* now_d, const float* now_stat, bf16x8 (&po)[2],
+                     bf16x8 (&so)[2]) __attribute__((always_inline)) {
+        f32x16 p[1], ds[1];
+        row_product<D>(p, rows_at, now_q, first, k);
+        row_product<D>(ds, rows_at, now_d, first, v);
+#pragma unroll
+        for (int e4 = 0; e4 < 4; ++e4) {
+            const f32x4 rr = *reinterpret_cast<const f32x4*>(now_stat + first_stat + 8 * e4 + 4 * h);
+            const f32x4 dd = *reinterpret_cast<const f32x4*>(now_stat + kKeys + first_stat + 8 * e4 + 4 * h);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int y = 4 * e4 + e;
+                p[0][y] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[0][y], c, -rr[e]));
+                ds[0][y] = p[0][y] * (ds[0][y] - dd[e]);
+            }
+        }
+        const int p0 = i0 + off, p1 = min(i0 + 32, end) - 1 + off;
+        if (a.mask.causal && (p0 < j0 + kRows - 1 || (a.mask.window > 0 && static_cast<int64_t>(p1) - a.mask.window >= j0))) {
+#pragma unroll
+            for (int y = 0; y < 16; ++y) {
+                const Seen s = seen_keys(i0 + 4 * h + reg_row(y), u.q_len, u.kv_len, a.mask);
+                const bool sees = j >= s.lo && j <= s.hi;
+                p[0][y] = sees ? p[0][y] : 0.0f;
+                ds[0][y] = sees ? ds[0][y] : 0.0f;
+            }
+        }
+        to_operands(po, p);
+        to_operands(so, ds);
     };
     auto step = [&](int64_t n, uint16_t* __restrict__ next_q, uint16_t* __restrict__ next_d, float* __restrict__ next_stat,
                     const uint16_t* __restrict__ now_q, const uint16_t* __restrict__ now_d, const float* __restrict__ now_stat)
@@ -300,56 +338,39 @@ __global__ __launch_bounds__(kPairThreads, 2) void attention_dkv_kernel(const Se
             sd.begin(tid, next_d, at(a.dout, u, u.q_start + next_r0, head), a.dout.row, dead - next_r0, end - next_r0, chunks);
             fetch_stat(next_g, next_r0);
         }
-        const int b0 = r0 + 32 * x + off, b1 = min(r0 + 32 * x + 32, end) - 1 + off;              // positions of the wave's block
-        const int c0 = r0 + 32 * (1 - x) + off, c1 = min(r0 + 32 * (1 - x) + 32, end) - 1 + off;  // and of the other's
-        const bool mine = !none(b0, b1), other = !none(c0, c1);
         bf16x8 po[2], so[2];
-        if (mine) {
-            f32x16 p[1], ds[1];
-            row_product<D>(p, rows_at, now_q, 0, k);
-            row_product<D>(ds, rows_at, now_d, 0, v);
-            const bool masked = a.mask.causal && (b0 < j0 + kRows - 1 || (a.mask.window > 0 && static_cast<int64_t>(b1) - a.mask.window >= j0));
+        if constexpr (kPair) {
+            const bool mine = !none(r0 + 32 * x), other = !none(r0 + 32 * (1 - x));
+            if (mine) {
+                block(r0 + 32 * x, 0, 32 * x, now_q, now_d, now_stat, po, so);
 #pragma unroll
-            for (int e4 = 0; e4 < 4; ++e4) {
-                const f32x4 rr = *reinterpret_cast<const f32x4*>(now_stat + 32 * x + 8 * e4 + 4 * h);
-                const f32x4 dd = *reinterpret_cast<const f32x4*>(now_stat + kKeys + 32 * x + 8 * e4 + 4 * h);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int y = 4 * e4 + e;
-                    p[0][y] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[0][y], c, -rr[e]));
-                    ds[0][y] = p[0][y] * (ds[0][y] - dd[e]);
+                for (int s = 0; s < 2; ++s) {
+                    lds.exchange[pair][x][s][lane] = po[s];
+                    lds.exchange[pair][x][2 + s][lane] = so[s];
                 }
             }
-            if (masked) {
+            lds_barrier();
+            if (mine) {
+                col_product(dv, mine_at, now_d, 0, po);
+                col_product(dk, mine_at, now_q, 0, so);
+            }
+            if (other) {
 #pragma unroll
-                for (int y = 0; y < 16; ++y) {
-                    const Seen s = seen_keys(r0 + 32 * x + 4 * h + reg_row(y), u.q_len, u.kv_len, a.mask);
-                    const bool sees = j >= s.lo && j <= s.hi;
-                    p[0][y] = sees ? p[0][y] : 0.0f;
-                    ds[0][y] = sees ? ds[0][y] : 0.0f;
+                for (int s = 0; s < 2; ++s) {
+                    po[s] = lds.exchange[pair][1 - x][s][lane];
+                    so[s] = lds.exchange[pair][1 - x][2 + s][lane];
                 }
+                col_product(dv, other_at, now_d, 0, po);
+                col_product(dk, other_at, now_q, 0, so);
             }
-            to_operands(po, p);
-            to_operands(so, ds);
+        } else {
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                lds.exchange[pair][x][s][lane] = po[s];
-                lds.exchange[pair][x][2 + s][lane] = so[s];
+            for (int y = 0; y < kBlocks; ++y) {
+                if (none(r0 + 32 * y)) continue;
+                block(r0 + 32 * y, 32 * y, 32 * y, now_q, now_d, now_stat, po, so);
+                col_product(dv, mine_at, now_d, 32 * y, po);
+                col_product(dk, mine_at, now_q, 32 * y, so);
             }
-        }
-        lds_barrier();
-        if (mine) {
-            col_product(dv, mine_at, now_d, 0, po);
-            col_product(dk, mine_at, now_q, 0, so);
-        }
-        if (other) {
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                po[s] = lds.exchange[pair][1 - x][s][lane];
-                so[s] = lds.exchange[pair][1 - x][2 + s][lane];
-            }
-            col_product(dv, other_at, now_d, 0, po);
-            col_product(dk, other_at, now_q, 0, so);
         }
         if (n + 1 < total) put(next_q, next_d, next_stat);
         r0 = next_r0;
@@ -401,10 +422,10 @@ hipError_t launch_attention_backward(const SequenceArgs& a, const Unit* q_units,
     if (n_kv > 0) {
         const bool direct = aligned_pieces(a.q) && aligned_pieces(a.dout);
         const unsigned grid = static_cast<unsigned>(n_kv);
-        if (a.dim <= 64 && direct) attention_dkv_kernel<64, true><<<grid, kPairThreads, 0, stream>>>(a, kv_units);
-        else if (a.dim <= 64) attention_dkv_kernel<64, false><<<grid, kPairThreads, 0, stream>>>(a, kv_units);
-        else if (direct) attention_dkv_kernel<128, true><<<grid, kPairThreads, 0, stream>>>(a, kv_units);
-        else attention_dkv_kernel<128, false><<<grid, kPairThreads, 0, stream>>>(a, kv_units);
+        if (a.dim <= 64 && direct) attention_dkv_kernel<64, true><<<grid, Dkv<64>::kThreads, 0, stream>>>(a, kv_units);
+        else if (a.dim <= 64) attention_dkv_kernel<64, false><<<grid, Dkv<64>::kThreads, 0, stream>>>(a, kv_units);
+        else if (direct) attention_dkv_kernel<128, true><<<grid, Dkv<128>::kThreads, 0, stream>>>(a, kv_units);
+        else attention_dkv_kernel<128, false><<<grid, Dkv<128>::kThreads, 0, stream>>>(a, kv_units);
         return hipGetLastError();
     }
     return hipSuccess;
