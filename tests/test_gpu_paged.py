@@ -254,7 +254,7 @@ def test_slots_bounds():
 # --------------------------------------------------------------------------------------- append
 @pytest.mark.parametrize("tokens,page,hk,d,layout", [
     (1, 16, 1, 8, "page_first"), (77, 16, 2, 64, "page_first"), (300, 24, 8, 128, "page_first"),
-    (50, 7, 3, 96, "heads_first"), (33, 1, 1, 40, "shifted")])
+    (50, 7, 3, 96, "heads_first"), (33, 1, 1, 40, "shifted"), (9001, 16, 8, 128, "page_first")])
 def test_append_writes_the_slots_and_nothing_else(tokens, page, hk, d, layout):
     g = torch.Generator().manual_seed(tokens)
     n_pages = -(-tokens // page) + 4
