@@ -1,5 +1,7 @@
 // Attention of ragged sequences in one pass over the keys, and its gradient, which forms the
 // probabilities again from the saved log-sum-exp of every row.
+#include <type_traits>
+
 #include "bsm_attention.hpp"
 
 namespace bsm_att {
@@ -29,7 +31,7 @@ __device__ __forceinline__ Seen seen_keys(int i, int q_len, int kv_len, Mask m) 
 // ------------------------------------------------------------------------------------ forward
 template <int D, bool DIRECT>
 __global__ __launch_bounds__(kThreads, 2) void attention_kernel(const SequenceArgs a, const Unit* __restrict__ units) {
-    __shared__ __align__(16) uint16_t lds[2][2][kKeys * D];  // buffer, K or V
+    __shared__ __align__(16) uint16_t lds[2][2][kKeys * Tile<D>::kPitch];  // buffer, K or V
     const Unit u = units[blockIdx.x];
     if (u.rows <= 0) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, li = lane & 31, h = lane >> 5;
@@ -53,6 +55,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_kernel(const SequenceAr
     Online<D> st;
     st.init();
     const float c = a.scale * kLog2e;
+    clear_tiles<D, DIRECT>(lds[0][0], sizeof(lds) / 2, tid, kThreads, chunks);
     sk.init(tid, a.k.row, chunks);
     sv.init(tid, a.v.row, chunks);
     if (begin < end) {
@@ -107,7 +110,7 @@ __device__ __forceinline__ float reference(float lse) { return lse == -kInf ? kI
 // stay in registers as in the forward pass, the keys stream through LDS.  Also leaves delta.
 template <int D, bool DIRECT>
 __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(const SequenceArgs a, const Unit* __restrict__ units) {
-    __shared__ __align__(16) uint16_t lds[2][2][kKeys * D];
+    __shared__ __align__(16) uint16_t lds[2][2][kKeys * Tile<D>::kPitch];
     const Unit u = units[blockIdx.x];
     if (u.rows <= 0) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, li = lane & 31, h = lane >> 5;
@@ -147,6 +150,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(const Sequenc
 #pragma unroll
     for (int t = 0; t < D / 32; ++t) dq[t] = zero16();
     const float c = a.scale * kLog2e;
+    clear_tiles<D, DIRECT>(lds[0][0], sizeof(lds) / 2, tid, kThreads, chunks);
     sk.init(tid, a.k.row, chunks);
     sv.init(tid, a.v.row, chunks);
     if (begin < end) {
@@ -202,17 +206,17 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(const Sequenc
 // dv_j = sum_i P_ij do_i and dk_j = scale * sum_i dS_ij q_i over the rows of all query heads that
 // share the key/value head: k, v and both sums stay in registers, the query rows stream through LDS, 64
 // at a time.  No sum crosses a workgroup, so the result does not depend on timing.
-// D = 64: a wave keeps 32 keys.  D = 128: two waves share 32 keys (kPair): wave x of the pair forms P and
+// D = 64: a wave keeps 32 keys.  D = 96, 128: two waves share 32 keys (kPair): wave x of the pair forms P and
 // dS for the 32 query rows of block x, the pair exchanges them through LDS as operands, and each adds up
-// half of the head dimension over both blocks.  That keeps a wave's sums at 64 registers, so that two
+// half of 128 columns over both blocks (of 96, wave 1 adds 32 that are not stored).  That keeps a wave's sums at 64 registers, so that two
 // waves fit a SIMD and one's exponentials run beside the other's products (a wave that held whole sums
 // took 400 registers and ran alone: 735 us against 500 us on six ragged causal sequences of 700 .. 4001
 // tokens, 32 / 8 heads of 128).
 template <int D>
 struct Dkv {
-    static constexpr bool kPair = D == 128;
+    static constexpr bool kPair = D > 64;
     static constexpr int kThreads = kPair ? 512 : 256;
-    static constexpr int kTiles = kPair ? D / 64 : D / 32;  // blocks of 32 columns that a wave adds up
+    static constexpr int kTiles = 2;  // blocks of 32 columns that a wave adds up
 };
 
 template <int D, bool DIRECT>
@@ -222,7 +226,7 @@ __global__ __launch_bounds__(Dkv<D>::kThreads, 2) void attention_dkv_kernel(cons
     // (One array: of several, the compiler forgets which tiles a step reads and writes, and waits for the
     // loads on their way before every read of LDS.)
     struct Shared {
-        uint16_t tile[2][2][kKeys * D];                             // buffer, q or dout
+        uint16_t tile[2][2][kKeys * Tile<D>::kPitch];                             // buffer, q or dout
         float stat[2][2 * kKeys];                                   // buffer; references, then deltas
         bf16x8 exchange[kPair ? 4 : 1][kBlocks][4][kPair ? kWave : 1];  // pair, block; P and dS of 16 rows
     };
@@ -258,6 +262,7 @@ __global__ __launch_bounds__(Dkv<D>::kThreads, 2) void attention_dkv_kernel(cons
     Stage<D, kKeys, Dkv<D>::kThreads, DIRECT> sq, sd;
     float lse = 0.0f, delta = 0.0f;  // of row `tid` % kKeys of the step to come
     int rows_left = 0;
+    clear_tiles<D, DIRECT>(lds.tile[0][0], sizeof(lds.tile) / 2, tid, Dkv<D>::kThreads, chunks);
     sq.init(tid, a.q.row, chunks);
     sd.init(tid, a.dout.row, chunks);
     auto fetch_stat = [&](int g, int r0) __attribute__((always_inline)) {
@@ -396,39 +401,40 @@ bool aligned_pieces(const Heads& t) {
     return reinterpret_cast<uintptr_t>(t.p) % 16 == 0 && (t.seq | t.row | t.head) % 8 == 0;
 }
 
+// Calls f with D and DIRECT as constants.
+template <class F>
+hipError_t with_dim(int dim, bool direct, F f) {
+    auto go = [&](auto d) {
+        if (direct) f(d, std::true_type{});
+        else f(d, std::false_type{});
+        return hipGetLastError();
+    };
+    switch (padded_dim(dim)) {
+        case 64: return go(std::integral_constant<int, 64>{});
+        case 96: return go(std::integral_constant<int, 96>{});
+        default: return go(std::integral_constant<int, 128>{});
+    }
+}
+
 hipError_t launch_attention(const SequenceArgs& a, const Unit* units, int64_t n, hipStream_t stream) {
     if (n == 0) return hipSuccess;
-    const bool direct = aligned_pieces(a.k) && aligned_pieces(a.v);
-    const unsigned grid = static_cast<unsigned>(n);
-    if (a.dim <= 64 && direct) attention_kernel<64, true><<<grid, kThreads, 0, stream>>>(a, units);
-    else if (a.dim <= 64) attention_kernel<64, false><<<grid, kThreads, 0, stream>>>(a, units);
-    else if (direct) attention_kernel<128, true><<<grid, kThreads, 0, stream>>>(a, units);
-    else attention_kernel<128, false><<<grid, kThreads, 0, stream>>>(a, units);
-    return hipGetLastError();
+    return with_dim(a.dim, aligned_pieces(a.k) && aligned_pieces(a.v), [&](auto d, auto direct) {
+        attention_kernel<d(), direct()><<<static_cast<unsigned>(n), kThreads, 0, stream>>>(a, units);
+    });
 }
 
 hipError_t launch_attention_backward(const SequenceArgs& a, const Unit* q_units, int64_t n_q, const Unit* kv_units,
                                      int64_t n_kv, hipStream_t stream) {
-    if (n_q > 0) {
-        const bool direct = aligned_pieces(a.k) && aligned_pieces(a.v);
-        const unsigned grid = static_cast<unsigned>(n_q);
-        if (a.dim <= 64 && direct) attention_dq_kernel<64, true><<<grid, kThreads, 0, stream>>>(a, q_units);
-        else if (a.dim <= 64) attention_dq_kernel<64, false><<<grid, kThreads, 0, stream>>>(a, q_units);
-        else if (direct) attention_dq_kernel<128, true><<<grid, kThreads, 0, stream>>>(a, q_units);
-        else attention_dq_kernel<128, false><<<grid, kThreads, 0, stream>>>(a, q_units);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
-    if (n_kv > 0) {
-        const bool direct = aligned_pieces(a.q) && aligned_pieces(a.dout);
-        const unsigned grid = static_cast<unsigned>(n_kv);
-        if (a.dim <= 64 && direct) attention_dkv_kernel<64, true><<<grid, Dkv<64>::kThreads, 0, stream>>>(a, kv_units);
-        else if (a.dim <= 64) attention_dkv_kernel<64, false><<<grid, Dkv<64>::kThreads, 0, stream>>>(a, kv_units);
-        else if (direct) attention_dkv_kernel<128, true><<<grid, Dkv<128>::kThreads, 0, stream>>>(a, kv_units);
-        else attention_dkv_kernel<128, false><<<grid, Dkv<128>::kThreads, 0, stream>>>(a, kv_units);
-        return hipGetLastError();
-    }
-    return hipSuccess;
+    hipError_t e = hipSuccess;
+    if (n_q > 0)
+        e = with_dim(a.dim, aligned_pieces(a.k) && aligned_pieces(a.v), [&](auto d, auto direct) {
+            attention_dq_kernel<d(), direct()><<<static_cast<unsigned>(n_q), kThreads, 0, stream>>>(a, q_units);
+        });
+    if (e == hipSuccess && n_kv > 0)
+        e = with_dim(a.dim, aligned_pieces(a.q) && aligned_pieces(a.dout), [&](auto d, auto direct) {
+            attention_dkv_kernel<d(), direct()><<<static_cast<unsigned>(n_kv), Dkv<d()>::kThreads, 0, stream>>>(a, kv_units);
+        });
+    return e;
 }
 
 }  // namespace bsm_att

@@ -47,15 +47,17 @@ constexpr int kMayCross = 0x6; // of the fixed order: vector and scalar arithmet
 // (an exclusive or with bits of the row).  Fragments are read two ways: 16 consecutive rows at one
 // chunk (row_frag), and 4 consecutive rows at 4 neighbouring chunks (col_frag); with these bits
 // both touch every one of the 64 banks once per 256 bytes.
+// D: head dimensions up to it, 64, 96 or 128; a row of 96 takes the place of one of 128.
 template <int D>
 struct Tile {
-    static_assert(D == 64 || D == 128, "head dimensions are padded to 64 or 128");
-    static constexpr int kChunks = D / 8;
+    static_assert(D == 64 || D == 96 || D == 128, "head dimensions are padded to 64, 96 or 128");
+    static constexpr int kChunks = D == 64 ? 8 : 16;
+    static constexpr int kPitch = 8 * kChunks;       // elements
+    static constexpr int kRowBytes = 2 * kPitch;
     __device__ static __forceinline__ int place(int row, int chunk) {
-        const int f = D == 128 ? ((row & 3) << 2) | ((row >> 2) & 3) : (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
+        const int f = D == 64 ? (((row >> 1) & 1) << 2) | ((row >> 2) & 3) : ((row & 3) << 2) | ((row >> 2) & 3);
         return row * kChunks + (chunk ^ f);
     }
-    static constexpr int kRowBytes = 2 * D;
 };
 
 // Where a lane's fragments lie, in bytes from the start of a tile: the same for every 16 rows, so that what
@@ -123,6 +125,7 @@ struct Stage {
     u32x4 r[DIRECT ? 1 : kN];
     uint32_t off[DIRECT ? kN : 1];  // bytes from the tile's first row, for whole tiles
     bool near;                      // the offsets fit
+    bool live;                      // the thread's chunks exist (they have the same number in all its rows)
     __device__ static __forceinline__ int row(int tid, int j) { return (tid + THREADS * j) / Tile<D>::kChunks; }
     __device__ static __forceinline__ int chunk(int tid, int j) {
         const int c = tid % Tile<D>::kChunks;
@@ -131,7 +134,9 @@ struct Stage {
     // `stride` of the rows of all the tiles to come
     __device__ __forceinline__ void init(int tid, int64_t stride, int chunks) {
         if constexpr (DIRECT) {
-            near = chunks == Tile<D>::kChunks && stride < (int64_t{1} << 24);
+            static_assert(THREADS / Tile<D>::kChunks % 16 == 0, "a thread's chunk is the same in all its rows");
+            near = stride < (int64_t{1} << 24);
+            live = chunk(tid, 0) < chunks;
 #pragma unroll
             for (int j = 0; j < kN; ++j) off[j] = static_cast<uint32_t>(2 * (row(tid, j) * stride + 8 * chunk(tid, j)));
         }
@@ -148,7 +153,8 @@ struct Stage {
     }
     __device__ __forceinline__ void begin(int tid, uint16_t* lds, const uint16_t* p, int64_t stride, int lo, int hi, int chunks) {
         if constexpr (DIRECT) {
-            if (near && lo <= 0 && hi >= ROWS) {  // nothing to leave out: one base, offsets as they are
+            if (near && lo <= 0 && hi >= ROWS) {  // no row to leave out: one base, offsets as they are
+                if (!live) return;                // (the chunk is zero since clear_tiles)
 #pragma unroll
                 for (int j = 0; j < kN; ++j)
                     __builtin_amdgcn_global_load_lds(
@@ -171,6 +177,16 @@ struct Stage {
         }
     }
 };
+
+// Zeros in the chunks of all tiles that no load of a whole tile touches, where the head dimension ends short
+// of D.
+template <int D, bool DIRECT>
+__device__ __forceinline__ void clear_tiles(uint16_t* tiles, int elems, int tid, int threads, int chunks) {
+    if (DIRECT && chunks < D / 8) {
+        for (int i = 8 * tid; i < elems; i += 8 * threads) *reinterpret_cast<u32x4*>(tiles + i) = u32x4{0, 0, 0, 0};
+        __syncthreads();
+    }
+}
 
 // The second operand of a product whose columns are 32 rows of a matrix in memory: lane (li, h)
 // holds elements 16 step + 8 h .. + 7 of its row; zero where the row does not exist.

@@ -20,6 +20,9 @@ static_assert(sizeof(Unit) == 48, "");
 
 constexpr int kTileRows = 128;
 
+// What the kernels pad a head dimension to.
+constexpr int padded_dim(int dim) { return dim <= 64 ? 64 : dim <= 96 ? 96 : 128; }
+
 // A caller's tensor: element (b, row, head, d) at p + b seq + row row + head head + d.
 struct Heads {
     uint16_t* p;

@@ -155,7 +155,7 @@ PagedCut cut_paged(int64_t batch, int64_t tokens, int32_t heads_kv, int32_t grou
                    int32_t max_kv, int n_cu) {
     PagedCut c{};
     const int64_t rows = std::min<int64_t>(max_q, tokens) * group, keys = std::max<int64_t>(1, max_kv);
-    const int padded = dim <= 64 ? 64 : 128;
+    const int padded = padded_dim(dim);
     // Few rows over many keys are bound by reading the cache, many rows by the products: each has a kernel.  A
     // batch that may hold both launches both (one chunk of 512 tokens over 4096 and 63 single tokens over
     // 5000, 8 kv heads: 732 us by tiles alone, 370 us by both); where no request is shorter than the

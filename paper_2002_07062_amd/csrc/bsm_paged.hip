@@ -181,7 +181,7 @@ struct PagedStage {
 // Many rows (chunks of prompts): a tile has 128 rows, 32 per wave, and the waves share the staged keys.
 template <int D, bool DIRECT>
 __global__ __launch_bounds__(kThreads, 2) void paged_kernel(const PagedArgs a) {
-    constexpr int kKeys = 64, kTileElems = kKeys * D;
+    constexpr int kKeys = 64, kTileElems = kKeys * Tile<D>::kPitch;
     // (One array: of several, the compiler forgets which tiles a step reads and writes, and waits for the
     // loads on their way before every read of LDS.)
     __shared__ __align__(16) uint16_t lds[2][2][kTileElems];  // buffer, K or V
@@ -340,7 +340,8 @@ __global__ __launch_bounds__(kThreads, 2) void paged_few_kernel(const PagedArgs 
     constexpr int kKeys = 32, kSteps = D / 32, kTiles = D / 16;
     static_assert(kKeys * kWaves == kFewKeys, "");
     constexpr int kRegs = NQ * kTiles * 4;  // outputs of a lane
-    constexpr int kBytes = kWaves * (kRegs * kWave * 4 > kKeys * D * 2 ? kRegs * kWave * 4 : kKeys * D * 2);
+    constexpr int kBlockBytes = kKeys * Tile<D>::kRowBytes;
+    constexpr int kBytes = kWaves * (kRegs * kWave * 4 > kBlockBytes ? kRegs * kWave * 4 : kBlockBytes);
     __shared__ __align__(16) unsigned char lds[kBytes];
     __shared__ float stat[2][kWaves][16 * NQ];
     __shared__ int64_t mem[kWaves], s_at[2];
@@ -378,7 +379,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_few_kernel(const PagedArgs 
     bool at_start = true;  // nothing of the share is done
     // The wave's V block.  A place does not depend on a multiple of 16 of the row, and chunk x ^ y lies at an
     // exclusive or of 16 y with the place of chunk x: one address each for writing and for reading.
-    unsigned char* turned = lds + wave * kKeys * D * 2;
+    unsigned char* turned = lds + wave * kBlockBytes;
     int put_at = 16 * Tile<D>::place(n, quad);  // row n, chunk quad; chunk 4 e + quad is 64 e away
     // lane (n, quad): column n of rows 4 quad + {0..3} (and of those 16 further); column 16 t + n is 32 t away
     int col_at = 16 * Tile<D>::place(4 * quad + (n >> 2), (n & 3) >> 1) + 8 * (n & 1);
@@ -592,10 +593,10 @@ __global__ __launch_bounds__(kThreads, 2) void paged_few_kernel(const PagedArgs 
 }
 
 // Joins n parts of a row, row i of the `rows` that a part holds, one wave: a lane per part for the statistics,
-// then a lane per D / 64 columns.  part(p) is the p-th part's first float.
+// then a lane per column or two.  part(p) is the p-th part's first float.
 template <int D, class Part>
 __device__ __forceinline__ void join_row(const PagedArgs& a, const Request& r, int rows, int row, int i, int n, Part part) {
-    constexpr int kPer = D / 64;
+    constexpr int kPer = (D + 63) / 64;
     const int lane = threadIdx.x & 63;
     float m = -kInf, total = 0.0f, acc[kPer];
 #pragma unroll
@@ -619,7 +620,7 @@ __device__ __forceinline__ void join_row(const PagedArgs& a, const Request& r, i
         const int count = min(n - p0, kWave);
         for (int p = 0; p < count; ++p) {
             const float fp = __shfl(f, p, 64);
-            const float* from = part(p0 + p) + i * D + kPer * lane;
+            const float* from = part(p0 + p) + i * D + min(kPer * lane, D - kPer);
 #pragma unroll
             for (int e = 0; e < kPer; ++e) acc[e] += fp * from[e];
         }
@@ -853,7 +854,11 @@ hipError_t launch_paged(const PagedArgs& a, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_attention_paged(const PagedArgs& a, hipStream_t stream) {
-    return a.cache.dim <= 64 ? launch_paged<64>(a, stream) : launch_paged<128>(a, stream);
+    switch (padded_dim(a.cache.dim)) {
+        case 64: return launch_paged<64>(a, stream);
+        case 96: return launch_paged<96>(a, stream);
+        default: return launch_paged<128>(a, stream);
+    }
 }
 
 hipError_t launch_cache_slots(const SlotArgs& a, int n_cu, hipStream_t stream) {
