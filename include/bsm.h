@@ -414,8 +414,9 @@ typedef struct bsm_attention_plan_s* bsm_attention_plan;
  *   head_dim           a multiple of 8 up to 128 (else BSM_ERR_UNSUPPORTED)
  *   causal, window     the mask; window > 0 needs causal
  *   schedule           order of the work, 128 rows of one head at a time: RR as the sequences
- *                      come; BALANCED the longest first; XCD every key/value head's work on one
- *                      XCD, the heads dealt to the XCDs by their cost, the longest first
+ *                      come; XCD every key/value head's work on one XCD, the heads dealt to the
+ *                      XCDs by their cost, the longest first; BALANCED the same, but an XCD that
+ *                      has done its own takes over from the one that has most left
  *   topology           NULL = the device's defaults; only n_xcd is used
  *   device             HIP device ordinal; -1 builds a host-only plan (topology required)
  * The plan's table is uploaded before this returns.  It serves any number of calls, streams and

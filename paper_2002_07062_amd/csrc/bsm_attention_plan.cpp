@@ -73,19 +73,14 @@ struct Costed {
 };
 
 std::vector<Unit> order(std::vector<Costed>& units, bsm_schedule schedule, int n_xcd, int64_t kv_heads) {
-    auto longest_first = [&](std::vector<int64_t>& index) {
-        std::stable_sort(index.begin(), index.end(), [&](int64_t x, int64_t y) { return units[x].cost > units[y].cost; });
-    };
     std::vector<Unit> out;
-    if (schedule != BSM_SCHED_XCD) {
-        std::vector<int64_t> index(units.size());
-        std::iota(index.begin(), index.end(), 0);
-        if (schedule == BSM_SCHED_BALANCED) longest_first(index);
+    if (schedule == BSM_SCHED_RR) {
         out.reserve(units.size());
-        for (int64_t i : index) out.push_back(units[i].unit);
+        for (const Costed& c : units) out.push_back(c.unit);
         return out;
     }
-    // the costliest key/value head goes to the least loaded XCD, and so on
+    // The costliest key/value head goes to the least loaded XCD, and so on: the units that read the same keys
+    // run on one XCD, at about the same time, and find them in its L2.
     std::vector<int64_t> cost(kv_heads, 0), by_cost(kv_heads), home(kv_heads), load(n_xcd, 0);
     for (const Costed& c : units) cost[c.kv_head] += c.cost;
     std::iota(by_cost.begin(), by_cost.end(), 0);
@@ -94,18 +89,31 @@ std::vector<Unit> order(std::vector<Costed>& units, bsm_schedule schedule, int n
         home[k] = std::min_element(load.begin(), load.end()) - load.begin();
         load[home[k]] += cost[k];
     }
-    std::vector<std::vector<int64_t>> lists(n_xcd);
+    std::vector<std::vector<int64_t>> lists(n_xcd);  // longest units first
     for (size_t i = 0; i < units.size(); ++i) lists[home[units[i].kv_head]].push_back(static_cast<int64_t>(i));
     size_t longest = 0;
     for (auto& list : lists) {
-        longest_first(list);
+        std::stable_sort(list.begin(), list.end(), [&](int64_t x, int64_t y) { return units[x].cost > units[y].cost; });
         longest = std::max(longest, list.size());
     }
-    Unit none{};
-    out.reserve(longest * n_xcd);
-    for (size_t i = 0; i < longest; ++i)
-        for (int x = 0; x < n_xcd; ++x) out.push_back(i < lists[x].size() ? units[lists[x][i]].unit : none);
-    while (!out.empty() && out.back().rows == 0) out.pop_back();
+    std::vector<size_t> at(n_xcd, 0);
+    const Unit none{};
+    if (schedule == BSM_SCHED_XCD) {
+        out.reserve(longest * n_xcd);
+        for (size_t i = 0; i < longest; ++i)
+            for (int x = 0; x < n_xcd; ++x) out.push_back(i < lists[x].size() ? units[lists[x][i]].unit : none);
+        while (!out.empty() && out.back().rows == 0) out.pop_back();
+        return out;
+    }
+    // BALANCED: an XCD whose list is done takes from the one that has most left
+    out.reserve(units.size());
+    for (size_t i = 0; i < units.size(); ++i) {
+        size_t x = i % n_xcd;
+        if (at[x] == lists[x].size())
+            for (size_t y = 0; y < lists.size(); ++y)
+                if (lists[y].size() - at[y] > lists[x].size() - at[x]) x = y;
+        out.push_back(units[lists[x][at[x]++]].unit);
+    }
     return out;
 }
 
