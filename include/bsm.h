@@ -378,7 +378,9 @@ bsm_status bsm_gemm(const void* a, const void* b, void* c, int64_t batch, int32_
  * makes its row NaN.
  *
  * Results depend on the operands and sizes only: no sum's order depends on timing, so repeated
- * calls give the same bits under every schedule. */
+ * calls give the same bits under every schedule.  (The last bits of dk and dv depend on the other
+ * sequences of the batch and the number of compute units as well: where the keys alone leave some
+ * without work, their query rows are added up in parts.) */
 
 /* Element (b, row, head, d) of an operand lies at data + b*seq + row*row + head*head + d, in
  * elements, so packed tokens (seq 0), padded batches, heads-first layouts and views of a fused
@@ -417,7 +419,7 @@ typedef struct bsm_attention_plan_s* bsm_attention_plan;
  *                      come; XCD every key/value head's work on one XCD, the heads dealt to the
  *                      XCDs by their cost, the longest first; BALANCED the same, but an XCD that
  *                      has done its own takes over from the one that has most left
- *   topology           NULL = the device's defaults; only n_xcd is used
+ *   topology           NULL = the device's defaults; only n_xcd and n_cu are used
  *   device             HIP device ordinal; -1 builds a host-only plan (topology required)
  * The plan's table is uploaded before this returns.  It serves any number of calls, streams and
  * layers, and must outlive every graph that captured one of them. */
@@ -448,7 +450,8 @@ bsm_status bsm_attention_execute(bsm_attention_plan plan, const bsm_heads* q, co
  * the gradients are written, not added to, for every row of every sequence.  A key/value row that
  * two sequences share, or an operand with a stride of 0, has no one place for its gradient: give
  * each (sequence, row, head) a place of its own and add them up.  workspace: workspace_bytes of
- * the plan's stats, not shared with a call that may run at the same time.  dq, dk and dv overlap
+ * the plan's stats (for delta_i, and at most 140 MB of parts), on a 16-byte boundary, not shared
+ * with a call that may run at the same time.  dq, dk and dv overlap
  * no operand (they may interleave with each other, as views of one tensor). */
 bsm_status bsm_attention_backward(bsm_attention_plan plan, const bsm_heads* q, const bsm_heads* k,
                                   const bsm_heads* v, const bsm_heads* o, const float* lse,

@@ -205,7 +205,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(const Sequenc
 
 // dv_j = sum_i P_ij do_i and dk_j = scale * sum_i dS_ij q_i over the rows of all query heads that
 // share the key/value head: k, v and both sums stay in registers, the query rows stream through LDS, 64
-// at a time.  No sum crosses a workgroup, so the result does not depend on timing.
+// at a time.  No two workgroups add to one sum, so the result does not depend on timing.
 // D = 64: a wave keeps 32 keys.  D = 96, 128: two waves share 32 keys (kPair): wave x of the pair forms P and
 // dS for the 32 query rows of block x, the pair exchanges them through LDS as operands, and each adds up
 // half of 128 columns over both blocks (of 96, wave 1 adds 32 that are not stored).  That keeps a wave's sums at 64 registers, so that two
@@ -256,7 +256,8 @@ __global__ __launch_bounds__(Dkv<D>::kThreads, 2) void attention_dkv_kernel(cons
         if (a.mask.window > 0 && static_cast<int64_t>(last) + a.mask.window - off < end) end = last + a.mask.window - off;
     }
     const int steps = end > begin ? (end - begin + kKeys - 1) / kKeys : 0;
-    const int64_t total = static_cast<int64_t>(steps) * a.group;
+    // the part's steps, of those of all query heads one after the other
+    const int64_t all = static_cast<int64_t>(steps) * a.group, n0 = all * u.part / u.parts, total = all * (u.part + 1) / u.parts;
     const bool any_row = j0 <= last;
 
     Stage<D, kKeys, Dkv<D>::kThreads, DIRECT> sq, sd;
@@ -280,14 +281,16 @@ __global__ __launch_bounds__(Dkv<D>::kThreads, 2) void attention_dkv_kernel(cons
             to_stat[kKeys + tid] = ref == kInf ? 0.0f : delta;
         }
     };
-    if (total > 0) {
-        const int head = u.head * a.group;
-        sq.begin(tid, lds.tile[0][0], at(a.q, u, u.q_start + begin, head), a.q.row, dead - begin, end - begin, chunks);
-        sd.begin(tid, lds.tile[0][1], at(a.dout, u, u.q_start + begin, head), a.dout.row, dead - begin, end - begin, chunks);
-        fetch_stat(0, begin);
+    int g = 0, r0 = begin;
+    if (n0 < total) {
+        g = static_cast<int>(n0 / steps);
+        r0 = begin + static_cast<int>(n0 % steps) * kKeys;
+        const int head = u.head * a.group + g;
+        sq.begin(tid, lds.tile[0][0], at(a.q, u, u.q_start + r0, head), a.q.row, dead - r0, end - r0, chunks);
+        sd.begin(tid, lds.tile[0][1], at(a.dout, u, u.q_start + r0, head), a.dout.row, dead - r0, end - r0, chunks);
+        fetch_stat(g, r0);
         put(lds.tile[0][0], lds.tile[0][1], lds.stat[0]);
     }
-    int r0 = begin, g = 0;
     constexpr int kBlockBytes = 32 * Tile<D>::kRowBytes;
     const RowFrags<D> rows_at(lane, x * kBlockBytes);
     const ColFrags<D, kTiles> mine_at(lane, x * kTiles, x * kBlockBytes), other_at(lane, x * kTiles, (1 - x) * kBlockBytes);
@@ -381,9 +384,23 @@ __global__ __launch_bounds__(Dkv<D>::kThreads, 2) void attention_dkv_kernel(cons
         r0 = next_r0;
         g = next_g;
     };
-    in_turn(0, total, 1, [&](int64_t n, auto buf) {
+    in_turn(n0, total, 1, [&](int64_t n, auto buf) {
         step(n, lds.tile[1 - buf][0], lds.tile[1 - buf][1], lds.stat[1 - buf], lds.tile[buf][0], lds.tile[buf][1], lds.stat[buf]);
     });
+    if (u.parts > 1) {
+        if (!live) return;
+        float* to = a.part + (u.part_row + u.part * u.rows + j - u.first) * 2 * D + 4 * h;
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+            for (int e4 = 0; e4 < 4; ++e4) {
+                const int d = 32 * (x * kTiles + t) + 8 * e4;
+                if (d >= D) continue;
+                *reinterpret_cast<f32x4*>(to + d) = f32x4{dk[t][4 * e4], dk[t][4 * e4 + 1], dk[t][4 * e4 + 2], dk[t][4 * e4 + 3]};
+                *reinterpret_cast<f32x4*>(to + D + d) = f32x4{dv[t][4 * e4], dv[t][4 * e4 + 1], dv[t][4 * e4 + 2], dv[t][4 * e4 + 3]};
+            }
+        return;
+    }
     const int64_t row = u.kv_start + j;
     uint16_t* to_k = a.dk.p + u.seq * a.dk.seq + row * a.dk.row + u.head * a.dk.head;
     uint16_t* to_v = a.dv.p + u.seq * a.dv.seq + row * a.dv.row + u.head * a.dv.head;
@@ -391,6 +408,37 @@ __global__ __launch_bounds__(Dkv<D>::kThreads, 2) void attention_dkv_kernel(cons
     for (int t = 0; t < kTiles; ++t) {
         store_block(to_k, live, dk[t], a.scale, x * kTiles + t, h, chunks);
         store_block(to_v, live, dv[t], 1.0f, x * kTiles + t, h, chunks);
+    }
+}
+
+// Adds up the parts of a unit's dk and dv, in order: a thread per 8 columns of a row of one of them.
+template <int D>
+__global__ __launch_bounds__(kThreads) void attention_dkv_join_kernel(const SequenceArgs a, const Unit* __restrict__ units) {
+    const Unit u = units[blockIdx.x];
+    const int chunks = a.dim / 8;
+    const int64_t step = static_cast<int64_t>(u.rows) * 2 * D;
+    for (int x = threadIdx.x; x < 2 * u.rows * chunks; x += kThreads) {
+        const int c = x % chunks, is_v = x / chunks % 2, j = x / chunks / 2;
+        const float* from = a.part + ((u.part_row + j) * 2 + is_v) * D + 8 * c;
+        f32x4 lo = {0.0f, 0.0f, 0.0f, 0.0f}, hi = lo;
+        for (int p = 0; p < u.parts; ++p) {
+            const f32x4 y = *reinterpret_cast<const f32x4*>(from + p * step), z = *reinterpret_cast<const f32x4*>(from + p * step + 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                lo[e] += y[e];
+                hi[e] += z[e];
+            }
+        }
+        const float f = is_v ? 1.0f : a.scale;
+        bf16x8 out;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            out[e] = static_cast<__bf16>(f * lo[e]);
+            out[4 + e] = static_cast<__bf16>(f * hi[e]);
+        }
+        const Heads& to = is_v ? a.dv : a.dk;
+        *reinterpret_cast<u32x4_any*>(to.p + u.seq * to.seq + (u.kv_start + u.first + j) * to.row + u.head * to.head + 8 * c) =
+            __builtin_bit_cast(u32x4, out);
     }
 }
 
@@ -424,7 +472,7 @@ hipError_t launch_attention(const SequenceArgs& a, const Unit* units, int64_t n,
 }
 
 hipError_t launch_attention_backward(const SequenceArgs& a, const Unit* q_units, int64_t n_q, const Unit* kv_units,
-                                     int64_t n_kv, hipStream_t stream) {
+                                     int64_t n_kv, int64_t n_join, hipStream_t stream) {
     hipError_t e = hipSuccess;
     if (n_q > 0)
         e = with_dim(a.dim, aligned_pieces(a.k) && aligned_pieces(a.v), [&](auto d, auto direct) {
@@ -433,6 +481,10 @@ hipError_t launch_attention_backward(const SequenceArgs& a, const Unit* q_units,
     if (e == hipSuccess && n_kv > 0)
         e = with_dim(a.dim, aligned_pieces(a.q) && aligned_pieces(a.dout), [&](auto d, auto direct) {
             attention_dkv_kernel<d(), direct()><<<static_cast<unsigned>(n_kv), Dkv<d()>::kThreads, 0, stream>>>(a, kv_units);
+        });
+    if (e == hipSuccess && n_join > 0)
+        e = with_dim(a.dim, true, [&](auto d, auto) {
+            attention_dkv_join_kernel<d()><<<static_cast<unsigned>(n_join), kThreads, 0, stream>>>(a, kv_units + n_kv);
         });
     return e;
 }

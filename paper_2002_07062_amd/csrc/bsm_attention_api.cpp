@@ -23,7 +23,7 @@ struct bsm_attention_plan_s {
     bsm_schedule schedule = BSM_SCHED_RR;
     int n_xcd = 1;
     bsm_att::Sequences seqs;
-    int64_t n_q = 0, n_kv = 0;
+    int64_t n_q = 0, n_kv = 0, n_join = 0, part_rows = 0;
     void* d_units = nullptr;  // query units, then key units
     std::atomic<bool> used{false};
 };
@@ -178,7 +178,7 @@ bsm_status create(bsm_attention_plan* out_plan, const int32_t* q_len, const int3
         return fail(BSM_ERR_INVALID_ARG, "unknown schedule %d", static_cast<int>(schedule));
     if (device < -1) return fail(BSM_ERR_INVALID_ARG, "device %d", device);
     if (device == -1 && !topology) return fail(BSM_ERR_INVALID_ARG, "a host-only plan (device -1) needs a topology");
-    int n_xcd = 8;
+    int n_xcd = 8, n_cu = 256;
     if (device >= 0) {
         int n = 0;
         const hipError_t e = hipGetDeviceCount(&n);
@@ -188,11 +188,14 @@ bsm_status create(bsm_attention_plan* out_plan, const int32_t* q_len, const int3
         st = bsm_default_topology(device, &t);
         if (st != BSM_OK) return st;
         n_xcd = t.n_xcd;
+        n_cu = t.n_cu;
     }
     if (topology) {
         if (topology->n_xcd < 0 || topology->n_xcd > BSM_MAX_XCD)
             return fail(BSM_ERR_INVALID_ARG, "topology: n_xcd %d", topology->n_xcd);
         if (topology->n_xcd > 0) n_xcd = topology->n_xcd;
+        if (topology->n_cu < 0 || topology->n_cu > 65536) return fail(BSM_ERR_INVALID_ARG, "topology: n_cu %d", topology->n_cu);
+        if (topology->n_cu > 0) n_cu = topology->n_cu;
     }
     for (int64_t b = 0; b < batch; ++b) {
         if (q_len[b] < 0 || kv_len[b] < 0 || q_len[b] > kMostRows || kv_len[b] > kMostRows)
@@ -219,16 +222,19 @@ bsm_status create(bsm_attention_plan* out_plan, const int32_t* q_len, const int3
                              (static_cast<double>(s.total_kv) / bsm_att::kTileRows + batch) * heads_kv;
         if (units > kMostWorkgroups) return fail(BSM_ERR_INVALID_ARG, "too many rows for one plan");
         std::vector<bsm_att::Unit> q = bsm_att::query_units(s, schedule, n_xcd);
-        const std::vector<bsm_att::Unit> kv = bsm_att::key_units(s, schedule, n_xcd);
+        const bsm_att::KeyUnits kv = bsm_att::key_units(s, schedule, n_xcd, n_cu);
         p->n_q = static_cast<int64_t>(q.size());
-        p->n_kv = static_cast<int64_t>(kv.size());
+        p->n_kv = static_cast<int64_t>(kv.units.size());
+        p->n_join = static_cast<int64_t>(kv.joins.size());
+        p->part_rows = kv.part_rows;
         if (std::max(p->n_q, p->n_kv) > kMostWorkgroups) return fail(BSM_ERR_INVALID_ARG, "too many rows for one plan");
         p->device = device;
         p->schedule = schedule;
         p->n_xcd = n_xcd;
         if (fails("host")) throw std::bad_alloc();
         if (device >= 0 && p->n_q + p->n_kv > 0) {
-            q.insert(q.end(), kv.begin(), kv.end());
+            q.insert(q.end(), kv.units.begin(), kv.units.end());
+            q.insert(q.end(), kv.joins.begin(), kv.joins.end());
             DeviceGuard g;
             hipError_t e = g.enter(device);
             if (e != hipSuccess) return hip_fail(e, "hipSetDevice");
@@ -293,7 +299,11 @@ bsm_status forward(bsm_attention_plan p, const bsm_heads* q, const bsm_heads* k,
     return BSM_OK;
 }
 
-int64_t workspace_of(const bsm_att::Sequences& s) { return 4 * s.heads_q * s.total_q; }
+// The workspace: delta of every query row and head, and the parts of dk and dv.
+int64_t delta_bytes(const bsm_att::Sequences& s) { return (4 * s.heads_q * s.total_q + 15) / 16 * 16; }
+int64_t workspace_of(bsm_attention_plan p) {
+    return delta_bytes(p->seqs) + 4 * 2 * p->part_rows * bsm_att::padded_dim(p->seqs.dim);
+}
 
 bsm_status backward(bsm_attention_plan p, const bsm_heads* q, const bsm_heads* k, const bsm_heads* v, const bsm_heads* o,
                     const float* lse, const bsm_heads* dout, const bsm_heads* dq, const bsm_heads* dk, const bsm_heads* dv, float scale,
@@ -314,14 +324,14 @@ bsm_status backward(bsm_attention_plan p, const bsm_heads* q, const bsm_heads* k
         (st = take("dk", dk, kr, s.heads_kv, s.dim, true, &a.dk, &out[1])) != BSM_OK ||
         (st = take("dv", dv, kr, s.heads_kv, s.dim, true, &a.dv, &out[2])) != BSM_OK)
         return st;
-    const int64_t need = workspace_of(s);
-    if (need > 0 && (!lse || !workspace)) return fail(BSM_ERR_INVALID_ARG, "lse or workspace is NULL");
+    const int64_t need = workspace_of(p), lse_bytes = 4 * s.heads_q * s.total_q;
+    if ((lse_bytes > 0 && !lse) || (need > 0 && !workspace)) return fail(BSM_ERR_INVALID_ARG, "lse or workspace is NULL");
     if (workspace_bytes < need)
         return fail(BSM_ERR_INVALID_ARG, "workspace of %lld bytes, %lld needed", static_cast<long long>(workspace_bytes),
                     static_cast<long long>(need));
-    if (reinterpret_cast<uintptr_t>(lse) % 4 != 0 || reinterpret_cast<uintptr_t>(workspace) % 4 != 0)
-        return fail(BSM_ERR_INVALID_ARG, "lse or workspace is not aligned to its element size");
-    in[5] = bytes_at(lse, need);
+    if (reinterpret_cast<uintptr_t>(lse) % 4 != 0) return fail(BSM_ERR_INVALID_ARG, "lse is not aligned to its element size");
+    if (reinterpret_cast<uintptr_t>(workspace) % 16 != 0) return fail(BSM_ERR_INVALID_ARG, "workspace is not aligned to 16 bytes");
+    in[5] = bytes_at(lse, lse_bytes);
     out[3] = bytes_at(workspace, need);
     in[6] = {};
     for (const Span& x : out)
@@ -334,6 +344,7 @@ bsm_status backward(bsm_attention_plan p, const bsm_heads* q, const bsm_heads* k
     }
     a.lse = const_cast<float*>(lse);
     a.delta = static_cast<float*>(workspace);
+    a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + delta_bytes(s));
     a.total_q = s.total_q;
     a.group = s.heads_q / s.heads_kv;
     a.dim = s.dim;
@@ -344,7 +355,7 @@ bsm_status backward(bsm_attention_plan p, const bsm_heads* q, const bsm_heads* k
     hipError_t e = g.enter(p->device);
     if (e != hipSuccess) return hip_fail(e, "hipSetDevice");
     const bsm_att::Unit* units = static_cast<const bsm_att::Unit*>(p->d_units);
-    e = bsm_att::launch_attention_backward(a, units, p->n_q, units + p->n_q, p->n_kv, static_cast<hipStream_t>(stream));
+    e = bsm_att::launch_attention_backward(a, units, p->n_q, units + p->n_q, p->n_kv, p->n_join, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "kernel launch");
     p->used = true;
     return BSM_OK;
@@ -568,7 +579,7 @@ bsm_status bsm_attention_plan_describe(bsm_attention_plan plan, bsm_attention_st
     stats->q_units = plan->n_q;
     stats->kv_units = plan->n_kv;
     stats->lse_elems = s.heads_q * s.total_q;
-    stats->workspace_bytes = workspace_of(s);
+    stats->workspace_bytes = workspace_of(plan);
     stats->pairs = s.pairs;
     stats->heads_q = s.heads_q;
     stats->heads_kv = s.heads_kv;

@@ -11,12 +11,14 @@ namespace bsm_att {
 // forward pass and dq, key rows for dk and dv.  A unit without rows (rows == 0) does nothing.
 struct Unit {
     int64_t q_start, kv_start;  // the sequence's first row in the caller's tensors
-    int64_t lse_row;            // its first row in the compact numbering of the plan
+    int64_t lse_row;            // its first query row in the compact numbering of the plan
+    int64_t part_row;           // first row of the unit's parts (see SequenceArgs)
     int32_t seq, head;          // head: query head, or key/value head
     int32_t first, rows;        // the unit's rows within the sequence
     int32_t q_len, kv_len;
+    int32_t part, parts;        // which of the unit's workgroups this is
 };
-static_assert(sizeof(Unit) == 48, "");
+static_assert(sizeof(Unit) == 64, "");
 
 constexpr int kTileRows = 128;
 
@@ -42,14 +44,18 @@ struct SequenceArgs {
     int32_t dim;
     Mask mask;
     float scale;
+    // Sums of key units that several workgroups share, a range of the steps each: row r of part p is row
+    // part_row + p rows + r of [row][dk, dv][padded_dim] fp32; added up in order.
+    float* part;
 };
 
 bool aligned_pieces(const Heads& t);  // 16-byte pieces on 16-byte boundaries
 
 hipError_t launch_attention(const SequenceArgs& a, const Unit* units, int64_t n, hipStream_t stream);
 // dq (and delta), then dk and dv, which read delta
+// and joins the parts of the n_join units behind the n_kv ones
 hipError_t launch_attention_backward(const SequenceArgs& a, const Unit* q_units, int64_t n_q, const Unit* kv_units,
-                                     int64_t n_kv, hipStream_t stream);
+                                     int64_t n_kv, int64_t n_join, hipStream_t stream);
 
 // ------------------------------------------------------------------------------ paged cache
 struct Cache {

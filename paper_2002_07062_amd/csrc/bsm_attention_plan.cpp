@@ -1,6 +1,7 @@
 #include "bsm_attention_plan.hpp"
 
 #include <algorithm>
+#include <functional>
 #include <numeric>
 
 namespace bsm_att {
@@ -65,6 +66,51 @@ int64_t key_steps(const Sequences& s, int64_t b, int64_t first, int64_t rows) {
         if (s.mask.window > 0) hi = std::min<int64_t>(hi, first + rows - 1 + s.mask.window - off);
     }
     return hi > lo ? (hi - lo / kStep * kStep + kStep - 1) / kStep * (s.heads_q / s.heads_kv) : 0;
+}
+
+// Workgroups that a key unit of `steps` is cut for, none of which is to take many more than `share`.  Parts
+// of fewer than eight steps would mostly load their keys and store their sums.
+int64_t parts_of(int64_t steps, int64_t share) {
+    return std::max<int64_t>(1, std::min<int64_t>({(steps + share - 1) / share, steps / 8, 64}));
+}
+
+// The share for which `slots` workgroups at a time, the longest first, are done soonest.  A cut costs its
+// parts' loads and stores, two steps each, and the joining launch, four.  At best the slots' shares are equal;
+// shares of up to half again as many steps can be faster, as with equal ones a few parts may be left over for
+// a round of their own.
+int64_t key_share(const Sequences& s, int64_t slots) {
+    std::vector<int64_t> steps;
+    int64_t total = 0, longest = 0;
+    for (int64_t b = 0; b < s.batch; ++b)
+        for (int64_t first = 0; first < s.kv_len[b]; first += kTileRows) {
+            const int64_t n = key_steps(s, b, first, std::min<int64_t>(kTileRows, s.kv_len[b] - first));
+            steps.push_back(n);
+            total += n * s.heads_kv;
+            longest = std::max(longest, n);
+        }
+    const int64_t uncut = std::max<int64_t>(1, longest), even = std::max<int64_t>(1, (total + slots - 1) / slots);
+    if (even >= uncut) return uncut;
+    int64_t best = 0, best_share = uncut;
+    std::vector<int64_t> costs, load;
+    for (int64_t share : {uncut, even, even + even / 8, even + even / 4, even + even / 2}) {
+        costs.clear();
+        for (int64_t n : steps)
+            for (int64_t i = 0, parts = parts_of(n, share); i < parts * s.heads_kv; ++i) costs.push_back(2 + (n + parts - 1) / parts);
+        std::sort(costs.begin(), costs.end(), std::greater<int64_t>());
+        load.assign(slots, 0);  // a heap, the least loaded slot first
+        int64_t end = 0;
+        for (int64_t c : costs) {
+            std::pop_heap(load.begin(), load.end(), std::greater<int64_t>());
+            end = std::max(end, load.back() += c);
+            std::push_heap(load.begin(), load.end(), std::greater<int64_t>());
+        }
+        if (costs.size() > steps.size() * s.heads_kv) end += 4;
+        if (best == 0 || end < best) {
+            best = end;
+            best_share = share;
+        }
+    }
+    return best_share;
 }
 
 struct Costed {
@@ -134,8 +180,8 @@ std::vector<Unit> query_units(const Sequences& s, bsm_schedule schedule, int n_x
         for (int head = 0; head < s.heads_q; ++head)
             for (int64_t first = 0; first < s.q_len[b]; first += kTileRows) {
                 const int64_t rows = std::min<int64_t>(kTileRows, s.q_len[b] - first);
-                units.push_back({{s.q_start[b], s.kv_start[b], lse_row, static_cast<int32_t>(b), head,
-                                  static_cast<int32_t>(first), static_cast<int32_t>(rows), s.q_len[b], s.kv_len[b]},
+                units.push_back({{s.q_start[b], s.kv_start[b], lse_row, 0, static_cast<int32_t>(b), head,
+                                  static_cast<int32_t>(first), static_cast<int32_t>(rows), s.q_len[b], s.kv_len[b], 0, 1},
                                  2 + query_steps(s, b, first, rows), b * s.heads_kv + head / group});
             }
         lse_row += s.q_len[b];
@@ -143,20 +189,29 @@ std::vector<Unit> query_units(const Sequences& s, bsm_schedule schedule, int n_x
     return order(units, schedule, n_xcd, s.batch * s.heads_kv);
 }
 
-std::vector<Unit> key_units(const Sequences& s, bsm_schedule schedule, int n_xcd) {
+KeyUnits key_units(const Sequences& s, bsm_schedule schedule, int n_xcd, int n_cu) {
+    const int64_t share = key_share(s, padded_dim(s.dim) > 64 ? n_cu : 2 * static_cast<int64_t>(n_cu));
+    KeyUnits out;
     std::vector<Costed> units;
     int64_t lse_row = 0;
     for (int64_t b = 0; b < s.batch; ++b) {
         for (int head = 0; head < s.heads_kv; ++head)
             for (int64_t first = 0; first < s.kv_len[b]; first += kTileRows) {
-                const int64_t rows = std::min<int64_t>(kTileRows, s.kv_len[b] - first);
-                units.push_back({{s.q_start[b], s.kv_start[b], lse_row, static_cast<int32_t>(b), head,
-                                  static_cast<int32_t>(first), static_cast<int32_t>(rows), s.q_len[b], s.kv_len[b]},
-                                 2 + key_steps(s, b, first, rows), b * s.heads_kv + head});
+                const int64_t rows = std::min<int64_t>(kTileRows, s.kv_len[b] - first), steps = key_steps(s, b, first, rows);
+                const int64_t parts = parts_of(steps, share);
+                Unit u{s.q_start[b], s.kv_start[b], lse_row, out.part_rows, static_cast<int32_t>(b), head,
+                       static_cast<int32_t>(first), static_cast<int32_t>(rows), s.q_len[b], s.kv_len[b], 0, static_cast<int32_t>(parts)};
+                if (parts > 1) {
+                    out.joins.push_back(u);
+                    out.part_rows += parts * rows;
+                }
+                for (u.part = 0; u.part < u.parts; ++u.part)
+                    units.push_back({u, 2 + steps / parts, b * s.heads_kv + head});
             }
         lse_row += s.q_len[b];
     }
-    return order(units, schedule, n_xcd, s.batch * s.heads_kv);
+    out.units = order(units, schedule, n_xcd, s.batch * s.heads_kv);
+    return out;
 }
 
 PagedCut cut_paged(int64_t batch, int64_t tokens, int32_t heads_kv, int32_t group, int32_t dim, int32_t max_q,

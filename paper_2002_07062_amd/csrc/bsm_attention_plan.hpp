@@ -27,10 +27,16 @@ struct Sequences {
 // Fills the starts (packed where null) and the totals from the lengths.
 void finish_sequences(Sequences* s, const int64_t* q_start, const int64_t* kv_start);
 
-// Units of 128 query rows (forward pass, dq) or of 128 keys (dk, dv), in launch order; the unit of
+// Units of 128 query rows (forward pass, dq), in launch order; the unit of
 // workgroup w is expected to run on XCD w mod n_xcd.
 std::vector<Unit> query_units(const Sequences& s, bsm_schedule schedule, int n_xcd);
-std::vector<Unit> key_units(const Sequences& s, bsm_schedule schedule, int n_xcd);
+
+// Of 128 keys (dk, dv).  Units that would still run when the others' CUs are done are cut into parts.
+struct KeyUnits {
+    std::vector<Unit> units, joins;  // joins: the units with parts
+    int64_t part_rows = 0;           // rows of all parts
+};
+KeyUnits key_units(const Sequences& s, bsm_schedule schedule, int n_xcd, int n_cu);
 
 // How attention over a paged cache is cut.
 struct PagedCut {

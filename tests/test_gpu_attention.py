@@ -88,6 +88,34 @@ def test_schedules_and_repeats_give_the_same_bits(case):
             assert torch.equal(x, y)
 
 
+# few keys for many query rows: several workgroups share the query rows of 128 keys
+PARTED = [
+    ([2048], None, 2, 1, 128, True, 0, "packed"),
+    ([1500], [1100], 4, 1, 64, False, 0, "shifted"),
+    ([1030, 0, 31, 700], [1500, 9, 0, 40], 4, 1, 80, True, 0, "padded"),
+    ([1700, 40], None, 8, 1, 96, True, 300, "fused"),
+    ([4000], [1], 1, 1, 40, False, 0, "heads_first"),
+]
+
+
+@pytest.mark.parametrize("case", PARTED, ids=_name)
+def test_gradients_of_few_keys(case):
+    batch, scale = _batch(case, 9), float(np.float32(1 / np.sqrt(case[4])))
+    plan, o, lse = _run(batch, case[5], case[6])
+    assert plan.workspace_bytes > 4 * lse.numel() + 16  # there are parts
+    dout = batch.operand("q")
+    seen = []
+    for schedule in ("balanced", "xcd", "rr"):
+        plan = bsm.bsm_attention_plan_create(**batch.plan_args(case[5], case[6], schedule))
+        dq, dk, dv = batch.empty("q"), batch.empty("kv"), batch.empty("kv")
+        ws = torch.full((plan.workspace_bytes,), 255, dtype=torch.uint8, device="cuda")  # NaN
+        bsm.bsm_attention_backward(plan, batch.q, batch.k, batch.v, o, lse, dout, dq, dk, dv, workspace=ws)
+        torch.cuda.synchronize()
+        check_backward(batch, o, lse, dout, dq, dk, dv, scale, case[5], case[6])
+        seen.append([x.contiguous().view(torch.int16) for x in (dq, dk, dv)])
+    assert all(torch.equal(x, y) for other in seen[1:] for x, y in zip(seen[0], other))
+
+
 @pytest.mark.parametrize("scale", [1e-3, 1.0, 8.0])
 def test_scales(scale):
     """Flat rows, and rows that one key takes almost whole (scores of several hundred)."""

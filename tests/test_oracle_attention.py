@@ -114,6 +114,26 @@ def test_plan_stats(q_len, kv_len, causal, window):
     assert (d["total_q"], d["total_kv"], d["causal"], d["window"]) == (sum(q_len), sum(kv_len), causal, window)
 
 
+@pytest.mark.parametrize("q_len,kv_len,parted", [([4096], [4096], True), ([4096] * 64, [4096] * 64, False),
+                                                 ([9], [4096], False),
+                                                 # causal: the last 130 queries alone see keys, 3 steps of 64 by 2 heads
+                                                 ([8192, 30], [130, 30], False)])
+def test_plan_parts_of_few_keys(q_len, kv_len, parted):
+    """Units that alone would keep few compute units busy are cut into parts, within bounds of the
+    work table and the workspace."""
+    whole = 2 * sum(-(-m // 128) for m in kv_len)
+    for n_cu in (0, 64, 256):
+        d = bsm.bsm_attention_plan_describe(_plan(q_len, kv_len, causal=True, topology=dict(n_xcd=8, n_cu=n_cu)))
+        slots = 2 * (n_cu or 256)  # head dimension 64: two workgroups on a compute unit
+        assert d["workspace_bytes"] <= 16 * sum(q_len) + 2 * slots * 128 * 1024
+        assert d["kv_units"] <= whole + 2 * slots
+        if not parted or n_cu != 64:
+            assert (d["kv_units"] > whole) == parted
+            assert (d["workspace_bytes"] > 16 * sum(q_len)) == parted
+    st, m = _status(_plan, topology=dict(n_xcd=8, n_cu=-1))
+    assert st == bsm.BSM_ERR_INVALID_ARG and "n_cu" in m
+
+
 def test_plan_allocation_failure(monkeypatch):
     monkeypatch.setenv("BSM_TEST_ALLOC_FAIL", "host")
     assert _status(_plan)[0] == bsm.BSM_ERR_OOM
