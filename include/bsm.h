@@ -378,9 +378,9 @@ bsm_status bsm_gemm(const void* a, const void* b, void* c, int64_t batch, int32_
  * makes its row NaN.
  *
  * Results depend on the operands and sizes only: no sum's order depends on timing, so repeated
- * calls give the same bits under every schedule.  (The last bits of dk and dv depend on the other
- * sequences of the batch and the number of compute units as well: where the keys alone leave some
- * without work, their query rows are added up in parts.) */
+ * calls give the same bits under every schedule.  (The last bits depend on the batch's other
+ * sequences and the number of compute units as well: where units of 128 rows would leave some
+ * without work, the sums of o, dq, dk and dv are taken in parts.) */
 
 /* Element (b, row, head, d) of an operand lies at data + b*seq + row*row + head*head + d, in
  * elements, so packed tokens (seq 0), padded batches, heads-first layouts and views of a fused
@@ -396,7 +396,7 @@ typedef struct bsm_heads {
 typedef struct bsm_attention_stats {
     int64_t batch;
     int64_t total_q, total_kv;     /* query rows and keys over all sequences */
-    int64_t q_units, kv_units;     /* workgroups of the forward pass and dq, and of dk and dv */
+    int64_t q_units, kv_units;     /* workgroups of the forward pass, and of dk and dv */
     int64_t lse_elems;             /* fp32 values of lse: heads_q * total_q */
     int64_t workspace_bytes;       /* what bsm_attention_backward needs */
     int64_t pairs;                 /* query/key pairs that the mask leaves, of one query head */
@@ -415,7 +415,7 @@ typedef struct bsm_attention_plan_s* bsm_attention_plan;
  *   heads_q, heads_kv  heads_q is a multiple of heads_kv
  *   head_dim           a multiple of 8 up to 128 (else BSM_ERR_UNSUPPORTED)
  *   causal, window     the mask; window > 0 needs causal
- *   schedule           order of the work, 128 rows of one head at a time: RR as the sequences
+ *   schedule           order of the work, up to 128 rows of one head at a time: RR as the sequences
  *                      come; XCD every key/value head's work on one XCD, the heads dealt to the
  *                      XCDs by their cost, the longest first; BALANCED the same, but an XCD that
  *                      has done its own takes over from the one that has most left

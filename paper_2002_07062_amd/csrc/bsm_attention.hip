@@ -28,15 +28,44 @@ __device__ __forceinline__ Seen seen_keys(int i, int q_len, int kv_len, Mask m) 
     return s;
 }
 
+// Where two waves that share query rows hand over sums and statistics, one lane's: word n at n * kWave.
+template <int D>
+__device__ __forceinline__ float* exchange(void* lds, int pair, int lane) {
+    static_assert(2 * (D / 2 + 2) * kWave * 4 <= 4 * kKeys * 2 * Tile<D>::kPitch, "two pairs within the tiles");
+    return static_cast<float*>(lds) + pair * (D / 2 + 2) * kWave + lane;
+}
+template <int TILES, class F>
+__device__ __forceinline__ void each_sum(f32x16 (&acc)[TILES], F f) {
+#pragma unroll
+    for (int t = 0; t < TILES; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            float v = acc[t][e];
+            f(16 * t + e, v);
+            acc[t][e] = v;
+        }
+}
+
 // ------------------------------------------------------------------------------------ forward
-template <int D, bool DIRECT>
+// o_i = sum_j exp(s_ij - lse_i) v_j in one pass over the keys (see Online): each wave keeps 32 query rows, its
+// operand of the scores, their output and statistics in registers, and the workgroup brings 64 keys and
+// values at a time through LDS, the next ones on their way meanwhile.  Two workgroups share a CU.  Whole
+// blocks that the mask hides are left out, and blocks that it does not touch are not masked.
+// KS = 1: four waves of 32 rows.  KS = 2: 64 rows, two waves of each 32 with half of every step's keys, joined
+// at the end; for plans whose longest units would outlast the others (see query_rows).
+// Bound by the matrix cores with the exponentials between them, and on random data by the power that both
+// take: 4 x 4096 causal rows, 32/8 heads of 128, 561 us = 980 TFLOP/s (two 8192^3 products of a library on the
+// same card: 1200 .. 1400); without the exponentials and sums it would be 13% less time.
+template <int D, bool DIRECT, int KS>
 __global__ __launch_bounds__(kThreads, 2) void attention_kernel(const SequenceArgs a, const Unit* __restrict__ units) {
     __shared__ __align__(16) uint16_t lds[2][2][kKeys * Tile<D>::kPitch];  // buffer, K or V
     const Unit u = units[blockIdx.x];
     if (u.rows <= 0) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, li = lane & 31, h = lane >> 5;
     const int chunks = a.dim / 8;
-    const int i0 = u.first + kRows * wave, i = i0 + li;
+    constexpr int kRowWaves = kThreads / kWave / KS, kBlocks = kKeys / 32 / KS;
+    const int i0 = u.first + kRows * (wave % kRowWaves), i = i0 + li;
+    const int x = wave / kRowWaves;  // which of every step's keys
     const bool live = i < u.first + u.rows;
     RowOperand<D> q;
     q.load(at(a.q, u, u.q_start + i, u.head), live, h, chunks);
@@ -64,8 +93,9 @@ __global__ __launch_bounds__(kThreads, 2) void attention_kernel(const SequenceAr
         sk.end(tid, lds[0][0]);
         sv.end(tid, lds[0][1]);
     }
-    const RowFrags<D> rows_at(lane);
-    const ColFrags<D> cols_at(lane);
+    const int offset = x * 32 * kBlocks;
+    const RowFrags<D> rows_at(lane, offset * Tile<D>::kRowBytes);
+    const ColFrags<D> cols_at(lane, 0, offset * Tile<D>::kRowBytes);
     // the tiles read and the tiles written in a step are apart
     auto step = [&](int j0, uint16_t* __restrict__ next_k, uint16_t* __restrict__ next_v, const uint16_t* __restrict__ now_k,
                     const uint16_t* __restrict__ now_v) __attribute__((always_inline)) {
@@ -75,15 +105,16 @@ __global__ __launch_bounds__(kThreads, 2) void attention_kernel(const SequenceAr
             sk.begin(tid, next_k, kp + next * a.k.row, a.k.row, 0, u.kv_len - next, chunks);
             sv.begin(tid, next_v, vp + next * a.v.row, a.v.row, 0, u.kv_len - next, chunks);
         }
-        if (any_row && j0 <= w1.hi && next > w0.lo) {
-            f32x16 s[kKeys / 32];
+        const int j = j0 + offset, j_end = j + 32 * kBlocks;
+        if (any_row && j <= w1.hi && j_end > w0.lo) {
+            f32x16 s[kBlocks];
             row_product<D>(s, rows_at, now_k, 0, q);
-            if (j0 < w1.lo || next - 1 > w0.hi) {
+            if (j < w1.lo || j_end - 1 > w0.hi) {
 #pragma unroll
-                for (int k = 0; k < kKeys / 32; ++k) mask_block(s[k], j0 + 32 * k, h, mine.lo, mine.hi);
+                for (int k = 0; k < kBlocks; ++k) mask_block(s[k], j + 32 * k, h, mine.lo, mine.hi);
             }
             st.weigh(s, c);
-            bf16x8 p[kKeys / 16];
+            bf16x8 p[2 * kBlocks];
             to_operands(p, s);
             col_product(st.o, cols_at, now_v, 0, p);
         }
@@ -93,7 +124,23 @@ __global__ __launch_bounds__(kThreads, 2) void attention_kernel(const SequenceAr
         }
     };
     in_turn(begin, end, kKeys, [&](int j0, auto buf) { step(j0, lds[1 - buf][0], lds[1 - buf][1], lds[buf][0], lds[buf][1]); });
-    const float total = st.row_sum();
+    float total = st.row_sum();
+    if constexpr (KS == 2) {  // the other wave's part of the row: under the larger reference of the two
+        float* other = exchange<D>(lds, wave % kRowWaves, lane);
+        lds_barrier();  // the tiles are read
+        if (x == 1) {
+            each_sum(st.o, [&](int n, float v) { other[n * kWave] = v; });
+            other[D / 2 * kWave] = st.m;
+            other[(D / 2 + 1) * kWave] = total;
+        }
+        lds_barrier();
+        if (x == 1) return;
+        const float m = other[D / 2 * kWave], ref = fmaxf(st.m, m);
+        const float f0 = st.m == -kInf ? 0.0f : __builtin_amdgcn_exp2f(st.m - ref), f1 = m == -kInf ? 0.0f : __builtin_amdgcn_exp2f(m - ref);
+        each_sum(st.o, [&](int n, float& v) { v = f0 * v + f1 * other[n * kWave]; });
+        total = f0 * total + f1 * other[(D / 2 + 1) * kWave];
+        st.m = ref;
+    }
     // a row that sees nothing, or only scores of -inf, is zero
     const float f = total == 0.0f ? 0.0f : 1.0f / total;
     uint16_t* out = a.o.p + u.seq * a.o.seq + (u.q_start + i) * a.o.row + u.head * a.o.head;
@@ -107,15 +154,18 @@ __global__ __launch_bounds__(kThreads, 2) void attention_kernel(const SequenceAr
 __device__ __forceinline__ float reference(float lse) { return lse == -kInf ? kInf : lse * kLog2e; }
 
 // dq = scale * sum_j dS_ij k_j, with dS = P (dP - delta), P = exp(s - lse), dP = do . v: query rows
-// stay in registers as in the forward pass, the keys stream through LDS.  Also leaves delta.
-template <int D, bool DIRECT>
+// stay in registers as in the forward pass, the keys stream through LDS.  Also leaves delta.  4 x 4096 causal
+// rows, 32/8 heads of 128: 830 us = 994 TFLOP/s.  KS as in the forward pass.
+template <int D, bool DIRECT, int KS>
 __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(const SequenceArgs a, const Unit* __restrict__ units) {
     __shared__ __align__(16) uint16_t lds[2][2][kKeys * Tile<D>::kPitch];
     const Unit u = units[blockIdx.x];
     if (u.rows <= 0) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, li = lane & 31, h = lane >> 5;
     const int chunks = a.dim / 8;
-    const int i0 = u.first + kRows * wave, i = i0 + li;
+    constexpr int kRowWaves = kThreads / kWave / KS, kBlocks = kKeys / 32 / KS;
+    const int i0 = u.first + kRows * (wave % kRowWaves), i = i0 + li;
+    const int x = wave / kRowWaves;  // which of every step's keys
     const bool live = i < u.first + u.rows;
     RowOperand<D> q, dout;
     q.load(at(a.q, u, u.q_start + i, u.head), live, h, chunks);
@@ -133,7 +183,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(const Sequenc
         const int64_t r = u.head * a.total_q + u.lse_row + i;
         if (live) {
             lse = a.lse[r];
-            if (h == 0) a.delta[r] = delta;
+            if (h == 0 && x == 0) a.delta[r] = delta;
         }
     }
     const float ref = reference(lse);
@@ -159,8 +209,9 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(const Sequenc
         sk.end(tid, lds[0][0]);
         sv.end(tid, lds[0][1]);
     }
-    const RowFrags<D> rows_at(lane);
-    const ColFrags<D> cols_at(lane);
+    const int offset = x * 32 * kBlocks;
+    const RowFrags<D> rows_at(lane, offset * Tile<D>::kRowBytes);
+    const ColFrags<D> cols_at(lane, 0, offset * Tile<D>::kRowBytes);
     auto step = [&](int j0, uint16_t* __restrict__ next_k, uint16_t* __restrict__ next_v, const uint16_t* __restrict__ now_k,
                     const uint16_t* __restrict__ now_v) __attribute__((always_inline)) {
         tile_barrier<DIRECT>();
@@ -169,14 +220,15 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(const Sequenc
             sk.begin(tid, next_k, kp + next * a.k.row, a.k.row, 0, u.kv_len - next, chunks);
             sv.begin(tid, next_v, vp + next * a.v.row, a.v.row, 0, u.kv_len - next, chunks);
         }
-        if (any_row && j0 <= w1.hi && next > w0.lo) {
-            const bool masked = j0 < w1.lo || next - 1 > w0.hi;
+        const int j = j0 + offset, j_end = j + 32 * kBlocks;
+        if (any_row && j <= w1.hi && j_end > w0.lo) {
+            const bool masked = j < w1.lo || j_end - 1 > w0.hi;
 #pragma unroll
-            for (int k = 0; k < kKeys / 32; ++k) {
+            for (int k = 0; k < kBlocks; ++k) {
                 f32x16 s[1], dp[1];
                 row_product<D>(s, rows_at, now_k, 32 * k, q);
                 row_product<D>(dp, rows_at, now_v, 32 * k, dout);
-                if (masked) mask_block(s[0], j0 + 32 * k, h, mine.lo, mine.hi);
+                if (masked) mask_block(s[0], j + 32 * k, h, mine.lo, mine.hi);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[0][e], c, -ref));
@@ -195,6 +247,16 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(const Sequenc
         }
     };
     in_turn(begin, end, kKeys, [&](int j0, auto buf) { step(j0, lds[1 - buf][0], lds[1 - buf][1], lds[buf][0], lds[buf][1]); });
+    if constexpr (KS == 2) {
+        float* other = exchange<D>(lds, wave % kRowWaves, lane);
+        lds_barrier();  // the tiles are read
+        if (x == 1) {
+            each_sum(dq, [&](int n, float v) { other[n * kWave] = v; });
+        }
+        lds_barrier();
+        if (x == 1) return;
+        each_sum(dq, [&](int n, float& v) { v += other[n * kWave]; });
+    }
     if (lse == -kInf) {  // the row saw nothing: no gradient, whatever dout holds
 #pragma unroll
         for (int t = 0; t < D / 32; ++t) dq[t] = zero16();
@@ -411,16 +473,20 @@ __global__ __launch_bounds__(Dkv<D>::kThreads, 2) void attention_dkv_kernel(cons
     }
 }
 
-// Adds up the parts of a unit's dk and dv, in order: a thread per 8 columns of a row of one of them.
+// Adds up the parts of a unit's dk and dv, in order: a thread per 8 columns of a row of one of them, and
+// kJoinSlices workgroups per unit, as a few units of many parts would keep too few CUs reading (one workgroup
+// each took 62 us for 32 units of 16 parts, 33 MB).
+constexpr int kJoinSlices = 8;
 template <int D>
 __global__ __launch_bounds__(kThreads) void attention_dkv_join_kernel(const SequenceArgs a, const Unit* __restrict__ units) {
     const Unit u = units[blockIdx.x];
     const int chunks = a.dim / 8;
     const int64_t step = static_cast<int64_t>(u.rows) * 2 * D;
-    for (int x = threadIdx.x; x < 2 * u.rows * chunks; x += kThreads) {
+    for (int x = blockIdx.y * kThreads + threadIdx.x; x < 2 * u.rows * chunks; x += kThreads * kJoinSlices) {
         const int c = x % chunks, is_v = x / chunks % 2, j = x / chunks / 2;
         const float* from = a.part + ((u.part_row + j) * 2 + is_v) * D + 8 * c;
         f32x4 lo = {0.0f, 0.0f, 0.0f, 0.0f}, hi = lo;
+#pragma unroll 4
         for (int p = 0; p < u.parts; ++p) {
             const f32x4 y = *reinterpret_cast<const f32x4*>(from + p * step), z = *reinterpret_cast<const f32x4*>(from + p * step + 4);
 #pragma unroll
@@ -467,7 +533,10 @@ hipError_t with_dim(int dim, bool direct, F f) {
 hipError_t launch_attention(const SequenceArgs& a, const Unit* units, int64_t n, hipStream_t stream) {
     if (n == 0) return hipSuccess;
     return with_dim(a.dim, aligned_pieces(a.k) && aligned_pieces(a.v), [&](auto d, auto direct) {
-        attention_kernel<d(), direct()><<<static_cast<unsigned>(n), kThreads, 0, stream>>>(a, units);
+        if (a.unit_rows == kTileRows)
+            attention_kernel<d(), direct(), 1><<<static_cast<unsigned>(n), kThreads, 0, stream>>>(a, units);
+        else
+            attention_kernel<d(), direct(), 2><<<static_cast<unsigned>(n), kThreads, 0, stream>>>(a, units);
     });
 }
 
@@ -476,7 +545,10 @@ hipError_t launch_attention_backward(const SequenceArgs& a, const Unit* q_units,
     hipError_t e = hipSuccess;
     if (n_q > 0)
         e = with_dim(a.dim, aligned_pieces(a.k) && aligned_pieces(a.v), [&](auto d, auto direct) {
-            attention_dq_kernel<d(), direct()><<<static_cast<unsigned>(n_q), kThreads, 0, stream>>>(a, q_units);
+            if (d() > 64 || a.unit_rows == kTileRows)
+                attention_dq_kernel<d(), direct(), 1><<<static_cast<unsigned>(n_q), kThreads, 0, stream>>>(a, q_units);
+            else
+                attention_dq_kernel<64, direct(), 2><<<static_cast<unsigned>(n_q), kThreads, 0, stream>>>(a, q_units);
         });
     if (e == hipSuccess && n_kv > 0)
         e = with_dim(a.dim, aligned_pieces(a.q) && aligned_pieces(a.dout), [&](auto d, auto direct) {
@@ -484,7 +556,7 @@ hipError_t launch_attention_backward(const SequenceArgs& a, const Unit* q_units,
         });
     if (e == hipSuccess && n_join > 0)
         e = with_dim(a.dim, true, [&](auto d, auto) {
-            attention_dkv_join_kernel<d()><<<static_cast<unsigned>(n_join), kThreads, 0, stream>>>(a, kv_units + n_kv);
+            attention_dkv_join_kernel<d()><<<dim3(static_cast<unsigned>(n_join), kJoinSlices), kThreads, 0, stream>>>(a, kv_units + n_kv);
         });
     return e;
 }

@@ -24,7 +24,9 @@ struct bsm_attention_plan_s {
     int n_xcd = 1;
     bsm_att::Sequences seqs;
     int64_t n_q = 0, n_kv = 0, n_join = 0, part_rows = 0;
-    void* d_units = nullptr;  // query units, then key units
+    int64_t n_forward = 0, first_dq = 0;  // units of the forward pass; where dq's n_q units begin
+    int32_t forward_rows = 0, dq_rows = 0;  // of these units
+    void* d_units = nullptr;  // units of the forward pass, of dq if they are others, of dk and dv, and their joins
     std::atomic<bool> used{false};
 };
 
@@ -221,31 +223,40 @@ bsm_status create(bsm_attention_plan* out_plan, const int32_t* q_len, const int3
         const double units = (static_cast<double>(s.total_q) / bsm_att::kTileRows + batch) * heads_q +
                              (static_cast<double>(s.total_kv) / bsm_att::kTileRows + batch) * heads_kv;
         if (units > kMostWorkgroups) return fail(BSM_ERR_INVALID_ARG, "too many rows for one plan");
-        std::vector<bsm_att::Unit> q = bsm_att::query_units(s, schedule, n_xcd);
+        p->forward_rows = bsm_att::query_rows(s, n_cu);
+        // (dq of longer heads has no half units: they need more registers than there are, and were no faster)
+        p->dq_rows = bsm_att::padded_dim(s.dim) > 64 ? bsm_att::kTileRows : p->forward_rows;
+        std::vector<bsm_att::Unit> table = bsm_att::query_units(s, schedule, n_xcd, p->forward_rows);
+        p->n_forward = static_cast<int64_t>(table.size());
+        if (p->dq_rows != p->forward_rows) {
+            const std::vector<bsm_att::Unit> dq = bsm_att::query_units(s, schedule, n_xcd, p->dq_rows);
+            p->first_dq = p->n_forward;
+            table.insert(table.end(), dq.begin(), dq.end());
+        }
+        p->n_q = static_cast<int64_t>(table.size()) - p->first_dq;
         const bsm_att::KeyUnits kv = bsm_att::key_units(s, schedule, n_xcd, n_cu);
-        p->n_q = static_cast<int64_t>(q.size());
         p->n_kv = static_cast<int64_t>(kv.units.size());
         p->n_join = static_cast<int64_t>(kv.joins.size());
         p->part_rows = kv.part_rows;
-        if (std::max(p->n_q, p->n_kv) > kMostWorkgroups) return fail(BSM_ERR_INVALID_ARG, "too many rows for one plan");
+        if (std::max(p->n_forward, p->n_kv) > kMostWorkgroups) return fail(BSM_ERR_INVALID_ARG, "too many rows for one plan");
         p->device = device;
         p->schedule = schedule;
         p->n_xcd = n_xcd;
         if (fails("host")) throw std::bad_alloc();
         if (device >= 0 && p->n_q + p->n_kv > 0) {
-            q.insert(q.end(), kv.units.begin(), kv.units.end());
-            q.insert(q.end(), kv.joins.begin(), kv.joins.end());
+            table.insert(table.end(), kv.units.begin(), kv.units.end());
+            table.insert(table.end(), kv.joins.begin(), kv.joins.end());
             DeviceGuard g;
             hipError_t e = g.enter(device);
             if (e != hipSuccess) return hip_fail(e, "hipSetDevice");
-            const size_t bytes = q.size() * sizeof(bsm_att::Unit);
+            const size_t bytes = table.size() * sizeof(bsm_att::Unit);
             e = fails("device") ? hipErrorOutOfMemory : hipMalloc(&p->d_units, bytes);
             if (e != hipSuccess) {
                 (void)hipGetLastError();
                 return fail(e == hipErrorOutOfMemory ? BSM_ERR_OOM : BSM_ERR_HIP, "hipMalloc(%zu) for the work table: %s", bytes,
                             hipGetErrorString(e));
             }
-            e = hipMemcpy(p->d_units, q.data(), bytes, hipMemcpyHostToDevice);
+            e = hipMemcpy(p->d_units, table.data(), bytes, hipMemcpyHostToDevice);
             if (e != hipSuccess) {
                 st = hip_fail(e, "uploading the work table");
                 (void)hipFree(p->d_units);
@@ -283,17 +294,18 @@ bsm_status forward(bsm_attention_plan p, const bsm_heads* q, const bsm_heads* k,
     if (overlap(so, sq) || overlap(so, sk) || overlap(so, sv)) return fail(BSM_ERR_ALIAS, "o overlaps an operand");
     if (overlap(sl, sq) || overlap(sl, sk) || overlap(sl, sv) || overlap(sl, so)) return fail(BSM_ERR_ALIAS, "lse overlaps an operand");
     if (reinterpret_cast<uintptr_t>(lse) % 4 != 0) return fail(BSM_ERR_INVALID_ARG, "lse is not aligned to its element size");
-    if (p->n_q == 0) return BSM_OK;
+    if (p->n_forward == 0) return BSM_OK;
     a.lse = lse;
     a.total_q = s.total_q;
     a.group = s.heads_q / s.heads_kv;
     a.dim = s.dim;
+    a.unit_rows = p->forward_rows;
     a.mask = s.mask;
     a.scale = scale;
     DeviceGuard g;
     hipError_t e = g.enter(p->device);
     if (e != hipSuccess) return hip_fail(e, "hipSetDevice");
-    e = bsm_att::launch_attention(a, static_cast<const bsm_att::Unit*>(p->d_units), p->n_q, static_cast<hipStream_t>(stream));
+    e = bsm_att::launch_attention(a, static_cast<const bsm_att::Unit*>(p->d_units), p->n_forward, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "kernel launch");
     p->used = true;
     return BSM_OK;
@@ -348,13 +360,14 @@ bsm_status backward(bsm_attention_plan p, const bsm_heads* q, const bsm_heads* k
     a.total_q = s.total_q;
     a.group = s.heads_q / s.heads_kv;
     a.dim = s.dim;
+    a.unit_rows = p->dq_rows;
     a.mask = s.mask;
     a.scale = scale;
     if (p->n_q + p->n_kv == 0) return BSM_OK;
     DeviceGuard g;
     hipError_t e = g.enter(p->device);
     if (e != hipSuccess) return hip_fail(e, "hipSetDevice");
-    const bsm_att::Unit* units = static_cast<const bsm_att::Unit*>(p->d_units);
+    const bsm_att::Unit* units = static_cast<const bsm_att::Unit*>(p->d_units) + p->first_dq;
     e = bsm_att::launch_attention_backward(a, units, p->n_q, units + p->n_q, p->n_kv, p->n_join, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "kernel launch");
     p->used = true;
@@ -576,7 +589,7 @@ bsm_status bsm_attention_plan_describe(bsm_attention_plan plan, bsm_attention_st
     stats->batch = s.batch;
     stats->total_q = s.total_q;
     stats->total_kv = s.total_kv;
-    stats->q_units = plan->n_q;
+    stats->q_units = plan->n_forward;
     stats->kv_units = plan->n_kv;
     stats->lse_elems = s.heads_q * s.total_q;
     stats->workspace_bytes = workspace_of(plan);

@@ -42,6 +42,7 @@ struct SequenceArgs {
     int64_t total_q;
     int32_t group;    // query heads per key/value head
     int32_t dim;
+    int32_t unit_rows;  // query rows of a query unit: kTileRows, or half of them
     Mask mask;
     float scale;
     // Sums of key units that several workgroups share, a range of the steps each: row r of part p is row

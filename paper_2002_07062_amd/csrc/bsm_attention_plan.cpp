@@ -172,17 +172,34 @@ void finish_sequences(Sequences* s, const int64_t* q_start, const int64_t* kv_st
     for (int64_t b = 0; b < s->batch; ++b) s->pairs += visible(s->q_len[b], s->kv_len[b], s->mask);
 }
 
-std::vector<Unit> query_units(const Sequences& s, bsm_schedule schedule, int n_xcd) {
+int32_t query_rows(const Sequences& s, int n_cu) {
+    // A workgroup of 64 rows takes half the time of one of 128, but brings the keys in for half the rows.  It
+    // pays where the longest unit takes 7/4 times an even share of what the CUs (two workgroups each) have to
+    // do, for longer heads 3 times.  us, 128 and 64 rows: heads of 64, 1.9 times 63.2, 53.5 (4096 rows, 16 heads,
+    // causal), an even share 88.6, 106 (the same without a mask); of 128, 3.9 times 78.6, 62.2 (8 heads, causal),
+    // 2.6 times 90.3, 90.9 (12 heads, causal), twice 83.2, 86.1 (8 heads without a mask).
+    int64_t total = 0, longest = 0;
+    for (int64_t b = 0; b < s.batch; ++b)
+        for (int64_t first = 0; first < s.q_len[b]; first += kTileRows) {
+            const int64_t n = query_steps(s, b, first, std::min<int64_t>(kTileRows, s.q_len[b] - first));
+            total += n * s.heads_q;
+            longest = std::max(longest, n);
+        }
+    const int64_t quarters = padded_dim(s.dim) > 64 ? 12 : 7;
+    return 4 * longest * 2 * n_cu > quarters * total ? kTileRows / 2 : kTileRows;
+}
+
+std::vector<Unit> query_units(const Sequences& s, bsm_schedule schedule, int n_xcd, int32_t rows) {
     std::vector<Costed> units;
     const int group = s.heads_q / s.heads_kv;
     int64_t lse_row = 0;
     for (int64_t b = 0; b < s.batch; ++b) {
         for (int head = 0; head < s.heads_q; ++head)
-            for (int64_t first = 0; first < s.q_len[b]; first += kTileRows) {
-                const int64_t rows = std::min<int64_t>(kTileRows, s.q_len[b] - first);
+            for (int64_t first = 0; first < s.q_len[b]; first += rows) {
+                const int64_t n = std::min<int64_t>(rows, s.q_len[b] - first);
                 units.push_back({{s.q_start[b], s.kv_start[b], lse_row, 0, static_cast<int32_t>(b), head,
-                                  static_cast<int32_t>(first), static_cast<int32_t>(rows), s.q_len[b], s.kv_len[b], 0, 1},
-                                 2 + query_steps(s, b, first, rows), b * s.heads_kv + head / group});
+                                  static_cast<int32_t>(first), static_cast<int32_t>(n), s.q_len[b], s.kv_len[b], 0, 1},
+                                 2 + query_steps(s, b, first, n), b * s.heads_kv + head / group});
             }
         lse_row += s.q_len[b];
     }

@@ -27,9 +27,12 @@ struct Sequences {
 // Fills the starts (packed where null) and the totals from the lengths.
 void finish_sequences(Sequences* s, const int64_t* q_start, const int64_t* kv_start);
 
-// Units of 128 query rows (forward pass, dq), in launch order; the unit of
-// workgroup w is expected to run on XCD w mod n_xcd.
-std::vector<Unit> query_units(const Sequences& s, bsm_schedule schedule, int n_xcd);
+// Rows of the forward pass's query units: 128, or 64 where the longest of 128 would outlast the others.
+int32_t query_rows(const Sequences& s, int n_cu);
+
+// Units of `rows` query rows (forward pass, dq), in launch order; the unit of workgroup w is expected
+// to run on XCD w mod n_xcd.
+std::vector<Unit> query_units(const Sequences& s, bsm_schedule schedule, int n_xcd, int32_t rows);
 
 // Of 128 keys (dk, dv).  Units that would still run when the others' CUs are done are cut into parts.
 struct KeyUnits {

@@ -42,8 +42,8 @@ def _batch(case, seed=3):
     return Batch(q_len, kv_len or q_len, hq, hk, d, layout, seed)
 
 
-def _run(batch, causal, window, schedule="balanced", scale=None, lse=True):
-    plan = bsm.bsm_attention_plan_create(**batch.plan_args(causal, window, schedule))
+def _run(batch, causal, window, schedule="balanced", scale=None, lse=True, n_cu=0):
+    plan = bsm.bsm_attention_plan_create(**batch.plan_args(causal, window, schedule), topology=dict(n_cu=n_cu) if n_cu else None)
     o = batch.empty("q")
     rows = torch.full((batch.hq, sum(batch.q_len)), 7.0, device="cuda") if lse else None
     bsm.bsm_attention_execute(plan, batch.q, batch.k, batch.v, o, lse=rows, scale=scale)
@@ -51,18 +51,21 @@ def _run(batch, causal, window, schedule="balanced", scale=None, lse=True):
     return plan, o, rows
 
 
+# planned for one compute unit the work is not cut into halves and parts, for all of them it is
+@pytest.mark.parametrize("n_cu", [0, 1])
 @pytest.mark.parametrize("case", CASES, ids=_name)
-def test_forward_matches_the_oracle(case):
+def test_forward_matches_the_oracle(case, n_cu):
     batch, scale = _batch(case), 1 / np.sqrt(case[4])
-    plan, o, lse = _run(batch, case[5], case[6])
+    plan, o, lse = _run(batch, case[5], case[6], n_cu=n_cu)
     check_forward(batch, o, lse, float(np.float32(scale)), case[5], case[6])
     plan.destroy()
 
 
+@pytest.mark.parametrize("n_cu", [0, 1])
 @pytest.mark.parametrize("case", CASES, ids=_name)
-def test_backward_matches_the_oracle(case):
+def test_backward_matches_the_oracle(case, n_cu):
     batch, scale = _batch(case, 5), float(np.float32(1 / np.sqrt(case[4])))
-    plan, o, lse = _run(batch, case[5], case[6])
+    plan, o, lse = _run(batch, case[5], case[6], n_cu=n_cu)
     dout = batch.operand("q")
     dq, dk, dv = batch.empty("q"), batch.empty("kv"), batch.empty("kv")
     bsm.bsm_attention_backward(plan, batch.q, batch.k, batch.v, o, lse, dout, dq, dk, dv)

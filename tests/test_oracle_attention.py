@@ -108,7 +108,7 @@ def test_plan_stats(q_len, kv_len, causal, window):
     p = _plan(q_len, kv_len, causal=causal, window=window)
     d = bsm.bsm_attention_plan_describe(p)
     assert d["pairs"] == sum(int(oa.seen(n, m, causal, window).sum()) for n, m in zip(q_len, kv_len))
-    assert d["q_units"] == 4 * sum(-(-n // 128) for n in q_len)
+    assert d["q_units"] == 4 * sum(-(-n // 64) for n in q_len)  # little work: units of 64 rows
     assert d["kv_units"] == 2 * sum(-(-m // 128) for m in kv_len)
     assert d["lse_elems"] == 4 * sum(q_len) and d["workspace_bytes"] == 16 * sum(q_len)
     assert (d["total_q"], d["total_kv"], d["causal"], d["window"]) == (sum(q_len), sum(kv_len), causal, window)
@@ -132,6 +132,14 @@ def test_plan_parts_of_few_keys(q_len, kv_len, parted):
             assert (d["workspace_bytes"] > 16 * sum(q_len)) == parted
     st, m = _status(_plan, topology=dict(n_xcd=8, n_cu=-1))
     assert st == bsm.BSM_ERR_INVALID_ARG and "n_cu" in m
+
+
+@pytest.mark.parametrize("q_len,dim,causal,rows", [
+    ([512] * 32, 64, False, 128), ([4096] * 16, 128, True, 128), ([4096], 64, True, 64), ([4096], 128, True, 64),
+    ([700] * 4, 96, False, 64), ([], 64, False, 64)])
+def test_plan_rows_of_query_units(q_len, dim, causal, rows):
+    d = bsm.bsm_attention_plan_describe(_plan(q_len, head_dim=dim, causal=causal))
+    assert d["q_units"] == 4 * sum(-(-n // rows) for n in q_len)
 
 
 def test_plan_allocation_failure(monkeypatch):
