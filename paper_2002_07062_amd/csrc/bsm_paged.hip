@@ -148,18 +148,42 @@ __device__ __forceinline__ Place place_of(const PagedArgs& a, int64_t w, int* me
 
 __device__ __forceinline__ bool names_page(const PagedArgs& a, int entry) { return entry >= 0 && entry < a.cache.n_pages; }
 
-// The rows of K and V that a thread stages: tile row i is key j0 + i of the request.  Keys past its
-// end, and keys of table entries that name no page, are zeros.
+// The rows of K and V that a thread stages: tile row i is key j0 + i of the request, the tiles follow each
+// other.  Keys past its end, and keys of table entries that name no page, are zeros.  Where a key lies is carried
+// on from tile to tile: a division by the page size takes as long as the exponentials of several keys.
 template <int D, int ROWS, int THREADS, bool DIRECT>
 struct PagedStage {
     using S = Stage<D, ROWS, THREADS, DIRECT>;
     S k, v;
+    int column[S::kN], row[S::kN];  // table column of the next tile's key, and its row within the page
+    int now[S::kN];                 // row of this tile's key
     int page[S::kN];  // table entries, looked at when they are used: they are loaded behind a tile's loads
-    // table entries of the tile at j0; the request has keys 0 .. end - 1
-    __device__ __forceinline__ void find(const PagedArgs& a, const int32_t* table, int tid, int j0, int end) {
+    int step_columns, step_rows, last_column;
+    bool near;  // strides of 32 bits
+    __device__ __forceinline__ void init(const PagedArgs& a, int tid, int j0, int end) {
+        step_columns = ROWS / a.cache.page_size;
+        step_rows = ROWS % a.cache.page_size;
+        last_column = (end - 1) / a.cache.page_size;
+        near = (a.cache.page | a.cache.row) >> 32 == 0;
 #pragma unroll
         for (int n = 0; n < S::kN; ++n) {
-            page[n] = table[min(j0 + S::row(tid, n), end - 1) / a.cache.page_size];
+            const int j = j0 + S::row(tid, n);
+            column[n] = j / a.cache.page_size;
+            row[n] = j - column[n] * a.cache.page_size;
+        }
+    }
+    // table entries of the next tile; the request has keys 0 .. end - 1
+    __device__ __forceinline__ void find(const PagedArgs& a, const int32_t* table) {
+#pragma unroll
+        for (int n = 0; n < S::kN; ++n) {
+            page[n] = table[min(column[n], last_column)];
+            now[n] = row[n];
+            column[n] += step_columns;
+            row[n] += step_rows;
+            if (row[n] >= a.cache.page_size) {
+                row[n] -= a.cache.page_size;
+                ++column[n];
+            }
         }
     }
     __device__ __forceinline__ void begin(const PagedArgs& a, int head, int tid, int j0, int end, int chunks, uint16_t* lds_k, uint16_t* lds_v) {
@@ -167,7 +191,13 @@ struct PagedStage {
         for (int n = 0; n < S::kN; ++n) {
             const int j = j0 + S::row(tid, n), c = S::chunk(tid, n);
             const bool live = j < end && names_page(a, page[n]) && c < chunks;
-            const int64_t from = page[n] * a.cache.page + j % a.cache.page_size * a.cache.row + head * a.cache.head + 8 * c;
+            int64_t from;  // (of 32-bit strides a product is one instruction)
+            if (near)
+                from = static_cast<int64_t>(static_cast<uint64_t>(static_cast<uint32_t>(page[n])) * static_cast<uint32_t>(a.cache.page) +
+                                            static_cast<uint64_t>(static_cast<uint32_t>(now[n])) * static_cast<uint32_t>(a.cache.row));
+            else
+                from = page[n] * a.cache.page + now[n] * a.cache.row;
+            from += head * a.cache.head + 8 * c;
             k.piece(tid, n, lds_k, a.cache.k + from, live);
             v.piece(tid, n, lds_v, a.cache.v + from, live);
         }
@@ -215,9 +245,10 @@ __global__ __launch_bounds__(kThreads, 2) void paged_kernel(const PagedArgs a) {
     const float c = a.scale * kLog2e;
     PagedStage<D, kKeys, kThreads, DIRECT> stage;
     if (begin < end) {
-        stage.find(a, table, tid, begin, r.kv_len);
+        stage.init(a, tid, begin, r.kv_len);
+        stage.find(a, table);
         stage.begin(a, r.head, tid, begin, r.kv_len, chunks, lds[0][0], lds[0][1]);
-        stage.find(a, table, tid, begin + kKeys, r.kv_len);
+        stage.find(a, table);
         stage.end(tid, lds[0][0], lds[0][1]);
     }
     const RowFrags<D> rows_at(lane);
@@ -229,7 +260,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_kernel(const PagedArgs a) {
         tile_barrier<DIRECT>();
         if (next < end) {
             stage.begin(a, r.head, tid, next, r.kv_len, chunks, next_k, next_v);
-            stage.find(a, table, tid, next + kKeys, r.kv_len);
+            stage.find(a, table);
         }
         if (any_row && j0 <= w1.hi && next > w0.lo) {
             f32x16 s[kKeys / 32];
