@@ -450,9 +450,9 @@ bsm_status bsm_attention_execute(bsm_attention_plan plan, const bsm_heads* q, co
  * the gradients are written, not added to, for every row of every sequence.  A key/value row that
  * two sequences share, or an operand with a stride of 0, has no one place for its gradient: give
  * each (sequence, row, head) a place of its own and add them up.  workspace: workspace_bytes of
- * the plan's stats (for delta_i, and at most 140 MB of parts), on a 16-byte boundary, not shared
- * with a call that may run at the same time.  dq, dk and dv overlap
- * no operand (they may interleave with each other, as views of one tensor). */
+ * the plan's stats (for D_i, and under 70 MB for parts on 256 compute units), on a 16-byte
+ * boundary, not shared with a call that may run at the same time.  dq, dk and dv overlap no operand
+ * (they may interleave with each other, as views of one tensor). */
 bsm_status bsm_attention_backward(bsm_attention_plan plan, const bsm_heads* q, const bsm_heads* k,
                                   const bsm_heads* v, const bsm_heads* o, const float* lse,
                                   const bsm_heads* dout, const bsm_heads* dq, const bsm_heads* dk,
@@ -517,7 +517,8 @@ bsm_status bsm_attention_paged(const bsm_cache* cache, const bsm_heads* q, const
                                float scale, void* workspace, int64_t workspace_bytes,
                                void* stream);
 
-/* Bytes of workspace (0 or more) that bsm_attention_paged needs on `device` for these sizes. */
+/* Bytes of workspace (0 or more) that bsm_attention_paged needs on `device` for these sizes; the
+ * max_kv that the call is given, for 0 the width * page_size that it stands for there. */
 bsm_status bsm_attention_paged_workspace(int64_t batch, int64_t tokens, int32_t heads_q,
                                          int32_t heads_kv, int32_t head_dim, int32_t max_q,
                                          int32_t max_kv, int device, int64_t* bytes);

@@ -39,7 +39,7 @@ constexpr float kLn2 = 0.69314718055994530942f;
 constexpr int kWave = 64;
 constexpr int kRows = 32;  // rows of the result per wave
 constexpr float kInf = __builtin_huge_valf();
-constexpr int kAhead = 3;      // fragments read ahead of their use (of 1 .. 6 the fastest; from 4 on dq spills)
+constexpr int kAhead = 3;      // fragments read ahead of their use (of 1 .. 6 the fastest; with more, dq spills more registers)
 constexpr int kMayCross = 0x6; // of the fixed order: vector and scalar arithmetic may move
 
 // ------------------------------------------------------------------------------- LDS tiles

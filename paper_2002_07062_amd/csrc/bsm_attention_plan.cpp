@@ -77,7 +77,8 @@ int64_t parts_of(int64_t steps, int64_t share) {
 // The share for which `slots` workgroups at a time, the longest first, are done soonest.  A cut costs its
 // parts' loads and stores, two steps each, and the joining launch, four.  At best the slots' shares are equal;
 // shares of up to half again as many steps can be faster, as with equal ones a few parts may be left over for
-// a round of their own.
+// a round of their own.  (That is tried out; of many units, where it would take the host long, a few left over
+// are little, and an eighth more than equal will do.)
 int64_t key_share(const Sequences& s, int64_t slots) {
     std::vector<int64_t> steps;
     int64_t total = 0, longest = 0;
@@ -90,6 +91,7 @@ int64_t key_share(const Sequences& s, int64_t slots) {
         }
     const int64_t uncut = std::max<int64_t>(1, longest), even = std::max<int64_t>(1, (total + slots - 1) / slots);
     if (even >= uncut) return uncut;
+    if (static_cast<int64_t>(steps.size()) * s.heads_kv > 16 * slots) return std::min(uncut, even + even / 8);
     int64_t best = 0, best_share = uncut;
     std::vector<int64_t> costs, load;
     for (int64_t share : {uncut, even, even + even / 8, even + even / 4, even + even / 2}) {

@@ -250,6 +250,33 @@ def test_shared_keys_and_values():
     check_backward(batch, o, lse, dout, *grads, 0.125, False)
 
 
+@pytest.mark.parametrize("stride,rows", [((1 << 24) - 8, 290), (45_000_000, 100)])
+def test_rows_past_32_bits(stride, rows):
+    """Operands and gradients whose rows are up to 2^32 elements and more from the first."""
+    batch = Batch([rows], [rows], 1, 1, 64, "packed", 53)
+    far = [torch.empty((rows - 1) * stride + 4 * 64, dtype=torch.bfloat16, device="cuda") for _ in range(3)]
+
+    def view(buffer, x):
+        return torch.as_strided(far[buffer], (rows, 1, 64), (stride, 64, 1), 64 * x)
+
+    q, k, v, dout = (view(0, x) for x in range(4))
+    o, dq, dk, dv = view(1, 0), view(2, 0), view(2, 1), view(2, 2)
+    for x, y in zip((q, k, v), (batch.q, batch.k, batch.v)):
+        x.copy_(y)
+    dout.copy_(batch.operand("q"))
+    plan = bsm.bsm_attention_plan_create([rows], heads_q=1, head_dim=64, causal=True)
+    lse = torch.empty((1, rows), device="cuda")
+    with pytest.raises(bsm.BsmError) as e:  # an output between the operands' rows
+        bsm.bsm_attention_execute(plan, q, k, v, dout)
+    assert e.value.status == bsm.BSM_ERR_ALIAS
+    bsm.bsm_attention_execute(plan, q, k, v, o, lse=lse)
+    bsm.bsm_attention_backward(plan, q, k, v, o, lse, dout, dq, dk, dv)
+    torch.cuda.synchronize()
+    check_forward(batch, o, lse, 0.125, True)
+    check_backward(batch, o, lse, dout, dq, dk, dv, 0.125, True)
+    plan.destroy()
+
+
 def test_two_streams_with_their_own_workspaces():
     batches = [Batch([300, 120], [300, 120], 4, 2, 128, "packed", s) for s in (41, 42)]
     plan, _, _ = _run(batches[0], True, 0)

@@ -1,6 +1,8 @@
 """The paged key/value cache through the C ABI: slot maps bit for bit, appended tokens, attention of
 chunks and single tokens over the pages against the fp64 oracle, and a serving loop of all three."""
 
+from types import SimpleNamespace
+
 import numpy as np
 import pytest
 import torch
@@ -132,6 +134,29 @@ def test_paged_attention_of_hundreds_of_requests(chunk, window):
                             max_q=max(new), max_kv=max(kv_len), window=window)
     torch.cuda.synchronize()
     _check(o, q, cache, new, kv_len, 2, 0.125, window)
+
+
+@pytest.mark.parametrize("stride,pages", [((1 << 32) + 128, [1, 0]), (1 << 31, [2, 0])])
+def test_pages_past_32_bits(stride, pages):
+    """Pages that lie more than 2^32 elements apart, written and read (a single token, a chunk)."""
+    page, hk, d, n_pages = 32, 2, 64, max(pages) + 1
+    buffer = torch.empty((n_pages - 1) * stride + 2 * page * hk * d, dtype=torch.bfloat16, device="cuda")
+    k_cache, v_cache = (torch.as_strided(buffer, (n_pages, page, hk, d), (stride, hk * d, d, 1), x * page * hk * d) for x in (0, 1))
+    k_cache.fill_(NAN)
+    v_cache.fill_(NAN)
+    g = torch.Generator().manual_seed(12)
+    n = 55
+    k, v = (torch.randn((n, hk, d), generator=g).to(torch.bfloat16).cuda() for _ in "kv")
+    slots = torch.tensor([pages[j // page] * page + j % page for j in range(n)], device="cuda")
+    bsm.bsm_cache_append(k, v, slots, k_cache, v_cache)
+    assert torch.equal(k_cache[pages[1], :n - page], k[page:]) and torch.equal(v_cache[pages[0]], v[:page])
+    cache = SimpleNamespace(tokens=[[to64(k), to64(v)]])
+    for new in (1, 50):
+        q = (2 * torch.randn((new, 4, d), generator=g)).to(torch.bfloat16).cuda()
+        o = torch.full_like(q, NAN)
+        bsm.bsm_attention_paged(q, k_cache, v_cache, i32([pages]), i32([0, new]), i32([n]), o, max_q=new)
+        torch.cuda.synchronize()
+        _check(o, q, cache, [new], [n], 2, 0.125)
 
 
 def test_bounds_keep_bad_lengths_and_pages_inside():
