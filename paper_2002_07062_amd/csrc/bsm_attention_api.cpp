@@ -474,7 +474,7 @@ bsm_status paged(const bsm_cache* cache, const bsm_heads* q, const bsm_heads* o,
     a.scale = scale;
     a.few_rows = cut.few_rows;
     a.shares = cut.shares;
-    a.least_share = cut.least_share;
+    a.round = cut.round;
     a.tiles = cut.tiles;
     a.splits = cut.splits;
     a.split_keys = cut.split_keys;

@@ -79,8 +79,8 @@ struct PagedArgs {
     float scale;
     // how the work is cut, from bounds on the lengths alone
     // Requests of up to few_rows rows of a key/value head (16 or 32; 0: none) go by shares: equal shares of
-    // their blocks of 128 keys, at least least_share blocks each; shares 0: one request each.
-    int32_t few_rows, shares, least_share;
+    // their blocks of kFewKeys keys, `round` of which run at once; shares 0: one request each.
+    int32_t few_rows, shares, round;
     // The others go by tiles of kTileRows rows, `tiles` per request and key/value head (0: there are none),
     // in `splits` pieces of the key axis of split_keys keys each, a multiple of kKeyTile.
     int32_t tiles, splits, split_keys;
@@ -88,6 +88,7 @@ struct PagedArgs {
 };
 
 constexpr int kKeyTile = 128;
+constexpr int kFewKeys = 128, kFewestBlocks = 4, kMostBlocks = 16;  // see cut_paged
 
 hipError_t launch_attention_paged(const PagedArgs& a, hipStream_t stream);
 

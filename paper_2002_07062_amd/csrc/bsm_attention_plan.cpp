@@ -246,12 +246,17 @@ PagedCut cut_paged(int64_t batch, int64_t tokens, int32_t heads_kv, int32_t grou
     else if (batch > 1 && group <= 32 && tokens < batch * max_q) c.few_rows = group <= 16 ? 16 : 32;
     if (c.few_rows > 0) {
         c.grid = batch * heads_kv;
-        if (keys > 1024) {  // up to eight rounds of a workgroup's 128 keys, a join would cost more than it saves
-            // Shares for eight rounds of two workgroups on a CU, of 2048 keys at least: CUs do not read equally
-            // fast (one round of equal shares left them idle for 30% of the time), but a workgroup also has
-            // to count the stream and find its first page before it reads any key.
-            c.shares = static_cast<int32_t>(std::max(1, 16 * n_cu / heads_kv));
-            c.least_share = 16;
+        // A workgroup reads about 36 GB/s (the same with twice the waves): up to eight rounds of its 128 keys a
+        // second kernel, which joins parts, would cost more than it saves.
+        if (keys > 1024) {
+            // Shares that fill the CUs once, of 4 to 16 blocks of 128 keys: fewer, and the counting of the stream
+            // and the joins take as long as the reading; more, and CUs that read faster than others end idle (one
+            // round of equal shares of 64 requests of 1k .. 32k keys left them so for 30% of the time).  us, with
+            // shares of 16 blocks at least and so: one request of 4096 keys, 8 kv heads of 128, 39.7, 19.4; four
+            // 41.0, 23.6; one of 131072 135.9, 121.3; 64 of 1k .. 32k 452, 448.
+ std::max(1, n_cu / heads_kv);
+            const int64_t blocks = batch * ((keys + kFewKeys - 1) / kFewKeys + 1);
+            c.shares = static_cast<int32_t>(std::min<int64_t>(16 * c.round, (blocks + kFewestBlocks - 1) / kFewestBlocks));
             c.grid = std::max(c.grid, static_cast<int64_t>(c.shares) * heads_kv);
             c.few_floats = 2 * static_cast<int64_t>(c.shares) * heads_kv * c.few_rows * (padded + 2);
         }

@@ -43,7 +43,7 @@ KeyUnits key_units(const Sequences& s, bsm_schedule schedule, int n_xcd, int n_c
 
 // How attention over a paged cache is cut.
 struct PagedCut {
-    int32_t few_rows, shares, least_share, tiles, splits, split_keys;  // as in PagedArgs
+    int32_t few_rows, shares, round, tiles, splits, split_keys;  // as in PagedArgs
     int64_t few_floats, tile_floats;                                   // of the parts
     int64_t grid;                                                      // workgroups of the largest launch
 };

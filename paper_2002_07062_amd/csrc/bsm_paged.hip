@@ -312,7 +312,6 @@ __global__ __launch_bounds__(kThreads, 2) void paged_kernel(const PagedArgs a) {
 // any lengths keep all CUs busy to the end; a request whose blocks lie in several shares is joined
 // afterwards.  The workgroups of a share run side by side, and with them the reads of a page's heads, which
 // lie side by side too.  Each workgroup counts the stream itself, 8 bytes a request from the cache.
-constexpr int kFewKeys = 128;
 
 // Blocks of one head of a request; one without keys has a block that writes zeros.
 struct Blocks {
@@ -338,29 +337,40 @@ __device__ __forceinline__ int64_t uniform(int64_t x) {
     return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
 }
 
-// Sum over the workgroup's threads.
-__device__ __forceinline__ int64_t sum_of_threads(int64_t x, int64_t* mem) {
+// Blocks of all requests, of one head, and of those before request b.
+struct Stream {
+    int64_t all, before;
+};
+__device__ __forceinline__ Stream count_blocks(const PagedArgs& a, int64_t b, int64_t (*mem)[2]) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    Stream x = {0, 0};
+    for (int64_t i = threadIdx.x; i < a.batch; i += kThreads) {
+        const int64_t n = blocks_of(a, request<true>(a, i, 0)).n;
+        x.all += n;
+        if (i < b) x.before += n;
+    }
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) x += __shfl_xor(x, d, 64);
+    for (int d = 1; d < 64; d *= 2) {
+        x.all += __shfl_xor(x.all, d, 64);
+        x.before += __shfl_xor(x.before, d, 64);
+    }
+    if (lane == 0) {
+        mem[wave][0] = x.all;
+        mem[wave][1] = x.before;
+    }
     __syncthreads();
-    if (lane == 0) mem[wave] = x;
-    __syncthreads();
-    int64_t all = 0;
+    x = {0, 0};
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) all += mem[w];
-    return uniform(all);
+    for (int w = 0; w < kWaves; ++w) {
+        x.all += mem[w][0];
+        x.before += mem[w][1];
+    }
+    return {uniform(x.all), uniform(x.before)};
 }
-
-// Blocks of the requests before b, of one head.
-__device__ __forceinline__ int64_t blocks_before(const PagedArgs& a, int64_t b, int64_t* mem) {
-    int64_t x = 0;
-    for (int64_t i = threadIdx.x; i < b; i += kThreads) x += blocks_of(a, request<true>(a, i, 0)).n;
-    return sum_of_threads(x, mem);
-}
+// Blocks of a share: what fills the CUs once, within kFewest .. kMost, but more where there are not as many shares.
 __device__ __forceinline__ int64_t share_of(const PagedArgs& a, int64_t blocks) {
-    const int64_t even = (blocks + a.shares - 1) / a.shares;
-    return even > a.least_share ? even : a.least_share;
+    const int64_t even = (blocks + a.shares - 1) / a.shares, once = (blocks + a.round - 1) / a.round;
+    return max(even, min(max(once, static_cast<int64_t>(kFewestBlocks)), static_cast<int64_t>(kMostBlocks)));
 }
 __device__ __forceinline__ int64_t few_part_at(const PagedArgs& a, int D, int64_t part) {
     return part * a.few_rows * (D + 2);
@@ -375,7 +385,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_few_kernel(const PagedArgs 
     constexpr int kBytes = kWaves * (kRegs * kWave * 4 > kBlockBytes ? kRegs * kWave * 4 : kBlockBytes);
     __shared__ __align__(16) unsigned char lds[kBytes];
     __shared__ float stat[2][kWaves][16 * NQ];
-    __shared__ int64_t mem[kWaves], s_at[2];
+    __shared__ int64_t mem[kWaves][2], s_at[2];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, quad = lane >> 4;
     const int chunks = a.cache.dim / 8;
 
@@ -388,7 +398,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_few_kernel(const PagedArgs 
         b = w;
         left = blocks_of(a, request<true>(a, b, 0)).n;
     } else {
-        const int64_t blocks = blocks_before(a, a.batch, mem), share = share_of(a, blocks), start = w * share;
+        const int64_t blocks = count_blocks(a, 0, mem).all, share = share_of(a, blocks), start = w * share;
         left = min(share, blocks - start);
         if (left > 0) {
             int64_t before = 0;
@@ -627,7 +637,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_few_kernel(const PagedArgs 
 // then a lane per column or two.  part(p) is the p-th part's first float.
 template <int D, class Part>
 __device__ __forceinline__ void join_row(const PagedArgs& a, const Request& r, int rows, int row, int i, int n, Part part) {
-    constexpr int kPer = (D + 63) / 64;
+    constexpr int kPer = (D + 63) / 64, kAtOnce = 8;
     const int lane = threadIdx.x & 63;
     float m = -kInf, total = 0.0f, acc[kPer];
 #pragma unroll
@@ -649,11 +659,20 @@ __device__ __forceinline__ void join_row(const PagedArgs& a, const Request& r, i
 #pragma unroll
         for (int e = 0; e < kPer; ++e) acc[e] *= old;
         const int count = min(n - p0, kWave);
-        for (int p = 0; p < count; ++p) {
-            const float fp = __shfl(f, p, 64);
-            const float* from = part(p0 + p) + i * D + min(kPer * lane, D - kPer);
+        for (int p = 0; p < count; p += kAtOnce) {  // with the loads of kAtOnce parts on their way
+            float x[kAtOnce][kPer];
 #pragma unroll
-            for (int e = 0; e < kPer; ++e) acc[e] += fp * from[e];
+            for (int y = 0; y < kAtOnce; ++y) {
+                const float* from = part(p0 + min(p + y, count - 1)) + i * D + min(kPer * lane, D - kPer);
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) x[y][e] = from[e];
+            }
+#pragma unroll
+            for (int y = 0; y < kAtOnce; ++y) {
+                const float fp = __shfl(f, min(p + y, count - 1), 64);
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) acc[e] += p + y < count ? fp * x[y][e] : 0.0f;
+            }
         }
     }
     const float inv = total == 0.0f ? 0.0f : 1.0f / total;
@@ -683,11 +702,12 @@ __global__ __launch_bounds__(kThreads) void paged_join_kernel(const PagedArgs a)
 // Joins the parts of the requests whose blocks lie in more than one share: a workgroup per request and head.
 template <int D>
 __global__ __launch_bounds__(kThreads) void paged_few_join_kernel(const PagedArgs a) {
-    __shared__ int64_t mem[kWaves];
+    __shared__ int64_t mem[kWaves][2];
     const int64_t b = blockIdx.x / a.cache.heads;
     const Request r = request<true>(a, b, static_cast<int>(blockIdx.x % a.cache.heads));
     const Blocks bl = blocks_of(a, r);
-    const int64_t start = blocks_before(a, b, mem), share = share_of(a, blocks_before(a, a.batch, mem));
+    const Stream stream = count_blocks(a, b, mem);
+    const int64_t start = stream.before, share = share_of(a, stream.all);
     const int64_t w0 = start / share;
     const int count = static_cast<int>((start + bl.n - 1) / share - w0) + 1;
     if (bl.n == 0 || count == 1) return;
