@@ -52,12 +52,16 @@ __device__ __forceinline__ void each_sum(f32x16 (&acc)[TILES], F f) {
 // values at a time through LDS, the next ones on their way meanwhile.  Two workgroups share a CU.  Whole
 // blocks that the mask hides are left out, and blocks that it does not touch are not masked.
 // KS = 1: four waves of 32 rows.  KS = 2: 64 rows, two waves of each 32 with half of every step's keys, joined
-// at the end; for plans whose longest units would outlast the others (see query_rows).
+// at the end; for plans whose longest units would outlast the others (see query_rows).  STEP: keys of a step;
+// 128 where few_units, as a wave alone on its SIMD takes 64 keys as fast as it takes 32, but would keep a third
+// workgroup off the CU (heads of 64, us with 64 and 128: 2 x 512 rows, 12 heads 8.9, 7.6; 4096, 8 heads, causal
+// 46.7, 37.5; 8 x 512, 12 heads, 768 units 11.3, 13.5; longer heads no faster).
 // Bound by the matrix cores with the exponentials between them, and on random data by the power that both
 // take: 4 x 4096 causal rows, 32/8 heads of 128, 561 us = 980 TFLOP/s (two 8192^3 products of a library on the
 // same card: 1200 .. 1400); without the exponentials and sums it would be 13% less time.
-template <int D, bool DIRECT, int KS>
+template <int D, bool DIRECT, int KS, int STEP>
 __global__ __launch_bounds__(kThreads, 2) void attention_kernel(const SequenceArgs a, const Unit* __restrict__ units) {
+    constexpr int kKeys = STEP;
     __shared__ __align__(16) uint16_t lds[2][2][kKeys * Tile<D>::kPitch];  // buffer, K or V
     const Unit u = units[blockIdx.x];
     if (u.rows <= 0) return;
@@ -155,9 +159,11 @@ __device__ __forceinline__ float reference(float lse) { return lse == -kInf ? kI
 
 // dq = scale * sum_j dS_ij k_j, with dS = P (dP - delta), P = exp(s - lse), dP = do . v: query rows
 // stay in registers as in the forward pass, the keys stream through LDS.  Also leaves delta.  4 x 4096 causal
-// rows, 32/8 heads of 128: 830 us = 994 TFLOP/s.  KS as in the forward pass.
-template <int D, bool DIRECT, int KS>
+// rows, 32/8 heads of 128: 830 us = 994 TFLOP/s.  KS and STEP as in the
+// forward pass.
+template <int D, bool DIRECT, int KS, int STEP>
 __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(const SequenceArgs a, const Unit* __restrict__ units) {
+    constexpr int kKeys = STEP;
     __shared__ __align__(16) uint16_t lds[2][2][kKeys * Tile<D>::kPitch];
     const Unit u = units[blockIdx.x];
     if (u.rows <= 0) return;
@@ -533,10 +539,10 @@ hipError_t with_dim(int dim, bool direct, F f) {
 hipError_t launch_attention(const SequenceArgs& a, const Unit* units, int64_t n, hipStream_t stream) {
     if (n == 0) return hipSuccess;
     return with_dim(a.dim, aligned_pieces(a.k) && aligned_pieces(a.v), [&](auto d, auto direct) {
-        if (a.unit_rows == kTileRows)
-            attention_kernel<d(), direct(), 1><<<static_cast<unsigned>(n), kThreads, 0, stream>>>(a, units);
-        else
-            attention_kernel<d(), direct(), 2><<<static_cast<unsigned>(n), kThreads, 0, stream>>>(a, units);
+        const unsigned grid = static_cast<unsigned>(n);
+        if (a.unit_rows == kTileRows) attention_kernel<d(), direct(), 1, kKeys><<<grid, kThreads, 0, stream>>>(a, units);
+        else if (d() == 64 && a.few_units) attention_kernel<64, direct(), 2, 2 * kKeys><<<grid, kThreads, 0, stream>>>(a, units);
+        else attention_kernel<d(), direct(), 2, kKeys><<<grid, kThreads, 0, stream>>>(a, units);
     });
 }
 
@@ -545,10 +551,10 @@ hipError_t launch_attention_backward(const SequenceArgs& a, const Unit* q_units,
     hipError_t e = hipSuccess;
     if (n_q > 0)
         e = with_dim(a.dim, aligned_pieces(a.k) && aligned_pieces(a.v), [&](auto d, auto direct) {
-            if (d() > 64 || a.unit_rows == kTileRows)
-                attention_dq_kernel<d(), direct(), 1><<<static_cast<unsigned>(n_q), kThreads, 0, stream>>>(a, q_units);
-            else
-                attention_dq_kernel<64, direct(), 2><<<static_cast<unsigned>(n_q), kThreads, 0, stream>>>(a, q_units);
+            const unsigned grid = static_cast<unsigned>(n_q);
+            if (d() > 64 || a.unit_rows == kTileRows) attention_dq_kernel<d(), direct(), 1, kKeys><<<grid, kThreads, 0, stream>>>(a, q_units);
+            else if (a.few_units) attention_dq_kernel<64, direct(), 2, 2 * kKeys><<<grid, kThreads, 0, stream>>>(a, q_units);
+            else attention_dq_kernel<64, direct(), 2, kKeys><<<grid, kThreads, 0, stream>>>(a, q_units);
         });
     if (e == hipSuccess && n_kv > 0)
         e = with_dim(a.dim, aligned_pieces(a.q) && aligned_pieces(a.dout), [&](auto d, auto direct) {

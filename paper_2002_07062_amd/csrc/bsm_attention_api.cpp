@@ -26,6 +26,7 @@ struct bsm_attention_plan_s {
     int64_t n_q = 0, n_kv = 0, n_join = 0, part_rows = 0;
     int64_t n_forward = 0, first_dq = 0;  // units of the forward pass; where dq's n_q units begin
     int32_t forward_rows = 0, dq_rows = 0;  // of these units
+    bool few_units = false;                 // as in SequenceArgs
     void* d_units = nullptr;  // units of the forward pass, of dq if they are others, of dk and dv, and their joins
     std::atomic<bool> used{false};
 };
@@ -228,6 +229,9 @@ bsm_status create(bsm_attention_plan* out_plan, const int32_t* q_len, const int3
         p->dq_rows = bsm_att::padded_dim(s.dim) > 64 ? bsm_att::kTileRows : p->forward_rows;
         std::vector<bsm_att::Unit> table = bsm_att::query_units(s, schedule, n_xcd, p->forward_rows);
         p->n_forward = static_cast<int64_t>(table.size());
+        int64_t with_rows = 0;  // (the table may have empty units between them)
+        for (int64_t b = 0; b < batch; ++b) with_rows += (s.q_len[b] + p->forward_rows - 1) / p->forward_rows * int64_t{heads_q};
+        p->few_units = with_rows <= 2 * static_cast<int64_t>(n_cu);
         if (p->dq_rows != p->forward_rows) {
             const std::vector<bsm_att::Unit> dq = bsm_att::query_units(s, schedule, n_xcd, p->dq_rows);
             p->first_dq = p->n_forward;
@@ -300,6 +304,7 @@ bsm_status forward(bsm_attention_plan p, const bsm_heads* q, const bsm_heads* k,
     a.group = s.heads_q / s.heads_kv;
     a.dim = s.dim;
     a.unit_rows = p->forward_rows;
+    a.few_units = p->few_units;
     a.mask = s.mask;
     a.scale = scale;
     DeviceGuard g;
@@ -361,6 +366,7 @@ bsm_status backward(bsm_attention_plan p, const bsm_heads* q, const bsm_heads* k
     a.group = s.heads_q / s.heads_kv;
     a.dim = s.dim;
     a.unit_rows = p->dq_rows;
+    a.few_units = p->few_units;
     a.mask = s.mask;
     a.scale = scale;
     if (p->n_q + p->n_kv == 0) return BSM_OK;
