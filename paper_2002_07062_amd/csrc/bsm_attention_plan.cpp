@@ -69,9 +69,9 @@ int64_t key_steps(const Sequences& s, int64_t b, int64_t first, int64_t rows) {
 }
 
 // Workgroups that a key unit of `steps` is cut for, none of which is to take many more than `share`.  Parts
-// of fewer than eight steps would mostly load their keys and store their sums.
+// of fewer than four steps would mostly load their keys and store their sums.
 int64_t parts_of(int64_t steps, int64_t share) {
-    return std::max<int64_t>(1, std::min<int64_t>({(steps + share - 1) / share, steps / 8, 64}));
+    return std::max<int64_t>(1, std::min<int64_t>({(steps + share - 1) / share, steps / 4, 64}));
 }
 
 // The share for which `slots` workgroups at a time, the longest first, are done soonest.  A cut costs its
