@@ -160,9 +160,10 @@ __device__ __forceinline__ float reference(float lse) { return lse == -kInf ? kI
 // dq = scale * sum_j dS_ij k_j, with dS = P (dP - delta), P = exp(s - lse), dP = do . v: query rows
 // stay in registers as in the forward pass, the keys stream through LDS.  Also leaves delta.  4 x 4096 causal
 // rows, 32/8 heads of 128: 830 us = 994 TFLOP/s.  KS and STEP as in the
-// forward pass.
+// forward pass; KS = 2 of heads over 64 takes more registers than two workgroups on a CU have, so it is for plans that
+// have one for each (1024 causal rows, 8 heads of 128: gradient 66.6 us with whole units, 54.6 so).
 template <int D, bool DIRECT, int KS, int STEP>
-__global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(const SequenceArgs a, const Unit* __restrict__ units) {
+__global__ __launch_bounds__(kThreads, D > 64 && KS == 2 ? 1 : 2) void attention_dq_kernel(const SequenceArgs a, const Unit* __restrict__ units) {
     constexpr int kKeys = STEP;
     __shared__ __align__(16) uint16_t lds[2][2][kKeys * Tile<D>::kPitch];
     const Unit u = units[blockIdx.x];
@@ -552,9 +553,9 @@ hipError_t launch_attention_backward(const SequenceArgs& a, const Unit* q_units,
     if (n_q > 0)
         e = with_dim(a.dim, aligned_pieces(a.k) && aligned_pieces(a.v), [&](auto d, auto direct) {
             const unsigned grid = static_cast<unsigned>(n_q);
-            if (d() > 64 || a.unit_rows == kTileRows) attention_dq_kernel<d(), direct(), 1, kKeys><<<grid, kThreads, 0, stream>>>(a, q_units);
-            else if (a.few_units) attention_dq_kernel<64, direct(), 2, 2 * kKeys><<<grid, kThreads, 0, stream>>>(a, q_units);
-            else attention_dq_kernel<64, direct(), 2, kKeys><<<grid, kThreads, 0, stream>>>(a, q_units);
+            if (a.unit_rows == kTileRows) attention_dq_kernel<d(), direct(), 1, kKeys><<<grid, kThreads, 0, stream>>>(a, q_units);
+            else if (d() == 64 && a.few_units) attention_dq_kernel<64, direct(), 2, 2 * kKeys><<<grid, kThreads, 0, stream>>>(a, q_units);
+            else attention_dq_kernel<d(), direct(), 2, kKeys><<<grid, kThreads, 0, stream>>>(a, q_units);
         });
     if (e == hipSuccess && n_kv > 0)
         e = with_dim(a.dim, aligned_pieces(a.q) && aligned_pieces(a.dout), [&](auto d, auto direct) {
