@@ -254,7 +254,7 @@ PagedCut cut_paged(int64_t batch, int64_t tokens, int32_t heads_kv, int32_t grou
             // round of equal shares of 64 requests of 1k .. 32k keys left them so for 30% of the time).  us, with
             // shares of 16 blocks at least and so: one request of 4096 keys, 8 kv heads of 128, 39.7, 19.4; four
             // 41.0, 23.6; one of 131072 135.9, 121.3; 64 of 1k .. 32k 452, 448.
- std::max(1, n_cu / heads_kv);
+            c.round = std::max(1, n_cu / heads_kv);
             const int64_t blocks = batch * ((keys + kFewKeys - 1) / kFewKeys + 1);
             c.shares = static_cast<int32_t>(std::min<int64_t>(16 * c.round, (blocks + kFewestBlocks - 1) / kFewestBlocks));
             c.grid = std::max(c.grid, static_cast<int64_t>(c.shares) * heads_kv);

@@ -159,6 +159,13 @@ def test_pages_past_32_bits(stride, pages):
         _check(o, q, cache, [new], [n], 2, 0.125)
 
 
+def test_long_requests_are_shared():
+    """Few rows over more than 1024 keys go to several workgroups, whose parts need a workspace."""
+    assert bsm.bsm_attention_paged_workspace(4, 4, 8, 8, 64, 1, 1024) == 0
+    for batch, keys in ((1, 1025), (4, 4096), (64, 32768)):
+        assert bsm.bsm_attention_paged_workspace(batch, batch, 8, 8, 64, 1, keys) > 0
+
+
 def test_bounds_keep_bad_lengths_and_pages_inside():
     """Entries that name no page read as zeros, lengths past the table count up to it, starts past
     the tokens are clamped, rows past max_q are left alone."""
