@@ -398,12 +398,28 @@ __global__ __launch_bounds__(kThreads, 2) void paged_few_kernel(const PagedArgs 
         b = w;
         left = blocks_of(a, request<true>(a, b, 0)).n;
     } else {
-        const int64_t blocks = count_blocks(a, 0, mem).all, share = share_of(a, blocks), start = w * share;
+// (a batch of up to kThreads requests is counted and searched in one look at it)
+        int64_t mine = 0, before = 0, blocks;
+        if (a.batch <= kThreads) {
+            if (tid < a.batch) mine = blocks_of(a, request<true>(a, tid, 0)).n;
+            Two total;
+            before = scan({mine, 0}, &total, mem).tokens;
+            blocks = uniform(total.tokens);
+        } else {
+            blocks = count_blocks(a, 0, mem).all;
+        }
+        const int64_t share = share_of(a, blocks), start = w * share;
         left = min(share, blocks - start);
         if (left > 0) {
-            int64_t before = 0;
-            for (int64_t b0 = 0; b0 < a.batch && before <= start; b0 += kThreads) {
-                const int64_t mine = b0 + tid < a.batch ? blocks_of(a, request<true>(a, b0 + tid, 0)).n : 0;
+            if (a.batch <= kThreads) {
+                if (start >= before && start < before + mine) {
+                    s_at[0] = tid;
+                    s_at[1] = start - before;
+                }
+                __syncthreads();
+            }
+            for (int64_t b0 = 0; a.batch > kThreads && b0 < a.batch && before <= start; b0 += kThreads) {
+                mine = b0 + tid < a.batch ? blocks_of(a, request<true>(a, b0 + tid, 0)).n : 0;
                 Two total;
                 const int64_t at = before + scan({mine, 0}, &total, reinterpret_cast<int64_t(*)[2]>(lds)).tokens;
                 if (start >= at && start < at + mine) {
