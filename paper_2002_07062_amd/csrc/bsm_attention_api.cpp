@@ -229,7 +229,7 @@ bsm_status create(bsm_attention_plan* out_plan, const int32_t* q_len, const int3
         p->n_forward = static_cast<int64_t>(table.size());
         int64_t with_rows = 0;  // (the table may have empty units between them)
         for (int64_t b = 0; b < batch; ++b) with_rows += (s.q_len[b] + p->forward_rows - 1) / p->forward_rows * int64_t{heads_q};
-        p->few_units = with_rows <= 2 * static_cast<int64_t>(n_cu);
+        p->few_units = with_rows <= 2 * static_cast<int64_t>(n_cu) && s.kv_longest > 64;
         // dq's units are the same, but of heads over 64 their halves need the registers of a whole CU
         p->dq_rows = bsm_att::padded_dim(s.dim) > 64 && with_rows > n_cu ? bsm_att::kTileRows : p->forward_rows;
         if (p->dq_rows != p->forward_rows) {
