@@ -248,15 +248,16 @@ PagedCut cut_paged(int64_t batch, int64_t tokens, int32_t heads_kv, int32_t grou
         c.grid = batch * heads_kv;
         // A workgroup reads about 36 GB/s (the same with twice the waves): up to eight rounds of its 128 keys a
         // second kernel, which joins parts, would cost more than it saves.
-        if (keys > 1024) {
+        if (keys > (padded > 64 ? 1152 : 1536)) {
             // Shares that fill the CUs once, of 4 to 16 blocks of 128 keys: fewer, and the counting of the stream
             // and the joins take as long as the reading; more, and CUs that read faster than others end idle (one
             // round of equal shares of 64 requests of 1k .. 32k keys left them so for 30% of the time).  us, with
             // shares of 16 blocks at least and so: one request of 4096 keys, 8 kv heads of 128, 39.7, 19.4; four
             // 41.0, 23.6; one of 131072 135.9, 121.3; 64 of 1k .. 32k 452, 448.
-            c.round = std::max(1, n_cu / heads_kv);
+            c.round = std::max(1, 1 * n_cu / heads_kv);
             const int64_t blocks = batch * ((keys + kFewKeys - 1) / kFewKeys + 1);
-            c.shares = static_cast<int32_t>(std::min<int64_t>(16 * c.round, (blocks + kFewestBlocks - 1) / kFewestBlocks));
+            const int64_t least = std::min<int64_t>(std::max<int64_t>(blocks / c.round, kFewestBlocks), kMostBlocks);
+            c.shares = static_cast<int32_t>(std::min<int64_t>(16 * c.round, (blocks + least - 1) / least));
             c.grid = std::max(c.grid, static_cast<int64_t>(c.shares) * heads_kv);
             c.few_floats = 2 * static_cast<int64_t>(c.shares) * heads_kv * c.few_rows * (padded + 2);
         }

@@ -367,10 +367,13 @@ __device__ __forceinline__ Stream count_blocks(const PagedArgs& a, int64_t b, in
     }
     return {uniform(x.all), uniform(x.before)};
 }
-// Blocks of a share: what fills the CUs once, within kFewest .. kMost, but more where there are not as many shares.
+// Blocks of a share.  The shares go round the CUs evenly: one to each, or else two, as often as it takes for shares of
+// up to kMostBlocks (a few more would leave most CUs waiting for some); but there are no more than a.shares.
 __device__ __forceinline__ int64_t share_of(const PagedArgs& a, int64_t blocks) {
-    const int64_t even = (blocks + a.shares - 1) / a.shares, once = (blocks + a.round - 1) / a.round;
-    return max(even, min(max(once, static_cast<int64_t>(kFewestBlocks)), static_cast<int64_t>(kMostBlocks)));
+    const int64_t even = (blocks + a.shares - 1) / a.shares, rounds = (blocks + 2 * kMostBlocks * a.round - 1) / (2 * kMostBlocks * a.round);
+    int64_t share = (blocks + a.round - 1) / a.round;
+    if (share > kMostBlocks) share = (blocks + 2 * rounds * a.round - 1) / (2 * rounds * a.round);
+    return max(even, max(share, static_cast<int64_t>(kFewestBlocks)));
 }
 __device__ __forceinline__ int64_t few_part_at(const PagedArgs& a, int D, int64_t part) {
     return part * a.few_rows * (D + 2);
