@@ -80,7 +80,8 @@ struct PagedArgs {
     float scale;
     // how the work is cut, from bounds on the lengths alone
     // Requests of up to few_rows rows of a key/value head (16 or 32; 0: none) go by shares: equal shares of
-    // their blocks of kFewKeys keys, `round` of which run at once; shares 0: one request each.
+    // their blocks of kFewKeys keys (see share_of), of which `round` for each head give every CU one; shares 0: one
+    // request each.
     int32_t few_rows, shares, round;
     // The others go by tiles of kTileRows rows, `tiles` per request and key/value head (0: there are none),
     // in `splits` pieces of the key axis of split_keys keys each, a multiple of kKeyTile.
@@ -89,7 +90,7 @@ struct PagedArgs {
 };
 
 constexpr int kKeyTile = 128;
-constexpr int kFewKeys = 128, kFewestBlocks = 4, kMostBlocks = 16;  // see cut_paged
+constexpr int kFewKeys = 128, kFewestBlocks = 4, kMostBlocks = 16;  // of a share, see share_of
 
 hipError_t launch_attention_paged(const PagedArgs& a, hipStream_t stream);
 

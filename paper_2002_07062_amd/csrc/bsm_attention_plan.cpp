@@ -246,15 +246,15 @@ PagedCut cut_paged(int64_t batch, int64_t tokens, int32_t heads_kv, int32_t grou
     else if (batch > 1 && group <= 32 && tokens < batch * max_q) c.few_rows = group <= 16 ? 16 : 32;
     if (c.few_rows > 0) {
         c.grid = batch * heads_kv;
-        // A workgroup reads about 36 GB/s (the same with twice the waves): up to eight rounds of its 128 keys a
-        // second kernel, which joins parts, would cost more than it saves.
+        // A workgroup reads about 36 GB/s, the same with twice the waves.  For 9 rounds of its 128 keys, of shorter heads
+        // 12, the counting of the stream and a second kernel, which joins parts, cost as much as they save (us, 8 kv
+        // heads of 128, shared and not: one request of 1100 keys 18.1, 20.2, 64 of them 90.6, 61.0; heads of 64: 4 requests
+        // of 1100, 2 kv heads 18.4, 13.3, 64 of up to 1500, 8 kv heads 28.8, 22.7).
         if (keys > (padded > 64 ? 1152 : 1536)) {
-            // Shares that fill the CUs once, of 4 to 16 blocks of 128 keys: fewer, and the counting of the stream
-            // and the joins take as long as the reading; more, and CUs that read faster than others end idle (one
-            // round of equal shares of 64 requests of 1k .. 32k keys left them so for 30% of the time).  us, with
-            // shares of 16 blocks at least and so: one request of 4096 keys, 8 kv heads of 128, 39.7, 19.4; four
-            // 41.0, 23.6; one of 131072 135.9, 121.3; 64 of 1k .. 32k 452, 448.
-            c.round = std::max(1, 1 * n_cu / heads_kv);
+            // At least as many shares as share_of makes of that many keys, at most 16 to a CU.  (With 16 blocks at least
+            // to a share, whatever the batch: one request of 4096 keys, 8 kv heads of 128, 39.7 us, 18.9 so; four 41.0,
+            // 23.3; one of 131072 136, 120.)
+            c.round = std::max(1, n_cu / heads_kv);
             const int64_t blocks = batch * ((keys + kFewKeys - 1) / kFewKeys + 1);
             const int64_t least = std::min<int64_t>(std::max<int64_t>(blocks / c.round, kFewestBlocks), kMostBlocks);
             c.shares = static_cast<int32_t>(std::min<int64_t>(16 * c.round, (blocks + least - 1) / least));

@@ -367,8 +367,11 @@ __device__ __forceinline__ Stream count_blocks(const PagedArgs& a, int64_t b, in
     }
     return {uniform(x.all), uniform(x.before)};
 }
-// Blocks of a share.  The shares go round the CUs evenly: one to each, or else two, as often as it takes for shares of
-// up to kMostBlocks (a few more would leave most CUs waiting for some); but there are no more than a.shares.
+// Blocks of a share: 4 at least, else counting them and joining takes as long as reading them.  The shares go round the
+// CUs evenly, one to each or two, as often as it takes for shares of up to 16: larger ones end too far apart (one round
+// of equal shares of 64 requests of 1k .. 32k keys left CUs idle for 30% of the time), and a few workgroups more than
+// go round keep the others waiting (64 ragged requests of up to 4096 keys, 8 kv heads of 128, 304 workgroups 100 us, 488
+// 84 us; up to 8192 149, 127 us).  But there are no more than a.shares.
 __device__ __forceinline__ int64_t share_of(const PagedArgs& a, int64_t blocks) {
     const int64_t even = (blocks + a.shares - 1) / a.shares, rounds = (blocks + 2 * kMostBlocks * a.round - 1) / (2 * kMostBlocks * a.round);
     int64_t share = (blocks + a.round - 1) / a.round;
