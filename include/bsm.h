@@ -450,7 +450,7 @@ bsm_status bsm_attention_execute(bsm_attention_plan plan, const bsm_heads* q, co
  * the gradients are written, not added to, for every row of every sequence.  A key/value row that
  * two sequences share, or an operand with a stride of 0, has no one place for its gradient: give
  * each (sequence, row, head) a place of its own and add them up.  workspace: workspace_bytes of
- * the plan's stats (for D_i, and under 70 MB for parts on 256 compute units), on a 16-byte
+ * the plan's stats (for D_i, and under 140 MB for parts on 256 compute units), on a 16-byte
  * boundary, not shared with a call that may run at the same time.  dq, dk and dv overlap no operand
  * (they may interleave with each other, as views of one tensor). */
 bsm_status bsm_attention_backward(bsm_attention_plan plan, const bsm_heads* q, const bsm_heads* k,

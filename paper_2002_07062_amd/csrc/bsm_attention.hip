@@ -162,7 +162,9 @@ __device__ __forceinline__ float reference(float lse) { return lse == -kInf ? kI
 // rows, 32/8 heads of 128: 830 us = 994 TFLOP/s.  KS and STEP as in the
 // forward pass; KS = 2 of heads over 64 takes more registers than two workgroups on a CU have, so it is for plans that
 // have one for each (1024 causal rows, 8 heads of 128: gradient 66.6 us with whole units, 54.6 so).
-template <int D, bool DIRECT, int KS, int STEP>
+// PARTS: some units are cut; without, the registers of that are free (6 of ragged sequences of 700 .. 4001, 32/8 heads
+// of 128: 875 us with, 847 without).
+template <int D, bool DIRECT, int KS, int STEP, bool PARTS>
 __global__ __launch_bounds__(kThreads, D > 64 && KS == 2 ? 1 : 2) void attention_dq_kernel(const SequenceArgs a, const Unit* __restrict__ units) {
     constexpr int kKeys = STEP;
     __shared__ __align__(16) uint16_t lds[2][2][kKeys * Tile<D>::kPitch];
@@ -190,7 +192,7 @@ __global__ __launch_bounds__(kThreads, D > 64 && KS == 2 ? 1 : 2) void attention
         const int64_t r = u.head * a.total_q + u.lse_row + i;
         if (live) {
             lse = a.lse[r];
-            if (h == 0 && x == 0) a.delta[r] = delta;
+            if (h == 0 && x == 0 && (!PARTS || u.part == 0)) a.delta[r] = delta;
         }
     }
     const float ref = reference(lse);
@@ -198,7 +200,12 @@ __global__ __launch_bounds__(kThreads, D > 64 && KS == 2 ? 1 : 2) void attention
     const int last = u.first + u.rows - 1;
     const Seen w0 = seen_keys(i0, u.q_len, u.kv_len, a.mask), w1 = seen_keys(i0 + kRows - 1, u.q_len, u.kv_len, a.mask);
     const Seen u0 = seen_keys(u.first, u.q_len, u.kv_len, a.mask), u1 = seen_keys(last, u.q_len, u.kv_len, a.mask);
-    const int begin = u0.lo / kKeys * kKeys, end = u1.hi + 1;
+    int begin = u0.lo / kKeys * kKeys, end = u1.hi + 1;
+    if constexpr (PARTS) {
+        const int64_t steps = end > begin ? (end - begin + kKeys - 1) / kKeys : 0;
+        end = min(end, begin + static_cast<int>(steps * (u.part + 1) / u.parts) * kKeys);
+        begin += static_cast<int>(steps * u.part / u.parts) * kKeys;
+    }
     const bool any_row = i0 <= last;
     const uint16_t* kp = at(a.k, u, u.kv_start, u.head / a.group);
     const uint16_t* vp = at(a.v, u, u.kv_start, u.head / a.group);
@@ -267,6 +274,17 @@ __global__ __launch_bounds__(kThreads, D > 64 && KS == 2 ? 1 : 2) void attention
     if (lse == -kInf) {  // the row saw nothing: no gradient, whatever dout holds
 #pragma unroll
         for (int t = 0; t < D / 32; ++t) dq[t] = zero16();
+    }
+    if (PARTS && u.parts > 1) {
+        if (!live) return;
+        float* to = a.dq_part + (u.part_row + u.part * u.rows + i - u.first) * D + 4 * h;
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+            for (int e4 = 0; e4 < 4; ++e4)
+                *reinterpret_cast<f32x4*>(to + 32 * t + 8 * e4) =
+                    f32x4{dq[t][4 * e4], dq[t][4 * e4 + 1], dq[t][4 * e4 + 2], dq[t][4 * e4 + 3]};
+        return;
     }
     uint16_t* out = a.dq.p + u.seq * a.dq.seq + (u.q_start + i) * a.dq.row + u.head * a.dq.head;
     store_row<D>(out, live, dq, a.scale, h, chunks);
@@ -480,18 +498,19 @@ __global__ __launch_bounds__(Dkv<D>::kThreads, 2) void attention_dkv_kernel(cons
     }
 }
 
-// Adds up the parts of a unit's dk and dv, in order: a thread per 8 columns of a row of one of them, and
+// Adds up the parts of a unit's dq, or dk and dv, in order: a thread per 8 columns of a row of one of them, and
 // kJoinSlices workgroups per unit, as a few units of many parts would keep too few CUs reading (one workgroup
-// each took 62 us for 32 units of 16 parts, 33 MB).
+// each took 62 us for 32 units of 16 parts, 33 MB).  The first n_dq units are dq's.
 constexpr int kJoinSlices = 8;
 template <int D>
-__global__ __launch_bounds__(kThreads) void attention_dkv_join_kernel(const SequenceArgs a, const Unit* __restrict__ units) {
+__global__ __launch_bounds__(kThreads) void attention_join_kernel(const SequenceArgs a, const Unit* __restrict__ units, int64_t n_dq) {
     const Unit u = units[blockIdx.x];
-    const int chunks = a.dim / 8;
-    const int64_t step = static_cast<int64_t>(u.rows) * 2 * D;
-    for (int x = blockIdx.y * kThreads + threadIdx.x; x < 2 * u.rows * chunks; x += kThreads * kJoinSlices) {
-        const int c = x % chunks, is_v = x / chunks % 2, j = x / chunks / 2;
-        const float* from = a.part + ((u.part_row + j) * 2 + is_v) * D + 8 * c;
+    const bool is_dq = blockIdx.x < n_dq;
+    const int chunks = a.dim / 8, sums = is_dq ? 1 : 2;
+    const int64_t step = static_cast<int64_t>(u.rows) * sums * D;
+    for (int x = blockIdx.y * kThreads + threadIdx.x; x < sums * u.rows * chunks; x += kThreads * kJoinSlices) {
+        const int c = x % chunks, sum = x / chunks % sums, j = x / chunks / sums;
+        const float* from = (is_dq ? a.dq_part : a.part) + ((u.part_row + j) * sums + sum) * D + 8 * c;
         f32x4 lo = {0.0f, 0.0f, 0.0f, 0.0f}, hi = lo;
 #pragma unroll 4
         for (int p = 0; p < u.parts; ++p) {
@@ -502,16 +521,16 @@ __global__ __launch_bounds__(kThreads) void attention_dkv_join_kernel(const Sequ
                 hi[e] += z[e];
             }
         }
-        const float f = is_v ? 1.0f : a.scale;
+        const float f = sum ? 1.0f : a.scale;
         bf16x8 out;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             out[e] = static_cast<__bf16>(f * lo[e]);
             out[4 + e] = static_cast<__bf16>(f * hi[e]);
         }
-        const Heads& to = is_v ? a.dv : a.dk;
-        *reinterpret_cast<u32x4_any*>(to.p + u.seq * to.seq + (u.kv_start + u.first + j) * to.row + u.head * to.head + 8 * c) =
-            __builtin_bit_cast(u32x4, out);
+        const Heads& to = is_dq ? a.dq : sum ? a.dv : a.dk;
+        const int64_t row = (is_dq ? u.q_start : u.kv_start) + u.first + j;
+        *reinterpret_cast<u32x4_any*>(to.p + u.seq * to.seq + row * to.row + u.head * to.head + 8 * c) = __builtin_bit_cast(u32x4, out);
     }
 }
 
@@ -547,23 +566,29 @@ hipError_t launch_attention(const SequenceArgs& a, const Unit* units, int64_t n,
     });
 }
 
-hipError_t launch_attention_backward(const SequenceArgs& a, const Unit* q_units, int64_t n_q, const Unit* kv_units,
-                                     int64_t n_kv, int64_t n_join, hipStream_t stream) {
+template <int D, bool DIRECT, bool PARTS>
+static void launch_dq(const SequenceArgs& a, const GradientUnits& u, hipStream_t stream) {
+    const unsigned grid = static_cast<unsigned>(u.n_q);
+    if (a.unit_rows == kTileRows) attention_dq_kernel<D, DIRECT, 1, kKeys, PARTS><<<grid, kThreads, 0, stream>>>(a, u.q);
+    else if (D == 64 && a.few_units) attention_dq_kernel<64, DIRECT, 2, 2 * kKeys, PARTS><<<grid, kThreads, 0, stream>>>(a, u.q);
+    else attention_dq_kernel<D, DIRECT, 2, kKeys, PARTS><<<grid, kThreads, 0, stream>>>(a, u.q);
+}
+
+hipError_t launch_attention_backward(const SequenceArgs& a, const GradientUnits& u, hipStream_t stream) {
     hipError_t e = hipSuccess;
-    if (n_q > 0)
+    if (u.n_q > 0)
         e = with_dim(a.dim, aligned_pieces(a.k) && aligned_pieces(a.v), [&](auto d, auto direct) {
-            const unsigned grid = static_cast<unsigned>(n_q);
-            if (a.unit_rows == kTileRows) attention_dq_kernel<d(), direct(), 1, kKeys><<<grid, kThreads, 0, stream>>>(a, q_units);
-            else if (d() == 64 && a.few_units) attention_dq_kernel<64, direct(), 2, 2 * kKeys><<<grid, kThreads, 0, stream>>>(a, q_units);
-            else attention_dq_kernel<d(), direct(), 2, kKeys><<<grid, kThreads, 0, stream>>>(a, q_units);
+            if (u.n_q_joins > 0) launch_dq<d(), direct(), true>(a, u, stream);
+            else launch_dq<d(), direct(), false>(a, u, stream);
         });
-    if (e == hipSuccess && n_kv > 0)
+    if (e == hipSuccess && u.n_kv > 0)
         e = with_dim(a.dim, aligned_pieces(a.q) && aligned_pieces(a.dout), [&](auto d, auto direct) {
-            attention_dkv_kernel<d(), direct()><<<static_cast<unsigned>(n_kv), Dkv<d()>::kThreads, 0, stream>>>(a, kv_units);
+            attention_dkv_kernel<d(), direct()><<<static_cast<unsigned>(u.n_kv), Dkv<d()>::kThreads, 0, stream>>>(a, u.kv);
         });
-    if (e == hipSuccess && n_join > 0)
+    const int64_t joins = u.n_q_joins + u.n_kv_joins;
+    if (e == hipSuccess && joins > 0)
         e = with_dim(a.dim, true, [&](auto d, auto) {
-            attention_dkv_join_kernel<d()><<<dim3(static_cast<unsigned>(n_join), kJoinSlices), kThreads, 0, stream>>>(a, kv_units + n_kv);
+            attention_join_kernel<d()><<<dim3(static_cast<unsigned>(joins), kJoinSlices), kThreads, 0, stream>>>(a, u.joins, u.n_q_joins);
         });
     return e;
 }

@@ -23,11 +23,11 @@ struct bsm_attention_plan_s {
     bsm_schedule schedule = BSM_SCHED_RR;
     int n_xcd = 1;
     bsm_att::Sequences seqs;
-    int64_t n_q = 0, n_kv = 0, n_join = 0, part_rows = 0;
-    int64_t n_forward = 0, first_dq = 0;  // units of the forward pass; where dq's n_q units begin
-    int32_t forward_rows = 0, dq_rows = 0;  // of these units
+    int64_t n_forward = 0, n_q = 0, n_kv = 0, n_q_joins = 0, n_kv_joins = 0;
+    int64_t q_part_rows = 0, kv_part_rows = 0;
+    int32_t forward_rows = 0, dq_rows = 0;  // of a unit of the forward pass and of dq
     bool few_units = false;                 // as in SequenceArgs
-    void* d_units = nullptr;  // units of the forward pass, of dq if they are others, of dk and dv, and their joins
+    void* d_units = nullptr;  // units of the forward pass, of dq, of dk and dv, and the joins of both
     std::atomic<bool> used{false};
 };
 
@@ -225,31 +225,34 @@ bsm_status create(bsm_attention_plan* out_plan, const int32_t* q_len, const int3
                              (static_cast<double>(s.total_kv) / bsm_att::kTileRows + batch) * heads_kv;
         if (units > kMostWorkgroups) return fail(BSM_ERR_INVALID_ARG, "too many rows for one plan");
         p->forward_rows = bsm_att::query_rows(s, n_cu);
-        std::vector<bsm_att::Unit> table = bsm_att::query_units(s, schedule, n_xcd, p->forward_rows);
-        p->n_forward = static_cast<int64_t>(table.size());
-        int64_t with_rows = 0;  // (the table may have empty units between them)
-        for (int64_t b = 0; b < batch; ++b) with_rows += (s.q_len[b] + p->forward_rows - 1) / p->forward_rows * int64_t{heads_q};
-        p->few_units = with_rows <= 2 * static_cast<int64_t>(n_cu) && s.kv_longest > 64;
+        int64_t halves = 0;  // units of 64 rows, where there are such
+        for (int64_t b = 0; b < batch; ++b) halves += (s.q_len[b] + p->forward_rows - 1) / p->forward_rows * int64_t{heads_q};
+        p->few_units = halves <= 2 * static_cast<int64_t>(n_cu) && s.kv_longest > 64;
         // dq's units are the same, but of heads over 64 their halves need the registers of a whole CU
-        p->dq_rows = bsm_att::padded_dim(s.dim) > 64 && with_rows > n_cu ? bsm_att::kTileRows : p->forward_rows;
-        if (p->dq_rows != p->forward_rows) {
-            const std::vector<bsm_att::Unit> dq = bsm_att::query_units(s, schedule, n_xcd, p->dq_rows);
-            p->first_dq = p->n_forward;
-            table.insert(table.end(), dq.begin(), dq.end());
-        }
-        p->n_q = static_cast<int64_t>(table.size()) - p->first_dq;
-        const bsm_att::KeyUnits kv = bsm_att::key_units(s, schedule, n_xcd, n_cu);
+        const bool long_heads = bsm_att::padded_dim(s.dim) > 64;
+        p->dq_rows = long_heads && halves > n_cu ? bsm_att::kTileRows : p->forward_rows;
+        // workgroups on a CU: two, but of the gradient's kernels for longer heads one, except whole units of dq
+        const int64_t cus = n_cu;
+        const bool pairs = !long_heads || p->dq_rows == bsm_att::kTileRows;
+        const bsm_att::Units f = bsm_att::make_units(s, false, p->forward_rows, 0, false, schedule, n_xcd);
+        const bsm_att::Units q = bsm_att::make_units(s, false, p->dq_rows, pairs ? 2 * cus : cus, pairs, schedule, n_xcd);
+        const bsm_att::Units kv = bsm_att::make_units(s, true, bsm_att::kTileRows, long_heads ? cus : 2 * cus, false, schedule, n_xcd);
+        p->n_forward = static_cast<int64_t>(f.units.size());
+        p->n_q = static_cast<int64_t>(q.units.size());
         p->n_kv = static_cast<int64_t>(kv.units.size());
-        p->n_join = static_cast<int64_t>(kv.joins.size());
-        p->part_rows = kv.part_rows;
-        if (std::max(p->n_forward, p->n_kv) > kMostWorkgroups) return fail(BSM_ERR_INVALID_ARG, "too many rows for one plan");
+        p->n_q_joins = static_cast<int64_t>(q.joins.size());
+        p->n_kv_joins = static_cast<int64_t>(kv.joins.size());
+        p->q_part_rows = q.part_rows;
+        p->kv_part_rows = kv.part_rows;
+        if (std::max({p->n_forward, p->n_q, p->n_kv}) > kMostWorkgroups) return fail(BSM_ERR_INVALID_ARG, "too many rows for one plan");
         p->device = device;
         p->schedule = schedule;
         p->n_xcd = n_xcd;
         if (fails("host")) throw std::bad_alloc();
         if (device >= 0 && p->n_q + p->n_kv > 0) {
-            table.insert(table.end(), kv.units.begin(), kv.units.end());
-            table.insert(table.end(), kv.joins.begin(), kv.joins.end());
+            std::vector<bsm_att::Unit> table;
+            for (const auto* units : {&f.units, &q.units, &kv.units, &q.joins, &kv.joins})
+                table.insert(table.end(), units->begin(), units->end());
             DeviceGuard g;
             hipError_t e = g.enter(device);
             if (e != hipSuccess) return hip_fail(e, "hipSetDevice");
@@ -316,10 +319,10 @@ bsm_status forward(bsm_attention_plan p, const bsm_heads* q, const bsm_heads* k,
     return BSM_OK;
 }
 
-// The workspace: delta of every query row and head, and the parts of dk and dv.
+// The workspace: delta of every query row and head, and the parts of dk and dv, and of dq.
 int64_t delta_bytes(const bsm_att::Sequences& s) { return (4 * s.heads_q * s.total_q + 15) / 16 * 16; }
 int64_t workspace_of(bsm_attention_plan p) {
-    return delta_bytes(p->seqs) + 4 * 2 * p->part_rows * bsm_att::padded_dim(p->seqs.dim);
+    return delta_bytes(p->seqs) + 4 * (2 * p->kv_part_rows + p->q_part_rows) * bsm_att::padded_dim(p->seqs.dim);
 }
 
 bsm_status backward(bsm_attention_plan p, const bsm_heads* q, const bsm_heads* k, const bsm_heads* v, const bsm_heads* o,
@@ -362,6 +365,7 @@ bsm_status backward(bsm_attention_plan p, const bsm_heads* q, const bsm_heads* k
     a.lse = const_cast<float*>(lse);
     a.delta = static_cast<float*>(workspace);
     a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + delta_bytes(s));
+    a.dq_part = a.part + 2 * p->kv_part_rows * bsm_att::padded_dim(s.dim);
     a.total_q = s.total_q;
     a.group = s.heads_q / s.heads_kv;
     a.dim = s.dim;
@@ -373,8 +377,15 @@ bsm_status backward(bsm_attention_plan p, const bsm_heads* q, const bsm_heads* k
     DeviceGuard g;
     hipError_t e = g.enter(p->device);
     if (e != hipSuccess) return hip_fail(e, "hipSetDevice");
-    const bsm_att::Unit* units = static_cast<const bsm_att::Unit*>(p->d_units) + p->first_dq;
-    e = bsm_att::launch_attention_backward(a, units, p->n_q, units + p->n_q, p->n_kv, p->n_join, static_cast<hipStream_t>(stream));
+    bsm_att::GradientUnits u{};
+    u.q = static_cast<const bsm_att::Unit*>(p->d_units) + p->n_forward;
+    u.kv = u.q + p->n_q;
+    u.joins = u.kv + p->n_kv;
+    u.n_q = p->n_q;
+    u.n_kv = p->n_kv;
+    u.n_q_joins = p->n_q_joins;
+    u.n_kv_joins = p->n_kv_joins;
+    e = bsm_att::launch_attention_backward(a, u, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "kernel launch");
     p->used = true;
     return BSM_OK;

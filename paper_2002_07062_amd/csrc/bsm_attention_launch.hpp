@@ -46,18 +46,21 @@ struct SequenceArgs {
     int32_t few_units;  // these run at once, two workgroups on a CU, and have more than 64 keys
     Mask mask;
     float scale;
-    // Sums of key units that several workgroups share, a range of the steps each: row r of part p is row
-    // part_row + p rows + r of [row][dk, dv][padded_dim] fp32; added up in order.
-    float* part;
+    // Sums of units that several workgroups share, a range of the steps each: row r of part p is row part_row +
+    // p rows + r of [row][dk, dv][padded_dim] or [row][padded_dim] fp32; added up in order.
+    float *part, *dq_part;
 };
 
 bool aligned_pieces(const Heads& t);  // 16-byte pieces on 16-byte boundaries
 
 hipError_t launch_attention(const SequenceArgs& a, const Unit* units, int64_t n, hipStream_t stream);
-// dq (and delta), then dk and dv, which read delta
-// and joins the parts of the n_join units behind the n_kv ones
-hipError_t launch_attention_backward(const SequenceArgs& a, const Unit* q_units, int64_t n_q, const Unit* kv_units,
-                                     int64_t n_kv, int64_t n_join, hipStream_t stream);
+// The units of a gradient: dq's, those of dk and dv, and the units of both that have parts.
+struct GradientUnits {
+    const Unit *q, *kv, *joins;  // the joins of dk and dv follow those of dq
+    int64_t n_q, n_kv, n_q_joins, n_kv_joins;
+};
+// dq (and delta), then dk and dv, which read delta, and the joins
+hipError_t launch_attention_backward(const SequenceArgs& a, const GradientUnits& u, hipStream_t stream);
 
 // ------------------------------------------------------------------------------ paged cache
 struct Cache {

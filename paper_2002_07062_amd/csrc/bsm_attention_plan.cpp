@@ -2,6 +2,7 @@
 
 #include <algorithm>
 #include <functional>
+#include <limits>
 #include <numeric>
 
 namespace bsm_att {
@@ -68,36 +69,35 @@ int64_t key_steps(const Sequences& s, int64_t b, int64_t first, int64_t rows) {
     return hi > lo ? (hi - lo / kStep * kStep + kStep - 1) / kStep * (s.heads_q / s.heads_kv) : 0;
 }
 
-// Workgroups that a key unit of `steps` is cut for, none of which is to take many more than `share`.  Parts
-// of fewer than four steps would mostly load their keys and store their sums.
+// Workgroups that a unit of `steps` is cut for, none of which is to take many more than `share`.  Parts of fewer
+// than four steps would mostly load their rows and store their sums.
 int64_t parts_of(int64_t steps, int64_t share) {
     return std::max<int64_t>(1, std::min<int64_t>({(steps + share - 1) / share, steps / 4, 64}));
 }
 
-// The share for which `slots` workgroups at a time, the longest first, are done soonest.  A cut costs its
-// parts' loads and stores, two steps each, and the joining launch, four.  At best the slots' shares are equal;
-// shares of up to half again as many steps can be faster, as with equal ones a few parts may be left over for
-// a round of their own.  (That is tried out; of many units, where it would take the host long, a few left over
-// are little, and an eighth more than equal will do.)
-int64_t key_share(const Sequences& s, int64_t slots) {
-    std::vector<int64_t> steps;
+// The share for which `slots` workgroups at a time, the longest first, are done soonest; `steps` of the units of one
+// head of `heads`.  A cut costs its parts' loads and stores, two steps each, and the joining launch, four.  At best
+// the slots' shares are equal; shares of up to half again as many steps can be faster, as with equal ones a few
+// parts may be left over for a round of their own.  with_care: a cut has to promise 3/8 of the time.  (dq shares its CUs
+// in pairs, of which one left alone runs faster: with a third less promised, the gradient of 2048 causal rows, 32/8
+// heads of 128, took 212 us instead of 201; dk and dv gain from less: 1024 causal rows, 8 heads of 64, 36 us instead of
+// 49.)  (The share is tried out; of many units, where it would take the host
+// long, a few left over are little, and an eighth more than equal will do.)
+int64_t best_share(const std::vector<int64_t>& steps, int64_t heads, int64_t slots, bool with_care) {
     int64_t total = 0, longest = 0;
-    for (int64_t b = 0; b < s.batch; ++b)
-        for (int64_t first = 0; first < s.kv_len[b]; first += kTileRows) {
-            const int64_t n = key_steps(s, b, first, std::min<int64_t>(kTileRows, s.kv_len[b] - first));
-            steps.push_back(n);
-            total += n * s.heads_kv;
-            longest = std::max(longest, n);
-        }
+    for (int64_t n : steps) {
+        total += n * heads;
+        longest = std::max(longest, n);
+    }
     const int64_t uncut = std::max<int64_t>(1, longest), even = std::max<int64_t>(1, (total + slots - 1) / slots);
     if (even >= uncut) return uncut;
-    if (static_cast<int64_t>(steps.size()) * s.heads_kv > 16 * slots) return std::min(uncut, even + even / 8);
+    if (static_cast<int64_t>(steps.size()) * heads > 16 * slots) return std::min(uncut, even + even / 8);
     int64_t best = 0, best_share = uncut;
     std::vector<int64_t> costs, load;
     for (int64_t share : {uncut, even, even + even / 8, even + even / 4, even + even / 2}) {
         costs.clear();
         for (int64_t n : steps)
-            for (int64_t i = 0, parts = parts_of(n, share); i < parts * s.heads_kv; ++i) costs.push_back(2 + (n + parts - 1) / parts);
+            for (int64_t i = 0, parts = parts_of(n, share); i < parts * heads; ++i) costs.push_back(2 + (n + parts - 1) / parts);
         std::sort(costs.begin(), costs.end(), std::greater<int64_t>());
         load.assign(slots, 0);  // a heap, the least loaded slot first
         int64_t end = 0;
@@ -106,7 +106,8 @@ int64_t key_share(const Sequences& s, int64_t slots) {
             end = std::max(end, load.back() += c);
             std::push_heap(load.begin(), load.end(), std::greater<int64_t>());
         }
-        if (costs.size() > steps.size() * s.heads_kv) end += 4;
+        if (costs.size() > steps.size() * heads) end += 4;
+        if (with_care && share != uncut) end = (8 * end + 4) / 5;
         if (best == 0 || end < best) {
             best = end;
             best_share = share;
@@ -191,42 +192,37 @@ int32_t query_rows(const Sequences& s, int n_cu) {
     return 4 * longest * 2 * n_cu > quarters * total ? kTileRows / 2 : kTileRows;
 }
 
-std::vector<Unit> query_units(const Sequences& s, bsm_schedule schedule, int n_xcd, int32_t rows) {
-    std::vector<Costed> units;
-    const int group = s.heads_q / s.heads_kv;
-    int64_t lse_row = 0;
-    for (int64_t b = 0; b < s.batch; ++b) {
-        for (int head = 0; head < s.heads_q; ++head)
-            for (int64_t first = 0; first < s.q_len[b]; first += rows) {
-                const int64_t n = std::min<int64_t>(rows, s.q_len[b] - first);
-                units.push_back({{s.q_start[b], s.kv_start[b], lse_row, 0, static_cast<int32_t>(b), head,
-                                  static_cast<int32_t>(first), static_cast<int32_t>(n), s.q_len[b], s.kv_len[b], 0, 1},
-                                 2 + query_steps(s, b, first, n), b * s.heads_kv + head / group});
-            }
-        lse_row += s.q_len[b];
-    }
-    return order(units, schedule, n_xcd, s.batch * s.heads_kv);
-}
+Units make_units(const Sequences& s, bool of_keys, int32_t rows, int64_t slots, bool with_care, bsm_schedule schedule, int n_xcd) {
+    const std::vector<int32_t>& len = of_keys ? s.kv_len : s.q_len;
+    const int heads = of_keys ? s.heads_kv : s.heads_q, group = heads / s.heads_kv;
+    std::vector<int64_t> steps;  // of the units of one head
+    for (int64_t b = 0; b < s.batch; ++b)
+        for (int64_t first = 0; first < len[b]; first += rows) {
+            const int64_t n = std::min<int64_t>(rows, len[b] - first);
+            steps.push_back(of_keys ? key_steps(s, b, first, n) : query_steps(s, b, first, n));
+        }
+    const int64_t share = slots > 0 ? best_share(steps, heads, slots, with_care) : std::numeric_limits<int32_t>::max();
 
-KeyUnits key_units(const Sequences& s, bsm_schedule schedule, int n_xcd, int n_cu) {
-    const int64_t share = key_share(s, padded_dim(s.dim) > 64 ? n_cu : 2 * static_cast<int64_t>(n_cu));
-    KeyUnits out;
+    Units out;
     std::vector<Costed> units;
     int64_t lse_row = 0;
+    size_t of_head = 0;
     for (int64_t b = 0; b < s.batch; ++b) {
-        for (int head = 0; head < s.heads_kv; ++head)
-            for (int64_t first = 0; first < s.kv_len[b]; first += kTileRows) {
-                const int64_t rows = std::min<int64_t>(kTileRows, s.kv_len[b] - first), steps = key_steps(s, b, first, rows);
-                const int64_t parts = parts_of(steps, share);
+        const size_t count = (len[b] + int64_t{rows} - 1) / rows;
+        for (int head = 0; head < heads; ++head)
+            for (size_t i = 0; i < count; ++i) {
+                const int64_t first = static_cast<int64_t>(i) * rows, n = std::min<int64_t>(rows, len[b] - first);
+                const int64_t mine = steps[of_head + i], parts = slots > 0 ? parts_of(mine, share) : 1;
                 Unit u{s.q_start[b], s.kv_start[b], lse_row, out.part_rows, static_cast<int32_t>(b), head,
-                       static_cast<int32_t>(first), static_cast<int32_t>(rows), s.q_len[b], s.kv_len[b], 0, static_cast<int32_t>(parts)};
+                       static_cast<int32_t>(first), static_cast<int32_t>(n), s.q_len[b], s.kv_len[b], 0, static_cast<int32_t>(parts)};
                 if (parts > 1) {
                     out.joins.push_back(u);
-                    out.part_rows += parts * rows;
+                    out.part_rows += parts * n;
                 }
                 for (u.part = 0; u.part < u.parts; ++u.part)
-                    units.push_back({u, 2 + steps / parts, b * s.heads_kv + head});
+                    units.push_back({u, 2 + mine / parts, b * s.heads_kv + head / group});
             }
+        of_head += count;
         lse_row += s.q_len[b];
     }
     out.units = order(units, schedule, n_xcd, s.batch * s.heads_kv);

@@ -30,16 +30,14 @@ void finish_sequences(Sequences* s, const int64_t* q_start, const int64_t* kv_st
 // Rows of the forward pass's query units: 128, or 64 where the longest of 128 would outlast the others.
 int32_t query_rows(const Sequences& s, int n_cu);
 
-// Units of `rows` query rows (forward pass, dq), in launch order; the unit of workgroup w is expected
-// to run on XCD w mod n_xcd.
-std::vector<Unit> query_units(const Sequences& s, bsm_schedule schedule, int n_xcd, int32_t rows);
-
-// Of 128 keys (dk, dv).  Units that would still run when the others' CUs are done are cut into parts.
-struct KeyUnits {
+// Units of `rows` query rows (forward pass, dq), or of keys (dk, dv), in launch order; the unit of
+// workgroup w is expected to run on XCD w mod n_xcd.  Where `slots` workgroups run at once, units that
+// would outlast the others are cut into parts (with_care: only by much); slots 0: none is.
+struct Units {
     std::vector<Unit> units, joins;  // joins: the units with parts
     int64_t part_rows = 0;           // rows of all parts
 };
-KeyUnits key_units(const Sequences& s, bsm_schedule schedule, int n_xcd, int n_cu);
+Units make_units(const Sequences& s, bool of_keys, int32_t rows, int64_t slots, bool with_care, bsm_schedule schedule, int n_xcd);
 
 // How attention over a paged cache is cut.
 struct PagedCut {

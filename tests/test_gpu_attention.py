@@ -91,18 +91,21 @@ def test_schedules_and_repeats_give_the_same_bits(case):
             assert torch.equal(x, y)
 
 
-# few keys for many query rows: several workgroups share the query rows of 128 keys
+# few keys for many query rows, or the reverse: several workgroups share a unit
 PARTED = [
     ([2048], None, 2, 1, 128, True, 0, "packed"),
     ([1500], [1100], 4, 1, 64, False, 0, "shifted"),
     ([1030, 0, 31, 700], [1500, 9, 0, 40], 4, 1, 80, True, 0, "padded"),
     ([1700, 40], None, 8, 1, 96, True, 300, "fused"),
     ([4000], [1], 1, 1, 40, False, 0, "heads_first"),
+    ([3, 40], [3000, 900], 2, 1, 64, True, 0, "packed"),     # few queries: several share a row's keys
+    ([150], [1600], 3, 1, 128, False, 0, "shifted"),
+    ([70, 1], [2000, 700], 2, 2, 96, True, 1500, "padded"),
 ]
 
 
 @pytest.mark.parametrize("case", PARTED, ids=_name)
-def test_gradients_of_few_keys(case):
+def test_gradients_of_few_rows(case):
     batch, scale = _batch(case, 9), float(np.float32(1 / np.sqrt(case[4])))
     plan, o, lse = _run(batch, case[5], case[6])
     assert plan.workspace_bytes > 4 * lse.numel() + 16  # there are parts
