@@ -269,7 +269,7 @@ PagedCut cut_paged(int64_t batch, int64_t tokens, int32_t heads_kv, int32_t grou
         c.split_keys = static_cast<int32_t>(each);
         c.splits = static_cast<int32_t>((keys + each - 1) / each);
         c.tile_floats = c.splits > 1 ? units * c.splits * kTileRows * (padded + 2) : 0;
-        c.grid = std::max(c.grid, units * std::max(c.splits, 8));  // the join has 8 workgroups for each tile
+        c.grid = std::max(c.grid, units * std::max(c.splits, 32));  // the join has up to 32 workgroups for each tile
     }
     return c;
 }

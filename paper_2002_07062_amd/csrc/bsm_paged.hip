@@ -110,8 +110,8 @@ __device__ __forceinline__ int64_t part_at(const PagedArgs& a, int D, const Requ
 }
 
 // What workgroup w does.  The requests follow each other, the one with the most keys first (with more
-// than kThreads of them, as they come), so that the CUs end together; of each its tiles, pieces and heads, the
-// heads side by side.  They are rotated from request to request: a page has its heads side by side, and
+// than kThreads of them, as they come), so that the CUs end together; of each its tiles (the last ones, which see
+// most keys, first), pieces and heads, the heads side by side.  They are rotated from request to request: a page has its heads side by side, and
 // an XCD that only ever read one of 8 heads of 128 (workgroups go to the 8 XCDs in turn) would use 2 of
 // its 16 L2 channels, which lie 256 bytes apart.
 struct Place {
@@ -122,7 +122,7 @@ __device__ __forceinline__ Place place_of(const PagedArgs& a, int64_t w, int* me
     const int64_t per = static_cast<int64_t>(a.tiles) * a.splits, unit = w / a.cache.heads;
     Place p;
     p.b = unit / per;
-    p.tile = static_cast<int>(unit % per) / a.splits;
+    p.tile = a.tiles - 1 - static_cast<int>(unit % per) / a.splits;
     p.piece = static_cast<int>(unit % per) % a.splits;
     p.head = static_cast<int>((w + p.b) % a.cache.heads);
     if (a.batch <= kThreads) {
@@ -705,19 +705,19 @@ __device__ __forceinline__ void join_row(const PagedArgs& a, const Request& r, i
         if (d + e < a.cache.dim) out[e] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(acc[e] * inv));
 }
 
-// Joins the pieces of the rows that more than one piece holds: a workgroup per 16 rows of a tile.
-constexpr int kJoinRows = 16;
+// Joins the pieces of the rows that more than one piece holds: a workgroup per `rows` rows of a tile.
 template <int D>
-__global__ __launch_bounds__(kThreads) void paged_join_kernel(const PagedArgs a) {
-    const int64_t groups = kTileRows / kJoinRows, unit = blockIdx.x / groups / a.cache.heads;
+__global__ __launch_bounds__(kThreads) void paged_join_kernel(const PagedArgs a, int rows) {
+    const int groups = kTileRows / rows;
+    const int64_t unit = blockIdx.x / groups / a.cache.heads;
     const Request r = request<false>(a, unit / a.tiles, static_cast<int>(blockIdx.x / groups % a.cache.heads));
-    const int tile = static_cast<int>(unit % a.tiles), tile0 = tile * kTileRows, i0 = static_cast<int>(blockIdx.x % groups) * kJoinRows;
+    const int tile = static_cast<int>(unit % a.tiles), tile0 = tile * kTileRows, i0 = static_cast<int>(blockIdx.x % groups) * rows;
     if (tile0 + i0 >= r.rows) return;
     const Pieces ps = pieces(a, r, tile0);
     if (ps.first == ps.last) return;
     const float* first = a.tile_part + part_at(a, D, r, tile, ps.first);
     const int64_t piece_floats = static_cast<int64_t>(kTileRows) * (D + 2);
-    for (int i = i0 + (threadIdx.x >> 6); i < i0 + kJoinRows && tile0 + i < r.rows; i += kWaves)
+    for (int i = i0 + (threadIdx.x >> 6); i < i0 + rows && tile0 + i < r.rows; i += kWaves)
         join_row<D>(a, r, kTileRows, tile0 + i, i, ps.last - ps.first + 1, [&](int p) { return first + p * piece_floats; });
 }
 
@@ -904,7 +904,10 @@ hipError_t launch_paged(const PagedArgs& a, hipStream_t stream) {
         else paged_kernel<D, false><<<grid, kThreads, 0, stream>>>(a);
         e = hipGetLastError();
         if (e == hipSuccess && a.splits > 1) {
-            paged_join_kernel<D><<<tiles * (kTileRows / kJoinRows), kThreads, 0, stream>>>(a);
+            // A wave joins four rows one after the other, but one where that leaves few workgroups (a chunk of 16
+            // tokens over 16384 keys, 32/8 heads of 128: 52 us with four, 30 us with one).
+            const int rows = tiles < 128 ? kWaves : 4 * kWaves;
+            paged_join_kernel<D><<<tiles * (kTileRows / rows), kThreads, 0, stream>>>(a, rows);
             e = hipGetLastError();
         }
     }
