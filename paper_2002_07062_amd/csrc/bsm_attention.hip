@@ -159,11 +159,11 @@ __device__ __forceinline__ float reference(float lse) { return lse == -kInf ? kI
 
 // dq = scale * sum_j dS_ij k_j, with dS = P (dP - delta), P = exp(s - lse), dP = do . v: query rows
 // stay in registers as in the forward pass, the keys stream through LDS.  Also leaves delta.  4 x 4096 causal
-// rows, 32/8 heads of 128: 830 us = 994 TFLOP/s.  KS and STEP as in the
-// forward pass; KS = 2 of heads over 64 takes more registers than two workgroups on a CU have, so it is for plans that
-// have one for each (1024 causal rows, 8 heads of 128: gradient 66.6 us with whole units, 54.6 so).
-// PARTS: some units are cut; without, the registers of that are free (6 of ragged sequences of 700 .. 4001, 32/8 heads
-// of 128: 875 us with, 847 without).
+// rows, 32/8 heads of 128: 830 us = 994 TFLOP/s.
+// KS and STEP as in the forward pass; KS = 2 of heads over 64 takes more registers than two workgroups on a CU
+// have, so it is for plans that have one for each (1024 causal rows, 8 heads of 128: gradient 66.6 us with whole
+// units, 54.6 so).  PARTS: some units are cut; without, the registers that it takes are free (six ragged sequences
+// of 700 .. 4001, 32/8 heads of 128: gradient 875 us with it, 847 without).
 template <int D, bool DIRECT, int KS, int STEP, bool PARTS>
 __global__ __launch_bounds__(kThreads, D > 64 && KS == 2 ? 1 : 2) void attention_dq_kernel(const SequenceArgs a, const Unit* __restrict__ units) {
     constexpr int kKeys = STEP;
@@ -295,10 +295,11 @@ __global__ __launch_bounds__(kThreads, D > 64 && KS == 2 ? 1 : 2) void attention
 // at a time.  No two workgroups add to one sum, so the result does not depend on timing.
 // D = 64: a wave keeps 32 keys.  D = 96, 128: two waves share 32 keys (kPair): wave x of the pair forms P and
 // dS for the 32 query rows of block x, the pair exchanges them through LDS as operands, and each adds up
-// half of 128 columns over both blocks (of 96, wave 1 adds 32 that are not stored).  That keeps a wave's sums at 64 registers, so that two
-// waves fit a SIMD and one's exponentials run beside the other's products (a wave that held whole sums
-// took 400 registers and ran alone: 735 us against 500 us on six ragged causal sequences of 700 .. 4001
-// tokens, 32 / 8 heads of 128).
+// half of 128 columns over both blocks (of 96, wave 1 adds 32 that are not stored).  That keeps a wave's sums
+// at 64 registers, so that two waves fit a SIMD and one's exponentials run beside the other's products (a wave
+// that held whole sums took 400 registers and ran alone: 735 us against 475 us on six ragged causal sequences
+// of 700 .. 4001 tokens, 32/8 heads of 128).  Bound as the forward pass; 4 x 4096 causal rows, 32/8 heads of 128,
+// 1285 us = 856 TFLOP/s in its four products.
 template <int D>
 struct Dkv {
     static constexpr bool kPair = D > 64;
