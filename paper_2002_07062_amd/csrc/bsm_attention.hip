@@ -300,6 +300,8 @@ __global__ __launch_bounds__(kThreads, D > 64 && KS == 2 ? 1 : 2) void attention
 // that held whole sums took 400 registers and ran alone: 735 us against 475 us on six ragged causal sequences
 // of 700 .. 4001 tokens, 32/8 heads of 128).  Bound as the forward pass; 4 x 4096 causal rows, 32/8 heads of 128,
 // 1285 us = 856 TFLOP/s in its four products.
+// KS = 2, heads of 64: 64 keys, two waves of each 32 with a block of every step's query rows; for plans with little to
+// do (see key_rows).
 template <int D>
 struct Dkv {
     static constexpr bool kPair = D > 64;
@@ -307,9 +309,10 @@ struct Dkv {
     static constexpr int kTiles = 2;  // blocks of 32 columns that a wave adds up
 };
 
-template <int D, bool DIRECT>
+template <int D, bool DIRECT, int KS>
 __global__ __launch_bounds__(Dkv<D>::kThreads, 2) void attention_dkv_kernel(const SequenceArgs a, const Unit* __restrict__ units) {
     constexpr bool kPair = Dkv<D>::kPair;
+    static_assert(KS == 1 || (KS == 2 && !kPair), "");
     constexpr int kTiles = Dkv<D>::kTiles, kBlocks = kKeys / 32;
     // (One array: of several, the compiler forgets which tiles a step reads and writes, and waits for the
     // loads on their way before every read of LDS.)
@@ -322,7 +325,8 @@ __global__ __launch_bounds__(Dkv<D>::kThreads, 2) void attention_dkv_kernel(cons
     const Unit u = units[blockIdx.x];
     if (u.rows <= 0) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), li = lane & 31, h = lane >> 5;
-    const int pair = kPair ? wave >> 1 : wave, x = kPair ? wave & 1 : 0;
+    const int pair = kPair ? wave >> 1 : wave % (4 / KS), x = kPair ? wave & 1 : 0;
+    const int mine_block = kPair ? x : wave / (4 / KS);  // of every step's query rows, where a wave takes one block
     const int chunks = a.dim / 8;
     const int j0 = u.first + kRows * pair, j = j0 + li;
     const bool live = j < u.first + u.rows;
@@ -380,8 +384,8 @@ __global__ __launch_bounds__(Dkv<D>::kThreads, 2) void attention_dkv_kernel(cons
         put(lds.tile[0][0], lds.tile[0][1], lds.stat[0]);
     }
     constexpr int kBlockBytes = 32 * Tile<D>::kRowBytes;
-    const RowFrags<D> rows_at(lane, x * kBlockBytes);
-    const ColFrags<D, kTiles> mine_at(lane, x * kTiles, x * kBlockBytes), other_at(lane, x * kTiles, (1 - x) * kBlockBytes);
+    const RowFrags<D> rows_at(lane, mine_block * kBlockBytes);
+    const ColFrags<D, kTiles> mine_at(lane, x * kTiles, mine_block * kBlockBytes), other_at(lane, x * kTiles, (1 - x) * kBlockBytes);
     // whether the mask hides every pair of the step's query rows i0 .. i0 + 31 and the wave's keys
     auto none = [&](int i0) __attribute__((always_inline)) {
         const int p0 = i0 + off, p1 = min(i0 + 32, end) - 1 + off;  // positions
@@ -459,6 +463,13 @@ __global__ __launch_bounds__(Dkv<D>::kThreads, 2) void attention_dkv_kernel(cons
                 col_product(dv, other_at, now_d, 0, po);
                 col_product(dk, other_at, now_q, 0, so);
             }
+        } else if constexpr (KS == 2) {
+            const int i0 = 32 * mine_block;
+            if (!none(r0 + i0)) {
+                block(r0 + i0, 0, i0, now_q, now_d, now_stat, po, so);
+                col_product(dv, mine_at, now_d, 0, po);
+                col_product(dk, mine_at, now_q, 0, so);
+            }
         } else {
 #pragma unroll
             for (int y = 0; y < kBlocks; ++y) {
@@ -475,6 +486,19 @@ __global__ __launch_bounds__(Dkv<D>::kThreads, 2) void attention_dkv_kernel(cons
     in_turn(n0, total, 1, [&](int64_t n, auto buf) {
         step(n, lds.tile[1 - buf][0], lds.tile[1 - buf][1], lds.stat[1 - buf], lds.tile[buf][0], lds.tile[buf][1], lds.stat[buf]);
     });
+    if constexpr (KS == 2) {  // the other wave's sums over the same keys
+        static_assert(2 * 32 * kTiles * kWave * 4 <= sizeof(lds.tile), "");
+        float* other = reinterpret_cast<float*>(lds.tile) + pair * 32 * kTiles * kWave + lane;
+        lds_barrier();  // the tiles are read
+        if (mine_block == 1) {
+            each_sum(dk, [&](int n, float y) { other[n * kWave] = y; });
+            each_sum(dv, [&](int n, float y) { other[(16 * kTiles + n) * kWave] = y; });
+        }
+        lds_barrier();
+        if (mine_block == 1) return;
+        each_sum(dk, [&](int n, float& y) { y += other[n * kWave]; });
+        each_sum(dv, [&](int n, float& y) { y += other[(16 * kTiles + n) * kWave]; });
+    }
     if (u.parts > 1) {
         if (!live) return;
         float* to = a.part + (u.part_row + u.part * u.rows + j - u.first) * 2 * D + 4 * h;
@@ -584,7 +608,11 @@ hipError_t launch_attention_backward(const SequenceArgs& a, const GradientUnits&
         });
     if (e == hipSuccess && u.n_kv > 0)
         e = with_dim(a.dim, aligned_pieces(a.q) && aligned_pieces(a.dout), [&](auto d, auto direct) {
-            attention_dkv_kernel<d(), direct()><<<static_cast<unsigned>(u.n_kv), Dkv<d()>::kThreads, 0, stream>>>(a, u.kv);
+            const unsigned grid = static_cast<unsigned>(u.n_kv);
+            if (d() == 64 && a.key_rows < kTileRows)
+                attention_dkv_kernel<64, direct(), 2><<<grid, Dkv<64>::kThreads, 0, stream>>>(a, u.kv);
+            else
+                attention_dkv_kernel<d(), direct(), 1><<<grid, Dkv<d()>::kThreads, 0, stream>>>(a, u.kv);
         });
     const int64_t joins = u.n_q_joins + u.n_kv_joins;
     if (e == hipSuccess && joins > 0)

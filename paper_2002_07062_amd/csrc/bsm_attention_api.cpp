@@ -25,7 +25,7 @@ struct bsm_attention_plan_s {
     bsm_att::Sequences seqs;
     int64_t n_forward = 0, n_q = 0, n_kv = 0, n_q_joins = 0, n_kv_joins = 0;
     int64_t q_part_rows = 0, kv_part_rows = 0;
-    int32_t forward_rows = 0, dq_rows = 0;  // of a unit of the forward pass and of dq
+    int32_t forward_rows = 0, dq_rows = 0, key_rows = 0;  // of a unit of the forward pass, of dq, of dk and dv
     bool few_units = false;                 // as in SequenceArgs
     void* d_units = nullptr;  // units of the forward pass, of dq, of dk and dv, and the joins of both
     std::atomic<bool> used{false};
@@ -236,7 +236,8 @@ bsm_status create(bsm_attention_plan* out_plan, const int32_t* q_len, const int3
         const bool pairs = !long_heads || p->dq_rows == bsm_att::kTileRows;
         const bsm_att::Units f = bsm_att::make_units(s, false, p->forward_rows, 0, false, schedule, n_xcd);
         const bsm_att::Units q = bsm_att::make_units(s, false, p->dq_rows, pairs ? 2 * cus : cus, pairs, schedule, n_xcd);
-        const bsm_att::Units kv = bsm_att::make_units(s, true, bsm_att::kTileRows, long_heads ? cus : 2 * cus, false, schedule, n_xcd);
+        p->key_rows = bsm_att::key_rows(s, n_cu);
+        const bsm_att::Units kv = bsm_att::make_units(s, true, p->key_rows, long_heads ? cus : 2 * cus, false, schedule, n_xcd);
         p->n_forward = static_cast<int64_t>(f.units.size());
         p->n_q = static_cast<int64_t>(q.units.size());
         p->n_kv = static_cast<int64_t>(kv.units.size());
@@ -370,6 +371,7 @@ bsm_status backward(bsm_attention_plan p, const bsm_heads* q, const bsm_heads* k
     a.group = s.heads_q / s.heads_kv;
     a.dim = s.dim;
     a.unit_rows = p->dq_rows;
+    a.key_rows = p->key_rows;
     a.few_units = p->few_units;
     a.mask = s.mask;
     a.scale = scale;

@@ -43,6 +43,7 @@ struct SequenceArgs {
     int32_t group;    // query heads per key/value head
     int32_t dim;
     int32_t unit_rows;  // query rows of a query unit: kTileRows, or half of them
+    int32_t key_rows;   // keys of a key unit: kTileRows, or of head dimensions up to 64 half of them
     int32_t few_units;  // these run at once, two workgroups on a CU, and have more than 64 keys
     Mask mask;
     float scale;

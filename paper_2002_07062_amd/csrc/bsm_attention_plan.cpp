@@ -192,6 +192,19 @@ int32_t query_rows(const Sequences& s, int n_cu) {
     return 4 * longest * 2 * n_cu > quarters * total ? kTileRows / 2 : kTileRows;
 }
 
+int32_t key_rows(const Sequences& s, int n_cu) {
+    // A workgroup of 64 keys takes a step in about half the time of one of 128 where it is alone on its CU, but two of
+    // them bring the query rows in twice.  It pays up to about four steps for each of two workgroups on a CU.  us, gradient
+    // with 128 and 64 keys, heads of 64: 1.5 steps 29.4, 23.3 (2 x 512 causal rows, 12 heads), 2.3 33.6, 31.8 (3 x 600, 8/2
+    // heads), 4 45.8, 45.3 (2000 rows, 4/1 heads), 16 114, 125 (4096 causal rows, 8 heads).
+    if (padded_dim(s.dim) > 64) return kTileRows;
+    int64_t total = 0;
+    for (int64_t b = 0; b < s.batch; ++b)
+        for (int64_t first = 0; first < s.kv_len[b]; first += kTileRows)
+            total += key_steps(s, b, first, std::min<int64_t>(kTileRows, s.kv_len[b] - first)) * s.heads_kv;
+    return total <= 4 * 2 * static_cast<int64_t>(n_cu) ? kTileRows / 2 : kTileRows;
+}
+
 Units make_units(const Sequences& s, bool of_keys, int32_t rows, int64_t slots, bool with_care, bsm_schedule schedule, int n_xcd) {
     const std::vector<int32_t>& len = of_keys ? s.kv_len : s.q_len;
     const int heads = of_keys ? s.heads_kv : s.heads_q, group = heads / s.heads_kv;

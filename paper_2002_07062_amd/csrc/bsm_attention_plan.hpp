@@ -29,6 +29,8 @@ void finish_sequences(Sequences* s, const int64_t* q_start, const int64_t* kv_st
 
 // Rows of the forward pass's query units: 128, or 64 where the longest of 128 would outlast the others.
 int32_t query_rows(const Sequences& s, int n_cu);
+// Keys of the units of dk and dv: 128, or 64 where there is little to do.
+int32_t key_rows(const Sequences& s, int n_cu);
 
 // Units of `rows` query rows (forward pass, dq), or of keys (dk, dv), in launch order; the unit of
 // workgroup w is expected to run on XCD w mod n_xcd.  Where `slots` workgroups run at once, units that
