@@ -495,6 +495,7 @@ bsm_status paged(const bsm_cache* cache, const bsm_heads* q, const bsm_heads* o,
     a.shares = cut.shares;
     a.round = cut.round;
     a.tiles = cut.tiles;
+    a.tile_count = cut.tile_count;
     a.splits = cut.splits;
     a.split_keys = cut.split_keys;
     a.few_part = static_cast<float*>(workspace);

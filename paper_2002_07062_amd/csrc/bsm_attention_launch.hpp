@@ -90,6 +90,7 @@ struct PagedArgs {
     // The others go by tiles of kTileRows rows, `tiles` per request and key/value head (0: there are none),
     // in `splits` pieces of the key axis of split_keys keys each, a multiple of kKeyTile.
     int32_t tiles, splits, split_keys;
+    int64_t tile_count;  // tiles with rows, of one head, at most
     float *few_part, *tile_part;  // outputs and statistics of what has to be joined
 };
 

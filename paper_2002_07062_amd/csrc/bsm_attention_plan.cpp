@@ -276,6 +276,9 @@ PagedCut cut_paged(int64_t batch, int64_t tokens, int32_t heads_kv, int32_t grou
         // Two workgroups fit a CU.  A piece's rows cost a write and a read of their own, so there are no more
         // pieces than fill the CUs once (8 chunks of 512 tokens over 1k..8k, 8 kv heads, which fill them
         // twice: 320 us, in two pieces 476 us).
+        // (a request's last tile may be empty in part; more than 256 requests' are not counted on the device)
+        c.tile_count = batch * c.tiles;
+        if (batch <= 256) c.tile_count = std::min(c.tile_count, tokens * group / kTileRows + std::min(batch, tokens));
         const int64_t units = std::max<int64_t>(1, batch * heads_kv * c.tiles), slots = 2 * static_cast<int64_t>(n_cu);
         // Of a mixed batch most tiles hold nothing: there are about as many as its tokens fill, and one for every fourth
         // request (21 requests of 1 .. 88 tokens over 500 .. 9900, 16/4 heads of 80: 113 us counting all tiles, 86 us so).
@@ -286,7 +289,7 @@ PagedCut cut_paged(int64_t batch, int64_t tokens, int32_t heads_kv, int32_t grou
         c.split_keys = static_cast<int32_t>(each);
         c.splits = static_cast<int32_t>((keys + each - 1) / each);
         c.tile_floats = c.splits > 1 ? units * c.splits * kTileRows * (padded + 2) : 0;
-        c.grid = std::max(c.grid, units * std::max(c.splits, 32));  // the join has up to 32 workgroups for each tile
+        c.grid = std::max(c.grid, c.tile_count * heads_kv * std::max(c.splits, 32));  // the join has up to 32 workgroups for each tile
     }
     return c;
 }

@@ -44,6 +44,7 @@ Units make_units(const Sequences& s, bool of_keys, int32_t rows, int64_t slots, 
 // How attention over a paged cache is cut.
 struct PagedCut {
     int32_t few_rows, shares, round, tiles, splits, split_keys;  // as in PagedArgs
+    int64_t tile_count;
     int64_t few_floats, tile_floats;                                   // of the parts
     int64_t grid;                                                      // workgroups of the largest launch
 };

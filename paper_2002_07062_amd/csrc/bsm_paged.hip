@@ -109,41 +109,39 @@ __device__ __forceinline__ int64_t part_at(const PagedArgs& a, int D, const Requ
     return (((static_cast<int64_t>(r.b) * a.cache.heads + r.head) * a.tiles + tile) * a.splits + piece) * kTileRows * (D + 2);
 }
 
-// What workgroup w does.  The requests follow each other, the one with the most keys first (with more
-// than kThreads of them, as they come), so that the CUs end together; of each its tiles (the last ones, which see
-// most keys, first), pieces and heads, the heads side by side.  They are rotated from request to request: a page has its heads side by side, and
-// an XCD that only ever read one of 8 heads of 128 (workgroups go to the 8 XCDs in turn) would use 2 of
-// its 16 L2 channels, which lie 256 bytes apart.
-struct Place {
-    int64_t b;
-    int head, tile, piece;
+// The n-th tile of all, of one head.  The requests follow each other, the one with the most keys first (with more than
+// kThreads of them, as they come), so that the CUs end together; of each the last tiles, which see most keys, first.
+// Of up to kThreads requests only the tiles that hold rows count: the others of a batch of single tokens and a few
+// chunks would cost a workgroup's start each (63 single tokens and a chunk of 512, 8 kv heads: 8192 of them, 8064 empty).
+// b < 0: there is none.
+struct TileOf {
+    int b, tile;
 };
-__device__ __forceinline__ Place place_of(const PagedArgs& a, int64_t w, int* mem) {
-    const int64_t per = static_cast<int64_t>(a.tiles) * a.splits, unit = w / a.cache.heads;
-    Place p;
-    p.b = unit / per;
-    p.tile = a.tiles - 1 - static_cast<int>(unit % per) / a.splits;
-    p.piece = static_cast<int>(unit % per) % a.splits;
-    p.head = static_cast<int>((w + p.b) % a.cache.heads);
-    if (a.batch <= kThreads) {
-        const int i = threadIdx.x, n = static_cast<int>(a.batch);
-        int mine = -1;
-        if (i < n) {
-            const Request r = request<false>(a, i, 0);
-            mine = r.rows > 0 ? r.kv_len : -1;
-            mem[1 + i] = mine;
-        }
-        __syncthreads();
-        if (i < n) {
-            int rank = 0;
-            for (int j = 0; j < n; ++j) rank += mem[1 + j] > mine || (mem[1 + j] == mine && j < i) ? 1 : 0;
-            if (rank == p.b) mem[0] = i;
-        }
-        __syncthreads();
-        p.b = __builtin_amdgcn_readfirstlane(mem[0]);
-        __syncthreads();
+constexpr int kTileOfInts = 2 + 2 * kThreads;
+__device__ __forceinline__ TileOf tile_of(const PagedArgs& a, int64_t n, int* mem) {
+    if (a.batch > kThreads) return {static_cast<int>(n / a.tiles), a.tiles - 1 - static_cast<int>(n % a.tiles)};
+    const int i = threadIdx.x, count = static_cast<int>(a.batch);
+    int *kv = mem + 2, *tiles = kv + kThreads, mine = -1, own = 0;
+    if (i < count) {
+        const Request r = request<false>(a, i, 0);
+        own = (r.rows + kTileRows - 1) / kTileRows;
+        kv[i] = mine = r.kv_len;
+        tiles[i] = own;
     }
-    return p;
+    if (i == 0) mem[0] = -1;
+    __syncthreads();
+    if (own > 0) {
+        int64_t before = 0;
+        for (int j = 0; j < count; ++j) before += kv[j] > mine || (kv[j] == mine && j < i) ? tiles[j] : 0;
+        if (n >= before && n < before + own) {
+            mem[0] = i;
+            mem[1] = own - 1 - static_cast<int>(n - before);
+        }
+    }
+    __syncthreads();
+    const TileOf t = {__builtin_amdgcn_readfirstlane(mem[0]), __builtin_amdgcn_readfirstlane(mem[1])};
+    __syncthreads();
+    return t;
 }
 
 __device__ __forceinline__ bool names_page(const PagedArgs& a, int entry) { return entry >= 0 && entry < a.cache.n_pages; }
@@ -217,9 +215,14 @@ __global__ __launch_bounds__(kThreads, 2) void paged_kernel(const PagedArgs a) {
     // (One array: of several, the compiler forgets which tiles a step reads and writes, and waits for the
     // loads on their way before every read of LDS.)
     __shared__ __align__(16) uint16_t lds[2][2][kTileElems];  // buffer, K or V
-    const Place at = place_of(a, blockIdx.x, reinterpret_cast<int*>(lds));
-    const int tile = at.tile, piece = at.piece;
-    const Request r = request<false>(a, at.b, at.head);
+    // A tile's pieces and heads follow each other, the heads side by side.  They are rotated from request to request: a page
+    // has its heads side by side, and an XCD that only ever read one of 8 heads of 128 (workgroups go to the 8 XCDs in
+    // turn) would use 2 of its 16 L2 channels, which lie 256 bytes apart.
+    const int64_t n = blockIdx.x / a.cache.heads;
+    const TileOf at = tile_of(a, n / a.splits, reinterpret_cast<int*>(lds));
+    if (at.b < 0) return;
+    const int tile = at.tile, piece = static_cast<int>(n % a.splits);
+    const Request r = request<false>(a, at.b, static_cast<int>((blockIdx.x + at.b) % a.cache.heads));
     const int tile0 = tile * kTileRows;
     if (tile0 >= r.rows) return;
     const Pieces ps = pieces(a, r, tile0);
@@ -401,7 +404,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_few_kernel(const PagedArgs 
 
     // the share: `left` blocks from block `block` of request b
     const int64_t w = blockIdx.x / a.cache.heads;
-    const int head = static_cast<int>((blockIdx.x + w) % a.cache.heads);  // rotated, see place_of
+    const int head = static_cast<int>((blockIdx.x + w) % a.cache.heads);  // rotated, see paged_kernel
     int64_t b = 0, left = 0;
     int block = 0;
     if (a.shares == 0) {  // one request each
@@ -712,10 +715,13 @@ __device__ __forceinline__ void join_row(const PagedArgs& a, const Request& r, i
 // Joins the pieces of the rows that more than one piece holds: a workgroup per `rows` rows of a tile.
 template <int D>
 __global__ __launch_bounds__(kThreads) void paged_join_kernel(const PagedArgs a, int rows) {
+    __shared__ int mem[kTileOfInts];
     const int groups = kTileRows / rows;
-    const int64_t unit = blockIdx.x / groups / a.cache.heads;
-    const Request r = request<false>(a, unit / a.tiles, static_cast<int>(blockIdx.x / groups % a.cache.heads));
-    const int tile = static_cast<int>(unit % a.tiles), tile0 = tile * kTileRows, i0 = static_cast<int>(blockIdx.x % groups) * rows;
+    const int64_t n = blockIdx.x / groups;
+    const TileOf at = tile_of(a, n / a.cache.heads, mem);
+    if (at.b < 0) return;
+    const Request r = request<false>(a, at.b, static_cast<int>(n % a.cache.heads));
+    const int tile = at.tile, tile0 = tile * kTileRows, i0 = static_cast<int>(blockIdx.x % groups) * rows;
     if (tile0 + i0 >= r.rows) return;
     const Pieces ps = pieces(a, r, tile0);
     if (ps.first == ps.last) return;
@@ -903,7 +909,7 @@ hipError_t launch_paged(const PagedArgs& a, hipStream_t stream) {
     const int64_t units = a.batch * a.cache.heads;
     hipError_t e = hipSuccess;
     if (a.tiles > 0) {
-        const unsigned tiles = static_cast<unsigned>(units * a.tiles), grid = tiles * a.splits;
+        const unsigned tiles = static_cast<unsigned>(a.tile_count * a.cache.heads), grid = tiles * a.splits;
         if (aligned_pieces({a.cache.k, a.cache.page, a.cache.row, a.cache.head}) && reinterpret_cast<uintptr_t>(a.cache.v) % 16 == 0)
             paged_kernel<D, true><<<grid, kThreads, 0, stream>>>(a);
         else paged_kernel<D, false><<<grid, kThreads, 0, stream>>>(a);
