@@ -245,7 +245,8 @@ bsm_status create(bsm_attention_plan* out_plan, const int32_t* q_len, const int3
         p->n_kv_joins = static_cast<int64_t>(kv.joins.size());
         p->q_part_rows = q.part_rows;
         p->kv_part_rows = kv.part_rows;
-        if (std::max({p->n_forward, p->n_q, p->n_kv}) > kMostWorkgroups) return fail(BSM_ERR_INVALID_ARG, "too many rows for one plan");
+        // (those of dk and dv of longer heads have 512 threads)
+        if (std::max({p->n_forward, p->n_q, p->n_kv * (long_heads ? 2 : 1)}) > kMostWorkgroups) return fail(BSM_ERR_INVALID_ARG, "too many rows for one plan");
         p->device = device;
         p->schedule = schedule;
         p->n_xcd = n_xcd;

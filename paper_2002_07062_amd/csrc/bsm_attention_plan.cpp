@@ -249,7 +249,7 @@ PagedCut cut_paged(int64_t batch, int64_t tokens, int32_t heads_kv, int32_t grou
     const int padded = padded_dim(dim);
     // Few rows over many keys are bound by reading the cache, many rows by the products: each has a kernel.  A
     // batch that may hold both launches both (one chunk of 512 tokens over 4096 and 63 single tokens over
-    // 5000, 8 kv heads: 732 us by tiles alone, 370 us by both); where no request is shorter than the
+    // 5000, 8 kv heads: 732 us by tiles alone, 377 us by both); where no request is shorter than the
     // longest chunk, or there is only one, the tiles do.
     if (rows <= 32) c.few_rows = rows <= 16 ? 16 : 32;
     else if (batch > 1 && group <= 32 && tokens < batch * max_q) c.few_rows = group <= 16 ? 16 : 32;
@@ -278,17 +278,17 @@ PagedCut cut_paged(int64_t batch, int64_t tokens, int32_t heads_kv, int32_t grou
         // twice: 320 us, in two pieces 476 us).
         // (a request's last tile may be empty in part; more than 256 requests' are not counted on the device)
         c.tile_count = batch * c.tiles;
-        if (batch <= 256) c.tile_count = std::min(c.tile_count, tokens * group / kTileRows + std::min(batch, tokens));
+        const bool counted = batch <= 256, mixed = counted && tokens < batch * max_q;
+        if (counted) c.tile_count = std::min(c.tile_count, tokens * group / kTileRows + std::min(batch, tokens));
         const int64_t units = std::max<int64_t>(1, batch * heads_kv * c.tiles), slots = 2 * static_cast<int64_t>(n_cu);
         // Of a mixed batch most tiles hold nothing: there are about as many as its tokens fill, and one for every fourth
         // request (21 requests of 1 .. 88 tokens over 500 .. 9900, 16/4 heads of 80: 113 us counting all tiles, 86 us so).
-        const bool mixed = tokens < batch * max_q;
         const int64_t held = std::max<int64_t>(1, mixed ? std::min(units, (tokens * group / kTileRows + (batch + 3) / 4) * heads_kv) : units);
         const int64_t splits = std::max<int64_t>(1, std::min((slots + held - 1) / held, (keys + 255) / 256));
         const int64_t each = ((keys + splits - 1) / splits + kKeyTile - 1) / kKeyTile * kKeyTile;
         c.split_keys = static_cast<int32_t>(each);
         c.splits = static_cast<int32_t>((keys + each - 1) / each);
-        c.tile_floats = c.splits > 1 ? units * c.splits * kTileRows * (padded + 2) : 0;
+        c.tile_floats = c.splits > 1 ? c.tile_count * heads_kv * c.splits * kTileRows * (padded + 2) : 0;
         c.grid = std::max(c.grid, c.tile_count * heads_kv * std::max(c.splits, 32));  // the join has up to 32 workgroups for each tile
     }
     return c;

@@ -104,9 +104,9 @@ __device__ __forceinline__ int64_t row_at(const PagedArgs& a, const Request& r, 
     return (r.q0 + row / a.group) * t.row + (r.head * a.group + row % a.group) * t.head;
 }
 
-// Floats of one piece's part: its rows' outputs, then their references and sums.
-__device__ __forceinline__ int64_t part_at(const PagedArgs& a, int D, const Request& r, int tile, int piece) {
-    return (((static_cast<int64_t>(r.b) * a.cache.heads + r.head) * a.tiles + tile) * a.splits + piece) * kTileRows * (D + 2);
+// Where the part of one piece of the n-th tile (see tile_of) begins: its rows' outputs, then their references and sums.
+__device__ __forceinline__ int64_t part_at(const PagedArgs& a, int D, int head, int64_t n, int piece) {
+    return ((n * a.cache.heads + head) * a.splits + piece) * kTileRows * (D + 2);
 }
 
 // The n-th tile of all, of one head.  The requests follow each other, the one with the most keys first (with more than
@@ -218,10 +218,10 @@ __global__ __launch_bounds__(kThreads, 2) void paged_kernel(const PagedArgs a) {
     // A tile's pieces and heads follow each other, the heads side by side.  They are rotated from request to request: a page
     // has its heads side by side, and an XCD that only ever read one of 8 heads of 128 (workgroups go to the 8 XCDs in
     // turn) would use 2 of its 16 L2 channels, which lie 256 bytes apart.
-    const int64_t n = blockIdx.x / a.cache.heads;
-    const TileOf at = tile_of(a, n / a.splits, reinterpret_cast<int*>(lds));
+    const int64_t n = blockIdx.x / a.cache.heads / a.splits;
+    const TileOf at = tile_of(a, n, reinterpret_cast<int*>(lds));
     if (at.b < 0) return;
-    const int tile = at.tile, piece = static_cast<int>(n % a.splits);
+    const int tile = at.tile, piece = static_cast<int>(blockIdx.x / a.cache.heads % a.splits);
     const Request r = request<false>(a, at.b, static_cast<int>((blockIdx.x + at.b) % a.cache.heads));
     const int tile0 = tile * kTileRows;
     if (tile0 >= r.rows) return;
@@ -287,7 +287,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_kernel(const PagedArgs a) {
         uint16_t* out = a.o.p + q_row * a.o.row + q_head * a.o.head;
         store_row<D>(out, live, st.o, total == 0.0f ? 0.0f : 1.0f / total, h, chunks);
     } else if (live) {
-        float* part = a.tile_part + part_at(a, D, r, tile, piece);
+        float* part = a.tile_part + part_at(a, D, r.head, n, piece);
         float* to = part + (row - tile0) * D + 4 * h;
 #pragma unroll
         for (int t = 0; t < D / 32; ++t)
@@ -717,15 +717,15 @@ template <int D>
 __global__ __launch_bounds__(kThreads) void paged_join_kernel(const PagedArgs a, int rows) {
     __shared__ int mem[kTileOfInts];
     const int groups = kTileRows / rows;
-    const int64_t n = blockIdx.x / groups;
-    const TileOf at = tile_of(a, n / a.cache.heads, mem);
+    const int64_t n = blockIdx.x / groups / a.cache.heads;
+    const TileOf at = tile_of(a, n, mem);
     if (at.b < 0) return;
-    const Request r = request<false>(a, at.b, static_cast<int>(n % a.cache.heads));
+    const Request r = request<false>(a, at.b, static_cast<int>(blockIdx.x / groups % a.cache.heads));
     const int tile = at.tile, tile0 = tile * kTileRows, i0 = static_cast<int>(blockIdx.x % groups) * rows;
     if (tile0 + i0 >= r.rows) return;
     const Pieces ps = pieces(a, r, tile0);
     if (ps.first == ps.last) return;
-    const float* first = a.tile_part + part_at(a, D, r, tile, ps.first);
+    const float* first = a.tile_part + part_at(a, D, r.head, n, ps.first);
     const int64_t piece_floats = static_cast<int64_t>(kTileRows) * (D + 2);
     for (int i = i0 + (threadIdx.x >> 6); i < i0 + rows && tile0 + i < r.rows; i += kWaves)
         join_row<D>(a, r, kTileRows, tile0 + i, i, ps.last - ps.first + 1, [&](int p) { return first + p * piece_floats; });

@@ -116,6 +116,25 @@ def test_paged_attention_matches_the_oracle(case):
         assert torch.isnan(o[tokens:]).all(), "rows behind the last request were written"
 
 
+@pytest.mark.parametrize("batch", [3, 40])
+def test_mixed_batches_in_pieces(batch):
+    """Chunks of many sizes beside single tokens and requests without any, over keys long enough for
+    pieces, some starting before the window of their rows."""
+    rng = np.random.default_rng(batch)
+    new = [int(rng.choice([0, 1, 2, 7, 30, 70, 140])) for _ in range(batch)]
+    new[0], new[-1] = 200, 1
+    kv_len = [n + int(rng.integers(0, 2600)) for n in new]
+    cache = Cache(kv_len, 16, 2, 64, 15)
+    g = torch.Generator().manual_seed(16)
+    q = (2 * torch.randn((sum(new), 6, 64), generator=g)).to(torch.bfloat16).cuda()
+    for window in (0, 900):
+        o = torch.full_like(q, NAN)
+        bsm.bsm_attention_paged(q, cache.k, cache.v, cache.table, i32([0] + list(np.cumsum(new))), i32(kv_len), o,
+                                max_q=max(new), max_kv=max(kv_len), window=window)
+        torch.cuda.synchronize()
+        _check(o, q, cache, new, kv_len, 3, 0.125, window)
+
+
 @pytest.mark.parametrize("chunk,window", [(1, 0), (1, 700), (45, 0)])
 def test_paged_attention_of_hundreds_of_requests(chunk, window):
     """More requests than a workgroup has threads, most of them short, some long, some without new
@@ -164,6 +183,9 @@ def test_long_requests_are_shared():
     assert bsm.bsm_attention_paged_workspace(4, 4, 8, 8, 64, 1, 1024) == 0
     for batch, keys in ((1, 1537), (4, 4096), (64, 32768)):
         assert bsm.bsm_attention_paged_workspace(batch, batch, 8, 8, 64, 1, keys) > 0
+    # a chunk beside many single tokens takes parts of its own rows, not of as many for each request
+    for batch in (2, 200, 2000):
+        assert bsm.bsm_attention_paged_workspace(batch, batch + 4096, 8, 1, 64, 4096, 8192) < 400 << 20
 
 
 def test_bounds_keep_bad_lengths_and_pages_inside():
