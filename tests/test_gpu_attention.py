@@ -331,3 +331,19 @@ def test_a_captured_step_replays():
             assert torch.equal(x, y)
     del graph
     plan.destroy()
+
+
+# "no limit" as a window: the largest numbers, beside rows that see nothing (more queries than keys)
+@pytest.mark.parametrize("n_cu", [0, 1])
+@pytest.mark.parametrize("window", [2**31 - 1, 2**31 - 40, 2**30 + 1])
+@pytest.mark.parametrize("q_len,kv_len,d", [([100], [50], 64), ([300, 40, 9], [131, 10, 9], 128), ([1500], [1100], 64)])
+def test_the_largest_windows_hide_nothing(q_len, kv_len, d, window, n_cu):
+    batch, scale = Batch(q_len, kv_len, 2, 1, d, "packed", 59), float(np.float32(d ** -0.5))
+    plan, o, lse = _run(batch, True, window, n_cu=n_cu)
+    check_forward(batch, o, lse, scale, True)
+    dout = batch.operand("q")
+    grads = [batch.empty("q"), batch.empty("kv"), batch.empty("kv")]
+    bsm.bsm_attention_backward(plan, batch.q, batch.k, batch.v, o, lse, dout, *grads)
+    torch.cuda.synchronize()
+    check_backward(batch, o, lse, dout, *grads, scale, True)
+    plan.destroy()

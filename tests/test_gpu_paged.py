@@ -385,3 +385,17 @@ def test_a_refused_request_comes_out_empty():
     assert taken.tolist() == [2, 1] and kv_len.tolist() == [20, 0] and (slots[20:] == -1).all()
     assert (o[20:] == 0).all() and torch.isfinite(o[:20].float()).all()
     assert torch.isnan(k_cache[[1, 3]]).all()
+
+
+# few rows, tiles, both; some rows see nothing (more new tokens than keys)
+@pytest.mark.parametrize("window", [2**31 - 1, 2**31 - 40])
+@pytest.mark.parametrize("new,kv_len", [([9, 5], [3, 5]), ([60, 20], [30, 20]), ([100, 6, 1], [70, 2, 40])])
+def test_the_largest_windows_hide_nothing(new, kv_len, window):
+    cache = Cache(kv_len, 16, 2, 64, 31)
+    g = torch.Generator().manual_seed(32)
+    q = (2 * torch.randn((sum(new), 4, 64), generator=g)).to(torch.bfloat16).cuda()
+    o = torch.full_like(q, NAN)
+    bsm.bsm_attention_paged(q, cache.k, cache.v, cache.table, i32([0] + list(np.cumsum(new))), i32(kv_len), o,
+                            max_q=max(new), max_kv=max(kv_len), window=window)
+    torch.cuda.synchronize()
+    _check(o, q, cache, new, kv_len, 2, 0.125)
