@@ -95,6 +95,10 @@ struct PagedArgs {
 };
 
 constexpr int kKeyTile = 128;
+// Rows of a tile that a workgroup joins, where `tiles` of all heads have pieces to join: a wave takes four of them one
+// after the other, but one where that leaves few workgroups (a chunk of 16 tokens over 16384 keys, 32/8 heads of 128:
+// 52 us with four, 30 us with one).
+constexpr int join_rows(int64_t tiles) { return tiles < 128 ? 4 : 16; }
 constexpr int kFewKeys = 128, kFewestBlocks = 4, kMostBlocks = 16;  // of a share, see share_of
 
 hipError_t launch_attention_paged(const PagedArgs& a, hipStream_t stream);

@@ -289,7 +289,9 @@ PagedCut cut_paged(int64_t batch, int64_t tokens, int32_t heads_kv, int32_t grou
         c.split_keys = static_cast<int32_t>(each);
         c.splits = static_cast<int32_t>((keys + each - 1) / each);
         c.tile_floats = c.splits > 1 ? c.tile_count * heads_kv * c.splits * kTileRows * (padded + 2) : 0;
-        c.grid = std::max(c.grid, c.tile_count * heads_kv * std::max(c.splits, 32));  // the join has up to 32 workgroups for each tile
+        const int64_t tiles = c.tile_count * heads_kv;
+        c.grid = std::max(c.grid, tiles * c.splits);
+        if (c.splits > 1) c.grid = std::max(c.grid, tiles * (kTileRows / join_rows(tiles)));
     }
     return c;
 }

@@ -915,9 +915,8 @@ hipError_t launch_paged(const PagedArgs& a, hipStream_t stream) {
         else paged_kernel<D, false><<<grid, kThreads, 0, stream>>>(a);
         e = hipGetLastError();
         if (e == hipSuccess && a.splits > 1) {
-            // A wave joins four rows one after the other, but one where that leaves few workgroups (a chunk of 16
-            // tokens over 16384 keys, 32/8 heads of 128: 52 us with four, 30 us with one).
-            const int rows = tiles < 128 ? kWaves : 4 * kWaves;
+            const int rows = join_rows(tiles);
+            static_assert(join_rows(1) % kWaves == 0 && join_rows(1 << 20) % kWaves == 0, "whole rounds of the waves");
             paged_join_kernel<D><<<tiles * (kTileRows / rows), kThreads, 0, stream>>>(a, rows);
             e = hipGetLastError();
         }

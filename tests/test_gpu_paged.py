@@ -399,3 +399,34 @@ def test_the_largest_windows_hide_nothing(new, kv_len, window):
                             max_q=max(new), max_kv=max(kv_len), window=window)
     torch.cuda.synchronize()
     _check(o, q, cache, new, kv_len, 2, 0.125)
+
+
+@pytest.mark.parametrize("batch,chunk,hq,hk", [(300, 4096, 64, 8), (512, 2048, 64, 8), (512, 4096, 32, 8), (512, 8192, 32, 8),
+                                               (257, 8192, 64, 8), (2000, 4096, 16, 2), (2000, 4096, 64, 8)])
+def test_hundreds_of_requests_beside_a_long_chunk_are_taken(batch, chunk, hq, hk):
+    """What a call launches decides whether it is too large, not a join that it does not need."""
+    assert bsm.bsm_attention_paged_workspace(batch, batch + chunk, hq, hk, 128, chunk, 2 * chunk) < 1 << 30
+    with pytest.raises(bsm.BsmError, match="too large"):
+        bsm.bsm_attention_paged_workspace(1 << 20, (1 << 20) + chunk, hq, hk, 128, chunk, 2 * chunk)
+
+
+def test_hundreds_of_requests_beside_a_chunk():
+    """300 requests, 64/8 heads, room for a chunk of 4096: single tokens, one chunk, some without any."""
+    rng = np.random.default_rng(8)
+    new = rng.integers(0, 2, 300).tolist()
+    new[0], new[255], new[256], new[280], new[299] = 1, 3, 1, 150, 40
+    kv_len = [n + int(rng.integers(0, 30)) for n in new]
+    kv_len[255], kv_len[256] = 700, 1300
+    cache = Cache(kv_len, 16, 8, 64, 33)
+    g = torch.Generator().manual_seed(34)
+    q = torch.full((4096 + 300, 64, 64), NAN, dtype=torch.bfloat16)
+    q[:sum(new)] = (2 * torch.randn((sum(new), 64, 64), generator=g)).to(torch.bfloat16)
+    q = q.cuda()
+    o = torch.full_like(q, NAN)
+    start = [0] + [int(x) for x in np.cumsum(new)]
+    bsm.bsm_attention_paged(q, cache.k, cache.v, cache.table, i32(start), i32(kv_len), o, max_q=4096, max_kv=8192)
+    torch.cuda.synchronize()
+    assert torch.isfinite(o[:start[-1]].float()).all() and torch.isnan(o[start[-1]:]).all()
+    for b in (0, 1, 100, 255, 256, 280, 298, 299):
+        rows, one = slice(start[b], start[b + 1]), SimpleNamespace(tokens=[cache.tokens[b]])
+        _check(o[rows], q[rows], one, [new[b]], [kv_len[b]], 8, 0.125)
