@@ -101,6 +101,17 @@ struct Rows {
     bool in_order = true;          // no sequence starts before the one before it
 };
 
+// Whether elements at sums of multiples of the strides, with `inner` contiguous ones at each, are apart.
+bool nested(std::vector<std::pair<int64_t, int64_t>> stride_count, int64_t inner) {
+    std::sort(stride_count.begin(), stride_count.end());
+    for (const auto& [stride, count] : stride_count) {
+        if (count <= 1) continue;
+        if (stride < inner) return false;
+        inner += stride * (count - 1);
+    }
+    return true;
+}
+
 // An operand with `heads` heads.  A written one must have a place of its own for each row.
 bsm_status take(const char* name, const bsm_heads* h, const Rows& r, int64_t heads, int64_t dim, bool written, Heads* out, Span* span) {
     if (!h) return fail(BSM_ERR_INVALID_ARG, "%s is NULL", name);
@@ -137,6 +148,8 @@ bsm_status take(const char* name, const bsm_heads* h, const Rows& r, int64_t hea
         const int64_t block = (r.end - 1) * h->row + (heads - 1) * h->head + dim;
         const int64_t own = (r.longest - 1) * h->row + (heads - 1) * h->head + dim;
         apart = apart && (h->seq >= block || (r.in_order && h->seq >= own));
+        // or sequences inside a row or a head, as where the rows or the heads come first
+        apart = apart || nested({{h->seq, batch}, {h->row, r.end}, {h->head, heads}}, dim);
     }
     if (!apart) return fail(BSM_ERR_INVALID_ARG, "%s: rows overlap each other", name);
     return BSM_OK;
@@ -539,17 +552,6 @@ bsm_status slots_of(const int32_t* cached, const int32_t* fresh, int64_t batch, 
     e = bsm_att::launch_cache_slots(a, n_cu, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "kernel launch");
     return BSM_OK;
-}
-
-// Whether elements at sums of multiples of the strides, with `inner` contiguous ones at each, are apart.
-bool nested(std::vector<std::pair<int64_t, int64_t>> stride_count, int64_t inner) {
-    std::sort(stride_count.begin(), stride_count.end());
-    for (const auto& [stride, count] : stride_count) {
-        if (count <= 1) continue;
-        if (stride < inner) return false;
-        inner += stride * (count - 1);
-    }
-    return true;
 }
 
 bsm_status append(const bsm_cache* cache, const bsm_heads* k, const bsm_heads* v, const int64_t* slots, int64_t tokens, void* stream) {

@@ -347,3 +347,29 @@ def test_the_largest_windows_hide_nothing(q_len, kv_len, d, window, n_cu):
     torch.cuda.synchronize()
     check_backward(batch, o, lse, dout, *grads, scale, True)
     plan.destroy()
+
+
+@pytest.mark.parametrize("order", [(1, 0, 2), (2, 0, 1), (1, 2, 0), (2, 1, 0)], ids=["rows-batch-heads", "heads-batch-rows", "rows-heads-batch", "heads-rows-batch"])
+def test_batches_inside_rows_or_heads(order):
+    """(batch, rows, heads, dim) operands and results whose sequences do not follow each other in memory:
+    dimension order[i] of the tensor is the i-th outermost."""
+    batch = Batch([40, 77, 5], [90, 77, 33], 4, 2, 64, "padded", 61)
+
+    def laid(x):
+        y = torch.full([x.shape[i] for i in order] + [64], float("nan"), dtype=torch.bfloat16, device="cuda")
+        back = [order.index(i) for i in range(3)]
+        return y.permute(*back, 3).copy_(x)
+
+    batch.q, batch.k, batch.v = (laid(x) for x in (batch.q, batch.k, batch.v))
+    o, dq, dk, dv = (laid(batch.empty(x)) for x in ("q", "q", "kv", "kv"))
+    dout, lse = laid(batch.operand("q")), torch.empty((4, 122), device="cuda")
+    plan = bsm.bsm_attention_plan_create(**batch.plan_args(True))
+    bsm.bsm_attention_execute(plan, batch.q, batch.k, batch.v, o, lse=lse)
+    bsm.bsm_attention_backward(plan, batch.q, batch.k, batch.v, o, lse, dout, dq, dk, dv)
+    torch.cuda.synchronize()
+    check_forward(batch, o, lse, 0.125, True)
+    check_backward(batch, o, lse, dout, dq, dk, dv, 0.125, True)
+    for bad in ((512, 64), (64, 64)):  # heads or sequences on top of each other
+        with pytest.raises(bsm.BsmError, match="overlap each other"):
+            bsm.bsm_attention_execute(plan, batch.q, batch.k, batch.v, torch.as_strided(o, o.shape, (64, *bad, 1)))
+    plan.destroy()
