@@ -452,7 +452,8 @@ bsm_status bsm_attention_execute(bsm_attention_plan plan, const bsm_heads* q, co
  * each (sequence, row, head) a place of its own and add them up.  workspace: workspace_bytes of
  * the plan's stats (for D_i, and under 140 MB for parts on 256 compute units), on a 16-byte
  * boundary, not shared with a call that may run at the same time.  dq, dk and dv overlap no operand
- * (they may interleave with each other, as views of one tensor). */
+ * and not each other; they may interleave as views of one tensor do, head by head, row by row or
+ * sequence by sequence (BSM_ERR_ALIAS otherwise). */
 bsm_status bsm_attention_backward(bsm_attention_plan plan, const bsm_heads* q, const bsm_heads* k,
                                   const bsm_heads* v, const bsm_heads* o, const float* lse,
                                   const bsm_heads* dout, const bsm_heads* dq, const bsm_heads* dk,

@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <array>
 #include <atomic>
 #include <cmath>
 #include <cstdarg>
@@ -153,6 +154,54 @@ bsm_status take(const char* name, const bsm_heads* h, const Rows& r, int64_t hea
     }
     if (!apart) return fail(BSM_ERR_INVALID_ARG, "%s: rows overlap each other", name);
     return BSM_OK;
+}
+
+// How often an operand steps by a stride.
+struct Axis {
+    int64_t stride, count;
+};
+// Whether two operands, each of blocks of `dim` elements at sums of its axes' steps, are apart because they interleave:
+// modulo one of the strides, which their larger strides are multiples of, they keep to different parts.
+bool interleave(const uint16_t* x, const std::array<Axis, 3>& xs, const uint16_t* y, const std::array<Axis, 3>& ys, int64_t dim) {
+    const auto part = [&](const std::array<Axis, 3>& axes, int64_t period) {  // elements of a period that may be used
+        int64_t n = dim;
+        for (const Axis& a : axes)
+            if (a.stride % period != 0) n += a.stride * (a.count - 1);
+        return n;
+    };
+    const int64_t bytes = static_cast<int64_t>(reinterpret_cast<uintptr_t>(y) - reinterpret_cast<uintptr_t>(x));
+    for (const auto* axes : {&xs, &ys})
+        for (const Axis& a : *axes) {
+            if (a.stride < dim || a.count < 2) continue;
+            const int64_t period = 2 * a.stride, at = (bytes % period + period) % period;  // of y behind x, in bytes
+            if (at >= 2 * part(xs, a.stride) && at + 2 * part(ys, a.stride) <= period) return true;
+        }
+    return false;
+}
+
+// Whether two operands are apart sequence by sequence.
+bool sequences_apart(const Heads& x, const Rows& xr, int64_t x_heads, const Heads& y, const Rows& yr, int64_t y_heads, int64_t dim) {
+    struct Block {
+        uintptr_t from, to;
+        int of;
+    };
+    std::vector<Block> blocks;
+    const auto add = [&](const Heads& t, const Rows& r, int64_t heads, int of) {
+        for (size_t b = 0; b < r.start->size(); ++b) {
+            if ((*r.len)[b] == 0) continue;
+            const uintptr_t from = reinterpret_cast<uintptr_t>(t.p + static_cast<int64_t>(b) * t.seq + (*r.start)[b] * t.row);
+            blocks.push_back({from, from + 2 * static_cast<uintptr_t>(((*r.len)[b] - 1) * t.row + (heads - 1) * t.head + dim), of});
+        }
+    };
+    add(x, xr, x_heads, 0);
+    add(y, yr, y_heads, 1);
+    std::sort(blocks.begin(), blocks.end(), [](const Block& p, const Block& q) { return p.from < q.from; });
+    uintptr_t end[2] = {0, 0};  // of the blocks so far
+    for (const Block& b : blocks) {
+        if (b.from < end[1 - b.of]) return false;
+        end[b.of] = std::max(end[b.of], b.to);
+    }
+    return true;
 }
 
 // The same without sequences: rows are token indices.
@@ -374,9 +423,22 @@ bsm_status backward(bsm_attention_plan p, const bsm_heads* q, const bsm_heads* k
             if (overlap(x, y)) return fail(BSM_ERR_ALIAS, "a gradient or the workspace overlaps an operand");
     for (int i = 0; i < 3; ++i) {
         if (overlap(out[i], out[3])) return fail(BSM_ERR_ALIAS, "a gradient overlaps the workspace");
-        for (int j = 0; j < i; ++j)
-            if (out[i].to > out[i].from && out[i].from == out[j].from) return fail(BSM_ERR_ALIAS, "two gradients have the same place");
     }
+    const struct {
+        const Heads& t;
+        const Rows& r;
+        int64_t heads;
+    } grads[3] = {{a.dq, qr, s.heads_q}, {a.dk, kr, s.heads_kv}, {a.dv, kr, s.heads_kv}};
+    for (int i = 0; i < 3; ++i)
+        for (int j = 0; j < i; ++j) {
+            if (!overlap(out[i], out[j])) continue;
+            const auto &x = grads[j], &y = grads[i];
+            const auto axes = [&](const auto& g) {
+                return std::array<Axis, 3>{{{g.t.seq, s.batch}, {g.t.row, g.r.end}, {g.t.head, g.heads}}};
+            };
+            if (!interleave(x.t.p, axes(x), y.t.p, axes(y), s.dim) && !sequences_apart(x.t, x.r, x.heads, y.t, y.r, y.heads, s.dim))
+                return fail(BSM_ERR_ALIAS, "two gradients overlap");
+        }
     a.lse = const_cast<float*>(lse);
     a.delta = static_cast<float*>(workspace);
     a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + delta_bytes(s));

@@ -373,3 +373,93 @@ def test_batches_inside_rows_or_heads(order):
         with pytest.raises(bsm.BsmError, match="overlap each other"):
             bsm.bsm_attention_execute(plan, batch.q, batch.k, batch.v, torch.as_strided(o, o.shape, (64, *bad, 1)))
     plan.destroy()
+
+
+def _one_tensor(layout, n=70, hq=2, hk=2, d=64):
+    """Two sequences of n rows: starts, and dq, dk, dv as views of one tensor, which comes last."""
+    def nan(*shape):
+        return torch.full(shape, float("nan"), dtype=torch.bfloat16, device="cuda")
+
+    w = hq + 2 * hk
+    if layout == "heads":           # beside each other in a row
+        x = nan(2 * n, w, d)
+        return None, None, x[:, :hq], x[:, hq:hq + hk], x[:, hq + hk:], x
+    if layout == "inside heads":
+        x = nan(2 * n, hq, 3, d)
+        return None, None, x[:, :, 0], x[:, :, 1], x[:, :, 2], x
+    if layout == "thirds":
+        x = nan(3, 2 * n, hq, d)
+        return None, None, x[0], x[1], x[2], x
+    if layout == "padded":
+        x = nan(2, n + 3, w, d)
+        return 0, 0, x[:, :, :hq], x[:, :, hq:hq + hk], x[:, :, hq + hk:], x
+    if layout == "heads first":
+        x = nan(2, w, n, d)
+        t = x.transpose(1, 2)
+        return 0, 0, t[:, :, :hq], t[:, :, hq:hq + hk], t[:, :, hq + hk:], x
+    if layout == "rows first":
+        x = nan(n, 2, w, d)
+        t = x.transpose(0, 1)
+        return 0, 0, t[:, :, :hq], t[:, :, hq:hq + hk], t[:, :, hq + hk:], x
+    x = nan(6 * n, hq, d)           # "blocks": a sequence's three after the other
+    return [0, 3 * n], [0, 3 * n], x[:4 * n], x[n:5 * n], x[2 * n:], x
+
+
+@pytest.mark.parametrize("layout,hq,hk", [("heads", 4, 2), ("inside heads", 2, 2), ("thirds", 2, 2), ("padded", 6, 3),
+                                          ("heads first", 4, 1), ("rows first", 2, 2), ("blocks", 2, 2)])
+def test_gradients_as_views_of_one_tensor(layout, hq, hk):
+    batch = Batch([70, 70], [70, 70], hq, hk, 64, "packed", 67)
+    plan, o, lse = _run(batch, True, 0)
+    dout = batch.operand("q")
+    want = [batch.empty("q"), batch.empty("kv"), batch.empty("kv")]
+    bsm.bsm_attention_backward(plan, batch.q, batch.k, batch.v, o, lse, dout, *want)
+    q_start, kv_start, *grads, x = _one_tensor(layout, hq=hq, hk=hk)
+    plan = bsm.bsm_attention_plan_create([70, 70], heads_q=hq, heads_kv=hk, head_dim=64, causal=True, q_start=q_start, kv_start=kv_start)
+
+    def rows(t, b):
+        return t[b, :70] if t.dim() == 4 else t[(q_start or [0, 70])[b]:][:70]
+
+    def laid(t, like):
+        y = torch.zeros_like(like)
+        for b in (0, 1):
+            rows(y, b).copy_(t[70 * b:70 * b + 70])
+        return y
+
+    dq, dk, dv = grads
+    bsm.bsm_attention_backward(plan, laid(batch.q, dq), laid(batch.k, dk), laid(batch.v, dv), laid(o, dq), lse, laid(dout, dq), dq, dk, dv)
+    torch.cuda.synchronize()
+    for mine, ref in zip(grads, want):
+        for b in (0, 1):
+            assert torch.equal(rows(mine, b), ref[70 * b:70 * b + 70])
+    for b in (0, 1):
+        for t in grads:
+            rows(t, b).fill_(float("nan"))
+    assert torch.isnan(x).all()
+
+
+def test_gradients_on_top_of_each_other_are_refused():
+    batch = Batch([70, 70], [70, 70], 2, 2, 64, "packed", 71)
+    plan, o, lse = _run(batch, True, 0)
+    dout = batch.operand("q")
+    x = torch.full((300, 6, 64), float("nan"), dtype=torch.bfloat16, device="cuda")
+    flat, apart = x.view(-1), batch.empty("kv")
+
+    def at(first, row=6 * 64, head=64):
+        return torch.as_strided(flat, (140, 2, 64), (row, head, 1), first)
+
+    def call(dq, dk, dv):
+        bsm.bsm_attention_backward(plan, batch.q, batch.k, batch.v, o, lse, dout, dq, dk, dv)
+
+    bad = [(at(0), at(0)), (at(0), at(64)), (at(64), at(0)), (at(0), at(8)), (at(0), at(6 * 64)), (at(0), at(20 * 6 * 64 + 64)),
+           (at(0), at(320)), (at(0), at(128, row=4 * 64)), (at(0, head=128), at(128, head=128)), (at(0, row=128), at(128 * 139, row=128))]
+    for one, two in bad:
+        for dq, dk, dv in ((one, two, apart), (one, apart, two), (apart, one, two)):
+            with pytest.raises(bsm.BsmError, match="two gradients overlap") as e:
+                call(dq, dk, dv)
+            assert e.value.status == bsm.BSM_ERR_ALIAS
+    torch.cuda.synchronize()
+    assert torch.isnan(x).all()
+    call(at(0), at(128), at(256))
+    call(at(256), at(0, head=128), at(64, head=128))  # every other head
+    call(at(0, row=128), at(128 * 140, row=128), apart)
+    plan.destroy()
