@@ -461,7 +461,8 @@ bsm_status bsm_attention_backward(bsm_attention_plan plan, const bsm_heads* q, c
                                   int64_t workspace_bytes, void* stream);
 
 /* A cache of keys and values in pages: element (page, row, head, d) at page*page_stride +
- * row*row_stride + head*head_stride + d, the same for k and v (bf16). */
+ * row*row_stride + head*head_stride + d, the same for k and v (bf16).  The two may interleave as views
+ * of one tensor do, page by page, row by row or head by head. */
 typedef struct bsm_cache {
     void* k;
     void* v;

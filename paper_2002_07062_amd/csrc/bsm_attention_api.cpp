@@ -633,6 +633,8 @@ bsm_status append(const bsm_cache* cache, const bsm_heads* k, const bsm_heads* v
     if (reinterpret_cast<uintptr_t>(slots) % 8 != 0) return fail(BSM_ERR_INVALID_ARG, "slots is not aligned to its element size");
     const Span ss = bytes_at(slots, 8 * tokens);
     if (sk.from == sv.from) return fail(BSM_ERR_ALIAS, "the cache's k and v have the same place");
+    const std::array<Axis, 3> axes = {{{c.page, c.n_pages}, {c.row, c.page_size}, {c.head, c.heads}}};
+    if (overlap(sk, sv) && !interleave(c.k, axes, c.v, axes, c.dim)) return fail(BSM_ERR_ALIAS, "the cache's k and v overlap");
     if (overlap(sk, fk) || overlap(sk, fv) || overlap(sv, fk) || overlap(sv, fv) || overlap(sk, ss) || overlap(sv, ss))
         return fail(BSM_ERR_ALIAS, "the cache overlaps an operand");
     int device = 0, n_cu = 0;

@@ -430,3 +430,23 @@ def test_hundreds_of_requests_beside_a_chunk():
     for b in (0, 1, 100, 255, 256, 280, 298, 299):
         rows, one = slice(start[b], start[b + 1]), SimpleNamespace(tokens=[cache.tokens[b]])
         _check(o[rows], q[rows], one, [new[b]], [kv_len[b]], 8, 0.125)
+
+
+@pytest.mark.parametrize("form", ["pages", "rows", "heads", "halves", "heads_first"])
+def test_keys_and_values_in_one_tensor(form):
+    """The cache's k and v as views of one tensor, in every way that they interleave."""
+    n_pages, page, hk, d = 9, 16, 2, 64
+    shape = {"pages": (n_pages, 2, page, hk, d), "rows": (n_pages, page, 2, hk, d), "heads": (n_pages, page, hk, 2, d),
+             "halves": (2, n_pages, page, hk, d), "heads_first": (n_pages, hk, 2, page, d)}[form]
+    x = torch.full(shape, NAN, dtype=torch.bfloat16, device="cuda")
+    k_cache, v_cache = x.unbind({"pages": 1, "rows": 2, "heads": 3, "halves": 0, "heads_first": 2}[form])
+    if form == "heads_first":
+        k_cache, v_cache = k_cache.transpose(1, 2), v_cache.transpose(1, 2)
+    g = torch.Generator().manual_seed(35)
+    k, v = (torch.randn((100, hk, d), generator=g).to(torch.bfloat16).cuda() for _ in "kv")
+    slots = torch.randperm(n_pages * page, generator=g)[:100].cuda()
+    bsm.bsm_cache_append(k, v, slots, k_cache, v_cache)
+    torch.cuda.synchronize()
+    for cache, y in ((k_cache, k), (v_cache, v)):
+        assert torch.equal(cache[slots // page, slots % page], y)
+    assert int(torch.isfinite(x.float()).sum()) == 2 * 100 * hk * d

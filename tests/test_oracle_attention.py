@@ -277,3 +277,15 @@ def test_host_only_plans_do_not_run():
     p = _plan()
     st = att._load().bsm_attention_execute(p.handle, *[_heads(1 << (40 + i)) for i in range(4)], None, 0.125, None)
     assert st == bsm.BSM_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("cache,offset", [
+    ({}, 64), ({}, 8), ({}, 128), ({}, 2048), ({}, -64), ({}, 3 * 2048 + 64),
+    (dict(page_stride=2 * 2048), 1024), (dict(page_stride=2 * 2048), 2048 - 8), (dict(row_stride=256, page_stride=16 * 256), 64),
+    (dict(row_stride=256, page_stride=16 * 256), 8 * 256), (dict(head_stride=128, row_stride=256, page_stride=16 * 256), 32),
+])
+def test_caches_on_top_of_each_other_are_refused(cache, offset):
+    """v lies `offset` elements behind k, in it."""
+    at = 1 << 30
+    assert _append(cache=_cache(k=at, v=at + 2 * offset, **cache)) == bsm.BSM_ERR_ALIAS
+    assert "overlap" in bsm.bsm_last_error()
