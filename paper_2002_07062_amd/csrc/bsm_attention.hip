@@ -569,11 +569,7 @@ bool aligned_pieces(const Heads& t) {
 // Calls f with D and DIRECT as constants.
 template <class F>
 hipError_t with_dim(int dim, bool direct, F f) {
-    auto go = [&](auto d) {
-        if (direct) f(d, std::true_type{});
-        else f(d, std::false_type{});
-        return hipGetLastError();
-    };
+    auto go = [&](auto d) { return direct ? f(d, std::true_type{}) : f(d, std::false_type{}); };
     switch (padded_dim(dim)) {
         case 64: return go(std::integral_constant<int, 64>{});
         case 96: return go(std::integral_constant<int, 96>{});
@@ -584,40 +580,39 @@ hipError_t with_dim(int dim, bool direct, F f) {
 hipError_t launch_attention(const SequenceArgs& a, const Unit* units, int64_t n, hipStream_t stream) {
     if (n == 0) return hipSuccess;
     return with_dim(a.dim, aligned_pieces(a.k) && aligned_pieces(a.v), [&](auto d, auto direct) {
-        const unsigned grid = static_cast<unsigned>(n);
-        if (a.unit_rows == kTileRows) attention_kernel<d(), direct(), 1, kKeys><<<grid, kThreads, 0, stream>>>(a, units);
-        else if (d() == 64 && a.few_units) attention_kernel<64, direct(), 2, 2 * kKeys><<<grid, kThreads, 0, stream>>>(a, units);
-        else attention_kernel<d(), direct(), 2, kKeys><<<grid, kThreads, 0, stream>>>(a, units);
+        const dim3 grid(static_cast<unsigned>(n));
+        if (a.unit_rows == kTileRows) return launch(attention_kernel<d(), direct(), 1, kKeys>, grid, kThreads, stream, a, units);
+        if (d() == 64 && a.few_units) return launch(attention_kernel<64, direct(), 2, 2 * kKeys>, grid, kThreads, stream, a, units);
+        return launch(attention_kernel<d(), direct(), 2, kKeys>, grid, kThreads, stream, a, units);
     });
 }
 
 template <int D, bool DIRECT, bool PARTS>
-static void launch_dq(const SequenceArgs& a, const GradientUnits& u, hipStream_t stream) {
-    const unsigned grid = static_cast<unsigned>(u.n_q);
-    if (a.unit_rows == kTileRows) attention_dq_kernel<D, DIRECT, 1, kKeys, PARTS><<<grid, kThreads, 0, stream>>>(a, u.q);
-    else if (D == 64 && a.few_units) attention_dq_kernel<64, DIRECT, 2, 2 * kKeys, PARTS><<<grid, kThreads, 0, stream>>>(a, u.q);
-    else attention_dq_kernel<D, DIRECT, 2, kKeys, PARTS><<<grid, kThreads, 0, stream>>>(a, u.q);
+static hipError_t launch_dq(const SequenceArgs& a, const GradientUnits& u, hipStream_t stream) {
+    const dim3 grid(static_cast<unsigned>(u.n_q));
+    if (a.unit_rows == kTileRows) return launch(attention_dq_kernel<D, DIRECT, 1, kKeys, PARTS>, grid, kThreads, stream, a, u.q);
+    if (D == 64 && a.few_units) return launch(attention_dq_kernel<64, DIRECT, 2, 2 * kKeys, PARTS>, grid, kThreads, stream, a, u.q);
+    return launch(attention_dq_kernel<D, DIRECT, 2, kKeys, PARTS>, grid, kThreads, stream, a, u.q);
 }
 
 hipError_t launch_attention_backward(const SequenceArgs& a, const GradientUnits& u, hipStream_t stream) {
     hipError_t e = hipSuccess;
     if (u.n_q > 0)
         e = with_dim(a.dim, aligned_pieces(a.k) && aligned_pieces(a.v), [&](auto d, auto direct) {
-            if (u.n_q_joins > 0) launch_dq<d(), direct(), true>(a, u, stream);
-            else launch_dq<d(), direct(), false>(a, u, stream);
+            return u.n_q_joins > 0 ? launch_dq<d(), direct(), true>(a, u, stream) : launch_dq<d(), direct(), false>(a, u, stream);
         });
     if (e == hipSuccess && u.n_kv > 0)
         e = with_dim(a.dim, aligned_pieces(a.q) && aligned_pieces(a.dout), [&](auto d, auto direct) {
-            const unsigned grid = static_cast<unsigned>(u.n_kv);
+            const dim3 grid(static_cast<unsigned>(u.n_kv));
             if (d() == 64 && a.key_rows < kTileRows)
-                attention_dkv_kernel<64, direct(), 2><<<grid, Dkv<64>::kThreads, 0, stream>>>(a, u.kv);
-            else
-                attention_dkv_kernel<d(), direct(), 1><<<grid, Dkv<d()>::kThreads, 0, stream>>>(a, u.kv);
+                return launch(attention_dkv_kernel<64, direct(), 2>, grid, Dkv<64>::kThreads, stream, a, u.kv);
+            return launch(attention_dkv_kernel<d(), direct(), 1>, grid, Dkv<d()>::kThreads, stream, a, u.kv);
         });
     const int64_t joins = u.n_q_joins + u.n_kv_joins;
     if (e == hipSuccess && joins > 0)
         e = with_dim(a.dim, true, [&](auto d, auto) {
-            attention_join_kernel<d()><<<dim3(static_cast<unsigned>(joins), kJoinSlices), kThreads, 0, stream>>>(a, u.joins, u.n_q_joins);
+            return launch(attention_join_kernel<d()>, dim3(static_cast<unsigned>(joins), kJoinSlices), kThreads, stream, a, u.joins,
+                          u.n_q_joins);
         });
     return e;
 }

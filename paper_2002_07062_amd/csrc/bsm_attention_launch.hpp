@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <tuple>
 
 namespace bsm_att {
 
@@ -21,6 +22,18 @@ struct Unit {
 static_assert(sizeof(Unit) == 64, "");
 
 constexpr int kTileRows = 128;
+
+// hipLaunchKernel reports a failed launch itself: the thread's last error may be another call's.
+template <class... P, class... A>
+hipError_t launch(void (*kernel)(P...), dim3 grid, unsigned threads, hipStream_t stream, const A&... args) {
+    std::tuple<P...> values(args...);
+    return std::apply(
+        [&](auto&... x) {
+            void* at[] = {&x...};
+            return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, dim3(threads), at, 0, stream);
+        },
+        values);
+}
 
 // What the kernels pad a head dimension to.
 constexpr int padded_dim(int dim) { return dim <= 64 ? 64 : dim <= 96 ? 96 : 128; }

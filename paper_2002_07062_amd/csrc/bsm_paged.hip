@@ -911,28 +911,23 @@ hipError_t launch_paged(const PagedArgs& a, hipStream_t stream) {
     if (a.tiles > 0) {
         const unsigned tiles = static_cast<unsigned>(a.tile_count * a.cache.heads), grid = tiles * a.splits;
         if (aligned_pieces({a.cache.k, a.cache.page, a.cache.row, a.cache.head}) && reinterpret_cast<uintptr_t>(a.cache.v) % 16 == 0)
-            paged_kernel<D, true><<<grid, kThreads, 0, stream>>>(a);
-        else paged_kernel<D, false><<<grid, kThreads, 0, stream>>>(a);
-        e = hipGetLastError();
+            e = launch(paged_kernel<D, true>, dim3(grid), kThreads, stream, a);
+        else e = launch(paged_kernel<D, false>, dim3(grid), kThreads, stream, a);
         if (e == hipSuccess && a.splits > 1) {
             const int rows = join_rows(tiles);
             static_assert(join_rows(1) % kWaves == 0 && join_rows(1 << 20) % kWaves == 0, "whole rounds of the waves");
-            paged_join_kernel<D><<<tiles * (kTileRows / rows), kThreads, 0, stream>>>(a, rows);
-            e = hipGetLastError();
+            e = launch(paged_join_kernel<D>, dim3(tiles * (kTileRows / rows)), kThreads, stream, a, rows);
         }
     }
     if (e == hipSuccess && a.few_rows > 0) {
         const bool full = a.cache.dim == D;
         const unsigned grid = static_cast<unsigned>(a.shares > 0 ? static_cast<int64_t>(a.shares) * a.cache.heads : units);
-        if (a.few_rows == 16 && full) paged_few_kernel<D, 1, true><<<grid, kThreads, 0, stream>>>(a);
-        else if (a.few_rows == 16) paged_few_kernel<D, 1, false><<<grid, kThreads, 0, stream>>>(a);
-        else if (full) paged_few_kernel<D, 2, true><<<grid, kThreads, 0, stream>>>(a);
-        else paged_few_kernel<D, 2, false><<<grid, kThreads, 0, stream>>>(a);
-        e = hipGetLastError();
-        if (e == hipSuccess && a.shares > 0) {
-            paged_few_join_kernel<D><<<static_cast<unsigned>(units), kThreads, 0, stream>>>(a);
-            e = hipGetLastError();
-        }
+        if (a.few_rows == 16 && full) e = launch(paged_few_kernel<D, 1, true>, dim3(grid), kThreads, stream, a);
+        else if (a.few_rows == 16) e = launch(paged_few_kernel<D, 1, false>, dim3(grid), kThreads, stream, a);
+        else if (full) e = launch(paged_few_kernel<D, 2, true>, dim3(grid), kThreads, stream, a);
+        else e = launch(paged_few_kernel<D, 2, false>, dim3(grid), kThreads, stream, a);
+        if (e == hipSuccess && a.shares > 0)
+            e = launch(paged_few_join_kernel<D>, dim3(static_cast<unsigned>(units)), kThreads, stream, a);
     }
     return e;
 }
@@ -950,8 +945,7 @@ hipError_t launch_attention_paged(const PagedArgs& a, hipStream_t stream) {
 hipError_t launch_cache_slots(const SlotArgs& a, int n_cu, hipStream_t stream) {
     const int64_t blocks = (a.n_slots + kThreads - 1) / kThreads;
     const unsigned grid = static_cast<unsigned>(blocks < 1 ? 1 : blocks < n_cu ? blocks : n_cu);
-    slots_kernel<<<grid, kThreads, 0, stream>>>(a);
-    return hipGetLastError();
+    return launch(slots_kernel, dim3(grid), kThreads, stream, a);
 }
 
 hipError_t launch_cache_append(const Cache& c, const Heads& k, const Heads& v, const int64_t* slots, int64_t tokens,
@@ -960,9 +954,8 @@ hipError_t launch_cache_append(const Cache& c, const Heads& k, const Heads& v, c
     const int64_t pieces = tokens * 2 * c.heads * (c.dim / 8), blocks = (pieces + kThreads * kPieces - 1) / (kThreads * kPieces);
     const int64_t most = 64 * static_cast<int64_t>(n_cu);
     const unsigned grid = static_cast<unsigned>(blocks < most ? blocks : most);
-    if (16 * pieces > kStreamBytes) append_kernel<true><<<grid, kThreads, 0, stream>>>(c, k, v, slots, tokens);
-    else append_kernel<false><<<grid, kThreads, 0, stream>>>(c, k, v, slots, tokens);
-    return hipGetLastError();
+    if (16 * pieces > kStreamBytes) return launch(append_kernel<true>, dim3(grid), kThreads, stream, c, k, v, slots, tokens);
+    return launch(append_kernel<false>, dim3(grid), kThreads, stream, c, k, v, slots, tokens);
 }
 
 }  // namespace bsm_att

@@ -463,3 +463,37 @@ def test_gradients_on_top_of_each_other_are_refused():
     call(at(256), at(0, head=128), at(64, head=128))  # every other head
     call(at(0, row=128), at(128 * 140, row=128), apart)
     plan.destroy()
+
+
+def test_an_error_of_another_call_is_not_reported():
+    """The thread's last error belongs to whoever made it: a call after it succeeds and leaves it there."""
+    hip = bsm.load()  # the runtime that the library is linked to
+    batch = Batch([200, 40], [200, 40], 2, 1, 64, "packed", 73)
+    plan = bsm.bsm_attention_plan_create(**batch.plan_args(True))
+    o, lse, dout = batch.empty("q"), torch.empty((2, 240), device="cuda"), batch.operand("q")
+    grads = [batch.empty("q"), batch.empty("kv"), batch.empty("kv")]
+    ws = torch.empty(plan.workspace_bytes, dtype=torch.uint8, device="cuda")
+    cache = [torch.zeros((16, 16, 1, 64), dtype=torch.bfloat16, device="cuda") for _ in "kv"]
+    slots = torch.empty(240, dtype=torch.int64, device="cuda")
+    table, lengths, zeros, free, n_free, start, kv, taken = (
+        torch.tensor(x, dtype=torch.int32, device="cuda")
+        for x in ([[0] * 13] * 2, [200, 40], [0, 0], list(range(16)), [16], [0] * 3, [0] * 2, [0] * 2))
+    o2 = torch.empty((240, 2, 64), dtype=torch.bfloat16, device="cuda")
+    ws2 = torch.empty(bsm.bsm_attention_paged_workspace(2, 240, 2, 1, 64, 200, 200), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    assert hip.hipGetLastError() == 0
+    assert hip.hipSetDevice(1 << 20) != 0
+    try:
+        bsm.bsm_attention_execute(plan, batch.q, batch.k, batch.v, o, lse=lse)
+        bsm.bsm_attention_backward(plan, batch.q, batch.k, batch.v, o, lse, dout, *grads, workspace=ws)
+        bsm.bsm_cache_slots(zeros, lengths, 16, 16, table, free, n_free, start, kv, slots, taken)
+        bsm.bsm_cache_append(batch.k, batch.v, slots, *cache)
+        bsm.bsm_attention_paged(batch.q, *cache, table, start, kv, o2, max_q=200, max_kv=200, workspace=ws2)
+    finally:
+        left = hip.hipGetLastError()
+    assert left != 0
+    torch.cuda.synchronize()
+    check_forward(batch, o, lse, 0.125, True)
+    check_forward(batch, o2, None, 0.125, True)
+    check_backward(batch, o, lse, dout, *grads, 0.125, True)
+    plan.destroy()
