@@ -745,8 +745,12 @@ bsm_status bsm_attention_paged_workspace(int64_t batch, int64_t tokens, int32_t 
     *bytes = 0;
     bsm_status st = check_paged_sizes(batch, tokens, heads_q, heads_kv, head_dim, max_q, max_kv);
     if (st != BSM_OK) return st;
-    int n_cu = 0;
-    const hipError_t e = compute_units(device, &n_cu);
+    if (device < 0) return fail(BSM_ERR_INVALID_ARG, "device %d", device);
+    int n = 0, n_cu = 0;
+    hipError_t e = hipGetDeviceCount(&n);
+    if (e != hipSuccess) return hip_fail(e, "hipGetDeviceCount");
+    if (device >= n) return fail(BSM_ERR_INVALID_ARG, "device %d of %d", device, n);
+    e = compute_units(device, &n_cu);
     if (e != hipSuccess) return hip_fail(e, "device query");
     bsm_att::PagedCut cut;
     if ((st = paged_cut(batch, tokens, heads_q, heads_kv, head_dim, max_q, max_kv, n_cu, &cut)) != BSM_OK) return st;

@@ -450,3 +450,11 @@ def test_keys_and_values_in_one_tensor(form):
     for cache, y in ((k_cache, k), (v_cache, v)):
         assert torch.equal(cache[slots // page, slots % page], y)
     assert int(torch.isfinite(x.float()).sum()) == 2 * 100 * hk * d
+
+
+@pytest.mark.parametrize("device", [-1, 64, 2**31 - 1])
+def test_a_workspace_for_no_device_is_refused(device):
+    with pytest.raises(bsm.BsmError) as e:
+        bsm.bsm_attention_paged_workspace(4, 4, 8, 8, 64, 1, 4096, device=device)
+    assert e.value.status == bsm.BSM_ERR_INVALID_ARG and "device" in e.value.message
+    assert bsm.load().hipGetLastError() == 0, "left for the next call that looks"

@@ -289,3 +289,8 @@ def test_caches_on_top_of_each_other_are_refused(cache, offset):
     at = 1 << 30
     assert _append(cache=_cache(k=at, v=at + 2 * offset, **cache)) == bsm.BSM_ERR_ALIAS
     assert "overlap" in bsm.bsm_last_error()
+
+
+def test_a_workspace_for_no_device_is_refused():
+    st, m = _status(bsm.bsm_attention_paged_workspace, 4, 4, 8, 8, 64, 1, 4096, device=-1)
+    assert st == bsm.BSM_ERR_INVALID_ARG and "device" in m
