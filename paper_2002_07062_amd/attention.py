@@ -360,7 +360,7 @@ def bsm_attention_paged(q, k_cache, v_cache, table, q_start, kv_len, o, max_q, m
                         window=0, scale=None, workspace=None, stream=None):
     """o = causal attention of every request's new tokens over its pages (see bsm.h). q, o:
     (tokens, heads, dim); table: int32 (batch, width); q_start: int32 (batch + 1); kv_len: int32
-    (batch). max_q, max_kv: host bounds on a chunk and on kv_len (default: the table's width).
+    (batch). max_q, max_kv: host bounds on a chunk and on kv_len (None or 0: the table's width).
     workspace: None (allocated for the call on the current stream) or a tensor of
     bsm_attention_paged_workspace bytes. Returns o."""
     fn = _load().bsm_attention_paged
@@ -377,7 +377,7 @@ def bsm_attention_paged(q, k_cache, v_cache, table, q_start, kv_len, o, max_q, m
     tp = _contiguous(table, i32, 0, "table", dev)
     sp = _contiguous(q_start, i32, batch + 1, "q_start", dev)
     lp = _contiguous(kv_len, i32, 0, "kv_len", dev)
-    max_kv = width * cache.page_size if max_kv is None else int(max_kv)
+    max_kv = width * cache.page_size if max_kv is None else int(max_kv) or width * cache.page_size
     wp, wn, workspace = _workspace(
         workspace, lambda: bsm_attention_paged_workspace(batch, tokens, heads_q, cache.heads, dim,
                                                          max_q, max_kv, dev), dev, stream)

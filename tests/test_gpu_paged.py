@@ -458,3 +458,20 @@ def test_a_workspace_for_no_device_is_refused(device):
         bsm.bsm_attention_paged_workspace(4, 4, 8, 8, 64, 1, 4096, device=device)
     assert e.value.status == bsm.BSM_ERR_INVALID_ARG and "device" in e.value.message
     assert bsm.load().hipGetLastError() == 0, "left for the next call that looks"
+
+
+@pytest.mark.parametrize("new", [[1, 1], [1, 40]])
+def test_no_bound_on_the_keys(new):
+    """max_kv of 0 stands for the table's width, as None does, in the workspace too."""
+    kv_len = [2500, 300]
+    cache = Cache(kv_len, 16, 1, 64, 37)
+    g = torch.Generator().manual_seed(38)
+    q = torch.randn((sum(new), 1, 64), generator=g).to(torch.bfloat16).cuda()
+    outs = []
+    for max_kv in (0, None):
+        o = torch.full_like(q, NAN)
+        bsm.bsm_attention_paged(q, cache.k, cache.v, cache.table, i32([0, 1, sum(new)]), i32(kv_len), o, max_q=max(new), max_kv=max_kv)
+        torch.cuda.synchronize()
+        _check(o, q, cache, new, kv_len, 1, 0.125)
+        outs.append(o)
+    assert torch.equal(*outs)
