@@ -155,6 +155,15 @@ def _ref(x):
     return ctypes.byref(x)
 
 
+def _int32(**values):
+    """The values as ints that the library's 32-bit arguments hold (ctypes would cut them off)."""
+    for name, x in values.items():
+        x = int(x)
+        if not -2**31 <= x < 2**31:
+            raise ValueError(f"{name} {x} must fit in 32 bits")
+        yield x
+
+
 # ------------------------------------------------------------------------- ragged sequences
 class AttentionPlan:
     """A plan of one batch's geometry (bsm_attention_plan). Use bsm_attention_plan_create."""
@@ -228,15 +237,17 @@ def bsm_attention_plan_create(q_len, kv_len=None, *, heads_q, heads_kv=None, hea
         topo = topology if isinstance(topology, bsm_topology) else bsm_topology(**topology)
     keep = [_arr(q_len, np.int32), _arr(kv_len, np.int32), _arr(q_start, np.int64),
             _arr(kv_start, np.int64)]
+    hq, hk, dim, window, device = _int32(
+        heads_q=heads_q, heads_kv=heads_q if heads_kv is None else heads_kv, head_dim=head_dim,
+        window=window, device=device)
     handle = _vp()
     _check(lib.bsm_attention_plan_create(
-        _ref(handle), keep[0][1], keep[1][1], keep[2][1], keep[3][1], q_len.size, int(heads_q),
-        int(heads_q if heads_kv is None else heads_kv), int(head_dim), int(bool(causal)),
-        int(window), _schedule_code(schedule), _ref(topo) if topo is not None else None,
-        int(device)))
+        _ref(handle), keep[0][1], keep[1][1], keep[2][1], keep[3][1], q_len.size, hq, hk, dim,
+        int(bool(causal)), window, _schedule_code(schedule),
+        _ref(topo) if topo is not None else None, device))
     st = bsm_attention_stats()
     _check(lib.bsm_attention_plan_describe(handle.value, _ref(st)))
-    return AttentionPlan(handle.value, int(device), st, q_end, kv_end)
+    return AttentionPlan(handle.value, device, st, q_end, kv_end)
 
 
 def bsm_attention_plan_describe(plan: AttentionPlan) -> dict:
@@ -323,7 +334,8 @@ def bsm_cache_slots(cached, fresh, page_size, n_pages, table, free_pages, n_free
         raise ValueError(f"table of shape {tuple(table.shape)} has no row for each of {batch}")
     i32 = torch.int32
     _call(dev, fn, _contiguous(cached, i32, batch, "cached", dev),
-          _contiguous(fresh, i32, batch, "fresh", dev), batch, int(page_size), int(n_pages),
+          _contiguous(fresh, i32, batch, "fresh", dev), batch, *_int32(page_size=page_size),
+          int(n_pages),
           _contiguous(table, i32, 0, "table", dev), table.shape[1],
           _contiguous(free_pages, i32, 0, "free_pages", dev), free_pages.numel(),
           _contiguous(n_free, i32, 1, "n_free", dev),
@@ -350,9 +362,9 @@ def bsm_attention_paged_workspace(batch, tokens, heads_q, heads_kv, head_dim, ma
                                   device=0) -> int:
     """Bytes of workspace that bsm_attention_paged needs for these sizes."""
     n = _i64()
-    _check(_load().bsm_attention_paged_workspace(int(batch), int(tokens), int(heads_q),
-                                                 int(heads_kv), int(head_dim), int(max_q),
-                                                 int(max_kv), int(device), _ref(n)))
+    _check(_load().bsm_attention_paged_workspace(
+        int(batch), int(tokens), *_int32(heads_q=heads_q, heads_kv=heads_kv, head_dim=head_dim,
+                                         max_q=max_q, max_kv=max_kv, device=device), _ref(n)))
     return int(n.value)
 
 
@@ -378,9 +390,10 @@ def bsm_attention_paged(q, k_cache, v_cache, table, q_start, kv_len, o, max_q, m
     sp = _contiguous(q_start, i32, batch + 1, "q_start", dev)
     lp = _contiguous(kv_len, i32, 0, "kv_len", dev)
     max_kv = width * cache.page_size if max_kv is None else int(max_kv) or width * cache.page_size
+    max_q, max_kv, window = _int32(max_q=max_q, max_kv=max_kv, window=window)
     wp, wn, workspace = _workspace(
         workspace, lambda: bsm_attention_paged_workspace(batch, tokens, heads_q, cache.heads, dim,
                                                          max_q, max_kv, dev), dev, stream)
-    _call(dev, fn, _ref(cache), qr, orr, tp, width, sp, lp, batch, tokens, heads_q, int(max_q),
-          max_kv, int(window), _scale_of(scale, dim), wp, wn, _stream(dev, stream))
+    _call(dev, fn, _ref(cache), qr, orr, tp, width, sp, lp, batch, tokens, heads_q, max_q, max_kv,
+          window, _scale_of(scale, dim), wp, wn, _stream(dev, stream))
     return o

@@ -475,3 +475,17 @@ def test_no_bound_on_the_keys(new):
         _check(o, q, cache, new, kv_len, 1, 0.125)
         outs.append(o)
     assert torch.equal(*outs)
+
+
+@pytest.mark.parametrize("name", ["max_q", "max_kv", "window"])
+def test_arguments_past_32_bits_are_refused(name):
+    """A bound of 2^32 is not one of 0, which would leave o as it is without a word."""
+    cache = Cache([40], 16, 1, 64, 39)
+    q = torch.ones((1, 1, 64), dtype=torch.bfloat16, device="cuda")
+    args = dict(max_q=1, max_kv=40, window=0)
+    for x in (2**32, 2**32 + 1, 2**31, -2**32 + 1):
+        with pytest.raises(ValueError, match=f"{name} .*32 bits"):
+            bsm.bsm_attention_paged(q, cache.k, cache.v, cache.table, i32([0, 1]), i32([40]), torch.empty_like(q), **{**args, name: x})
+    with pytest.raises(ValueError, match="page_size .*32 bits"):
+        bsm.bsm_cache_slots(i32([0]), i32([1]), 2**32 + 16, 8, i32([[0]]), i32([1]), i32([1]), i32([0, 0]), i32([0]),
+                            torch.empty(1, dtype=torch.int64, device="cuda"), i32([0, 0]))

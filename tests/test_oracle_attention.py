@@ -294,3 +294,20 @@ def test_caches_on_top_of_each_other_are_refused(cache, offset):
 def test_a_workspace_for_no_device_is_refused():
     st, m = _status(bsm.bsm_attention_paged_workspace, 4, 4, 8, 8, 64, 1, 4096, device=-1)
     assert st == bsm.BSM_ERR_INVALID_ARG and "device" in m
+
+
+@pytest.mark.parametrize("name", ["heads_q", "heads_kv", "head_dim", "window", "device"])
+@pytest.mark.parametrize("beyond", [2**32, -2**32, 2**31])
+def test_plan_arguments_past_32_bits_are_refused(name, beyond):
+    """Not cut off to the value that is left of them, here a good one."""
+    good = dict(heads_q=4, heads_kv=2, head_dim=64, window=0, device=-1)[name]
+    with pytest.raises(ValueError, match=f"{name} .*32 bits"):
+        _plan(**{"causal": True, name: good + beyond if beyond != 2**31 else beyond})
+
+
+@pytest.mark.parametrize("name", ["heads_q", "heads_kv", "head_dim", "max_q", "max_kv", "device"])
+def test_workspace_arguments_past_32_bits_are_refused(name):
+    args = dict(heads_q=8, heads_kv=8, head_dim=64, max_q=1, max_kv=1024, device=0)
+    args[name] += 2**32
+    with pytest.raises(ValueError, match=f"{name} .*32 bits"):
+        bsm.bsm_attention_paged_workspace(4, 4, **args)
