@@ -537,6 +537,8 @@ bsm_status paged(const bsm_cache* cache, const bsm_heads* q, const bsm_heads* o,
     if (overlap(so, sq) || overlap(so, sk) || overlap(so, sv)) return fail(BSM_ERR_ALIAS, "o overlaps an operand");
     if (batch == 0 || tokens == 0 || max_q == 0) return BSM_OK;
     if (!q_start || !kv_len || (!table && width > 0)) return fail(BSM_ERR_INVALID_ARG, "table, q_start or kv_len is NULL");
+    if ((reinterpret_cast<uintptr_t>(table) | reinterpret_cast<uintptr_t>(q_start) | reinterpret_cast<uintptr_t>(kv_len)) % 4 != 0)
+        return fail(BSM_ERR_INVALID_ARG, "table, q_start or kv_len is not aligned to its element size");
     if (overlap(so, bytes_at(table, 4 * batch * width)) || overlap(so, bytes_at(q_start, 4 * batch + 4)) ||
         overlap(so, bytes_at(kv_len, 4 * batch)))
         return fail(BSM_ERR_ALIAS, "o overlaps an operand");

@@ -311,3 +311,10 @@ def test_workspace_arguments_past_32_bits_are_refused(name):
     args[name] += 2**32
     with pytest.raises(ValueError, match=f"{name} .*32 bits"):
         bsm.bsm_attention_paged_workspace(4, 4, **args)
+
+
+@pytest.mark.parametrize("name", ["table", "q_start", "kv_len"])
+@pytest.mark.parametrize("off", [1, 2])
+def test_paged_arrays_off_their_alignment_are_refused(name, off):
+    assert _paged(**{name: (1 << 40) + off}) == bsm.BSM_ERR_INVALID_ARG
+    assert "aligned" in bsm.bsm_last_error()
