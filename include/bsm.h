@@ -485,9 +485,9 @@ typedef struct bsm_cache {
  *   taken          [2] out: pages taken from the free list, requests refused
  * Requests are served in order.  One is refused, whole, if its pages do not fit the table's width,
  * the free list has too few left (it and all later ones that need pages), or its tokens go past
- * n_slots: its slots are -1, its kv_len is 0, so that attention over it gives zeros, and its table
- * row is left as it is.  A table or free-list entry that names no page gives slots of -1.  The
- * outputs, the table and the inputs must not overlap. */
+ * n_slots (one without new tokens has none that do): its slots are -1, its kv_len is 0, so that
+ * attention over it gives zeros, and its table row is left as it is.  A table or free-list entry
+ * that names no page gives slots of -1.  The outputs, the table and the inputs must not overlap. */
 bsm_status bsm_cache_slots(const int32_t* cached, const int32_t* fresh, int64_t batch,
                            int32_t page_size, int64_t n_pages, int32_t* table, int32_t width,
                            const int32_t* free_pages, int64_t free_cap, const int32_t* n_free,

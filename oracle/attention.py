@@ -60,7 +60,7 @@ def slots(cached, fresh, page_size, n_pages, table, free_pages, n_free, n_slots)
         c, f = max(0, int(c)), max(0, int(f))
         held, full = -(-c // page_size), -(-(c + f) // page_size)
         need = 0 if full > width else full - held
-        ok = full <= width and tokens + f <= n_slots and (need == 0 or at + need <= n_free)
+        ok = full <= width and (f == 0 or tokens + f <= n_slots) and (need == 0 or at + need <= n_free)
         if ok:
             for i in range(need):
                 page = int(free_pages[at + i])

@@ -782,7 +782,7 @@ __global__ __launch_bounds__(kThreads) void slots_kernel(const SlotArgs a) {
         Two total;
         const Two at = scan({fresh, need}, &total, mem);
         const int64_t first = base.tokens + at.tokens, page = base.pages + at.pages;
-        const bool granted = !wide && first + fresh <= a.n_slots && (need == 0 || page + need <= n_free);
+        const bool granted = !wide && (fresh == 0 || first + fresh <= a.n_slots) && (need == 0 || page + need <= n_free);
         s_first[tid] = first;
         s_page[tid] = page;
         s_cached[tid] = static_cast<int>(cached);

@@ -489,3 +489,10 @@ def test_arguments_past_32_bits_are_refused(name):
     with pytest.raises(ValueError, match="page_size .*32 bits"):
         bsm.bsm_cache_slots(i32([0]), i32([1]), 2**32 + 16, 8, i32([[0]]), i32([1]), i32([1]), i32([0, 0]), i32([0]),
                             torch.empty(1, dtype=torch.int64, device="cuda"), i32([0, 0]))
+
+
+def test_slots_of_idle_requests():
+    """A request without new tokens keeps its cache when an earlier one's tokens go past the slots."""
+    _slots([1, 2, 7, 0], [3, 4, 0, 1], 4, 12, [[4, -1], [5, -1], [6, 7], [-1, -1]], [8, 9], 2, 6)
+    _slots([9] * 300, [5] + [0] * 299, 4, 12, [[1, 2, 3, 4]] * 300, [8, 9], 2, 3)
+    _slots([0, 4, 9], [1, 0, 0], 4, 12, [[1], [2], [3]], [8, 9], 2, 0)  # the last one's pages do not fit

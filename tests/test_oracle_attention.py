@@ -318,3 +318,12 @@ def test_workspace_arguments_past_32_bits_are_refused(name):
 def test_paged_arrays_off_their_alignment_are_refused(name, off):
     assert _paged(**{name: (1 << 40) + off}) == bsm.BSM_ERR_INVALID_ARG
     assert "aligned" in bsm.bsm_last_error()
+
+
+def test_oracle_slots_of_idle_requests_by_hand():
+    """Room for 6 tokens: request 1's go past it, and with them 3's; 0 and 2 keep what they have, 2 without
+    asking for anything."""
+    table = [[4, -1], [5, -1], [6, 7], [-1, -1]]
+    q_start, kv_len, out, slots, taken = oa.slots([1, 2, 7, 0], [3, 4, 0, 1], 4, 12, table, [8, 9], 2, 6)
+    assert kv_len == [4, 0, 7, 0] and q_start == [0, 3, 6, 6, 6] and taken == [0, 2]
+    assert out.tolist() == table and slots.tolist() == [17, 18, 19, -1, -1, -1]
