@@ -393,6 +393,14 @@ typedef struct bsm_heads {
     int64_t head; /* ... between heads */
 } bsm_heads;
 
+/* Which kernels a plan's calls run, bits of bsm_attention_stats.forms. */
+#define BSM_ATTENTION_HALF_FORWARD 1 /* the forward pass's units are 64 query rows, not 128 */
+#define BSM_ATTENTION_HALF_DQ 2      /* dq's units are */
+#define BSM_ATTENTION_HALF_KEYS 4    /* the units of dk and dv are 64 keys, not 128 */
+#define BSM_ATTENTION_LONG_STEPS 8   /* units of 64 query rows take 128 keys at a time, not 64 */
+#define BSM_ATTENTION_DQ_PARTS 16    /* some units of dq are cut into parts, which are added up */
+#define BSM_ATTENTION_KEY_PARTS 32   /* some of dk and dv are */
+
 typedef struct bsm_attention_stats {
     int64_t batch;
     int64_t total_q, total_kv;     /* query rows and keys over all sequences */
@@ -403,7 +411,7 @@ typedef struct bsm_attention_stats {
     int32_t heads_q, heads_kv, head_dim;
     int32_t causal, window;
     int32_t schedule, n_xcd;
-    int32_t reserved;
+    int32_t forms;                 /* BSM_ATTENTION_ bits */
 } bsm_attention_stats;
 
 typedef struct bsm_attention_plan_s* bsm_attention_plan;

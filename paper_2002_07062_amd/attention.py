@@ -22,6 +22,10 @@ from .bsm import _arr, _check, _schedule_code, _stream_of, bsm_topology
 
 _vp, _i64, _i32, _f32 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_float
 
+# bits of a plan's "forms": which kernels its calls run
+BSM_ATTENTION_HALF_FORWARD, BSM_ATTENTION_HALF_DQ, BSM_ATTENTION_HALF_KEYS = 1, 2, 4
+BSM_ATTENTION_LONG_STEPS, BSM_ATTENTION_DQ_PARTS, BSM_ATTENTION_KEY_PARTS = 8, 16, 32
+
 
 class bsm_heads(ctypes.Structure):
     _fields_ = [("data", _vp), ("seq", _i64), ("row", _i64), ("head", _i64)]
@@ -38,7 +42,7 @@ class bsm_attention_stats(ctypes.Structure):
                 ("kv_units", _i64), ("lse_elems", _i64), ("workspace_bytes", _i64),
                 ("pairs", _i64), ("heads_q", _i32), ("heads_kv", _i32), ("head_dim", _i32),
                 ("causal", _i32), ("window", _i32), ("schedule", _i32), ("n_xcd", _i32),
-                ("reserved", _i32)]
+                ("forms", _i32)]
 
 
 _lib = None
@@ -253,7 +257,7 @@ def bsm_attention_plan_create(q_len, kv_len=None, *, heads_q, heads_kv=None, hea
 def bsm_attention_plan_describe(plan: AttentionPlan) -> dict:
     st = bsm_attention_stats()
     _check(_load().bsm_attention_plan_describe(plan.handle, _ref(st)))
-    return {name: getattr(st, name) for name, _ in st._fields_ if name != "reserved"}
+    return {name: getattr(st, name) for name, _ in st._fields_}
 
 
 def bsm_attention_plan_destroy(plan: AttentionPlan) -> None:

@@ -690,6 +690,12 @@ bsm_status bsm_attention_plan_describe(bsm_attention_plan plan, bsm_attention_st
     stats->window = s.mask.window;
     stats->schedule = plan->schedule;
     stats->n_xcd = plan->n_xcd;
+    const bool half_forward = plan->forward_rows < bsm_att::kTileRows, half_dq = plan->dq_rows < bsm_att::kTileRows;
+    const bool long_steps = plan->few_units && bsm_att::padded_dim(s.dim) == 64;
+    stats->forms = (half_forward ? BSM_ATTENTION_HALF_FORWARD : 0) | (half_dq ? BSM_ATTENTION_HALF_DQ : 0) |
+                   (plan->key_rows < bsm_att::kTileRows ? BSM_ATTENTION_HALF_KEYS : 0) |
+                   (long_steps && (half_forward || half_dq) ? BSM_ATTENTION_LONG_STEPS : 0) |
+                   (plan->n_q_joins > 0 ? BSM_ATTENTION_DQ_PARTS : 0) | (plan->n_kv_joins > 0 ? BSM_ATTENTION_KEY_PARTS : 0);
     return BSM_OK;
 }
 

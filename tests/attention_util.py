@@ -63,6 +63,37 @@ def backward_bound(q, k, v, o, lse, dout, scale, causal, window, dq, dk, dv):
     return b_dq, b_dk, b_dv
 
 
+# Batches that between them run every kernel of the forward pass and of the gradient, each as
+# (q_len, kv_len, query heads, kv heads, head dim, causal, window, compute units to plan for); in the
+# layouts "packed" (tiles go straight to LDS) and "shifted" (through registers).
+FORMS = [
+    ([368, 111, 50], [201, 41, 502], 4, 2, 96, True, 312, 1),
+    ([31, 84, 198], [2440, 3602, 3687], 2, 2, 40, True, 287, 6),
+    ([33, 14, 498], [997, 1289, 1453], 1, 1, 128, True, 110, 2),
+    ([90, 159, 314], [887, 1815, 1245], 2, 1, 64, True, 695, 12),
+    ([26, 357, 38], [2945, 1633, 621], 2, 1, 72, True, 543, 24),
+    ([46, 446, 36], [2256, 988, 1695], 2, 1, 128, True, 252, 24),
+    ([302, 497, 202], [64, 314, 1081], 4, 2, 40, True, 302, 24),
+    ([376, 140, 235], [1294, 2642, 94], 2, 1, 40, False, 0, 24),
+    ([34, 141, 171], [2088, 1178, 2246], 1, 1, 104, True, 544, 24),
+    ([352, 13, 233], [215, 1398, 1066], 2, 1, 96, True, 610, 24),
+    ([89, 50, 122], [1357, 60, 58], 2, 2, 104, True, 874, 8),
+    ([264, 244, 341], [161, 1385, 68], 1, 1, 96, True, 880, 8),
+    ([240, 64, 36], [562, 5346, 3987], 3, 1, 64, False, 0, 8),
+    ([167, 65], [828, 11128], 3, 3, 64, False, 0, 3),
+]
+
+
+def kernels_of(head_dim, forms):
+    """The kernels that a plan of these forms runs, as (pass, padded head dimension, rows of a unit, keys
+    of a step, parts)."""
+    d = 64 if head_dim <= 64 else 96 if head_dim <= 96 else 128
+    half_forward, half_dq, half_keys, long_steps, dq_parts, key_parts = (bool(forms & 1 << i) for i in range(6))
+    return {("forward", d, 64 if half_forward else 128, 128 if half_forward and long_steps else 64, False),
+            ("dq", d, 64 if half_dq else 128, 128 if half_dq and long_steps else 64, dq_parts),
+            ("dk and dv", d, 64 if half_keys else 128, 64, key_parts)}
+
+
 class Batch:
     """Sequences in one layout on the GPU. layouts: packed (tokens, heads, dim); fused (q, k, v
     views of one tensor; needs q_len == kv_len); padded (batch, rows, heads, dim); heads_first

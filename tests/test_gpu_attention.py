@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import paper_2002_07062_amd as bsm
-from attention_util import Batch, check_backward, check_forward
+from attention_util import FORMS, Batch, check_backward, check_forward, kernels_of
 
 pytestmark = pytest.mark.gpu
 
@@ -496,4 +496,21 @@ def test_an_error_of_another_call_is_not_reported():
     check_forward(batch, o, lse, 0.125, True)
     check_forward(batch, o2, None, 0.125, True)
     check_backward(batch, o, lse, dout, *grads, 0.125, True)
+    plan.destroy()
+
+
+@pytest.mark.parametrize("layout", ["packed", "shifted"])
+@pytest.mark.parametrize("case", FORMS, ids=_name)
+def test_every_kernel_matches_the_oracle(case, layout):
+    q_len, kv_len, hq, hk, d, causal, window, n_cu = case
+    batch, scale = Batch(q_len, kv_len, hq, hk, d, layout, 79), float(np.float32(d ** -0.5))
+    plan, o, lse = _run(batch, causal, window, n_cu=n_cu)
+    print(sorted(kernels_of(d, bsm.bsm_attention_plan_describe(plan)["forms"])))
+    check_forward(batch, o, lse, scale, causal, window)
+    dout = batch.operand("q")
+    grads = [batch.empty("q"), batch.empty("kv"), batch.empty("kv")]
+    ws = torch.full((plan.workspace_bytes,), 255, dtype=torch.uint8, device="cuda")  # NaN
+    bsm.bsm_attention_backward(plan, batch.q, batch.k, batch.v, o, lse, dout, *grads, workspace=ws)
+    torch.cuda.synchronize()
+    check_backward(batch, o, lse, dout, *grads, scale, causal, window)
     plan.destroy()

@@ -9,6 +9,7 @@ import torch
 
 import oracle.attention as oa
 import paper_2002_07062_amd as bsm
+from attention_util import FORMS, kernels_of
 from paper_2002_07062_amd import attention as att
 
 TOPO = dict(n_xcd=8)
@@ -327,3 +328,19 @@ def test_oracle_slots_of_idle_requests_by_hand():
     q_start, kv_len, out, slots, taken = oa.slots([1, 2, 7, 0], [3, 4, 0, 1], 4, 12, table, [8, 9], 2, 6)
     assert kv_len == [4, 0, 7, 0] and q_start == [0, 3, 6, 6, 6] and taken == [0, 2]
     assert out.tolist() == table and slots.tolist() == [17, 18, 19, -1, -1, -1]
+
+
+def test_every_kernel_of_sequences_has_a_tested_batch():
+    """Heads up to 64 have units of 64 and 128 rows of either kind, with steps of 128 keys in the smaller
+    query units of few; longer heads have units of 128 keys only. Units of the gradient may have parts."""
+    want = set()
+    for d in (64, 96, 128):
+        queries = [(128, 64), (64, 64)] + ([(64, 128)] if d == 64 else [])
+        want |= {("forward", d, rows, step, False) for rows, step in queries}
+        want |= {("dq", d, rows, step, parts) for rows, step in queries for parts in (False, True)}
+        want |= {("dk and dv", d, rows, 64, parts) for rows in ((128, 64) if d == 64 else (128,)) for parts in (False, True)}
+    have = set()
+    for q_len, kv_len, hq, hk, d, causal, window, n_cu in FORMS:
+        p = _plan(q_len, kv_len, heads_q=hq, heads_kv=hk, head_dim=d, causal=causal, window=window, topology=dict(n_xcd=8, n_cu=n_cu))
+        have |= kernels_of(d, bsm.bsm_attention_plan_describe(p)["forms"])
+    assert have == want
