@@ -496,3 +496,42 @@ def test_slots_of_idle_requests():
     _slots([1, 2, 7, 0], [3, 4, 0, 1], 4, 12, [[4, -1], [5, -1], [6, 7], [-1, -1]], [8, 9], 2, 6)
     _slots([9] * 300, [5] + [0] * 299, 4, 12, [[1, 2, 3, 4]] * 300, [8, 9], 2, 3)
     _slots([0, 4, 9], [1, 0, 0], 4, 12, [[1], [2], [3]], [8, 9], 2, 0)  # the last one's pages do not fit
+
+
+# new tokens and query heads of a kv head: up to 16 rows, up to 32, tiles beside up to 16 and up to 32, tiles alone
+ROWS = {"16": ([1, 2], 4), "32": ([5, 3], 4), "tiles+16": ([40, 3], 4), "tiles+32": ([3, 1], 20), "tiles": ([40], 4)}
+
+
+@pytest.mark.parametrize("layout", ["page_first", "shifted"])
+@pytest.mark.parametrize("keys", [[300, 77], [2600, 1900]], ids=["short", "long"])  # whole, and in shares or pieces
+@pytest.mark.parametrize("rows", list(ROWS))
+@pytest.mark.parametrize("d", [40, 64, 72, 96, 104, 128])
+def test_every_kernel_matches_the_oracle(d, rows, keys, layout):
+    new, group = ROWS[rows]
+    kv_len = keys[:len(new)]
+    cache = Cache(kv_len, 16, 2, d, 41, layout=layout)
+    g = torch.Generator().manual_seed(42)
+    q = (2 * torch.randn((sum(new), 2 * group, d), generator=g)).to(torch.bfloat16).cuda()
+    o = torch.full_like(q, NAN)
+    n = bsm.bsm_attention_paged_workspace(len(new), sum(new), 2 * group, 2, d, max(new), max(kv_len))
+    assert (n > 0) == (keys[0] > 300 or "tiles" in rows)
+    ws = torch.full((n,), 255, dtype=torch.uint8, device="cuda")  # NaN
+    bsm.bsm_attention_paged(q, cache.k, cache.v, cache.table, i32([0] + list(np.cumsum(new))), i32(kv_len), o, max_q=max(new),
+                            max_kv=max(kv_len), workspace=ws)
+    torch.cuda.synchronize()
+    _check(o, q, cache, new, kv_len, group, float(np.float32(d ** -0.5)))
+
+
+@pytest.mark.parametrize("d", [64, 96, 128])
+def test_pieces_of_many_tiles(d):
+    """Tiles that fill the compute units in a few pieces: a workgroup joins 16 rows of one."""
+    cache = Cache([2600], 16, 8, d, 43)
+    g = torch.Generator().manual_seed(44)
+    q = (2 * torch.randn((512, 32, d), generator=g)).to(torch.bfloat16).cuda()
+    o = torch.full_like(q, NAN)
+    bsm.bsm_attention_paged(q, cache.k, cache.v, cache.table, i32([0, 512]), i32([2600]), o, max_q=512, max_kv=2600)
+    torch.cuda.synchronize()
+    assert torch.isfinite(o.float()).all()
+    for h in (0, 5, 7):
+        one = SimpleNamespace(tokens=[[x[:, h:h + 1] for x in cache.tokens[0]]])
+        _check(o[:, 4 * h + 1:4 * h + 2], q[:, 4 * h + 1:4 * h + 2], one, [512], [2600], 1, float(np.float32(d ** -0.5)))
