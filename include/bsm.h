@@ -444,7 +444,7 @@ bsm_status bsm_attention_plan_describe(bsm_attention_plan plan, bsm_attention_st
 bsm_status bsm_attention_plan_destroy(bsm_attention_plan plan);
 
 /* Forward pass.  lse: NULL, or heads_q * total_q fp32 values, row (head, n) for the n-th query row
- * of the batch counted over the sequences in order.  scale is finite and > 0.  o overlaps no
+ * of the batch counted over the sequences in order.  0 < scale <= 2^127.  o overlaps no
  * operand and its rows do not overlap each other (rows of two sequences that share query rows
  * would: BSM_ERR_INVALID_ARG); rows that belong to no sequence are left as they are. */
 bsm_status bsm_attention_execute(bsm_attention_plan plan, const bsm_heads* q, const bsm_heads* k,

@@ -83,7 +83,8 @@ bsm_status check_dims(int64_t heads_q, int64_t heads_kv, int64_t dim) {
 }
 
 bsm_status check_scale(float scale) {
-    if (!std::isfinite(scale) || !(scale > 0.0f)) return fail(BSM_ERR_INVALID_ARG, "scale must be finite and > 0");
+    // (past 2^127 its product with log2(e) would be infinite, and a score of 0 NaN)
+    if (!(scale > 0.0f) || !(scale <= 0x1p127f)) return fail(BSM_ERR_INVALID_ARG, "scale must be > 0 and at most 2^127");
     return BSM_OK;
 }
 

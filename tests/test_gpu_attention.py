@@ -514,3 +514,15 @@ def test_every_kernel_matches_the_oracle(case, layout):
     torch.cuda.synchronize()
     check_backward(batch, o, lse, dout, *grads, scale, causal, window)
     plan.destroy()
+
+
+def test_the_largest_scale():
+    """Scores of 0 stay equal, others leave one key."""
+    batch = Batch([3], [40], 1, 1, 64, "packed", 83)
+    batch.q[:] = 0
+    batch.q[1, 0, 0], batch.q[2, 0, 0] = 1.0, -1.0
+    batch.k[:] = 0
+    batch.k[7, 0, 0] = 2.0 ** -100
+    plan, o, lse = _run(batch, False, 0, scale=2.0 ** 127)
+    check_forward(batch, o, lse, 2.0 ** 127, False)
+    plan.destroy()

@@ -344,3 +344,9 @@ def test_every_kernel_of_sequences_has_a_tested_batch():
         p = _plan(q_len, kv_len, heads_q=hq, heads_kv=hk, head_dim=d, causal=causal, window=window, topology=dict(n_xcd=8, n_cu=n_cu))
         have |= kernels_of(d, bsm.bsm_attention_plan_describe(p)["forms"])
     assert have == want
+
+
+@pytest.mark.parametrize("scale", [3e38, float(np.nextafter(np.float32(2.0 ** 127), np.float32(np.inf))), float("inf"), -1.0])
+def test_scales_whose_exponents_have_no_room_are_refused(scale):
+    assert _paged(scale=scale) == bsm.BSM_ERR_INVALID_ARG
+    assert "scale" in bsm.bsm_last_error()
