@@ -84,7 +84,10 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
 def _stream(index, stream):
+    """The handle of `stream` (None: the current one) for a call on GPU `index`."""
     if stream is not None:
+        if getattr(stream, "device_index", index) != index:
+            raise ValueError(f"the stream is on cuda:{stream.device_index}, the tensors are on cuda:{index}")
         return _stream_of(None, stream)
     if _raw_stream is not None:
         return _raw_stream(index)

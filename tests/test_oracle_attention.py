@@ -2,6 +2,7 @@
 before any HIP call (no GPU here)."""
 
 import ctypes
+from types import SimpleNamespace
 
 import numpy as np
 import pytest
@@ -350,3 +351,10 @@ def test_every_kernel_of_sequences_has_a_tested_batch():
 def test_scales_whose_exponents_have_no_room_are_refused(scale):
     assert _paged(scale=scale) == bsm.BSM_ERR_INVALID_ARG
     assert "scale" in bsm.bsm_last_error()
+
+
+def test_streams_of_other_devices_are_refused():
+    stream = SimpleNamespace(cuda_stream=1234, device_index=1)
+    assert att._stream(1, stream) == 1234 and att._stream(0, 5678) == 5678
+    with pytest.raises(ValueError, match="cuda:1.*cuda:0"):
+        att._stream(0, stream)
