@@ -57,8 +57,9 @@ __device__ __forceinline__ void each_sum(f32x16 (&acc)[TILES], F f) {
 // workgroup off the CU (heads of 64, us with 64 and 128: 2 x 512 rows, 12 heads 8.9, 7.6; 4096, 8 heads, causal
 // 46.7, 37.5; 8 x 512, 12 heads, 768 units 11.3, 13.5; longer heads no faster).
 // Bound by the matrix cores with the exponentials between them, and on random data by the power that both
-// take: 4 x 4096 causal rows, 32/8 heads of 128, 561 us = 980 TFLOP/s (two 8192^3 products of a library on the
-// same card: 1200 .. 1400); without the exponentials and sums it would be 13% less time.
+// take: 4 x 4096 causal rows, 32/8 heads of 128, 570 .. 585 us = 940 .. 964 TFLOP/s (a library's 8192^3 product on the
+// same card: 1220), of whose cycles the matrix cores are busy for 48% and the vector units for another 48%, at a clock of
+// 2.0 of 2.4 GHz; 475 us on zeros.
 template <int D, bool DIRECT, int KS, int STEP>
 __global__ __launch_bounds__(kThreads, 2) void attention_kernel(const SequenceArgs a, const Unit* __restrict__ units) {
     constexpr int kKeys = STEP;
@@ -159,7 +160,7 @@ __device__ __forceinline__ float reference(float lse) { return lse == -kInf ? kI
 
 // dq = scale * sum_j dS_ij k_j, with dS = P (dP - delta), P = exp(s - lse), dP = do . v: query rows
 // stay in registers as in the forward pass, the keys stream through LDS.  Also leaves delta.  4 x 4096 causal
-// rows, 32/8 heads of 128: 830 us = 994 TFLOP/s.
+// rows, 32/8 heads of 128: 826 us = 998 TFLOP/s.
 // KS and STEP as in the forward pass; KS = 2 of heads over 64 takes more registers than two workgroups on a CU
 // have, so it is for plans that have one for each (1024 causal rows, 8 heads of 128: gradient 66.6 us with whole
 // units, 54.6 so).  PARTS: some units are cut; without, the registers that it takes are free (six ragged sequences
@@ -298,8 +299,9 @@ __global__ __launch_bounds__(kThreads, D > 64 && KS == 2 ? 1 : 2) void attention
 // half of 128 columns over both blocks (of 96, wave 1 adds 32 that are not stored).  That keeps a wave's sums
 // at 64 registers, so that two waves fit a SIMD and one's exponentials run beside the other's products (a wave
 // that held whole sums took 400 registers and ran alone: 735 us against 475 us on six ragged causal sequences
-// of 700 .. 4001 tokens, 32/8 heads of 128).  Bound as the forward pass; 4 x 4096 causal rows, 32/8 heads of 128,
-// 1285 us = 856 TFLOP/s in its four products.
+// of 700 .. 4001 tokens, 32/8 heads of 128).  4 x 4096 causal rows, 32/8 heads of 128, 1287 us = 855
+// TFLOP/s in its four products; on the six ragged ones the matrix cores are busy for 36% of the cycles, and the waves wait
+// for 37% of theirs (32 x 512 rows, 12 heads of 64: 33% both).
 // KS = 2, heads of 64: 64 keys, two waves of each 32 with a block of every step's query rows; for plans with little to
 // do (see key_rows).
 template <int D>
