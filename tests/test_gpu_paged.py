@@ -535,3 +535,64 @@ def test_pieces_of_many_tiles(d):
     for h in (0, 5, 7):
         one = SimpleNamespace(tokens=[[x[:, h:h + 1] for x in cache.tokens[0]]])
         _check(o[:, 4 * h + 1:4 * h + 2], q[:, 4 * h + 1:4 * h + 2], one, [512], [2600], 1, float(np.float32(d ** -0.5)))
+
+
+@pytest.mark.parametrize("new", [[1, 2], [40, 1]])
+def test_joins_of_more_parts_than_a_wave_has_lanes(new):
+    """40000 keys of one kv head: 79 shares of single tokens, 157 pieces of a chunk's tile."""
+    kv_len = [40000, 600]
+    cache = Cache(kv_len, 64, 1, 64, 45)
+    g = torch.Generator().manual_seed(46)
+    q = (2 * torch.randn((sum(new), 2, 64), generator=g)).to(torch.bfloat16).cuda()
+    o = torch.full_like(q, NAN)
+    bsm.bsm_attention_paged(q, cache.k, cache.v, cache.table, i32([0, new[0], sum(new)]), i32(kv_len), o, max_q=max(new), max_kv=40000)
+    torch.cuda.synchronize()
+    _check(o, q, cache, new, kv_len, 2, 0.125)
+
+
+def test_mixed_batches_on_two_streams_and_replayed():
+    """A chunk beside single tokens, four kernels a call: on two streams at once with workspaces of their own,
+    and captured, replayed with other lengths between eager calls."""
+    lens = [[1700, 900, 2500], [2500, 1700, 900]]
+    cache = Cache([2500, 1700, 900], 16, 2, 64, 47)
+    tables = [cache.table[[1, 2, 0]].contiguous(), cache.table]
+    g = torch.Generator().manual_seed(48)
+    q = [(2 * torch.randn((70, 6, 64), generator=g)).to(torch.bfloat16).cuda() for _ in "ab"]
+    new = [[1, 60, 3], [50, 1, 1]]
+    starts, kv = [i32([0] + list(np.cumsum(n))) for n in new], [i32(x) for x in lens]
+    n = bsm.bsm_attention_paged_workspace(3, 70, 6, 2, 64, 60, 2500)
+    ws = [torch.empty(n, dtype=torch.uint8, device="cuda") for _ in "ab"]
+    out = [torch.full_like(x, NAN) for x in q]
+    streams = [torch.cuda.Stream() for _ in "ab"]
+    torch.cuda.synchronize()
+
+    def call(i, o, w, **k):
+        bsm.bsm_attention_paged(q[i], cache.k, cache.v, tables[i], starts[i], kv[i], o, max_q=60, max_kv=2500, workspace=w, **k)
+
+    def check(i, o):
+        order = [1, 2, 0] if i == 0 else [0, 1, 2]
+        one = SimpleNamespace(tokens=[cache.tokens[b] for b in order])
+        _check(o, q[i], one, new[i], lens[i], 3, 0.125)
+
+    for _ in range(5):
+        for i in (0, 1):
+            call(i, out[i], ws[i], stream=streams[i])
+    torch.cuda.synchronize()
+    for i in (0, 1):
+        check(i, out[i])
+    # captured with the first batch's arrays, which then hold either batch
+    o, mine = torch.full_like(q[0], NAN), [x.clone() for x in (q[0], tables[0], starts[0], kv[0])]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        bsm.bsm_attention_paged(mine[0], cache.k, cache.v, *mine[1:], o, max_q=60, max_kv=2500, workspace=ws[0])
+    for i in (1, 0, 1):
+        for x, y in zip(mine, (q[i], tables[i], starts[i], kv[i])):
+            x.copy_(y)
+        o.fill_(NAN)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o.view(torch.int16)[:sum(new[i])], out[i].view(torch.int16)[:sum(new[i])])
+        eager = torch.full_like(o, NAN)
+        call(i, eager, ws[1])
+        torch.cuda.synchronize()
+        assert torch.equal(o.view(torch.int16), eager.view(torch.int16))
