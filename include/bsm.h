@@ -373,9 +373,11 @@ bsm_status bsm_gemm(const void* a, const void* b, void* c, int64_t batch, int32_
  *
  * NaN and infinities: what lies outside a sequence's rows (other rows of a padded batch, the rest
  * of a page, pages of other requests) is never read or counts as nothing.  Inside a sequence, a
- * NaN or infinity in v (in the backward pass: in q, k, v, dout too) can reach every row whose mask
- * hides it but not all of its 64-row block, since 0 * NaN = NaN.  A NaN score, or one of +inf,
- * makes its row NaN.
+ * NaN or infinity in v (in the backward pass: in q, k, v, dout too) can reach rows that do not see
+ * it, since 0 * NaN = NaN, but only by its block: query rows are taken in blocks of 32 (over a
+ * cache, of (token, query head) pairs), keys in blocks of 64, each from the sequence's first, and
+ * what no row of a block sees, or no key of it is seen by, does not reach it.  A NaN score, or one
+ * of +inf, makes its row NaN.
  *
  * Results depend on the operands and sizes only: no sum's order depends on timing, so repeated
  * calls give the same bits under every schedule.  (The last bits depend on the batch's other

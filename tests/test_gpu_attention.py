@@ -526,3 +526,47 @@ def test_the_largest_scale():
     plan, o, lse = _run(batch, False, 0, scale=2.0 ** 127)
     check_forward(batch, o, lse, 2.0 ** 127, False)
     plan.destroy()
+
+
+@pytest.mark.parametrize("n_cu", [0, 1])
+@pytest.mark.parametrize("q_len,kv_len,d,window", [(200, 263, 64, 0), (200, 263, 128, 40), (300, 300, 96, 100), (150, 90, 64, 0)])
+def test_how_far_a_hidden_nan_reaches(q_len, kv_len, d, window, n_cu):
+    """A NaN at a row or key: what shares no visible pair of its blocks (32 rows, 64 keys) keeps its bits."""
+    import oracle.attention as oa
+    seen = oa.seen(q_len, kv_len, True, window)
+    rows, keys = np.arange(q_len), np.arange(kv_len)
+    # pairs (block of rows, block of keys) some of which are visible
+    near = np.zeros((-(-q_len // 32), -(-kv_len // 64)), bool)
+    np.logical_or.at(near, (rows[:, None] // 32, keys[None, :] // 64), seen)
+
+    def run(batch, dout):
+        plan, o, lse = _run(batch, True, window, n_cu=n_cu)
+        grads = [batch.empty("q"), batch.empty("kv"), batch.empty("kv")]
+        bsm.bsm_attention_backward(plan, batch.q, batch.k, batch.v, o, lse, dout, *grads)
+        torch.cuda.synchronize()
+        plan.destroy()
+        return [x.view(torch.int16).cpu().numpy() for x in (o, *grads)]
+
+    batch = Batch([q_len], [kv_len], 2, 1, d, "packed", 89)
+    dout = batch.operand("q")
+    clean = run(batch, dout)
+    for key in (0, 70, kv_len - 1):
+        kept = batch.v[key].clone()
+        batch.v[key] = float("nan")
+        got = run(batch, dout)
+        batch.v[key] = kept
+        far = ~near[rows // 32, key // 64]
+        for x, y in zip(got[:2], clean[:2]):  # o and dq
+            assert np.array_equal(x[far], y[far])
+    for row in (0, 100, q_len - 1):
+        for x in (batch.q, dout):
+            kept = x[row].clone()
+            x[row] = float("nan")
+            got = run(batch, dout)
+            x[row] = kept
+            far = ~near[row // 32, keys // 64]
+            for a, b in zip(got[2:], clean[2:]):  # dk and dv
+                assert np.array_equal(a[far], b[far])
+            others = np.arange(q_len) != row
+            for a, b in zip(got[:2], clean[:2]):
+                assert np.array_equal(a[others], b[others])
