@@ -501,7 +501,8 @@ __global__ __launch_bounds__(kThreads, 2) void paged_few_kernel(const PagedArgs 
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
                     const int j = j0 + 16 * y + n;
-                    const bool live = j < r.kv_len && names_page(a, page[y]);
+                    // (keys that no row sees, as those of pages that a window has left behind, count as zeros)
+                    const bool live = j >= bl.keys.lo && j <= bl.keys.hi && names_page(a, page[y]);
                     const int64_t at = page[y] * a.cache.page + (j % a.cache.page_size) * a.cache.row + r.head * a.cache.head + 8 * quad;
                     const uint16_t* kp = live ? a.cache.k + at : kZeros + 8 * quad;
                     const uint16_t* vp = live ? a.cache.v + at : kZeros + 8 * quad;

@@ -596,3 +596,26 @@ def test_mixed_batches_on_two_streams_and_replayed():
         call(i, eager, ws[1])
         torch.cuda.synchronize()
         assert torch.equal(o.view(torch.int16), eager.view(torch.int16))
+
+
+@pytest.mark.parametrize("window", [0, 1, 25, 100])
+@pytest.mark.parametrize("new,kv_len", [([1], [1000]), ([1, 3], [3001, 130]), ([10, 1], [300, 2600]), ([50], [700])])
+def test_how_far_a_hidden_nan_reaches(new, kv_len, window):
+    """NaN in every value whose block of 64 keys no row sees (the table may still hold pages that a window
+    has left behind): the results keep their bits."""
+    cache = Cache(kv_len, 16, 1, 64, 49)
+    g = torch.Generator().manual_seed(50)
+    q = (2 * torch.randn((sum(new), 2, 64), generator=g)).to(torch.bfloat16).cuda()
+    outs = []
+    for _ in range(2):
+        o = torch.full_like(q, NAN)
+        bsm.bsm_attention_paged(q, cache.k, cache.v, cache.table, i32([0] + list(np.cumsum(new))), i32(kv_len), o, max_q=max(new),
+                                max_kv=max(kv_len), window=window)
+        torch.cuda.synchronize()
+        outs.append(o.view(torch.int16))
+        for b, n in enumerate(kv_len):
+            blocks = oa.seen(new[b], n, True, window).any(0)
+            for key in range(n):
+                if not blocks[key // 64 * 64:key // 64 * 64 + 64].any():
+                    cache.v[cache.table[b, key // 16], key % 16] = NAN
+    assert torch.equal(*outs)
