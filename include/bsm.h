@@ -521,7 +521,9 @@ bsm_status bsm_cache_append(const bsm_cache* cache, const bsm_heads* k, const bs
  *            slow); 0: width * page_size
  * A kv_len past the table's width counts up to it.  A table entry that names no page reads as a
  * page of zeros.  workspace: bsm_attention_paged_workspace bytes for the same sizes, not shared
- * with a call that may run at the same time.  o overlaps no operand. */
+ * with a call that may run at the same time.  o overlaps no operand.  Of a batch of more than 256
+ * requests each counts as a chunk of max_q; a call that comes to 2^24 workgroups (of 128 rows and a
+ * key/value head each) is refused. */
 bsm_status bsm_attention_paged(const bsm_cache* cache, const bsm_heads* q, const bsm_heads* o,
                                const int32_t* table, int32_t width, const int32_t* q_start,
                                const int32_t* kv_len, int64_t batch, int64_t tokens,

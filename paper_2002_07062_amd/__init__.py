@@ -15,6 +15,8 @@ from .bsm import (  # noqa: F401
     bsm_gemm_execute, bsm_gemm_plan_create,
     bsm_topology, load)
 from .attention import (  # noqa: F401
+    BSM_ATTENTION_DQ_PARTS, BSM_ATTENTION_HALF_DQ, BSM_ATTENTION_HALF_FORWARD,
+    BSM_ATTENTION_HALF_KEYS, BSM_ATTENTION_KEY_PARTS, BSM_ATTENTION_LONG_STEPS,
     AttentionPlan, bsm_attention_backward, bsm_attention_execute, bsm_attention_paged,
     bsm_attention_paged_workspace, bsm_attention_plan_create, bsm_attention_plan_describe,
     bsm_attention_plan_destroy, bsm_cache_append, bsm_cache_slots)

@@ -286,8 +286,8 @@ def bsm_attention_execute(plan: AttentionPlan, q, k, v, o, lse=None, scale=None,
 def bsm_attention_backward(plan: AttentionPlan, q, k, v, o, lse, dout, dq, dk, dv, scale=None,
                            workspace=None, stream=None):
     """Gradients of bsm_attention_execute: dq, dk and dv from q, k, v, its o and lse, and dout
-    (see bsm.h). workspace: None (allocated for the call on the current stream) or a tensor of
-    plan.workspace_bytes bytes. Returns (dq, dk, dv)."""
+    (see bsm.h). workspace: None (allocated for the call on the current stream; a call with a stream
+    of its own brings its own) or a tensor of plan.workspace_bytes bytes. Returns (dq, dk, dv)."""
     fn = _load().bsm_attention_backward
     dev = plan.device
     refs = _refs(plan._q(q, "q"), plan._kv(k, "k"), plan._kv(v, "v"), plan._q(o, "o"),
@@ -380,8 +380,8 @@ def bsm_attention_paged(q, k_cache, v_cache, table, q_start, kv_len, o, max_q, m
     """o = causal attention of every request's new tokens over its pages (see bsm.h). q, o:
     (tokens, heads, dim); table: int32 (batch, width); q_start: int32 (batch + 1); kv_len: int32
     (batch). max_q, max_kv: host bounds on a chunk and on kv_len (None or 0: the table's width).
-    workspace: None (allocated for the call on the current stream) or a tensor of
-    bsm_attention_paged_workspace bytes. Returns o."""
+    workspace: None (allocated for the call on the current stream; a call with a stream of its own
+    brings its own) or a tensor of bsm_attention_paged_workspace bytes. Returns o."""
     fn = _load().bsm_attention_paged
     cache, dev = _cache_of(k_cache, v_cache)
     if q.dim() != 3 or o.dim() != 3:

@@ -57,9 +57,9 @@ __device__ __forceinline__ void each_sum(f32x16 (&acc)[TILES], F f) {
 // workgroup off the CU (heads of 64, us with 64 and 128: 2 x 512 rows, 12 heads 8.9, 7.6; 4096, 8 heads, causal
 // 46.7, 37.5; 8 x 512, 12 heads, 768 units 11.3, 13.5; longer heads no faster).
 // Bound by the matrix cores with the exponentials between them, and on random data by the power that both
-// take: 4 x 4096 causal rows, 32/8 heads of 128, 570 .. 585 us = 940 .. 964 TFLOP/s (a library's 8192^3 product on the
-// same card: 1220), of whose cycles the matrix cores are busy for 48% and the vector units for another 48%, at a clock of
-// 2.0 of 2.4 GHz; 475 us on zeros.
+// take: 4 x 4096 causal rows, 32/8 heads of 128, 570 .. 610 us = 901 .. 964 TFLOP/s with the card's clock (a
+// library's 8192^3 product: 1203 .. 1221), of whose cycles the matrix cores are busy for 49% and the vector units for
+// another 48%, at 1.9 .. 2.0 of 2.4 GHz; 475 us on zeros.
 template <int D, bool DIRECT, int KS, int STEP>
 __global__ __launch_bounds__(kThreads, 2) void attention_kernel(const SequenceArgs a, const Unit* __restrict__ units) {
     constexpr int kKeys = STEP;
