@@ -23,7 +23,7 @@ __device__ __forceinline__ Seen seen_keys(int i, int q_len, int kv_len, Mask m) 
     if (m.causal) {
         const int p = i + kv_len - q_len;
         s.hi = p < s.hi ? p : s.hi;
-        if (m.window > 0 && p >= m.window) s.lo = p - m.window + 1;  // (any window: p < 0 has no room for the difference)
+        if (m.window > 0 && p - m.window + 1 > 0) s.lo = p - m.window + 1;  // (of at most kMostRows each, which fits)
     }
     return s;
 }

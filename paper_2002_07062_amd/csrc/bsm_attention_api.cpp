@@ -24,6 +24,7 @@ struct bsm_attention_plan_s {
     bsm_schedule schedule = BSM_SCHED_RR;
     int n_xcd = 1;
     bsm_att::Sequences seqs;
+    int32_t window = 0;  // as given
     int64_t n_forward = 0, n_q = 0, n_kv = 0, n_q_joins = 0, n_kv_joins = 0;
     int64_t q_part_rows = 0, kv_part_rows = 0;
     int32_t forward_rows = 0, dq_rows = 0, key_rows = 0;  // of a unit of the forward pass, of dq, of dk and dv
@@ -35,6 +36,7 @@ struct bsm_attention_plan_s {
 namespace {
 
 using bsm_att::Heads;
+using bsm_att::kMostRows;
 
 bsm_status fail(bsm_status st, const char* fmt, ...) {
     char buf[512];
@@ -68,7 +70,6 @@ struct DeviceGuard {
     }
 };
 
-constexpr int32_t kMostRows = 1 << 30;
 constexpr int64_t kMostStride = int64_t{1} << 40;
 constexpr int64_t kMostWorkgroups = (int64_t{1} << 24) - 1;  // of 256 threads: a launch has less than 2^32
 
@@ -282,7 +283,8 @@ bsm_status create(bsm_attention_plan* out_plan, const int32_t* q_len, const int3
         s.heads_q = heads_q;
         s.heads_kv = heads_kv;
         s.dim = head_dim;
-        s.mask = {causal ? 1 : 0, window};
+        s.mask = {causal ? 1 : 0, bsm_att::held_window(window)};
+        p->window = window;
         bsm_att::finish_sequences(&s, q_start, kv_start);
         const double units = (static_cast<double>(s.total_q) / bsm_att::kTileRows + batch) * heads_q +
                              (static_cast<double>(s.total_kv) / bsm_att::kTileRows + batch) * heads_kv;
@@ -568,7 +570,7 @@ bsm_status paged(const bsm_cache* cache, const bsm_heads* q, const bsm_heads* o,
     a.width = width;
     a.max_q = max_q;
     a.group = heads_q / cache->heads;
-    a.window = window;
+    a.window = bsm_att::held_window(window);
     a.scale = scale;
     a.few_rows = cut.few_rows;
     a.shares = cut.shares;
@@ -688,7 +690,7 @@ bsm_status bsm_attention_plan_describe(bsm_attention_plan plan, bsm_attention_st
     stats->heads_kv = s.heads_kv;
     stats->head_dim = s.dim;
     stats->causal = s.mask.causal;
-    stats->window = s.mask.window;
+    stats->window = plan->window;
     stats->schedule = plan->schedule;
     stats->n_xcd = plan->n_xcd;
     const bool half_forward = plan->forward_rows < bsm_att::kTileRows, half_dq = plan->dq_rows < bsm_att::kTileRows;

@@ -44,9 +44,16 @@ struct Heads {
     int64_t seq, row, head;
 };
 
+// The most rows and keys of a sequence, tokens of a paged call, and keys of a request.
+constexpr int32_t kMostRows = 1 << 30;
+
+// window 0: none; of a larger one than kMostRows, which hides as little, the kernels get that: a position from -kMostRows
+// on less the window then fits 32 bits.  (With p >= window compared first, any window would do, but dq of heads over 96
+// spills two registers more: gradient of 4 x 4096 causal rows, 32/8 heads of 128, 2116 .. 2153 us, 2084 .. 2114 so.)
 struct Mask {
-    int32_t causal, window;  // window 0: none
+    int32_t causal, window;
 };
+constexpr int32_t held_window(int32_t window) { return window < kMostRows ? window : kMostRows; }
 
 struct SequenceArgs {
     Heads q, k, v, o, dout, dq, dk, dv;

@@ -75,7 +75,7 @@ struct Keys {
 __device__ __forceinline__ Keys seen_keys(const PagedArgs& a, const Request& r, int token) {
     const int p = token + r.kv_len - r.q_len;
     Keys k = {0, p < r.kv_len - 1 ? p : r.kv_len - 1};
-    if (a.window > 0 && p >= a.window) k.lo = p - a.window + 1;  // (any window: p < 0 has no room for the difference)
+    if (a.window > 0 && p - a.window + 1 > 0) k.lo = p - a.window + 1;  // (of at most kMostRows each, which fits)
     return k;
 }
 

@@ -358,3 +358,9 @@ def test_streams_of_other_devices_are_refused():
     assert att._stream(1, stream) == 1234 and att._stream(0, 5678) == 5678
     with pytest.raises(ValueError, match="cuda:1.*cuda:0"):
         att._stream(0, stream)
+
+
+@pytest.mark.parametrize("window", [2**31 - 1, 2**30 + 1, 2**30, 2**30 - 1])
+def test_the_largest_windows_hide_nothing(window):
+    d = bsm.bsm_attention_plan_describe(_plan([100, 5], [50, 700], causal=True, window=window))
+    assert d["window"] == window and d["pairs"] == sum(int(oa.seen(n, m, True).sum()) for n, m in ((100, 50), (5, 700)))
