@@ -299,9 +299,9 @@ __global__ __launch_bounds__(kThreads, D > 64 && KS == 2 ? 1 : 2) void attention
 // half of 128 columns over both blocks (of 96, wave 1 adds 32 that are not stored).  That keeps a wave's sums
 // at 64 registers, so that two waves fit a SIMD and one's exponentials run beside the other's products (a wave
 // that held whole sums took 400 registers and ran alone: 735 us against 475 us on six ragged causal sequences
-// of 700 .. 4001 tokens, 32/8 heads of 128).  4 x 4096 causal rows, 32/8 heads of 128, 1287 us = 855
-// TFLOP/s in its four products; on the six ragged ones the matrix cores are busy for 36% of the cycles, and the waves wait
-// for 37% of theirs (32 x 512 rows, 12 heads of 64: 33% both).
+// of 700 .. 4001 tokens, 32/8 heads of 128).  4 x 4096 causal rows, 32/8 heads of 128, 1245 .. 1287 us =
+// 855 .. 884 TFLOP/s in its four products; on the six ragged ones the matrix cores are busy for 37% of the cycles, and the
+// waves wait for 36% of theirs (32 x 512 rows, 12 heads of 64: 33% both).
 // KS = 2, heads of 64: 64 keys, two waves of each 32 with a block of every step's query rows; for plans with little to
 // do (see key_rows).
 template <int D>

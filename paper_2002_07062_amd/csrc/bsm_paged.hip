@@ -317,7 +317,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_kernel(const PagedArgs a) {
 // any lengths keep all CUs busy to the end; a request whose blocks lie in several shares is joined
 // afterwards.  The workgroups of a share run side by side, and with them the reads of a page's heads, which
 // lie side by side too.  Each workgroup counts the stream itself, 8 bytes a request from the cache.
-// 64 requests of 1k .. 32k keys, 8 kv heads of 128, 2.3 GB: 436 us = 5.3 TB/s, the joins 8 us (a plain read of as
+// 64 requests of 1k .. 32k keys, 8 kv heads of 128, 2.3 GB: 434 us = 5.3 TB/s, the joins 8 us (a plain read of as
 // much: 6.0 TB/s).
 
 // Blocks of one head of a request; one without keys has a block that writes zeros.
